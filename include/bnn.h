@@ -385,6 +385,77 @@ int bnn_net_fc_run(const bnn_net* net, int batch, int recorded, int* layers);
  * length in words, rows the number of rows (batch, or batch*P*Q). */
 int bnn_net_layer_bits(const bnn_net* net, int layer, const uint32_t** bits, int64_t* rows, int* words_per_row);
 
+/* ------------------------------------------------------------------------------------------
+ * A key/value cache in 4 bits, and attention over it: what a language model of binarized layers needs beside them.
+ *
+ * The cache consists of pages of `page` tokens; a page table says which pages hold a sequence, so sequences grow without
+ * copies and may share pages.  Its memory is bytes [pages][kv_heads][record], and a record, of bnn_cache4_record_bytes, is
+ *     K codes [page][D/2] | V codes [page][D/2] | K scales [D/32][page] | V scales [D/32][page] | signs of K [page][D/32] words
+ * (D = head_dim; the signs only where the cache keeps them).
+ *  - Codes are E2M1: bit 3 the sign, magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6; element d is nibble d % 2 (low first) of byte d / 2.
+ *  - 32 elements share a scale, a power of two 2^e stored as the byte e + 127: e is the smallest integer in [-100, 100] with
+ *    max|x| <= 6 * 2^e.  A code is the magnitude nearest to x * 2^-e, ties to the even code; what is beyond 6 * 2^100 saturates.  A group
+ *    with an infinity or a NaN gets the byte 255 and reads as NaN throughout.
+ *  - Sign bits in the library's packed layout (bit = (k >= 0), before rounding).
+ * Memory of tokens that were never written need not be initialised.
+ *
+ * Rows of a call: sequence b contributes its newest tokens, as start[b + 1] - start[b] consecutive rows (start[0] = 0, start[batch] = tokens); row i
+ * of n is the token at position lens[b] - n + i.  With start == NULL every sequence has tokens / batch rows.  lens[b] counts the tokens that sequence b
+ * has after this call's are in.  Token i lies in page table[b][i / page], at i % page; a table entry that is no page (such as -1: given back, or
+ * not needed) holds nothing: writes to it are dropped, reads give 0, and attention and selection pass it over.  The three arrays are on the device and
+ * are read by the kernels; whatever they hold, no access leaves the cache or the call's arrays, but rows outside every sequence keep what they held.
+ * ---------------------------------------------------------------------------------------- */
+#define BNN_F32 0
+#define BNN_BF16 1
+#define BNN_F16 2
+
+typedef struct bnn_cache4 {
+    void* data;          /* 16-byte aligned */
+    int64_t pages;       /* < 2^31 */
+    int kv_heads;
+    int head_dim;        /* 64, 96, 128, 192 or 256 */
+    int page;            /* a power of two, 16 to 256 */
+    int signs;           /* 1: with the signs of K, which selection needs */
+} bnn_cache4;
+
+typedef struct bnn_cache4_rows {
+    const int32_t* table;    /* [batch][table_pages] */
+    const int32_t* lens;     /* [batch] */
+    const int32_t* start;    /* [batch + 1], or NULL */
+    int batch;
+    int table_pages;         /* table_pages * page < 2^31 */
+    int tokens;              /* rows in all; 0: nothing is done */
+} bnn_cache4_rows;
+
+/* Bytes of a record, a multiple of 16; 0 for a head_dim or page that is not supported. */
+size_t bnn_cache4_record_bytes(int head_dim, int page, int signs);
+/* Quantises the rows' keys and values into the cache.  k, v: [tokens][kv_heads][head_dim] of `dtype` (BNN_F32, BNN_BF16, BNN_F16), the elements of a head side by
+ * side, tokens and heads *_token and *_head elements apart; pointers and distances multiples of 16 bytes.  A token that two rows name is written by either. */
+int bnn_cache4_write(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* k, const void* v, int dtype,
+                     int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, void* stream);
+/* The rows' keys and values as the cache holds them, rounded once to `dtype`: k, v [tokens][kv_heads][head_dim], contiguous. */
+int bnn_cache4_read(const bnn_cache4* cache, const bnn_cache4_rows* rows, void* k, void* v, int dtype, void* stream);
+/* For every row and kv head the `keep` blocks (pages of its sequence, counted from 0) to attend to, ascending, the rest -1: the first `first` blocks
+ * and the last `last` up to the row's own, and of the others those with the best score.  A block's score is the sum, over the query
+ * heads of the kv head, of the most sign bits in which the query agrees with a key of the block (D - popc(q xor k), the library's product up to a factor),
+ * over the keys up to the row's own; ties go to the lower block.
+ *   q [tokens][heads][head_dim], elements as in bnn_cache4_write; kv head h serves query heads h * heads / kv_heads and on; heads / kv_heads * head_dim <= 16000.
+ *   blocks [tokens][kv_heads][keep];  keep >= first + last, first, last >= 0. */
+size_t bnn_cache4_select_workspace_bytes(const bnn_cache4* cache, const bnn_cache4_rows* rows);
+int bnn_cache4_select(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads,
+                      int keep, int first, int last, int32_t* blocks, void* workspace, size_t workspace_bytes, void* stream);
+/* Attention: out = sum_i softmax_i(scale * q . k_i) v_i over the keys that the row sees: with `causal` those up to its own position, and with
+ * window > 0 (causal only) the last `window` of them; without, all lens[b] keys.  blocks, or NULL: [tokens][kv_heads][keep], as
+ * bnn_cache4_select gives it, leaves only the keys of the listed blocks (entries below 0 or past the table are passed over; a block listed twice counts twice).
+ *   q as in bnn_cache4_select;  out [tokens][heads][head_dim] of `dtype`, contiguous;  lse [tokens][heads] fp32 or NULL: log sum_i exp(scale * q . k_i).
+ *   A row that sees no key gets 0, and -infinity in lse.  scale > 0.
+ * Products are formed of bf16 terms with fp32 sums; the cache's values are exact in bf16, queries enter exactly, softmax weights with 8 (bf16),
+ * 16 (fp16) or 24 bits (fp32).  Keys that a row does not see do not reach it, NaN or not. */
+size_t bnn_cache4_attend_workspace_bytes(const bnn_cache4* cache, const bnn_cache4_rows* rows, int dtype, int heads, int window, int keep);
+int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads,
+                      float scale, int causal, int window, const int32_t* blocks, int keep, void* out, float* lse,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

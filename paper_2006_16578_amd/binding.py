@@ -18,7 +18,7 @@ import torch
 
 __all__ = ["BnnError", "lib_path", "load", "PAD_MINUS_ONE", "PAD_EXCLUDE", "PATH_AUTO", "PATH_VALU", "PATH_MFMA",
            "nwords", "round_up", "bmm", "bmm_thr", "bconv", "bconv_thr", "threshold_pack", "pack_u8", "pack_f32",
-           "unpack_i32", "tile_b", "bmm_tiled", "bmm_thr_tiled", "panels_from_rows", "rows_from_panels", "bmm_panels", "bmm_thr_panels", "probe_load_stride", "probe_pipeline", "probe_pipeline_enqueue", "PROBES", "sign_pack_f32", "bmm_general_f32", "bconv_general_f32", "maxpool_or", "conv_f32_thr", "conv_f32_split_thr", "bwn_conv_thr", "head_f32", "Net", "EXPORTS", "bmm_kernel_name", "bconv_kernel_name"]
+           "unpack_i32", "tile_b", "bmm_tiled", "bmm_thr_tiled", "panels_from_rows", "rows_from_panels", "bmm_panels", "bmm_thr_panels", "probe_load_stride", "probe_pipeline", "probe_pipeline_enqueue", "PROBES", "sign_pack_f32", "bmm_general_f32", "bconv_general_f32", "maxpool_or", "conv_f32_thr", "conv_f32_split_thr", "bwn_conv_thr", "head_f32", "Net", "Cache4", "EXPORTS", "bmm_kernel_name", "bconv_kernel_name"]
 
 PAD_MINUS_ONE, PAD_EXCLUDE = 0, 1
 PATH_AUTO, PATH_VALU, PATH_MFMA = 0, 1, 2
@@ -32,7 +32,9 @@ EXPORTS = ["bnn_status_string", "bnn_version", "bnn_bmm_kernel_name", "bnn_bconv
            "bnn_bconv_general_workspace_bytes", "bnn_bconv_general_f32", "bnn_unpack_i32", "bnn_maxpool_or", "bnn_conv_f32_thr", "bnn_conv_f32_split_workspace_bytes", "bnn_conv_f32_split_thr", "bnn_conv_f32_split_thr_ex", "bnn_bwn_workspace_bytes", "bnn_bwn_conv_thr", "bnn_head_f32", "bnn_net_create",
            "bnn_net_destroy", "bnn_net_input_u8", "bnn_net_input_bits", "bnn_net_input_conv_f32", "bnn_net_input_bwn_f32", "bnn_net_add_fc",
            "bnn_net_add_conv", "bnn_net_add_pool", "bnn_net_add_block", "bnn_net_add_head_f32", "bnn_net_workspace_bytes",
-           "bnn_net_forward", "bnn_net_forward_static", "bnn_static_workspace_init", "bnn_net_forward_persistent", "bnn_net_persistent_status", "bnn_net_fc_run", "bnn_net_layer_bits"]
+           "bnn_net_forward", "bnn_net_forward_static", "bnn_static_workspace_init", "bnn_net_forward_persistent", "bnn_net_persistent_status", "bnn_net_fc_run", "bnn_net_layer_bits",
+           "bnn_cache4_record_bytes", "bnn_cache4_write", "bnn_cache4_read", "bnn_cache4_select_workspace_bytes", "bnn_cache4_select",
+           "bnn_cache4_attend_workspace_bytes", "bnn_cache4_attend"]
 
 
 class BnnError(RuntimeError):
@@ -68,6 +70,9 @@ def load() -> ctypes.CDLL:
         lib.bnn_conv_f32_split_workspace_bytes.restype = ctypes.c_size_t
         lib.bnn_bmm_general_workspace_bytes.restype = ctypes.c_size_t
         lib.bnn_bconv_general_workspace_bytes.restype = ctypes.c_size_t
+        lib.bnn_cache4_record_bytes.restype = ctypes.c_size_t
+        lib.bnn_cache4_select_workspace_bytes.restype = ctypes.c_size_t
+        lib.bnn_cache4_attend_workspace_bytes.restype = ctypes.c_size_t
         for name in EXPORTS:
             getattr(lib, name)          # fail loudly on a missing export
         _lib = lib
@@ -795,3 +800,127 @@ class Net:
         off = p.value - self._ws.data_ptr()
         n = rows.value * wpr.value * 4
         return self._ws[off:off + n].view(_BITS).view(rows.value, wpr.value).clone()
+
+
+class _Cache4Struct(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int64), ("kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("page", ctypes.c_int),
+                ("signs", ctypes.c_int)]
+
+
+class _Rows4Struct(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("lens", ctypes.c_void_p), ("start", ctypes.c_void_p), ("batch", ctypes.c_int), ("table_pages", ctypes.c_int),
+                ("tokens", ctypes.c_int)]
+
+
+_ELEMENTS = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # BNN_F32, BNN_BF16, BNN_F16
+
+
+class Cache4:
+    """Key/value cache in 4 bits (bnn_cache4_*): pages of `page` tokens, a page table per batch, E2M1 codes with a power of two per 32 elements.
+
+    ``data`` (uint8 [pages][kv_heads][record]) is the cache's memory, allocated here unless given; the layout is in include/bnn.h.
+    Every call takes the plan of a batch: ``table`` int32 [batch][pages of the longest], ``lens`` int32 [batch], tokens per sequence including
+    those of this call, and, where sequences contribute different numbers of rows, ``start`` int32 [batch + 1].  The rows of a sequence are
+    its newest tokens.  Tensors of elements are fp32, bf16 or fp16."""
+
+    def __init__(self, pages: int | None = None, *, kv_heads: int, head_dim: int, page: int = 64, signs: bool = True, data=None, device="cuda"):
+        record = int(load().bnn_cache4_record_bytes(int(head_dim), int(page), int(bool(signs))))
+        if record == 0:
+            raise ValueError("head_dim of 64, 96, 128, 192 or 256 and pages of 16 to 256 tokens, a power of two, expected")
+        if data is None:
+            if pages is None:
+                raise ValueError("pages or data expected")
+            data = torch.empty((int(pages), int(kv_heads), record), dtype=torch.uint8, device=device)
+        _dev(data, torch.uint8, 3, "data")
+        if data.shape[1] != kv_heads or data.shape[2] != record or pages not in (None, data.shape[0]):
+            raise ValueError("data must be [pages][kv_heads][%d]" % record)
+        self.data, self.kv_heads, self.head_dim, self.page, self.signs = data, int(kv_heads), int(head_dim), int(page), bool(signs)
+        self._c = _Cache4Struct(data.data_ptr(), data.shape[0], self.kv_heads, self.head_dim, self.page, int(self.signs))
+
+    def _rows(self, table, lens, start, tokens):
+        _dev(table, torch.int32, 2, "table"); _dev(lens, torch.int32, 1, "lens")
+        batch, width = table.shape
+        if lens.shape[0] != batch:
+            raise ValueError("lens must have an entry for every sequence of table")
+        if start is not None and _dev(start, torch.int32, 1, "start").shape[0] != batch + 1:
+            raise ValueError("start must have one entry more than table has sequences")
+        for t in (table, lens, start):
+            if t is not None and t.device != self.data.device:
+                raise ValueError("the plan must be on the cache's device")
+        return _Rows4Struct(table.data_ptr(), lens.data_ptr(), 0 if start is None else start.data_ptr(), batch, width, int(tokens))
+
+    def _elements(self, x, heads, name):
+        """Type code and distances of x [tokens][heads][head_dim]; only the elements of a head need be contiguous."""
+        if not isinstance(x, torch.Tensor) or not x.is_cuda:
+            raise TypeError("%s must be a device tensor" % name)
+        if x.dtype not in _ELEMENTS:
+            raise TypeError("%s must be fp32, bf16 or fp16, got %s" % (name, x.dtype))
+        if x.dim() != 3 or x.shape[2] != self.head_dim or (heads is not None and x.shape[1] != heads):
+            raise ValueError("%s must be [tokens][%s][%d]" % (name, "heads" if heads is None else heads, self.head_dim))
+        if x.device != self.data.device:
+            raise ValueError("%s must be on the cache's device" % name)
+        if x.stride(2) != 1 and x.numel() != 0:
+            raise ValueError("the elements of a head of %s must be contiguous" % name)
+        return _ELEMENTS[x.dtype], ctypes.c_int64(x.stride(0)), ctypes.c_int64(x.stride(1))
+
+    def write(self, k, v, table, lens, start=None):
+        """Quantises k, v [tokens][kv_heads][head_dim], the newest tokens of every sequence, into the cache."""
+        code, kt, kh = self._elements(k, self.kv_heads, "k")
+        code_v, vt, vh = self._elements(v, self.kv_heads, "v")
+        if code != code_v or k.shape != v.shape:
+            raise ValueError("k and v must agree in type and shape")
+        rows = self._rows(table, lens, start, k.shape[0])
+        with _on(k):
+            _check(load().bnn_cache4_write(ctypes.byref(self._c), ctypes.byref(rows), _ptr(k), _ptr(v), code, kt, kh, vt, vh, _stream(k)), "bnn_cache4_write")
+
+    def read(self, table, lens, start=None, tokens: int | None = None, dtype=torch.bfloat16):
+        """(k, v) [tokens][kv_heads][head_dim]: the newest tokens of every sequence as the cache holds them.  tokens: rows in all (default: one of every sequence)."""
+        if dtype not in _ELEMENTS:
+            raise TypeError("fp32, bf16 or fp16 expected, got %s" % dtype)
+        tokens = table.shape[0] if tokens is None else int(tokens)
+        rows = self._rows(table, lens, start, tokens)
+        k, v = (torch.empty((tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.data.device) for _ in range(2))
+        with _on(k):
+            _check(load().bnn_cache4_read(ctypes.byref(self._c), ctypes.byref(rows), _ptr(k), _ptr(v), _ELEMENTS[dtype], _stream(k)), "bnn_cache4_read")
+        return k, v
+
+    def select(self, q, table, lens, keep: int, start=None, first: int = 1, last: int = 1, workspace=None):
+        """int32 [tokens][kv_heads][keep]: the blocks (pages of a sequence) that every row of q [tokens][heads][head_dim] attends to, by the
+        agreement of sign bits; the first `first` and the `last` most recent always; ascending, the rest -1."""
+        code, qt, qh = self._elements(q, None, "q")
+        rows = self._rows(table, lens, start, q.shape[0])
+        blocks = torch.empty((q.shape[0], self.kv_heads, max(int(keep), 0)), dtype=torch.int32, device=q.device)
+        if workspace is None:
+            need = int(load().bnn_cache4_select_workspace_bytes(ctypes.byref(self._c), ctypes.byref(rows)))
+            workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        with _on(q):
+            _check(load().bnn_cache4_select(ctypes.byref(self._c), ctypes.byref(rows), _ptr(q), code, qt, qh, q.shape[1], int(keep), int(first), int(last),
+                                            _ptr(blocks), _ptr(workspace), ctypes.c_size_t(workspace.numel()), _stream(q)), "bnn_cache4_select")
+        return blocks
+
+    def attend(self, q, table, lens, start=None, scale: float | None = None, causal: bool = True, window: int = 0, blocks=None, want_lse: bool = False,
+               out=None, workspace=None):
+        """Attention of q [tokens][heads][head_dim], the newest tokens of every sequence, over the cache -> [tokens][heads][head_dim] of q's type (and
+        the logarithm of the weights' sum, fp32 [tokens][heads]).  blocks: only those (from select).  scale: 1 / sqrt(head_dim) by default."""
+        code, qt, qh = self._elements(q, None, "q")
+        rows = self._rows(table, lens, start, q.shape[0])
+        keep = 0
+        if blocks is not None:
+            _dev(blocks, torch.int32, 3, "blocks")
+            keep = blocks.shape[2]
+            if blocks.shape[0] != q.shape[0] or blocks.shape[1] != self.kv_heads or blocks.device != q.device:
+                raise ValueError("blocks must be [tokens][kv_heads][keep], on q's device")
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        elif _dev(out, q.dtype, 3, "out").shape != q.shape or out.device != q.device:
+            raise ValueError("out must have q's shape and device")
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
+        if workspace is None:
+            need = int(load().bnn_cache4_attend_workspace_bytes(ctypes.byref(self._c), ctypes.byref(rows), code, q.shape[1], int(window), keep))
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        scale = self.head_dim ** -0.5 if scale is None else float(scale)
+        with _on(q):
+            _check(load().bnn_cache4_attend(ctypes.byref(self._c), ctypes.byref(rows), _ptr(q), code, qt, qh, q.shape[1], ctypes.c_float(scale),
+                                            int(bool(causal)), int(window), _ptr(blocks), keep, _ptr(out), _ptr(lse), _ptr(workspace),
+                                            ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream(q)), "bnn_cache4_attend")
+        return (out, lse) if want_lse else out

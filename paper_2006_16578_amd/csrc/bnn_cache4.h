@@ -1,0 +1,176 @@
+// Declarations shared by the kernels of the 4-bit key/value cache (not part of the ABI; the layout and the operators are stated in include/bnn.h).
+#ifndef BNN_CACHE4_H
+#define BNN_CACHE4_H
+
+#include "bnn_internal.h"
+
+namespace bnn {
+
+// What a stored scale may be: 2^(byte - 127), byte in [C4_EXP_MIN, C4_EXP_MAX]; C4_EXP_NAN marks a group that held an infinity or a NaN.
+// Six times the largest and half the smallest are ordinary numbers in fp32 and bf16, so no value of the cache overflows or is subnormal there.
+constexpr int C4_EXP_MIN = 27, C4_EXP_MAX = 227, C4_EXP_NAN = 255;
+constexpr int C4_GROUP = 32;                 // elements that share a scale: the width of the matrix instructions' own block scales
+
+// A cache as the kernels see it.  Offsets of a record's parts are in bytes.
+struct Cache4 {
+    uint8_t* data;
+    long long pages;
+    int kv_heads, dim, page, page_shift;
+    int record;                              // bytes of one (page, head)
+    int v_codes, k_exps, v_exps, signs;      // K codes at 0
+};
+
+// The rows of a call: sequence b's newest start[b + 1] - start[b] tokens (start == nullptr: `each` of every sequence).
+struct Rows4 {
+    const int32_t* table;
+    const int32_t* lens;
+    const int32_t* start;
+    int batch, table_pages, tokens, each;
+    FastDiv div_each;
+};
+
+// One sequence of a call: its first row, its number of rows, its length.  Row i (of the sequence) is the token at length - rows + i.
+struct Sequence4 {
+    int first, rows, length;
+};
+
+__device__ __forceinline__ Sequence4 c4_sequence(const Rows4& r, const Cache4& c, int b) {
+    Sequence4 s;
+    if (r.start == nullptr) {
+        s.first = b * r.each;
+        s.rows = r.each;
+    } else {                                 // clamped: no content of start leads out of the callers' arrays
+        s.first = min(max(r.start[b], 0), r.tokens);
+        s.rows = min(max(r.start[b + 1], s.first), r.tokens) - s.first;
+    }
+    const long long most = (long long)r.table_pages << c.page_shift;
+    s.length = max(r.lens[b], 0);
+    if (s.length > most) s.length = (int)most;
+    return s;
+}
+
+// The sequence that row t belongs to: the last one that starts at or before t.
+__device__ __forceinline__ int c4_sequence_of(const Rows4& r, int t) {
+    if (r.start == nullptr) return fast_div(t, r.div_each);
+    int lo = 0, hi = r.batch - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (r.start[mid] <= t) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+
+// The page that holds a token of sequence b, or -1: out of the table, or an entry that is no page.
+__device__ __forceinline__ int c4_page(const Rows4& r, const Cache4& c, int b, int token) {
+    const int at = token >> c.page_shift;
+    if (token < 0 || at >= r.table_pages) return -1;
+    const int p = r.table[(long long)b * r.table_pages + at];
+    return p >= 0 && p < c.pages ? p : -1;
+}
+__device__ __forceinline__ uint8_t* c4_record(const Cache4& c, int page, int head) {
+    return c.data + ((long long)page * c.kv_heads + head) * c.record;
+}
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+// Eight consecutive elements as fp32, from 16-byte aligned memory.
+template <class T>
+__device__ __forceinline__ void c4_load8(const T* p, float (&x)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+    } else {
+        typedef T t8 __attribute__((ext_vector_type(8)));
+        const t8 a = *reinterpret_cast<const t8*>(p);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
+    }
+}
+template <class T>
+__device__ __forceinline__ void c4_store8(T* p, const float (&x)[8]) {
+    if constexpr (sizeof(T) == 4) {
+        f32x4 a, b;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { a[i] = x[i]; b[i] = x[4 + i]; }
+        reinterpret_cast<f32x4*>(p)[0] = a;
+        reinterpret_cast<f32x4*>(p)[1] = b;
+    } else {
+        typedef T t8 __attribute__((ext_vector_type(8)));
+        t8 a;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) a[i] = (T)x[i];
+        *reinterpret_cast<t8*>(p) = a;
+    }
+}
+
+// The scale that a byte stands for.  The NaN byte becomes a NaN: so does what is converted with it.
+__device__ __forceinline__ float c4_scale(uint32_t byte) {
+    return __uint_as_float(byte == C4_EXP_NAN ? 0x7fc00000u : byte << 23);
+}
+
+// The attention call as the kernels see it.
+struct Attend4 {
+    Cache4 c;
+    Rows4 r;
+    const void* q;
+    long long q_token, q_head;               // elements between tokens and between heads
+    int group;                               // query heads of a kv head
+    FastDiv div_group;
+    float scale;                             // times log2(e): scores are powers of two
+    int causal, window;
+    const int32_t* blocks;                   // [tokens][kv_heads][keep], or nullptr: every key
+    int keep;
+    void* out;
+    float* lse;
+    int tiles;                               // row tiles of the launch
+    int seq_tiles;                           // row tiles of a sequence, where all have as many rows
+    FastDiv div_seq_tiles;
+    int splits, chunk;                       // parts the keys are cut into: of `chunk` steps of 32 keys
+    FastDiv div_splits, div_heads;
+    float* part;                             // [tiles][kv_heads][splits][rows of a tile][dim]
+    float* part_ml;                          // ... [2]: maximum and sum
+};
+
+// How a call is cut up.  qtiles: groups of 16 rows that a workgroup carries.
+struct AttendPlan4 {
+    int qtiles, tiles, seq_tiles, splits, chunk;
+    size_t part_bytes, workspace_bytes;
+};
+
+// The most groups of 16 rows that a workgroup carries: per group a lane keeps D / 4 registers of sums and D / 8 of every term of Q.
+constexpr int cache4_qtiles(int dim, int dtype) {
+    const int terms = dtype == BNN_BF16 ? 1 : dtype == BNN_F16 ? 2 : 3;
+    const int each = dim / 4 + terms * (dim / 8);
+    return 4 * each <= 200 ? 4 : 2 * each <= 200 ? 2 : 1;
+}
+
+int launch_cache4_attend64(const Attend4& a, int dtype, int qtiles, hipStream_t s);
+int launch_cache4_attend96(const Attend4& a, int dtype, int qtiles, hipStream_t s);
+int launch_cache4_attend128(const Attend4& a, int dtype, int qtiles, hipStream_t s);
+int launch_cache4_attend192(const Attend4& a, int dtype, int qtiles, hipStream_t s);
+int launch_cache4_attend256(const Attend4& a, int dtype, int qtiles, hipStream_t s);
+
+// The selection call as the kernels see it.
+struct Select4 {
+    Cache4 c;
+    Rows4 r;
+    const void* q;
+    long long q_token, q_head;
+    int group;
+    int keep, first, last;
+    int32_t* blocks;                         // [tokens][kv_heads][keep]
+    uint16_t* scores;                        // [tokens][kv_heads][table_pages]
+};
+int launch_cache4_select(const Select4& a, int dtype, hipStream_t s);
+int launch_cache4_write(const Cache4& c, const Rows4& r, const void* k, const void* v, int dtype, long long k_token, long long k_head,
+                        long long v_token, long long v_head, hipStream_t s);
+int launch_cache4_read(const Cache4& c, const Rows4& r, void* k, void* v, int dtype, hipStream_t s);
+
+}  // namespace bnn
+#endif

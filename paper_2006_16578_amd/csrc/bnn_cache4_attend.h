@@ -1,0 +1,517 @@
+// Attention over the 4-bit cache, one template for single tokens, drafts, chunks and whole prompts; instantiated per head dimension in bnn_cache4_attend*.hip.
+//
+// Rows of queries that share a kv head -- its query heads, for one token or for several -- are the columns of the products, keys their rows:
+//   S^T [keys][rows] = K Q^T,   O^T [dim][rows] += V^T P^T   (v_mfma_f32_16x16x32_bf16).
+// A lane then holds, of 32 keys, the scores of ONE row at 8 keys, and exactly those eight are its operand of the second product: softmax weights never cross
+// lanes.  Four waves share the 16 * QT rows of a workgroup and take steps of 32 keys in turn, each with a running maximum and sum of its own; they meet in LDS once, at the end.
+// The cache's values are exact in bf16: the conversion instruction applies the scale.
+//
+// K: lane l supplies key l % 16 of a step's half and, of every 128 elements, the 32 of group l / 16: one 16-byte load and one scale.  Which elements a matrix
+// instruction contracts together does not matter as long as Q agrees.  V: its operand wants eight keys of one element in a lane, memory has the elements of
+// a key side by side; lane l loads, for its eight keys, the elements 8 (l % 16) .. + 7, converts pairs and interleaves the halves of registers.
+// Element 8 i + j is then row i of product j.  64 and 32 elements that are left over of a head dimension work alike with 4 and 2 elements.
+//
+// The maximum follows the scores in steps: it is raised (and the sums rescaled) only when a score passes it by more than 8 (as powers of two), which a wave tests without
+// any exchange between lanes; weights are at most 2^8 then, and nothing is lost, as weights and sums scale alike.
+//
+// Queries and weights enter the products as sums of 1 (bf16), 2 (fp16) or 3 (fp32) bf16 terms: queries exactly; weights to 8, 16 and 24 bits.
+#ifndef BNN_CACHE4_ATTEND_H
+#define BNN_CACHE4_ATTEND_H
+
+#include "bnn_cache4.h"
+
+namespace bnn {
+namespace {
+
+constexpr float C4_LOW = -3.0e38f;           // below every score: a row that has seen nothing
+constexpr float C4_SLACK = 8.f;
+
+template <int DTYPE> struct C4Type { using type = float; static constexpr int terms = 3; };
+template <> struct C4Type<BNN_BF16> { using type = __bf16; static constexpr int terms = 1; };
+template <> struct C4Type<BNN_F16> { using type = _Float16; static constexpr int terms = 2; };
+
+// The largest over the four lanes of a row (lanes l, l + 16, l + 32, l + 48).
+__device__ __forceinline__ float row_max(float v) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+__device__ __forceinline__ float row_sum(float v) {
+    auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+__device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    const u32x4 v = {a, b, c, d};
+    return __builtin_bit_cast(bf16x8, v);
+}
+__device__ __forceinline__ uint32_t pair_bits(bf16x2 v) { return __builtin_bit_cast(uint32_t, v); }
+
+// x as a sum of TERMS bf16 numbers, the largest first.
+template <int TERMS>
+__device__ __forceinline__ void split_terms(float x, __bf16 (&t)[TERMS]) {
+#pragma unroll
+    for (int i = 0; i < TERMS; ++i) {
+        t[i] = (__bf16)x;
+        x -= (float)t[i];
+    }
+}
+
+// The row tile of a workgroup: rows `row0 ..` of sequence b, counted over (token, head of the group), heads fastest.
+struct Tile4 {
+    int b, row0, rows;                       // rows of this tile, 0: nothing to do
+    Sequence4 s;
+};
+
+// ROWS: rows of a tile.  Tiles never span sequences, and with blocks of their own (sparse) never tokens.
+template <int ROWS, bool SPARSE>
+__device__ __forceinline__ Tile4 find_tile(const Attend4& a, int tile) {
+    Tile4 t = {};
+    if constexpr (SPARSE) {
+        const int per = (a.group + ROWS - 1) / ROWS, token = per == 1 ? tile : tile / per, part = tile - token * per;
+        t.b = c4_sequence_of(a.r, token);
+        t.s = c4_sequence(a.r, a.c, t.b);
+        const int i = token - t.s.first;
+        if (i < 0 || i >= t.s.rows) return t;
+        t.row0 = i * a.group + part * ROWS;
+        t.rows = min(ROWS, a.group - part * ROWS);
+        return t;
+    } else {
+        int local = 0;
+        if (a.r.start == nullptr) {
+            t.b = fast_div(tile, a.div_seq_tiles);
+            local = tile - t.b * a.seq_tiles;
+        } else {                             // 64 sequences at a time: a running count of their tiles
+            const int lane = (int)threadIdx.x & 63;
+            int before = 0;
+            bool found = false;
+            for (int b0 = 0; b0 < a.r.batch && !found; b0 += 64) {
+                int n = 0;
+                if (b0 + lane < a.r.batch) {
+                    const int first = min(max(a.r.start[b0 + lane], 0), a.r.tokens);
+                    n = (int)(((long long)(min(max(a.r.start[b0 + lane + 1], first), a.r.tokens) - first) * a.group + ROWS - 1) / ROWS);
+                }
+                int sum = n;
+#pragma unroll
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int other = __shfl_up(sum, d);
+                    if (lane >= d) sum += other;
+                }
+                const unsigned long long past = __ballot(before + sum > tile);
+                if (past != 0) {
+                    const int at = __ffsll(past) - 1;
+                    t.b = b0 + at;
+                    local = tile - (before + __shfl(sum, at) - __shfl(n, at));
+                    found = true;
+                }
+                before += __shfl(sum, 63);
+            }
+            if (!found) return t;
+            t.b = __builtin_amdgcn_readfirstlane(t.b);
+            local = __builtin_amdgcn_readfirstlane(local);
+        }
+        t.s = c4_sequence(a.r, a.c, t.b);
+        const int all = t.s.rows * a.group;
+        t.row0 = local * ROWS;
+        t.rows = max(0, min(ROWS, all - t.row0));
+        if (a.causal) {                      // the rows with the most keys first: short ones fill the gaps at the end
+            const int last = (all - 1) / ROWS - local;
+            t.row0 = max(last, 0) * ROWS;
+            t.rows = max(0, min(ROWS, all - t.row0));
+            if (last < 0) t.rows = 0;
+        }
+        return t;
+    }
+}
+
+// Steps of 32 keys that a tile visits.  Dense: step i covers keys 32 i .. + 31.  Sparse: halves of 16 keys of the listed blocks, in the list's order.
+struct Range4 {
+    int first, count;
+};
+template <bool SPARSE>
+__device__ __forceinline__ Range4 tile_steps(const Attend4& a, const Tile4& t) {
+    Range4 r = {0, 0};
+    if (t.rows <= 0) return r;
+    if constexpr (SPARSE) {
+        r.count = (int)((((long long)a.keep << (a.c.page_shift - 4)) + 1) >> 1);
+        return r;
+    } else {
+        const int base = t.s.length - t.s.rows;
+        const int top = a.causal ? base + fast_div(t.row0 + t.rows - 1, a.div_group) + 1 : t.s.length;      // keys below it are visited
+        const int low = a.window > 0 ? max(0, base + fast_div(t.row0, a.div_group) - a.window + 1) : 0;
+        if (top <= low) return r;
+        r.first = low >> 5;
+        r.count = ((top + 31) >> 5) - r.first;
+        return r;
+    }
+}
+
+// Eight values of K for one matrix instruction from a dword of codes.
+__device__ __forceinline__ bf16x8 eight_of(uint32_t codes, float scale) {
+    return as_bf16x8(pair_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)), pair_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
+                     pair_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)), pair_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3)));
+}
+
+// How a head dimension is cut up: pieces of 128, then 64, then 32 elements.
+template <int D>
+struct Pieces {
+    static constexpr int n128 = D / 128, n64 = D % 128 / 64, n32 = D % 64 / 32;
+    static constexpr int count = n128 + n64 + n32;
+    static constexpr int width(int p) { return p < n128 ? 128 : p < n128 + n64 ? 64 : 32; }
+    static constexpr int base(int p) { return p < n128 ? 128 * p : p < n128 + n64 ? 128 * n128 : 128 * n128 + 64 * n64; }
+};
+
+// A half step's place: 16 keys, all of one page.
+struct Half4 {
+    const uint8_t* at;                       // the record
+    int offset;                              // of the first key in the page
+    int key;                                 // its number in the sequence
+    bool there;
+};
+
+template <int D, int DTYPE, int QT, bool SPARSE>
+__global__ __launch_bounds__(256) void attend_kernel(Attend4 a) {
+    using T = typename C4Type<DTYPE>::type;
+    constexpr int TERMS = C4Type<DTYPE>::terms;
+    constexpr int ROWS = 16 * QT, M = D / 32, J = D / 16;
+    constexpr int LD = D + 4;                // floats of a row in LDS: rows of the 16 lanes fall on different banks
+    using P = Pieces<D>;
+    __shared__ __align__(16) float sums[4][16][LD];
+    __shared__ float stats[4][ROWS][2];
+
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int c = lane & 15, h4 = lane >> 4;
+    // heads fastest: workgroups go to the eight dies in turn, so with eight kv heads (or a divisor) those that share keys share a die's cache
+    int unit = (int)blockIdx.x;
+    const int rest = fast_div(unit, a.div_heads), head = unit - rest * a.c.kv_heads;
+    const int tile = fast_div(rest, a.div_splits), split = rest - tile * a.splits;
+    const Tile4 t = find_tile<ROWS, SPARSE>(a, tile);
+    if (t.rows <= 0) return;
+    const Range4 range = tile_steps<SPARSE>(a, t);
+    const int begin = split * a.chunk, end = min(range.count, begin + a.chunk);
+    if (split > 0 && begin >= end) return;
+    const bool whole = range.count <= a.chunk;
+
+    // Q, in the order of elements that K's loads give
+    bf16x8 q[QT][TERMS][M];
+    int pos[QT];                             // position of the lane's row; -1: no row
+    const int base = t.s.length - t.s.rows;
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        const int row = t.row0 + 16 * u + c;
+        const int token = fast_div(row, a.div_group), g = row - token * a.group;
+        const bool valid = 16 * u + c < t.rows;
+        pos[u] = valid ? base + token : -1;
+        const T* src = static_cast<const T*>(a.q) + (t.s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head;
+        static_for<P::count>([&](auto pc) {
+            constexpr int p = pc.value, W = P::width(p), B = P::base(p);
+#pragma unroll
+            for (int i = 0; i < W / 32; ++i) {
+                float x[8] = {};
+                if (valid) c4_load8(src + B + W / 4 * h4 + 8 * i, x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    __bf16 terms[TERMS];
+                    split_terms<TERMS>(x[e], terms);
+#pragma unroll
+                    for (int n = 0; n < TERMS; ++n) q[u][n][B / 32 + i][e] = terms[n];
+                }
+            }
+        });
+    }
+
+    f32x4 o[QT][J];
+    float m[QT], l[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        m[u] = C4_LOW;
+        l[u] = 0.f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    // keys that every row of the tile sees, if none is missing: [all_low, all_top]
+    const int top_first = a.causal ? base + fast_div(t.row0, a.div_group) : t.s.length - 1;
+    const int top_last = a.causal ? base + fast_div(t.row0 + t.rows - 1, a.div_group) : t.s.length - 1;
+    const int low_last = a.window > 0 ? base + fast_div(t.row0 + t.rows - 1, a.div_group) - a.window + 1 : 0;
+    const int32_t* list = SPARSE ? a.blocks + ((long long)(t.s.first + fast_div(t.row0, a.div_group)) * a.c.kv_heads + head) * a.keep : nullptr;
+    const int per_page = a.c.page >> 4;
+
+    for (int step = begin + wave; step < end; step += 4) {
+        Half4 half[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            int key;
+            bool listed = true;
+            if constexpr (SPARSE) {
+                const int i = 2 * step + s, entry = i / per_page;
+                const int block = entry < a.keep ? list[entry] : -1;
+                listed = block >= 0 && block < a.r.table_pages;
+                key = listed ? (block << a.c.page_shift) + 16 * (i - entry * per_page) : 0;
+            } else {
+                key = 32 * (range.first + step) + 16 * s;
+            }
+            const int page = listed ? c4_page(a.r, a.c, t.b, key) : -1;
+            half[s].there = page >= 0;
+            half[s].at = c4_record(a.c, page >= 0 ? page : 0, head);
+            half[s].offset = key & (a.c.page - 1);
+            half[s].key = key;
+        }
+        bool full = true;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) full = full && half[s].there && half[s].key + 15 <= top_first && half[s].key >= low_last;
+
+        // K and the scores
+        f32x4 score[QT][2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+#pragma unroll
+            for (int u = 0; u < QT; ++u) score[u][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const uint8_t* row = half[s].at + (half[s].offset + c) * (D / 2);
+            const uint8_t* exps = half[s].at + a.c.k_exps + half[s].offset + c;
+            static_for<P::count>([&](auto pc) {
+                constexpr int p = pc.value, W = P::width(p), B = P::base(p);
+                uint32_t codes[W / 32];
+                if constexpr (W == 128) {
+                    const u32x4 v = *reinterpret_cast<const u32x4*>(row + B / 2 + 16 * h4);
+                    codes[0] = v[0]; codes[1] = v[1]; codes[2] = v[2]; codes[3] = v[3];
+                } else if constexpr (W == 64) {
+                    const u32x2 v = *reinterpret_cast<const u32x2*>(row + B / 2 + 8 * h4);
+                    codes[0] = v[0]; codes[1] = v[1];
+                } else {
+                    codes[0] = *reinterpret_cast<const uint32_t*>(row + B / 2 + 4 * h4);
+                }
+                const float scale = c4_scale(exps[(B / 32 + h4 * W / 128) * a.c.page]);
+#pragma unroll
+                for (int i = 0; i < W / 32; ++i) {
+                    const bf16x8 k = eight_of(codes[i], scale);
+#pragma unroll
+                    for (int u = 0; u < QT; ++u)
+#pragma unroll
+                        for (int n = 0; n < TERMS; ++n) score[u][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[u][n][B / 32 + i], score[u][s], 0, 0, 0);
+                }
+            });
+        }
+        if (!full) {
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                const int top = a.causal ? pos[u] : top_last, low = a.window > 0 ? pos[u] - a.window + 1 : 0;
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int key = half[s].key + 4 * h4 + i;
+                        if (!(half[s].there && key <= top && key >= low)) score[u][s][i] = -__builtin_inff();
+                    }
+            }
+        }
+
+        // weights
+        bf16x8 w[QT][TERMS];
+        bf16x8 seen[QT];                     // 1 where the row sees the key (only made for steps with masks)
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            float high = score[u][0][0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) high = fmaxf(high, score[u][i >> 2][i & 3]);
+            if (__ballot(high * a.scale > m[u] + C4_SLACK) != 0) {
+                const float raised = fmaxf(m[u], row_max(high) * a.scale);
+                const float factor = __builtin_amdgcn_exp2f(m[u] - raised);
+                m[u] = raised;
+                l[u] *= factor;
+#pragma unroll
+                for (int j = 0; j < J; ++j) o[u][j] *= factor;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float x = __builtin_amdgcn_exp2f(fmaf(score[u][i >> 2][i & 3], a.scale, -m[u]));
+                l[u] += x;
+                __bf16 terms[TERMS];
+                split_terms<TERMS>(x, terms);
+#pragma unroll
+                for (int n = 0; n < TERMS; ++n) w[u][n][i] = terms[n];
+                seen[u][i] = score[u][i >> 2][i & 3] > -__builtin_inff() ? (__bf16)1.f : (__bf16)0.f;
+            }
+        }
+
+        // V
+        static_for<P::count>([&](auto pc) {
+            constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;       // E elements of each of 8 keys
+            uint32_t codes[8];
+            float scale[8];
+            bool bad = false;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint8_t* row = half[s].at + a.c.v_codes + (half[s].offset + 4 * h4) * (D / 2) + B / 2 + E / 2 * c;
+                const uint32_t bytes = *reinterpret_cast<const uint32_t*>(half[s].at + a.c.v_exps + (B / 32 + c * E / 32) * a.c.page + half[s].offset + 4 * h4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if constexpr (E == 8) codes[4 * s + i] = *reinterpret_cast<const uint32_t*>(row + i * (D / 2));
+                    else if constexpr (E == 4) codes[4 * s + i] = *reinterpret_cast<const uint16_t*>(row + i * (D / 2));
+                    else codes[4 * s + i] = row[i * (D / 2)];
+                    uint32_t byte = bytes >> 8 * i & 255u;
+                    if (!full && byte > C4_EXP_MAX) {
+                        bad = true;
+                        byte = 0;
+                    }
+                    scale[4 * s + i] = c4_scale(byte);
+                }
+            }
+            static_for<E / 2>([&](auto ec) {
+                constexpr int e = ec.value;
+                uint32_t v[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[i] = pair_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale[i], e));
+                const bf16x8 even = as_bf16x8(__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u),
+                                              __builtin_amdgcn_perm(v[5], v[4], 0x05040100u), __builtin_amdgcn_perm(v[7], v[6], 0x05040100u));
+                const bf16x8 odd = as_bf16x8(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u),
+                                             __builtin_amdgcn_perm(v[5], v[4], 0x07060302u), __builtin_amdgcn_perm(v[7], v[6], 0x07060302u));
+#pragma unroll
+                for (int u = 0; u < QT; ++u)
+#pragma unroll
+                    for (int n = 0; n < TERMS; ++n) {
+                        o[u][B / 16 + 2 * e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(even, w[u][n], o[u][B / 16 + 2 * e], 0, 0, 0);
+                        o[u][B / 16 + 2 * e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, w[u][n], o[u][B / 16 + 2 * e + 1], 0, 0, 0);
+                    }
+            });
+            // Where a mask is at work, a NaN must reach the rows that see its key and no other: its values were taken as finite above, and here every row counts the
+            // NaN groups among the keys that it sees.
+            if (!full && __ballot(bad) != 0) {
+                bf16x8 marks;
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    const uint32_t bytes = *reinterpret_cast<const uint32_t*>(half[s].at + a.c.v_exps + (B / 32 + c * E / 32) * a.c.page + half[s].offset + 4 * h4);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) marks[4 * s + i] = (bytes >> 8 * i & 255u) > C4_EXP_MAX ? (__bf16)1.f : (__bf16)0.f;
+                }
+#pragma unroll
+                for (int u = 0; u < QT; ++u) {
+                    const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(marks, seen[u], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                    for (int j = 0; j < E; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (count[i] > 0.f) o[u][B / 16 + j][i] = __builtin_nanf("");
+                }
+            }
+        });
+    }
+
+    // The waves meet: 16 rows at a time.
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        const float sum = row_sum(l[u]);
+        if (h4 == 0) {
+            stats[wave][16 * u + c][0] = m[u];
+            stats[wave][16 * u + c][1] = sum;
+        }
+    }
+    const long long slot = ((long long)tile * a.c.kv_heads + head) * a.splits + split;
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        if (16 * u >= t.rows) break;
+        if (u > 0) __syncthreads();
+        static_for<P::count>([&](auto pc) {
+            constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < E; ++j) sums[wave][c][B + E * (4 * h4 + i) + j] = o[u][B / 16 + j][i];
+        });
+        __syncthreads();
+        for (int x = (int)threadIdx.x; x < 16 * (D / 8); x += 256) {
+            const int row = x / (D / 8), d = x % (D / 8) * 8, r = 16 * u + row;
+            if (r >= t.rows) continue;
+            float high = C4_LOW, total = 0.f, y[8] = {};
+#pragma unroll
+            for (int v = 0; v < 4; ++v) high = fmaxf(high, stats[v][r][0]);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const float f = __builtin_amdgcn_exp2f(stats[v][r][0] - high);
+                total = fmaf(stats[v][r][1], f, total);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = fmaf(sums[v][row][d + e], f, y[e]);
+            }
+            if (whole) {
+                const int token = fast_div(t.row0 + r, a.div_group), g = t.row0 + r - token * a.group;
+                const long long at = ((long long)(t.s.first + token) * a.c.kv_heads + head) * a.group + g;
+                const float f = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = total == 0.f ? 0.f : y[e] * f;
+                c4_store8(static_cast<T*>(a.out) + at * D + d, y);
+                if (a.lse != nullptr && d == 0) a.lse[at] = total == 0.f ? -__builtin_inff() : (high + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+            } else {
+                c4_store8(a.part + (slot * ROWS + r) * D + d, y);
+                if (d == 0) {
+                    a.part_ml[(slot * ROWS + r) * 2] = high;
+                    a.part_ml[(slot * ROWS + r) * 2 + 1] = total;
+                }
+            }
+        }
+    }
+}
+
+// Joins the parts of the tiles whose keys were cut up.
+template <int D, int DTYPE, int QT, bool SPARSE>
+__global__ __launch_bounds__(256) void join_kernel(Attend4 a) {
+    using T = typename C4Type<DTYPE>::type;
+    constexpr int ROWS = 16 * QT;
+    const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads, tile = rest;
+    const Tile4 t = find_tile<ROWS, SPARSE>(a, tile);
+    if (t.rows <= 0) return;
+    const Range4 range = tile_steps<SPARSE>(a, t);
+    if (range.count <= a.chunk) return;      // written already
+    const int parts = (range.count + a.chunk - 1) / a.chunk;
+    const long long slot = ((long long)tile * a.c.kv_heads + head) * a.splits;
+    for (int x = (int)threadIdx.x; x < t.rows * (D / 8); x += 256) {
+        const int r = x / (D / 8), d = x % (D / 8) * 8;
+        const float* ml = a.part_ml + (slot * ROWS + r) * 2;
+        float high = C4_LOW, total = 0.f, y[8] = {};
+        for (int p = 0; p < parts; ++p) high = fmaxf(high, ml[(long long)p * ROWS * 2]);
+        for (int p = 0; p < parts; ++p) {
+            const float f = __builtin_amdgcn_exp2f(ml[(long long)p * ROWS * 2] - high);
+            total = fmaf(ml[(long long)p * ROWS * 2 + 1], f, total);
+            float part[8];
+            c4_load8(a.part + ((slot + p) * ROWS + r) * D + d, part);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = fmaf(part[e], f, y[e]);
+        }
+        const int token = fast_div(t.row0 + r, a.div_group), g = t.row0 + r - token * a.group;
+        const long long at = ((long long)(t.s.first + token) * a.c.kv_heads + head) * a.group + g;
+        const float f = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] = total == 0.f ? 0.f : y[e] * f;
+        c4_store8(static_cast<T*>(a.out) + at * D + d, y);
+        if (a.lse != nullptr && d == 0) a.lse[at] = total == 0.f ? -__builtin_inff() : (high + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+    }
+}
+
+template <int D, int DTYPE, int QT, bool SPARSE>
+int launch_attend(const Attend4& a, hipStream_t s) {
+    const unsigned heads = (unsigned)a.c.kv_heads;
+    launch(attend_kernel<D, DTYPE, QT, SPARSE>, dim3((unsigned)a.tiles * (unsigned)a.splits * heads), dim3(256), 0, s, a);
+    if (a.splits > 1) launch(join_kernel<D, DTYPE, QT, SPARSE>, dim3((unsigned)a.tiles * heads), dim3(256), 0, s, a);
+    return check_launch();
+}
+
+template <int D, int DTYPE>
+int launch_attend_rows(const Attend4& a, int qtiles, hipStream_t s) {
+    if (a.blocks != nullptr) return launch_attend<D, DTYPE, 1, true>(a, s);
+    if (qtiles == 1) return launch_attend<D, DTYPE, 1, false>(a, s);
+    if constexpr (cache4_qtiles(D, DTYPE) >= 2) if (qtiles == 2) return launch_attend<D, DTYPE, 2, false>(a, s);
+    if constexpr (cache4_qtiles(D, DTYPE) >= 4) if (qtiles == 4) return launch_attend<D, DTYPE, 4, false>(a, s);
+    return BNN_ERR_UNSUPPORTED;
+}
+
+template <int D>
+int launch_attend_type(const Attend4& a, int dtype, int qtiles, hipStream_t s) {
+    if (dtype == BNN_BF16) return launch_attend_rows<D, BNN_BF16>(a, qtiles, s);
+    if (dtype == BNN_F16) return launch_attend_rows<D, BNN_F16>(a, qtiles, s);
+    return launch_attend_rows<D, BNN_F32>(a, qtiles, s);
+}
+
+}  // namespace
+}  // namespace bnn
+#endif

@@ -1,0 +1,6 @@
+// Attention over the 4-bit cache, heads of 256 elements.
+#include "bnn_cache4_attend.h"
+
+namespace bnn {
+int launch_cache4_attend256(const Attend4& a, int dtype, int qtiles, hipStream_t s) { return launch_attend_type<256>(a, dtype, qtiles, s); }
+}  // namespace bnn

@@ -30,6 +30,8 @@ template <int DTYPE> struct C4Type { using type = float; static constexpr int te
 template <> struct C4Type<BNN_BF16> { using type = __bf16; static constexpr int terms = 1; };
 template <> struct C4Type<BNN_F16> { using type = _Float16; static constexpr int terms = 2; };
 
+template <int DTYPE> constexpr int TERMS4 = C4Type<DTYPE>::terms;
+
 // The largest over the four lanes of a row (lanes l, l + 16, l + 32, l + 48).
 __device__ __forceinline__ float row_max(float v) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -164,16 +166,74 @@ struct Pieces {
     static constexpr int base(int p) { return p < n128 ? 128 * p : p < n128 + n64 ? 128 * n128 : 128 * n128 + 64 * n64; }
 };
 
-// A half step's place: 16 keys, all of one page.
+// Where the 16 keys of half a step lie: all in one page.
 struct Half4 {
-    const uint8_t* at;                       // the record
-    int offset;                              // of the first key in the page
-    int key;                                 // its number in the sequence
-    bool there;
+    int page;                                // -1: nowhere
+    int key;                                 // number of the first in the sequence
 };
 
+// What a lane holds of a step's codes and scales between the loads and the products.
+template <int D>
+struct Raw4 {
+    using P = Pieces<D>;
+    uint32_t k[2][D / 32];
+    uint32_t k_exp[2][P::count];
+    uint32_t v[P::count][8];
+    uint32_t v_exp[P::count][2];
+};
+
+template <int D>
+__device__ __forceinline__ void load_k(const Cache4& c, const Half4 (&half)[2], int head, int lane, Raw4<D>& raw) {
+    using P = Pieces<D>;
+    const int col = lane & 15, h4 = lane >> 4;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const uint8_t* rec = c4_record(c, max(half[s].page, 0), head);
+        const int offset = half[s].key & (c.page - 1);
+        const uint8_t* row = rec + (offset + col) * (D / 2);
+        const uint8_t* exps = rec + c.k_exps + offset + col;
+        static_for<P::count>([&](auto pc) {
+            constexpr int p = pc.value, W = P::width(p), B = P::base(p);
+            if constexpr (W == 128) {
+                const u32x4 v = *reinterpret_cast<const u32x4*>(row + B / 2 + 16 * h4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) raw.k[s][B / 32 + i] = v[i];
+            } else if constexpr (W == 64) {
+                const u32x2 v = *reinterpret_cast<const u32x2*>(row + B / 2 + 8 * h4);
+                raw.k[s][B / 32] = v[0];
+                raw.k[s][B / 32 + 1] = v[1];
+            } else {
+                raw.k[s][B / 32] = *reinterpret_cast<const uint32_t*>(row + B / 2 + 4 * h4);
+            }
+            raw.k_exp[s][p] = exps[(B / 32 + h4 * W / 128) * c.page];
+        });
+    }
+}
+
+template <int D>
+__device__ __forceinline__ void load_v(const Cache4& c, const Half4 (&half)[2], int head, int lane, Raw4<D>& raw) {
+    using P = Pieces<D>;
+    const int col = lane & 15, h4 = lane >> 4;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const uint8_t* rec = c4_record(c, max(half[s].page, 0), head);
+        const int offset = (half[s].key & (c.page - 1)) + 4 * h4;
+        static_for<P::count>([&](auto pc) {
+            constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;       // E elements of each of 8 keys
+            const uint8_t* row = rec + c.v_codes + offset * (D / 2) + B / 2 + E / 2 * col;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (E == 8) raw.v[p][4 * s + i] = *reinterpret_cast<const uint32_t*>(row + i * (D / 2));
+                else if constexpr (E == 4) raw.v[p][4 * s + i] = *reinterpret_cast<const uint16_t*>(row + i * (D / 2));
+                else raw.v[p][4 * s + i] = row[i * (D / 2)];
+            }
+            raw.v_exp[p][s] = *reinterpret_cast<const uint32_t*>(rec + c.v_exps + (B / 32 + col * E / 32) * c.page + offset);
+        });
+    }
+}
+
 template <int D, int DTYPE, int QT, bool SPARSE>
-__global__ __launch_bounds__(256) void attend_kernel(Attend4 a) {
+__global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ? 1 : 2) void attend_kernel(Attend4 a) {
     using T = typename C4Type<DTYPE>::type;
     constexpr int TERMS = C4Type<DTYPE>::terms;
     constexpr int ROWS = 16 * QT, M = D / 32, J = D / 16;
@@ -195,10 +255,38 @@ __global__ __launch_bounds__(256) void attend_kernel(Attend4 a) {
     if (split > 0 && begin >= end) return;
     const bool whole = range.count <= a.chunk;
 
+    const int base = t.s.length - t.s.rows;
+    const int32_t* list = SPARSE ? a.blocks + ((long long)(t.s.first + fast_div(t.row0, a.div_group)) * a.c.kv_heads + head) * a.keep : nullptr;
+    const int per_shift = a.c.page_shift - 4;                        // halves of steps in a page
+    auto locate = [&](int step, Half4 (&half)[2]) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            bool listed = true;
+            if constexpr (SPARSE) {
+                const int i = 2 * step + s, entry = i >> per_shift;
+                const int block = entry < a.keep ? list[entry] : -1;
+                listed = block >= 0 && block < a.r.table_pages;
+                half[s].key = listed ? (block << a.c.page_shift) + 16 * (i - (entry << per_shift)) : 0;
+            } else {
+                half[s].key = 32 * (range.first + step) + 16 * s;
+            }
+            half[s].page = __builtin_amdgcn_readfirstlane(listed ? c4_page(a.r, a.c, t.b, half[s].key) : -1);
+            half[s].key = __builtin_amdgcn_readfirstlane(half[s].key);
+        }
+    };
+
+    Half4 now[2], next[2];
+    Raw4<D> raw;
+    if (begin + wave < end) {
+        locate(begin + wave, now);
+        load_k<D>(a.c, now, head, lane, raw);
+        load_v<D>(a.c, now, head, lane, raw);
+        locate(min(begin + wave + 4, end - 1), next);
+    }
+
     // Q, in the order of elements that K's loads give
     bf16x8 q[QT][TERMS][M];
     int pos[QT];                             // position of the lane's row; -1: no row
-    const int base = t.s.length - t.s.rows;
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         const int row = t.row0 + 16 * u + c;
@@ -232,36 +320,14 @@ __global__ __launch_bounds__(256) void attend_kernel(Attend4 a) {
 #pragma unroll
         for (int j = 0; j < J; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    // keys that every row of the tile sees, if none is missing: [all_low, all_top]
+    // keys that every row of the tile sees, if none is missing: [low_last, top_first]
     const int top_first = a.causal ? base + fast_div(t.row0, a.div_group) : t.s.length - 1;
-    const int top_last = a.causal ? base + fast_div(t.row0 + t.rows - 1, a.div_group) : t.s.length - 1;
     const int low_last = a.window > 0 ? base + fast_div(t.row0 + t.rows - 1, a.div_group) - a.window + 1 : 0;
-    const int32_t* list = SPARSE ? a.blocks + ((long long)(t.s.first + fast_div(t.row0, a.div_group)) * a.c.kv_heads + head) * a.keep : nullptr;
-    const int per_page = a.c.page >> 4;
 
     for (int step = begin + wave; step < end; step += 4) {
-        Half4 half[2];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            int key;
-            bool listed = true;
-            if constexpr (SPARSE) {
-                const int i = 2 * step + s, entry = i / per_page;
-                const int block = entry < a.keep ? list[entry] : -1;
-                listed = block >= 0 && block < a.r.table_pages;
-                key = listed ? (block << a.c.page_shift) + 16 * (i - entry * per_page) : 0;
-            } else {
-                key = 32 * (range.first + step) + 16 * s;
-            }
-            const int page = listed ? c4_page(a.r, a.c, t.b, key) : -1;
-            half[s].there = page >= 0;
-            half[s].at = c4_record(a.c, page >= 0 ? page : 0, head);
-            half[s].offset = key & (a.c.page - 1);
-            half[s].key = key;
-        }
         bool full = true;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) full = full && half[s].there && half[s].key + 15 <= top_first && half[s].key >= low_last;
+        for (int s = 0; s < 2; ++s) full = full && now[s].page >= 0 && now[s].key + 15 <= top_first && now[s].key >= low_last;
 
         // K and the scores
         f32x4 score[QT][2];
@@ -269,24 +335,12 @@ __global__ __launch_bounds__(256) void attend_kernel(Attend4 a) {
         for (int s = 0; s < 2; ++s) {
 #pragma unroll
             for (int u = 0; u < QT; ++u) score[u][s] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const uint8_t* row = half[s].at + (half[s].offset + c) * (D / 2);
-            const uint8_t* exps = half[s].at + a.c.k_exps + half[s].offset + c;
             static_for<P::count>([&](auto pc) {
                 constexpr int p = pc.value, W = P::width(p), B = P::base(p);
-                uint32_t codes[W / 32];
-                if constexpr (W == 128) {
-                    const u32x4 v = *reinterpret_cast<const u32x4*>(row + B / 2 + 16 * h4);
-                    codes[0] = v[0]; codes[1] = v[1]; codes[2] = v[2]; codes[3] = v[3];
-                } else if constexpr (W == 64) {
-                    const u32x2 v = *reinterpret_cast<const u32x2*>(row + B / 2 + 8 * h4);
-                    codes[0] = v[0]; codes[1] = v[1];
-                } else {
-                    codes[0] = *reinterpret_cast<const uint32_t*>(row + B / 2 + 4 * h4);
-                }
-                const float scale = c4_scale(exps[(B / 32 + h4 * W / 128) * a.c.page]);
+                const float scale = c4_scale(raw.k_exp[s][p]);
 #pragma unroll
                 for (int i = 0; i < W / 32; ++i) {
-                    const bf16x8 k = eight_of(codes[i], scale);
+                    const bf16x8 k = eight_of(raw.k[s][B / 32 + i], scale);
 #pragma unroll
                     for (int u = 0; u < QT; ++u)
 #pragma unroll
@@ -294,23 +348,27 @@ __global__ __launch_bounds__(256) void attend_kernel(Attend4 a) {
                 }
             });
         }
+        // the next step's K into the same registers; where the one after it lies
+        load_k<D>(a.c, next, head, lane, raw);
+        Half4 after[2];
+        locate(min(step + 8, end - 1), after);
+
         if (!full) {
 #pragma unroll
             for (int u = 0; u < QT; ++u) {
-                const int top = a.causal ? pos[u] : top_last, low = a.window > 0 ? pos[u] - a.window + 1 : 0;
+                const int top = a.causal ? pos[u] : t.s.length - 1, low = a.window > 0 ? pos[u] - a.window + 1 : 0;
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int key = half[s].key + 4 * h4 + i;
-                        if (!(half[s].there && key <= top && key >= low)) score[u][s][i] = -__builtin_inff();
+                        const int key = now[s].key + 4 * h4 + i;
+                        if (!(now[s].page >= 0 && key <= top && key >= low)) score[u][s][i] = -__builtin_inff();
                     }
             }
         }
 
         // weights
         bf16x8 w[QT][TERMS];
-        bf16x8 seen[QT];                     // 1 where the row sees the key (only made for steps with masks)
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
             float high = score[u][0][0];
@@ -332,38 +390,48 @@ __global__ __launch_bounds__(256) void attend_kernel(Attend4 a) {
                 split_terms<TERMS>(x, terms);
 #pragma unroll
                 for (int n = 0; n < TERMS; ++n) w[u][n][i] = terms[n];
-                seen[u][i] = score[u][i >> 2][i & 3] > -__builtin_inff() ? (__bf16)1.f : (__bf16)0.f;
             }
         }
 
         // V
         static_for<P::count>([&](auto pc) {
             constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;       // E elements of each of 8 keys
-            uint32_t codes[8];
             float scale[8];
-            bool bad = false;
+            uint32_t bad = 0;                // keys with a NaN group
+            if (!full) {
+                // Where a mask is at work, a NaN must reach the rows that see its key and no other: its values are taken as finite here, and every row
+                // counts the NaN groups among the keys that it sees.
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const uint8_t* row = half[s].at + a.c.v_codes + (half[s].offset + 4 * h4) * (D / 2) + B / 2 + E / 2 * c;
-                const uint32_t bytes = *reinterpret_cast<const uint32_t*>(half[s].at + a.c.v_exps + (B / 32 + c * E / 32) * a.c.page + half[s].offset + 4 * h4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if constexpr (E == 8) codes[4 * s + i] = *reinterpret_cast<const uint32_t*>(row + i * (D / 2));
-                    else if constexpr (E == 4) codes[4 * s + i] = *reinterpret_cast<const uint16_t*>(row + i * (D / 2));
-                    else codes[4 * s + i] = row[i * (D / 2)];
-                    uint32_t byte = bytes >> 8 * i & 255u;
-                    if (!full && byte > C4_EXP_MAX) {
-                        bad = true;
-                        byte = 0;
+                for (int i = 0; i < 8; ++i)
+                    if ((raw.v_exp[p][i >> 2] >> 8 * (i & 3) & 255u) > C4_EXP_MAX) {
+                        bad |= 1u << i;
+                        raw.v_exp[p][i >> 2] &= ~(255u << 8 * (i & 3));
                     }
-                    scale[4 * s + i] = c4_scale(byte);
+                if (__ballot(bad != 0) != 0) {
+                    bf16x8 marks;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) marks[i] = (bad >> i & 1u) ? (__bf16)1.f : (__bf16)0.f;
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) {
+                        bf16x8 seen;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) seen[i] = score[u][i >> 2][i & 3] == -__builtin_inff() ? (__bf16)0.f : (__bf16)1.f;
+                        const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(marks, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < E; ++j)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (count[i] > 0.f) o[u][B / 16 + j][i] = __builtin_nanf("");
+                    }
                 }
             }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) scale[i] = c4_scale(raw.v_exp[p][i >> 2] >> 8 * (i & 3) & 255u);
             static_for<E / 2>([&](auto ec) {
                 constexpr int e = ec.value;
                 uint32_t v[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = pair_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale[i], e));
+                for (int i = 0; i < 8; ++i) v[i] = pair_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw.v[p][i], scale[i], e));
                 const bf16x8 even = as_bf16x8(__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u),
                                               __builtin_amdgcn_perm(v[5], v[4], 0x05040100u), __builtin_amdgcn_perm(v[7], v[6], 0x05040100u));
                 const bf16x8 odd = as_bf16x8(__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u),
@@ -376,27 +444,13 @@ __global__ __launch_bounds__(256) void attend_kernel(Attend4 a) {
                         o[u][B / 16 + 2 * e + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(odd, w[u][n], o[u][B / 16 + 2 * e + 1], 0, 0, 0);
                     }
             });
-            // Where a mask is at work, a NaN must reach the rows that see its key and no other: its values were taken as finite above, and here every row counts the
-            // NaN groups among the keys that it sees.
-            if (!full && __ballot(bad) != 0) {
-                bf16x8 marks;
-#pragma unroll
-                for (int s = 0; s < 2; ++s) {
-                    const uint32_t bytes = *reinterpret_cast<const uint32_t*>(half[s].at + a.c.v_exps + (B / 32 + c * E / 32) * a.c.page + half[s].offset + 4 * h4);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) marks[4 * s + i] = (bytes >> 8 * i & 255u) > C4_EXP_MAX ? (__bf16)1.f : (__bf16)0.f;
-                }
-#pragma unroll
-                for (int u = 0; u < QT; ++u) {
-                    const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(marks, seen[u], f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                    for (int j = 0; j < E; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (count[i] > 0.f) o[u][B / 16 + j][i] = __builtin_nanf("");
-                }
-            }
         });
+        load_v<D>(a.c, next, head, lane, raw);
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            now[s] = next[s];
+            next[s] = after[s];
+        }
     }
 
     // The waves meet: 16 rows at a time.
@@ -453,46 +507,65 @@ __global__ __launch_bounds__(256) void attend_kernel(Attend4 a) {
     }
 }
 
-// Joins the parts of the tiles whose keys were cut up.
+// Joins the parts of the tiles whose keys were cut up: a workgroup per row of a tile.  D / 8 lanes hold a row's elements, eight each; the groups of so many lanes take
+// the parts in turn and meet in LDS.
 template <int D, int DTYPE, int QT, bool SPARSE>
 __global__ __launch_bounds__(256) void join_kernel(Attend4 a) {
     using T = typename C4Type<DTYPE>::type;
-    constexpr int ROWS = 16 * QT;
-    const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads, tile = rest;
+    constexpr int ROWS = 16 * QT, LANES = D / 8, GROUPS = 256 / LANES;
+    __shared__ __align__(16) float sums[GROUPS][D + 4];
+    __shared__ float totals[GROUPS];
+    const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads, tile = rest, r = (int)blockIdx.y;
     const Tile4 t = find_tile<ROWS, SPARSE>(a, tile);
-    if (t.rows <= 0) return;
+    if (r >= t.rows) return;
     const Range4 range = tile_steps<SPARSE>(a, t);
     if (range.count <= a.chunk) return;      // written already
     const int parts = (range.count + a.chunk - 1) / a.chunk;
-    const long long slot = ((long long)tile * a.c.kv_heads + head) * a.splits;
-    for (int x = (int)threadIdx.x; x < t.rows * (D / 8); x += 256) {
-        const int r = x / (D / 8), d = x % (D / 8) * 8;
-        const float* ml = a.part_ml + (slot * ROWS + r) * 2;
-        float high = C4_LOW, total = 0.f, y[8] = {};
-        for (int p = 0; p < parts; ++p) high = fmaxf(high, ml[(long long)p * ROWS * 2]);
-        for (int p = 0; p < parts; ++p) {
+    const long long slot = (((long long)tile * a.c.kv_heads + head) * a.splits) * ROWS + r;
+    const int group = (int)threadIdx.x / LANES, d = (int)threadIdx.x % LANES * 8;
+    const float* ml = a.part_ml + slot * 2;
+    float high = C4_LOW, total = 0.f, y[8] = {};
+    for (int p = (int)threadIdx.x & 63; p < parts; p += 64) high = fmaxf(high, ml[(long long)p * ROWS * 2]);
+    high = row_max(high);
+#pragma unroll
+    for (int x = 1; x < 16; x <<= 1) high = fmaxf(high, __shfl_xor(high, x));
+    if (group < GROUPS) {
+        for (int p = group; p < parts; p += GROUPS) {
             const float f = __builtin_amdgcn_exp2f(ml[(long long)p * ROWS * 2] - high);
             total = fmaf(ml[(long long)p * ROWS * 2 + 1], f, total);
             float part[8];
-            c4_load8(a.part + ((slot + p) * ROWS + r) * D + d, part);
+            c4_load8(a.part + (slot + (long long)p * ROWS) * D + d, part);
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = fmaf(part[e], f, y[e]);
         }
-        const int token = fast_div(t.row0 + r, a.div_group), g = t.row0 + r - token * a.group;
-        const long long at = ((long long)(t.s.first + token) * a.c.kv_heads + head) * a.group + g;
-        const float f = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = total == 0.f ? 0.f : y[e] * f;
-        c4_store8(static_cast<T*>(a.out) + at * D + d, y);
-        if (a.lse != nullptr && d == 0) a.lse[at] = total == 0.f ? -__builtin_inff() : (high + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+        c4_store8(&sums[group][d], y);
+        if (d == 0) totals[group] = total;
     }
+    __syncthreads();
+    if (group > 0) return;
+    const int groups = min(GROUPS, parts);
+    for (int g = 1; g < groups; ++g) {
+        float part[8];
+        c4_load8(&sums[g][d], part);
+        total += totals[g];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) y[e] += part[e];
+    }
+    const int token = fast_div(t.row0 + r, a.div_group), g = t.row0 + r - token * a.group;
+    const long long at = ((long long)(t.s.first + token) * a.c.kv_heads + head) * a.group + g;
+    const float f = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = total == 0.f ? 0.f : y[e] * f;
+    c4_store8(static_cast<T*>(a.out) + at * D + d, y);
+    if (a.lse != nullptr && d == 0) a.lse[at] = total == 0.f ? -__builtin_inff() : (high + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
 }
 
 template <int D, int DTYPE, int QT, bool SPARSE>
 int launch_attend(const Attend4& a, hipStream_t s) {
     const unsigned heads = (unsigned)a.c.kv_heads;
     launch(attend_kernel<D, DTYPE, QT, SPARSE>, dim3((unsigned)a.tiles * (unsigned)a.splits * heads), dim3(256), 0, s, a);
-    if (a.splits > 1) launch(join_kernel<D, DTYPE, QT, SPARSE>, dim3((unsigned)a.tiles * heads), dim3(256), 0, s, a);
+    const unsigned rows = (unsigned)(SPARSE && a.group < 16 ? a.group : 16 * QT);
+    if (a.splits > 1) launch(join_kernel<D, DTYPE, QT, SPARSE>, dim3((unsigned)a.tiles * heads, rows), dim3(256), 0, s, a);
     return check_launch();
 }
 

@@ -835,7 +835,10 @@ class Cache4:
         if data.shape[1] != kv_heads or data.shape[2] != record or pages not in (None, data.shape[0]):
             raise ValueError("data must be [pages][kv_heads][%d]" % record)
         self.data, self.kv_heads, self.head_dim, self.page, self.signs = data, int(kv_heads), int(head_dim), int(page), bool(signs)
-        self._c = _Cache4Struct(data.data_ptr(), data.shape[0], self.kv_heads, self.head_dim, self.page, int(self.signs))
+        self._plain = (data, self.kv_heads, self.head_dim, self.page, int(self.signs))         # what the native module takes
+
+    def _struct(self):
+        return ctypes.byref(_Cache4Struct(self.data.data_ptr(), self.data.shape[0], self.kv_heads, self.head_dim, self.page, int(self.signs)))
 
     def _rows(self, table, lens, start, tokens):
         _dev(table, torch.int32, 2, "table"); _dev(lens, torch.int32, 1, "lens")
@@ -865,36 +868,45 @@ class Cache4:
 
     def write(self, k, v, table, lens, start=None):
         """Quantises k, v [tokens][kv_heads][head_dim], the newest tokens of every sequence, into the cache."""
+        if (_native or _load_native()).cache4_write(*self._plain, table, lens, start, k, v):
+            return
         code, kt, kh = self._elements(k, self.kv_heads, "k")
         code_v, vt, vh = self._elements(v, self.kv_heads, "v")
         if code != code_v or k.shape != v.shape:
             raise ValueError("k and v must agree in type and shape")
         rows = self._rows(table, lens, start, k.shape[0])
         with _on(k):
-            _check(load().bnn_cache4_write(ctypes.byref(self._c), ctypes.byref(rows), _ptr(k), _ptr(v), code, kt, kh, vt, vh, _stream(k)), "bnn_cache4_write")
+            _check(load().bnn_cache4_write(self._struct(), ctypes.byref(rows), _ptr(k), _ptr(v), code, kt, kh, vt, vh, _stream(k)), "bnn_cache4_write")
 
     def read(self, table, lens, start=None, tokens: int | None = None, dtype=torch.bfloat16):
         """(k, v) [tokens][kv_heads][head_dim]: the newest tokens of every sequence as the cache holds them.  tokens: rows in all (default: one of every sequence)."""
         if dtype not in _ELEMENTS:
             raise TypeError("fp32, bf16 or fp16 expected, got %s" % dtype)
         tokens = table.shape[0] if tokens is None else int(tokens)
+        done = (_native or _load_native()).cache4_read(*self._plain, table, lens, start, tokens, _ELEMENTS[dtype])
+        if done is not None:
+            return done
         rows = self._rows(table, lens, start, tokens)
         k, v = (torch.empty((tokens, self.kv_heads, self.head_dim), dtype=dtype, device=self.data.device) for _ in range(2))
         with _on(k):
-            _check(load().bnn_cache4_read(ctypes.byref(self._c), ctypes.byref(rows), _ptr(k), _ptr(v), _ELEMENTS[dtype], _stream(k)), "bnn_cache4_read")
+            _check(load().bnn_cache4_read(self._struct(), ctypes.byref(rows), _ptr(k), _ptr(v), _ELEMENTS[dtype], _stream(k)), "bnn_cache4_read")
         return k, v
 
     def select(self, q, table, lens, keep: int, start=None, first: int = 1, last: int = 1, workspace=None):
         """int32 [tokens][kv_heads][keep]: the blocks (pages of a sequence) that every row of q [tokens][heads][head_dim] attends to, by the
         agreement of sign bits; the first `first` and the `last` most recent always; ascending, the rest -1."""
+        if workspace is None:
+            done = (_native or _load_native()).cache4_select(*self._plain, table, lens, start, q, keep, first, last)
+            if done is not None:
+                return done
         code, qt, qh = self._elements(q, None, "q")
         rows = self._rows(table, lens, start, q.shape[0])
         blocks = torch.empty((q.shape[0], self.kv_heads, max(int(keep), 0)), dtype=torch.int32, device=q.device)
         if workspace is None:
-            need = int(load().bnn_cache4_select_workspace_bytes(ctypes.byref(self._c), ctypes.byref(rows)))
+            need = int(load().bnn_cache4_select_workspace_bytes(self._struct(), ctypes.byref(rows)))
             workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
         with _on(q):
-            _check(load().bnn_cache4_select(ctypes.byref(self._c), ctypes.byref(rows), _ptr(q), code, qt, qh, q.shape[1], int(keep), int(first), int(last),
+            _check(load().bnn_cache4_select(self._struct(), ctypes.byref(rows), _ptr(q), code, qt, qh, q.shape[1], int(keep), int(first), int(last),
                                             _ptr(blocks), _ptr(workspace), ctypes.c_size_t(workspace.numel()), _stream(q)), "bnn_cache4_select")
         return blocks
 
@@ -902,6 +914,11 @@ class Cache4:
                out=None, workspace=None):
         """Attention of q [tokens][heads][head_dim], the newest tokens of every sequence, over the cache -> [tokens][heads][head_dim] of q's type (and
         the logarithm of the weights' sum, fp32 [tokens][heads]).  blocks: only those (from select).  scale: 1 / sqrt(head_dim) by default."""
+        scale = self.head_dim ** -0.5 if scale is None else float(scale)
+        if out is None and workspace is None:
+            done = (_native or _load_native()).cache4_attend(*self._plain, table, lens, start, q, scale, causal, window, blocks, want_lse)
+            if done is not None:
+                return done
         code, qt, qh = self._elements(q, None, "q")
         rows = self._rows(table, lens, start, q.shape[0])
         keep = 0
@@ -916,11 +933,10 @@ class Cache4:
             raise ValueError("out must have q's shape and device")
         lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device) if want_lse else None
         if workspace is None:
-            need = int(load().bnn_cache4_attend_workspace_bytes(ctypes.byref(self._c), ctypes.byref(rows), code, q.shape[1], int(window), keep))
+            need = int(load().bnn_cache4_attend_workspace_bytes(self._struct(), ctypes.byref(rows), code, q.shape[1], int(window), keep))
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-        scale = self.head_dim ** -0.5 if scale is None else float(scale)
         with _on(q):
-            _check(load().bnn_cache4_attend(ctypes.byref(self._c), ctypes.byref(rows), _ptr(q), code, qt, qh, q.shape[1], ctypes.c_float(scale),
+            _check(load().bnn_cache4_attend(self._struct(), ctypes.byref(rows), _ptr(q), code, qt, qh, q.shape[1], ctypes.c_float(scale),
                                             int(bool(causal)), int(window), _ptr(blocks), keep, _ptr(out), _ptr(lse), _ptr(workspace),
                                             ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream(q)), "bnn_cache4_attend")
         return (out, lse) if want_lse else out

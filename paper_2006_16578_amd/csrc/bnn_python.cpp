@@ -22,7 +22,9 @@ namespace {
 #define BNN_ENTRIES(X)                                                                                                                   \
     X(bnn_bmm_ex) X(bnn_bmm_thr_ex) X(bnn_bconv_ex) X(bnn_bconv_thr_ex) X(bnn_threshold_pack) X(bnn_maxpool_or)                            \
     X(bnn_bmm_general_workspace_bytes) X(bnn_bmm_general_f32) X(bnn_bwn_workspace_bytes) X(bnn_bwn_conv_thr)                               \
-    X(bnn_conv_f32_split_workspace_bytes) X(bnn_conv_f32_split_thr_ex) X(bnn_net_workspace_bytes) X(bnn_net_forward)
+    X(bnn_conv_f32_split_workspace_bytes) X(bnn_conv_f32_split_thr_ex) X(bnn_net_workspace_bytes) X(bnn_net_forward)                       \
+    X(bnn_cache4_write) X(bnn_cache4_read) X(bnn_cache4_select_workspace_bytes) X(bnn_cache4_select)                                       \
+    X(bnn_cache4_attend_workspace_bytes) X(bnn_cache4_attend)
 #define DECLARE(name) decltype(&::name) p_##name = nullptr;
 BNN_ENTRIES(DECLARE)
 
@@ -47,6 +49,24 @@ struct Call {
         device = t.get_device();
         for (const int64_t n : t.sizes()) ok = ok && n <= INT_MAX;
         return &t;
+    }
+    // [tokens][heads][dim] in fp32, bf16 or fp16, the elements of a head side by side; code: the library's number for the type.
+    const Tensor* elements(PyObject* o, int dim, int& code) {
+        static const Tensor none;
+        if (!ok || !THPVariable_CheckExact(o)) { ok = false; return &none; }
+        const Tensor& t = THPVariable_Unpack(o);
+        const at::TensorImpl* impl = t.unsafeGetTensorImpl();
+        ok = t.defined() && t.is_cuda() && t.dim() == 3 && t.layout() == at::kStrided && impl->has_storage() && !impl->is_python_dispatch() && t.get_device() == device &&
+             t.size(2) == dim && t.stride(2) == 1 && t.size(0) <= INT_MAX && t.size(1) <= INT_MAX;
+        if (!ok) return &none;
+        const at::ScalarType type = t.scalar_type();
+        code = type == at::kFloat ? BNN_F32 : type == at::kBFloat16 ? BNN_BF16 : BNN_F16;
+        ok = type == at::kFloat || type == at::kBFloat16 || type == at::kHalf;
+        return &t;
+    }
+    bool truth(PyObject* o) {
+        ok = ok && (o == Py_True || o == Py_False);
+        return o == Py_True;
     }
     int number(PyObject* o) {
         if (!ok || !PyLong_CheckExact(o)) { ok = false; return 0; }
@@ -306,6 +326,127 @@ PyObject* net_forward(PyObject*, PyObject* const* a, Py_ssize_t nargs) {
     });
 }
 
+// The 4-bit cache and a call's plan, which every function on it begins with: data, kv_heads, head_dim, page, signs, table, lens, start.
+struct Plan4 {
+    static constexpr int N = 8;
+    bnn_cache4 cache = {};
+    bnn_cache4_rows rows = {};
+    const Tensor* data = nullptr;
+
+    // Reads the arguments; those that may throw (pointers) come in finish(), after ready().
+    Plan4(Call& c, PyObject* const* a) {
+        data = c.tensor(a[0], at::kByte, 3);
+        cache.kv_heads = c.number(a[1]);
+        cache.head_dim = c.number(a[2]);
+        cache.page = c.number(a[3]);
+        cache.signs = c.number(a[4]);
+        table = c.tensor(a[5], at::kInt, 2);
+        lens = c.tensor(a[6], at::kInt, 1);
+        if (a[7] != Py_None) start = c.tensor(a[7], at::kInt, 1);
+        if (c.ok) c.ok = lens->size(0) == table->size(0) && (!start || start->size(0) == table->size(0) + 1);
+    }
+    void finish(int tokens) {
+        cache.data = data->data_ptr();
+        cache.pages = data->size(0);
+        rows.table = ptr<int32_t>(*table);
+        rows.lens = ptr<int32_t>(*lens);
+        rows.start = start ? ptr<int32_t>(*start) : nullptr;
+        rows.batch = (int)table->size(0);
+        rows.table_pages = (int)table->size(1);
+        rows.tokens = tokens;
+    }
+
+private:
+    const Tensor *table = nullptr, *lens = nullptr, *start = nullptr;
+};
+
+constexpr at::ScalarType ELEMENTS[] = {at::kFloat, at::kBFloat16, at::kHalf};      // BNN_F32, BNN_BF16, BNN_F16
+
+PyObject* pair(const Tensor& x, const Tensor& y) {
+    PyObject* result = PyTuple_New(2);
+    if (!result) return nullptr;
+    PyTuple_SET_ITEM(result, 0, THPVariable_Wrap(x));
+    PyTuple_SET_ITEM(result, 1, THPVariable_Wrap(y));
+    return result;
+}
+
+PyObject* cache4_write(PyObject*, PyObject* const* a, Py_ssize_t nargs) {    // plan, k, v -> True
+    ARGS(Plan4::N + 2)
+    return guarded([&]() -> PyObject* {
+        Call c;
+        Plan4 p(c, a);
+        int code = 0, code_v = 0;
+        const Tensor &k = *c.elements(a[8], p.cache.head_dim, code), &v = *c.elements(a[9], p.cache.head_dim, code_v);
+        PLAIN(c);
+        if (code != code_v || k.size(0) != v.size(0) || k.size(1) != p.cache.kv_heads || v.size(1) != p.cache.kv_heads) Py_RETURN_NONE;
+        p.finish((int)k.size(0));
+        if (!run(c, "bnn_cache4_write", p_bnn_cache4_write, &p.cache, &p.rows, k.data_ptr(), v.data_ptr(), code, k.stride(0), k.stride(1), v.stride(0), v.stride(1)))
+            return nullptr;
+        Py_RETURN_TRUE;
+    });
+}
+
+PyObject* cache4_read(PyObject*, PyObject* const* a, Py_ssize_t nargs) {     // plan, tokens, type
+    ARGS(Plan4::N + 2)
+    return guarded([&]() -> PyObject* {
+        Call c;
+        Plan4 p(c, a);
+        const int tokens = c.number(a[8]), code = c.number(a[9]);
+        PLAIN(c);
+        if (tokens < 0 || code < 0 || code > 2) Py_RETURN_NONE;
+        p.finish(tokens);
+        const Tensor k = empty(*p.data, {tokens, p.cache.kv_heads, p.cache.head_dim}, ELEMENTS[code]), v = empty(*p.data, k.sizes(), ELEMENTS[code]);
+        return run(c, "bnn_cache4_read", p_bnn_cache4_read, &p.cache, &p.rows, k.data_ptr(), v.data_ptr(), code) ? pair(k, v) : nullptr;
+    });
+}
+
+PyObject* cache4_select(PyObject*, PyObject* const* a, Py_ssize_t nargs) {   // plan, q, keep, first, last
+    ARGS(Plan4::N + 4)
+    return guarded([&]() -> PyObject* {
+        Call c;
+        Plan4 p(c, a);
+        int code = 0;
+        const Tensor& q = *c.elements(a[8], p.cache.head_dim, code);
+        const int keep = c.number(a[9]), first = c.number(a[10]), last = c.number(a[11]);
+        PLAIN(c);
+        if (keep < 0) Py_RETURN_NONE;
+        p.finish((int)q.size(0));
+        const Tensor blocks = empty(q, {q.size(0), p.cache.kv_heads, keep}, at::kInt);
+        const Tensor work = empty(q, {std::max<int64_t>((int64_t)p_bnn_cache4_select_workspace_bytes(&p.cache, &p.rows), 16)}, at::kByte);
+        const bool done = run(c, "bnn_cache4_select", p_bnn_cache4_select, &p.cache, &p.rows, q.data_ptr(), code, q.stride(0), q.stride(1), (int)q.size(1), keep, first, last,
+                              ptr<int32_t>(blocks), work.data_ptr(), (size_t)work.numel());
+        return done ? THPVariable_Wrap(blocks) : nullptr;
+    });
+}
+
+PyObject* cache4_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs) {   // plan, q, scale, causal, window, blocks, want_lse
+    ARGS(Plan4::N + 6)
+    return guarded([&]() -> PyObject* {
+        Call c;
+        Plan4 p(c, a);
+        int code = 0;
+        const Tensor& q = *c.elements(a[8], p.cache.head_dim, code);
+        if (!PyFloat_CheckExact(a[9])) Py_RETURN_NONE;
+        const float scale = (float)PyFloat_AS_DOUBLE(a[9]);
+        const bool causal = c.truth(a[10]), want_lse = c.truth(a[13]);
+        const int window = c.number(a[11]);
+        const Tensor* blocks = a[12] == Py_None ? nullptr : c.tensor(a[12], at::kInt, 3);
+        PLAIN(c);
+        if (blocks && (blocks->size(0) != q.size(0) || blocks->size(1) != p.cache.kv_heads)) Py_RETURN_NONE;
+        p.finish((int)q.size(0));
+        const int heads = (int)q.size(1), keep = blocks ? (int)blocks->size(2) : 0;
+        const Tensor out = empty(q, q.sizes(), ELEMENTS[code]);
+        Tensor lse, work;
+        if (want_lse) lse = empty(q, {q.size(0), heads}, at::kFloat);
+        const size_t need = p_bnn_cache4_attend_workspace_bytes(&p.cache, &p.rows, code, heads, window, keep);
+        if (need) work = empty(q, {(int64_t)need}, at::kByte);
+        const bool done = run(c, "bnn_cache4_attend", p_bnn_cache4_attend, &p.cache, &p.rows, q.data_ptr(), code, q.stride(0), q.stride(1), heads, scale, (int)causal, window,
+                              blocks ? ptr<int32_t>(*blocks) : nullptr, keep, out.data_ptr(), want_lse ? ptr<float>(lse) : nullptr, need ? work.data_ptr() : nullptr, need);
+        if (!done) return nullptr;
+        return want_lse ? pair(out, lse) : THPVariable_Wrap(out);
+    });
+}
+
 PyObject* init(PyObject*, PyObject* args) {        // {name: address}, the raw stream function, _check
     PyObject *addresses, *stream_fn, *check_fn;
     if (!PyArg_ParseTuple(args, "O!OO", &PyDict_Type, &addresses, &stream_fn, &check_fn)) return nullptr;
@@ -325,7 +466,8 @@ PyObject* init(PyObject*, PyObject* args) {        // {name: address}, the raw s
 
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bmm), METHOD(bmm_thr), METHOD(bconv), METHOD(bconv_thr), METHOD(threshold_pack), METHOD(maxpool_or), METHOD(bmm_general_f32),
-                         METHOD(bwn_conv_thr), METHOD(conv_f32_split_thr), METHOD(net_forward), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         METHOD(bwn_conv_thr), METHOD(conv_f32_split_thr), METHOD(net_forward), METHOD(cache4_write), METHOD(cache4_read), METHOD(cache4_select),
+                         METHOD(cache4_attend), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

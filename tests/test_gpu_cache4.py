@@ -376,6 +376,38 @@ def test_recorded_into_a_graph(bnn):
         assert all(torch.equal(torch.nan_to_num(a.float(), 777), torch.nan_to_num(b.float(), 777)) for a, b in zip(got, step())), i
 
 
+def test_native_module_and_ctypes_agree(bnn, monkeypatch):
+    # the native module serves ordinary calls; without it, and for what is out of the ordinary, ctypes gives the same
+    from paper_2006_16578_amd import binding
+    su = Setup(bnn, 18, [300, 40, 77], [4, 1, 3], 2, 64, 16, width=40)
+    q, k = dev(su.queries(4), "bf16"), dev(su.queries(2), "bf16")
+    binding._load_native()
+    native, served = binding._native, []
+
+    class Counted:
+        def __getattr__(self, name):
+            return lambda *args: served.append((name, getattr(native, name)(*args))) or served[-1][1]
+
+    def calls(keep=5):
+        su.gpu.write(k, k, **su.plan)
+        blocks = su.gpu.select(q, keep=keep, **su.plan)
+        return (blocks, *su.gpu.read(tokens=8, dtype=torch.float32, **su.plan), su.gpu.attend(q, **su.plan), su.gpu.attend(q, blocks=blocks, **su.plan),
+                *su.gpu.attend(q, want_lse=True, window=9, scale=0.3, **su.plan))
+
+    monkeypatch.setattr(binding, "_native", Counted())
+    fast = calls()
+    assert [n for n, r in served] == ["cache4_write", "cache4_select", "cache4_read"] + ["cache4_attend"] * 3 and all(r is not None for n, r in served)
+    slow_too = calls(np.int64(5))                                    # a number that is no int: select goes by ctypes
+    assert served[len(served) // 2 + 1][1] is None
+    monkeypatch.setattr(binding, "_native", binding._PythonOnly())
+    for a, b, c in zip(fast, calls(), slow_too):
+        assert a.dtype == b.dtype and torch.equal(torch.nan_to_num(a.float(), 7), torch.nan_to_num(b.float(), 7)) and torch.equal(torch.nan_to_num(a.float(), 7), torch.nan_to_num(c.float(), 7))
+    monkeypatch.setattr(binding, "_native", native)
+    torch._C._set_throw_on_mutable_data_ptr(q)                       # no pointer: raised, with the interpreter lock held
+    with pytest.raises(RuntimeError, match="data pointer"):
+        su.gpu.attend(q, **su.plan)
+
+
 def test_refusals(bnn):
     su = Setup(bnn, 17, [30, 9], None, 2, 64, 16)
     q, k = dev(su.queries(4), "bf16"), dev(su.queries(2), "bf16")
@@ -389,7 +421,7 @@ def test_refusals(bnn):
                       (lambda: su.gpu.attend(q, blocks=torch.zeros((1, 2, 3), dtype=torch.int32, device="cuda"), **plan), ValueError),
                       (lambda: su.gpu.attend(q[:, :3], **plan), bnn.BnnError), (lambda: su.gpu.attend(q[:1], **plan), bnn.BnnError),
                       (lambda: su.gpu.attend(q, scale=0.0, **plan), bnn.BnnError), (lambda: su.gpu.attend(q, window=3, causal=False, **plan), bnn.BnnError),
-                      (lambda: su.gpu.select(q, keep=1, **plan), bnn.BnnError), (lambda: su.gpu.read(dtype=torch.float64, plan=None, **plan), TypeError),
+                      (lambda: su.gpu.select(q, keep=1, **plan), bnn.BnnError), (lambda: su.gpu.read(dtype=torch.float64, **plan), TypeError),
                       (lambda: bnn.Cache4(kv_heads=2, head_dim=64, page=32, data=su.gpu.data), ValueError), (lambda: bnn.Cache4(kv_heads=2, head_dim=64), ValueError)):
         with pytest.raises(error):
             fn()

@@ -2,6 +2,8 @@
 #ifndef BNN_CACHE4_H
 #define BNN_CACHE4_H
 
+#include <algorithm>
+
 #include "bnn_internal.h"
 
 namespace bnn {
@@ -14,8 +16,7 @@ constexpr int C4_GROUP = 32;                 // elements that share a scale: the
 // A cache as the kernels see it.  Offsets of a record's parts are in bytes.
 struct Cache4 {
     uint8_t* data;
-    long long pages;
-    int kv_heads, dim, page, page_shift;
+    int pages, kv_heads, dim, page, page_shift;
     int record;                              // bytes of one (page, head)
     int v_codes, k_exps, v_exps, signs;      // K codes at 0
 };
@@ -60,15 +61,54 @@ __device__ __forceinline__ int c4_sequence_of(const Rows4& r, int t) {
     return lo;
 }
 
-// The page that holds a token of sequence b, or -1: out of the table, or an entry that is no page.
+// The page that holds a token of sequence b, or -1: out of the table, or an entry that is no page.  Without branches, so that loads of several can be under way.
 __device__ __forceinline__ int c4_page(const Rows4& r, const Cache4& c, int b, int token) {
-    const int at = token >> c.page_shift;
-    if (token < 0 || at >= r.table_pages) return -1;
-    const int p = r.table[(long long)b * r.table_pages + at];
-    return p >= 0 && p < c.pages ? p : -1;
+    const int at = token >> c.page_shift;                    // negative for a negative token
+    const int p = r.table[(long long)b * r.table_pages + min(max(at, 0), r.table_pages - 1)];
+    return at >= 0 && at < r.table_pages && (uint32_t)p < (uint32_t)c.pages ? p : -1;
 }
 __device__ __forceinline__ uint8_t* c4_record(const Cache4& c, int page, int head) {
     return c.data + ((long long)page * c.kv_heads + head) * c.record;
+}
+
+// Tiles of ROWS rows (units: rows of a token) that never span sequences: the sequence of `tile`, and its number in it; false: there are fewer tiles.
+// With start == nullptr every sequence has seq_tiles; else a wave counts the tiles of 64 sequences at a time.
+template <int ROWS>
+__device__ __forceinline__ bool c4_find_tile(const Rows4& r, int units, int tile, int seq_tiles, const FastDiv& div_seq_tiles, int& b, int& local) {
+    if (r.start == nullptr) {
+        b = fast_div(tile, div_seq_tiles);
+        local = tile - b * seq_tiles;
+        return b < r.batch;
+    }
+    const int lane = (int)threadIdx.x & 63;
+    int before = 0;
+    for (int b0 = 0; b0 < r.batch; b0 += 64) {
+        int n = 0;
+        if (b0 + lane < r.batch) {
+            const int first = min(max(r.start[b0 + lane], 0), r.tokens);
+            n = (int)(((long long)(min(max(r.start[b0 + lane + 1], first), r.tokens) - first) * units + ROWS - 1) / ROWS);
+        }
+        int sum = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(sum, d);
+            if (lane >= d) sum += other;
+        }
+        const unsigned long long past = __ballot(before + sum > tile);
+        if (past != 0) {
+            const int at = __ffsll(past) - 1;
+            b = b0 + at;
+            local = __builtin_amdgcn_readfirstlane(tile - (before + __shfl(sum, at) - __shfl(n, at)));
+            return true;
+        }
+        before += __shfl(sum, 63);
+    }
+    return false;
+}
+// How many such tiles a launch needs at most (with start: a partly filled one for every sequence).
+inline long long c4_tiles(const Rows4& r, int units, int rows, int* seq_tiles) {
+    *seq_tiles = r.start ? 0 : (int)cdiv((long long)r.each * units, rows);
+    return r.start ? (long long)r.tokens * units / rows + r.batch : (long long)r.batch * *seq_tiles;
 }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -109,10 +149,8 @@ __device__ __forceinline__ void c4_store8(T* p, const float (&x)[8]) {
     }
 }
 
-// The scale that a byte stands for.  The NaN byte becomes a NaN: so does what is converted with it.
-__device__ __forceinline__ float c4_scale(uint32_t byte) {
-    return __uint_as_float(byte == C4_EXP_NAN ? 0x7fc00000u : byte << 23);
-}
+// The scale that a byte stands for, for the conversion instructions: with the NaN byte's (the bits of an infinity) they give NaN for every code, 0 included.
+__device__ __forceinline__ float c4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
 // The attention call as the kernels see it.
 struct Attend4 {
@@ -165,9 +203,13 @@ struct Select4 {
     int group;
     int keep, first, last;
     int32_t* blocks;                         // [tokens][kv_heads][keep]
-    uint16_t* scores;                        // [tokens][kv_heads][table_pages]
+    uint16_t* scores;                        // [tokens][kv_heads][table_pages]: score + 1, 0 where the row sees no key of the block
+    // of the launch that scores
+    int columns_shift;                       // a token has 2^columns_shift of the 32 columns: its query heads, rounded up
+    int tiles, seq_tiles, parts;
+    FastDiv div_seq_tiles, div_parts, div_heads;
 };
-int launch_cache4_select(const Select4& a, int dtype, hipStream_t s);
+int launch_cache4_select(Select4 a, int dtype, hipStream_t s);
 int launch_cache4_write(const Cache4& c, const Rows4& r, const void* k, const void* v, int dtype, long long k_token, long long k_head,
                         long long v_token, long long v_head, hipStream_t s);
 int launch_cache4_read(const Cache4& c, const Rows4& r, void* k, void* v, int dtype, hipStream_t s);

@@ -20,7 +20,7 @@ int make_cache(const bnn_cache4* in, Cache4& c) {
     if (in->pages >= (1LL << 31) || in->kv_heads > 65535 || !known_dim(in->head_dim) || !known_page(in->page)) return BNN_ERR_UNSUPPORTED;
     if (!aligned16(in->data)) return BNN_ERR_ALIGNMENT;
     c.data = static_cast<uint8_t*>(in->data);
-    c.pages = in->pages;
+    c.pages = (int)in->pages;
     c.kv_heads = in->kv_heads;
     c.dim = in->head_dim;
     c.page = in->page;
@@ -74,12 +74,7 @@ AttendPlan4 plan_attend(const Cache4& c, const Rows4& r, int dtype, int group, i
         const long long rows = cdiv((long long)r.tokens * group, r.batch);
         p.qtiles = 1;
         while (p.qtiles < cache4_qtiles(c.dim, dtype) && 16 * p.qtiles < rows) p.qtiles *= 2;
-        if (r.start) {
-            tiles = (long long)r.tokens * group / (16 * p.qtiles) + r.batch;
-        } else {
-            p.seq_tiles = (int)cdiv((long long)r.each * group, 16 * p.qtiles);
-            tiles = (long long)r.batch * p.seq_tiles;
-        }
+        tiles = c4_tiles(r, group, 16 * p.qtiles, &p.seq_tiles);
         long long keys = (long long)r.table_pages << c.page_shift;
         if (window > 0) keys = std::min(keys, (long long)window + cdiv(16 * p.qtiles, group) + 64);
         steps = cdiv(keys, 32);

@@ -82,39 +82,8 @@ __device__ __forceinline__ Tile4 find_tile(const Attend4& a, int tile) {
         t.rows = min(ROWS, a.group - part * ROWS);
         return t;
     } else {
-        int local = 0;
-        if (a.r.start == nullptr) {
-            t.b = fast_div(tile, a.div_seq_tiles);
-            local = tile - t.b * a.seq_tiles;
-        } else {                             // 64 sequences at a time: a running count of their tiles
-            const int lane = (int)threadIdx.x & 63;
-            int before = 0;
-            bool found = false;
-            for (int b0 = 0; b0 < a.r.batch && !found; b0 += 64) {
-                int n = 0;
-                if (b0 + lane < a.r.batch) {
-                    const int first = min(max(a.r.start[b0 + lane], 0), a.r.tokens);
-                    n = (int)(((long long)(min(max(a.r.start[b0 + lane + 1], first), a.r.tokens) - first) * a.group + ROWS - 1) / ROWS);
-                }
-                int sum = n;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int other = __shfl_up(sum, d);
-                    if (lane >= d) sum += other;
-                }
-                const unsigned long long past = __ballot(before + sum > tile);
-                if (past != 0) {
-                    const int at = __ffsll(past) - 1;
-                    t.b = b0 + at;
-                    local = tile - (before + __shfl(sum, at) - __shfl(n, at));
-                    found = true;
-                }
-                before += __shfl(sum, 63);
-            }
-            if (!found) return t;
-            t.b = __builtin_amdgcn_readfirstlane(t.b);
-            local = __builtin_amdgcn_readfirstlane(local);
-        }
+        int local;
+        if (!c4_find_tile<ROWS>(a.r, a.group, tile, a.seq_tiles, a.div_seq_tiles, t.b, local)) return t;
         t.s = c4_sequence(a.r, a.c, t.b);
         const int all = t.s.rows * a.group;
         t.row0 = local * ROWS;
@@ -166,10 +135,12 @@ struct Pieces {
     static constexpr int base(int p) { return p < n128 ? 128 * p : p < n128 + n64 ? 128 * n128 : 128 * n128 + 64 * n64; }
 };
 
-// Where the 16 keys of half a step lie: all in one page.
+// Where the 16 keys of half a step lie, all in one page.  Uniform over a wave.
 struct Half4 {
-    int page;                                // -1: nowhere
-    int key;                                 // number of the first in the sequence
+    const uint8_t* record;
+    int offset;                              // of the first key in the page
+    int key;                                 // its number in the sequence
+    bool there;
 };
 
 // What a lane holds of a step's codes and scales between the loads and the products.
@@ -182,52 +153,51 @@ struct Raw4 {
     uint32_t v_exp[P::count][2];
 };
 
+// (The parts of an address that differ between lanes are 32-bit numbers that no step changes; the rest is scalar.)
 template <int D>
-__device__ __forceinline__ void load_k(const Cache4& c, const Half4 (&half)[2], int head, int lane, Raw4<D>& raw) {
+__device__ __forceinline__ void load_k(const Cache4& c, const Half4 (&half)[2], int lane, Raw4<D>& raw) {
     using P = Pieces<D>;
-    const int col = lane & 15, h4 = lane >> 4;
+    const uint32_t col = lane & 15, h4 = lane >> 4;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const uint8_t* rec = c4_record(c, max(half[s].page, 0), head);
-        const int offset = half[s].key & (c.page - 1);
-        const uint8_t* row = rec + (offset + col) * (D / 2);
-        const uint8_t* exps = rec + c.k_exps + offset + col;
+        const uint8_t* row = half[s].record + half[s].offset * (D / 2);
+        const uint8_t* exps = half[s].record + c.k_exps + half[s].offset;
         static_for<P::count>([&](auto pc) {
             constexpr int p = pc.value, W = P::width(p), B = P::base(p);
             if constexpr (W == 128) {
-                const u32x4 v = *reinterpret_cast<const u32x4*>(row + B / 2 + 16 * h4);
+                const u32x4 v = *reinterpret_cast<const u32x4*>(row + (col * (D / 2) + B / 2 + 16 * h4));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) raw.k[s][B / 32 + i] = v[i];
             } else if constexpr (W == 64) {
-                const u32x2 v = *reinterpret_cast<const u32x2*>(row + B / 2 + 8 * h4);
+                const u32x2 v = *reinterpret_cast<const u32x2*>(row + (col * (D / 2) + B / 2 + 8 * h4));
                 raw.k[s][B / 32] = v[0];
                 raw.k[s][B / 32 + 1] = v[1];
             } else {
-                raw.k[s][B / 32] = *reinterpret_cast<const uint32_t*>(row + B / 2 + 4 * h4);
+                raw.k[s][B / 32] = *reinterpret_cast<const uint32_t*>(row + (col * (D / 2) + B / 2 + 4 * h4));
             }
-            raw.k_exp[s][p] = exps[(B / 32 + h4 * W / 128) * c.page];
+            raw.k_exp[s][p] = exps[(B / 32 + h4 * W / 128) * (uint32_t)c.page + col];
         });
     }
 }
 
 template <int D>
-__device__ __forceinline__ void load_v(const Cache4& c, const Half4 (&half)[2], int head, int lane, Raw4<D>& raw) {
+__device__ __forceinline__ void load_v(const Cache4& c, const Half4 (&half)[2], int lane, Raw4<D>& raw) {
     using P = Pieces<D>;
-    const int col = lane & 15, h4 = lane >> 4;
+    const uint32_t col = lane & 15, h4 = lane >> 4;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-        const uint8_t* rec = c4_record(c, max(half[s].page, 0), head);
-        const int offset = (half[s].key & (c.page - 1)) + 4 * h4;
+        const uint8_t* codes = half[s].record + c.v_codes + half[s].offset * (D / 2);
+        const uint8_t* exps = half[s].record + c.v_exps + half[s].offset;
         static_for<P::count>([&](auto pc) {
             constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;       // E elements of each of 8 keys
-            const uint8_t* row = rec + c.v_codes + offset * (D / 2) + B / 2 + E / 2 * col;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if constexpr (E == 8) raw.v[p][4 * s + i] = *reinterpret_cast<const uint32_t*>(row + i * (D / 2));
-                else if constexpr (E == 4) raw.v[p][4 * s + i] = *reinterpret_cast<const uint16_t*>(row + i * (D / 2));
-                else raw.v[p][4 * s + i] = row[i * (D / 2)];
+                const uint8_t* at = codes + ((4 * h4 + i) * (D / 2) + B / 2 + E / 2 * col);
+                if constexpr (E == 8) raw.v[p][4 * s + i] = *reinterpret_cast<const uint32_t*>(at);
+                else if constexpr (E == 4) raw.v[p][4 * s + i] = *reinterpret_cast<const uint16_t*>(at);
+                else raw.v[p][4 * s + i] = *at;
             }
-            raw.v_exp[p][s] = *reinterpret_cast<const uint32_t*>(rec + c.v_exps + (B / 32 + col * E / 32) * c.page + offset);
+            raw.v_exp[p][s] = *reinterpret_cast<const uint32_t*>(exps + ((B / 32 + col * E / 32) * (uint32_t)c.page + 4 * h4));
         });
     }
 }
@@ -258,30 +228,48 @@ __global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ?
     const int base = t.s.length - t.s.rows;
     const int32_t* list = SPARSE ? a.blocks + ((long long)(t.s.first + fast_div(t.row0, a.div_group)) * a.c.kv_heads + head) * a.keep : nullptr;
     const int per_shift = a.c.page_shift - 4;                        // halves of steps in a page
-    auto locate = [&](int step, Half4 (&half)[2]) {
+    // Where the halves of this wave's next 32 steps lie, a lane each: the record's offset in the cache, the first key's number (sparse), whether there is a page.
+    const int turns = (end - begin - wave + 3) / 4;                  // steps of this wave
+    uint32_t low = 0, high = 0;
+    int keys = 0;
+    unsigned long long present = 0;
+    auto locate = [&](int turn) {                                    // turn: a multiple of 32
+        const int i = 2 * (range.first + begin + wave + 4 * (turn + (lane >> 1))) + (lane & 1);
+        bool listed = true;
+        if constexpr (SPARSE) {
+            const int entry = i >> per_shift;
+            const int block = list[min(entry, a.keep - 1)];
+            listed = entry < a.keep && block >= 0 && block < a.r.table_pages;
+            keys = listed ? (block << a.c.page_shift) + 16 * (i & ((1 << per_shift) - 1)) : 0;
+        } else {
+            keys = 16 * min(i, 2 * (range.first + range.count) - 1);
+        }
+        const int page = c4_page(a.r, a.c, t.b, keys);
+        present = __ballot(listed && page >= 0);
+        const uint64_t at = (uint64_t)(c4_record(a.c, max(page, 0), head) - a.c.data);
+        low = (uint32_t)at;
+        high = (uint32_t)(at >> 32);
+    };
+    auto fetch = [&](int turn, Half4 (&half)[2]) {
+        if (turn % 32 == 0) locate(turn);
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            bool listed = true;
-            if constexpr (SPARSE) {
-                const int i = 2 * step + s, entry = i >> per_shift;
-                const int block = entry < a.keep ? list[entry] : -1;
-                listed = block >= 0 && block < a.r.table_pages;
-                half[s].key = listed ? (block << a.c.page_shift) + 16 * (i - (entry << per_shift)) : 0;
-            } else {
-                half[s].key = 32 * (range.first + step) + 16 * s;
-            }
-            half[s].page = __builtin_amdgcn_readfirstlane(listed ? c4_page(a.r, a.c, t.b, half[s].key) : -1);
-            half[s].key = __builtin_amdgcn_readfirstlane(half[s].key);
+            const int at = 2 * (turn % 32) + s;
+            half[s].record = a.c.data + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)high, at) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)low, at));
+            half[s].key = SPARSE ? __builtin_amdgcn_readlane(keys, at) : 32 * (range.first + begin + wave + 4 * turn) + 16 * s;
+            half[s].offset = half[s].key & (a.c.page - 1);
+            half[s].there = present >> at & 1;
         }
     };
 
     Half4 now[2], next[2];
     Raw4<D> raw;
-    if (begin + wave < end) {
-        locate(begin + wave, now);
-        load_k<D>(a.c, now, head, lane, raw);
-        load_v<D>(a.c, now, head, lane, raw);
-        locate(min(begin + wave + 4, end - 1), next);
+    if (turns > 0) {
+        fetch(0, now);
+        load_k<D>(a.c, now, lane, raw);
+        load_v<D>(a.c, now, lane, raw);
+        next[0] = now[0];
+        next[1] = now[1];
     }
 
     // Q, in the order of elements that K's loads give
@@ -324,10 +312,10 @@ __global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ?
     const int top_first = a.causal ? base + fast_div(t.row0, a.div_group) : t.s.length - 1;
     const int low_last = a.window > 0 ? base + fast_div(t.row0 + t.rows - 1, a.div_group) - a.window + 1 : 0;
 
-    for (int step = begin + wave; step < end; step += 4) {
+    for (int turn = 0; turn < turns; ++turn) {
         bool full = true;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) full = full && now[s].page >= 0 && now[s].key + 15 <= top_first && now[s].key >= low_last;
+        for (int s = 0; s < 2; ++s) full = full && now[s].there && now[s].key + 15 <= top_first && now[s].key >= low_last;
 
         // K and the scores
         f32x4 score[QT][2];
@@ -348,10 +336,9 @@ __global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ?
                 }
             });
         }
-        // the next step's K into the same registers; where the one after it lies
-        load_k<D>(a.c, next, head, lane, raw);
-        Half4 after[2];
-        locate(min(step + 8, end - 1), after);
+        // the next step's K into the same registers (the last step's once more at the end)
+        if (turn + 1 < turns) fetch(turn + 1, next);
+        load_k<D>(a.c, next, lane, raw);
 
         if (!full) {
 #pragma unroll
@@ -362,7 +349,7 @@ __global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ?
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int key = now[s].key + 4 * h4 + i;
-                        if (!(now[s].page >= 0 && key <= top && key >= low)) score[u][s][i] = -__builtin_inff();
+                        if (!(now[s].there && key <= top && key >= low)) score[u][s][i] = -__builtin_inff();
                     }
             }
         }
@@ -445,12 +432,9 @@ __global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ?
                     }
             });
         });
-        load_v<D>(a.c, next, head, lane, raw);
+        load_v<D>(a.c, next, lane, raw);
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            now[s] = next[s];
-            next[s] = after[s];
-        }
+        for (int s = 0; s < 2; ++s) now[s] = next[s];
     }
 
     // The waves meet: 16 rows at a time.

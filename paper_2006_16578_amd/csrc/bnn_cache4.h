@@ -132,22 +132,21 @@ __device__ __forceinline__ void c4_load8(const T* p, float (&x)[8]) {
         for (int i = 0; i < 8; ++i) x[i] = (float)a[i];
     }
 }
-template <class T>
-__device__ __forceinline__ void c4_store8(T* p, const float (&x)[8]) {
-    if constexpr (sizeof(T) == 4) {
-        f32x4 a, b;
+// N consecutive elements (2, 4 or 8), aligned to their bytes, 16 at most.
+template <int N, class T>
+__device__ __forceinline__ void c4_store(T* p, const float (&x)[N]) {
+    constexpr int W = N * sizeof(T) > 16 ? 16 / sizeof(T) : N;
+    typedef T tw __attribute__((ext_vector_type(W)));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { a[i] = x[i]; b[i] = x[4 + i]; }
-        reinterpret_cast<f32x4*>(p)[0] = a;
-        reinterpret_cast<f32x4*>(p)[1] = b;
-    } else {
-        typedef T t8 __attribute__((ext_vector_type(8)));
-        t8 a;
+    for (int b = 0; b < N; b += W) {
+        tw a;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) a[i] = (T)x[i];
-        *reinterpret_cast<t8*>(p) = a;
+        for (int i = 0; i < W; ++i) a[i] = (T)x[b + i];
+        *reinterpret_cast<tw*>(p + b) = a;
     }
 }
+template <class T>
+__device__ __forceinline__ void c4_store8(T* p, const float (&x)[8]) { c4_store<8>(p, x); }
 
 // The scale that a byte stands for, for the conversion instructions: with the NaN byte's (the bits of an infinity) they give NaN for every code, 0 included.
 __device__ __forceinline__ float c4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
@@ -175,24 +174,23 @@ struct Attend4 {
     float* part_ml;                          // ... [2]: maximum and sum
 };
 
-// How a call is cut up.  qtiles: groups of 16 rows that a workgroup carries.
+// How a call is cut up.  rows: of a workgroup.
 struct AttendPlan4 {
-    int qtiles, tiles, seq_tiles, splits, chunk;
+    int rows, tiles, seq_tiles, splits, chunk;
     size_t part_bytes, workspace_bytes;
 };
 
-// The most groups of 16 rows that a workgroup carries: per group a lane keeps D / 4 registers of sums and D / 8 of every term of Q.
-constexpr int cache4_qtiles(int dim, int dtype) {
-    const int terms = dtype == BNN_BF16 ? 1 : dtype == BNN_F16 ? 2 : 3;
-    const int each = dim / 4 + terms * (dim / 8);
-    return 4 * each <= 200 ? 4 : 2 * each <= 200 ? 2 : 1;
-}
+// Groups of 16 rows that a wave carries, by what fits 256 registers: per group a lane keeps D / 4 of sums and D / 8 of every term of Q.  (With twice as many, at one
+// wave a SIMD, nothing runs while a wave waits: two prompts of 4096 tokens 631 us instead of 416.)
+constexpr int cache4_row_registers(int dim, int dtype) { return dim / 4 + (dtype == BNN_BF16 ? 1 : dtype == BNN_F16 ? 2 : 3) * (dim / 8); }
+constexpr int cache4_qtiles(int dim, int dtype) { return 2 * cache4_row_registers(dim, dtype) <= 150 ? 2 : 1; }          // a workgroup's rows, each wave has all
+constexpr int cache4_wide_qtiles(int dim, int dtype) { return 2 * cache4_row_registers(dim, dtype) <= 130 ? 2 : 1; }     // a wave's, of four with different rows
 
-int launch_cache4_attend64(const Attend4& a, int dtype, int qtiles, hipStream_t s);
-int launch_cache4_attend96(const Attend4& a, int dtype, int qtiles, hipStream_t s);
-int launch_cache4_attend128(const Attend4& a, int dtype, int qtiles, hipStream_t s);
-int launch_cache4_attend192(const Attend4& a, int dtype, int qtiles, hipStream_t s);
-int launch_cache4_attend256(const Attend4& a, int dtype, int qtiles, hipStream_t s);
+int launch_cache4_attend64(const Attend4& a, int dtype, int rows, hipStream_t s);
+int launch_cache4_attend96(const Attend4& a, int dtype, int rows, hipStream_t s);
+int launch_cache4_attend128(const Attend4& a, int dtype, int rows, hipStream_t s);
+int launch_cache4_attend192(const Attend4& a, int dtype, int rows, hipStream_t s);
+int launch_cache4_attend256(const Attend4& a, int dtype, int rows, hipStream_t s);
 
 // The selection call as the kernels see it.
 struct Select4 {

@@ -61,31 +61,31 @@ int check_elements(const void* p, int dtype, int64_t token, int64_t head) {
     return BNN_OK;
 }
 
-// How attention is cut up.  Groups of 16 rows to a workgroup: enough for the rows of a sequence, as far as registers go, since what a workgroup reads and converts
-// serves all its rows.  Parts of the keys: as many as give the chip 1024 workgroups, but of 512 keys at least.
+// How attention is cut up.  Rows of a workgroup: 64 or 128 where the rows of a sequence fill them, else 16, or 32 where that saves a workgroup.  Parts of the keys: as many
+// as give the chip 1024 workgroups, but of 512 keys at least.
 AttendPlan4 plan_attend(const Cache4& c, const Rows4& r, int dtype, int group, int window, int keep) {
     AttendPlan4 p = {};
     long long tiles, steps;
     if (keep > 0) {
-        p.qtiles = 1;
+        p.rows = 16;
         tiles = (long long)r.tokens * cdiv(group, 16);
         steps = cdiv((long long)keep * (c.page / 16), 2);
     } else {
         const long long rows = cdiv((long long)r.tokens * group, r.batch);
-        p.qtiles = 1;
-        while (p.qtiles < cache4_qtiles(c.dim, dtype) && 16 * p.qtiles < rows) p.qtiles *= 2;
-        tiles = c4_tiles(r, group, 16 * p.qtiles, &p.seq_tiles);
+        const int wide = 64 * cache4_wide_qtiles(c.dim, dtype);
+        p.rows = rows >= 64 ? wide : rows > 16 ? 16 * cache4_qtiles(c.dim, dtype) : 16;
+        tiles = c4_tiles(r, group, p.rows, &p.seq_tiles);
         long long keys = (long long)r.table_pages << c.page_shift;
-        if (window > 0) keys = std::min(keys, (long long)window + cdiv(16 * p.qtiles, group) + 64);
+        if (window > 0) keys = std::min(keys, (long long)window + cdiv(p.rows, group) + 64);
         steps = cdiv(keys, 32);
     }
     const long long units = tiles * c.kv_heads;
-    const long long splits = std::max(1LL, std::min(cdiv(1024, units), cdiv(steps, 16)));
+    const long long splits = std::max(1LL, std::min(1024 / units, cdiv(steps, 16)));
     p.chunk = (int)(cdiv(cdiv(steps, splits), 4) * 4);
     p.splits = (int)cdiv(steps, p.chunk);
     p.tiles = (int)std::min(tiles, (long long)INT32_MAX);
     if (p.splits > 1) {
-        const size_t rows = (size_t)tiles * c.kv_heads * p.splits * 16 * p.qtiles;
+        const size_t rows = (size_t)tiles * c.kv_heads * p.splits * p.rows;
         p.part_bytes = rows * c.dim * 4;
         p.workspace_bytes = p.part_bytes + rows * 8;
     }
@@ -195,11 +195,11 @@ int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
     a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes);
     hipStream_t s = static_cast<hipStream_t>(stream);
     switch (a.c.dim) {
-        case 64: return launch_cache4_attend64(a, dtype, p.qtiles, s);
-        case 96: return launch_cache4_attend96(a, dtype, p.qtiles, s);
-        case 128: return launch_cache4_attend128(a, dtype, p.qtiles, s);
-        case 192: return launch_cache4_attend192(a, dtype, p.qtiles, s);
-        default: return launch_cache4_attend256(a, dtype, p.qtiles, s);
+        case 64: return launch_cache4_attend64(a, dtype, p.rows, s);
+        case 96: return launch_cache4_attend96(a, dtype, p.rows, s);
+        case 128: return launch_cache4_attend128(a, dtype, p.rows, s);
+        case 192: return launch_cache4_attend192(a, dtype, p.rows, s);
+        default: return launch_cache4_attend256(a, dtype, p.rows, s);
     }
 }
 

@@ -155,51 +155,77 @@ struct Raw4 {
 
 // (The parts of an address that differ between lanes are 32-bit numbers that no step changes; the rest is scalar.)
 template <int D>
-__device__ __forceinline__ void load_k(const Cache4& c, const Half4 (&half)[2], int lane, Raw4<D>& raw) {
+__device__ __forceinline__ void load_k_half(const Cache4& c, const Half4& half, int lane, uint32_t (&codes)[D / 32], uint32_t (&exp)[Pieces<D>::count]) {
     using P = Pieces<D>;
     const uint32_t col = lane & 15, h4 = lane >> 4;
+    const uint8_t* row = half.record + half.offset * (D / 2);
+    const uint8_t* exps = half.record + c.k_exps + half.offset;
+    static_for<P::count>([&](auto pc) {
+        constexpr int p = pc.value, W = P::width(p), B = P::base(p);
+        if constexpr (W == 128) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(row + (col * (D / 2) + B / 2 + 16 * h4));
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const uint8_t* row = half[s].record + half[s].offset * (D / 2);
-        const uint8_t* exps = half[s].record + c.k_exps + half[s].offset;
-        static_for<P::count>([&](auto pc) {
-            constexpr int p = pc.value, W = P::width(p), B = P::base(p);
-            if constexpr (W == 128) {
-                const u32x4 v = *reinterpret_cast<const u32x4*>(row + (col * (D / 2) + B / 2 + 16 * h4));
-#pragma unroll
-                for (int i = 0; i < 4; ++i) raw.k[s][B / 32 + i] = v[i];
-            } else if constexpr (W == 64) {
-                const u32x2 v = *reinterpret_cast<const u32x2*>(row + (col * (D / 2) + B / 2 + 8 * h4));
-                raw.k[s][B / 32] = v[0];
-                raw.k[s][B / 32 + 1] = v[1];
-            } else {
-                raw.k[s][B / 32] = *reinterpret_cast<const uint32_t*>(row + (col * (D / 2) + B / 2 + 4 * h4));
-            }
-            raw.k_exp[s][p] = exps[(B / 32 + h4 * W / 128) * (uint32_t)c.page + col];
-        });
-    }
+            for (int i = 0; i < 4; ++i) codes[B / 32 + i] = v[i];
+        } else if constexpr (W == 64) {
+            const u32x2 v = *reinterpret_cast<const u32x2*>(row + (col * (D / 2) + B / 2 + 8 * h4));
+            codes[B / 32] = v[0];
+            codes[B / 32 + 1] = v[1];
+        } else {
+            codes[B / 32] = *reinterpret_cast<const uint32_t*>(row + (col * (D / 2) + B / 2 + 4 * h4));
+        }
+        exp[p] = exps[(B / 32 + h4 * W / 128) * (uint32_t)c.page + col];
+    });
 }
-
+// codes[p][0..3] and exp[p]: of the keys 4 (lane / 16) .. + 3 of the half.
+template <int D, int N>
+__device__ __forceinline__ void load_v_half(const Cache4& c, const Half4& half, int lane, uint32_t (&codes)[Pieces<D>::count][N], uint32_t (&exp)[Pieces<D>::count][N / 4],
+                                            int s) {
+    using P = Pieces<D>;
+    const uint32_t col = lane & 15, h4 = lane >> 4;
+    const uint8_t* from = half.record + c.v_codes + half.offset * (D / 2);
+    const uint8_t* exps = half.record + c.v_exps + half.offset;
+    static_for<P::count>([&](auto pc) {
+        constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;           // E elements of each of 4 keys
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint8_t* at = from + ((4 * h4 + i) * (D / 2) + B / 2 + E / 2 * col);
+            if constexpr (E == 8) codes[p][4 * s + i] = *reinterpret_cast<const uint32_t*>(at);
+            else if constexpr (E == 4) codes[p][4 * s + i] = *reinterpret_cast<const uint16_t*>(at);
+            else codes[p][4 * s + i] = *at;
+        }
+        exp[p][s] = *reinterpret_cast<const uint32_t*>(exps + ((B / 32 + col * E / 32) * (uint32_t)c.page + 4 * h4));
+    });
+}
+template <int D>
+__device__ __forceinline__ void load_k(const Cache4& c, const Half4 (&half)[2], int lane, Raw4<D>& raw) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) load_k_half<D>(c, half[s], lane, raw.k[s], raw.k_exp[s]);
+}
 template <int D>
 __device__ __forceinline__ void load_v(const Cache4& c, const Half4 (&half)[2], int lane, Raw4<D>& raw) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) load_v_half<D, 8>(c, half[s], lane, raw.v, raw.v_exp, s);
+}
+
+// Q of the lane's row, in the order of elements that K's loads give, as a sum of TERMS bf16 numbers; zero without a row.
+template <int D, int TERMS, class T>
+__device__ __forceinline__ void load_q(const T* src, bool valid, int lane, bf16x8 (&q)[TERMS][D / 32]) {
     using P = Pieces<D>;
-    const uint32_t col = lane & 15, h4 = lane >> 4;
+    static_for<P::count>([&](auto pc) {
+        constexpr int p = pc.value, W = P::width(p), B = P::base(p);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const uint8_t* codes = half[s].record + c.v_codes + half[s].offset * (D / 2);
-        const uint8_t* exps = half[s].record + c.v_exps + half[s].offset;
-        static_for<P::count>([&](auto pc) {
-            constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;       // E elements of each of 8 keys
+        for (int i = 0; i < W / 32; ++i) {
+            float x[8] = {};
+            if (valid) c4_load8(src + B + W / 4 * (lane >> 4) + 8 * i, x);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint8_t* at = codes + ((4 * h4 + i) * (D / 2) + B / 2 + E / 2 * col);
-                if constexpr (E == 8) raw.v[p][4 * s + i] = *reinterpret_cast<const uint32_t*>(at);
-                else if constexpr (E == 4) raw.v[p][4 * s + i] = *reinterpret_cast<const uint16_t*>(at);
-                else raw.v[p][4 * s + i] = *at;
+            for (int e = 0; e < 8; ++e) {
+                __bf16 terms[TERMS];
+                split_terms<TERMS>(x[e], terms);
+#pragma unroll
+                for (int n = 0; n < TERMS; ++n) q[n][B / 32 + i][e] = terms[n];
             }
-            raw.v_exp[p][s] = *reinterpret_cast<const uint32_t*>(exps + ((B / 32 + col * E / 32) * (uint32_t)c.page + 4 * h4));
-        });
-    }
+        }
+    });
 }
 
 template <int D, int DTYPE, int QT, bool SPARSE>
@@ -281,22 +307,7 @@ __global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ?
         const int token = fast_div(row, a.div_group), g = row - token * a.group;
         const bool valid = 16 * u + c < t.rows;
         pos[u] = valid ? base + token : -1;
-        const T* src = static_cast<const T*>(a.q) + (t.s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head;
-        static_for<P::count>([&](auto pc) {
-            constexpr int p = pc.value, W = P::width(p), B = P::base(p);
-#pragma unroll
-            for (int i = 0; i < W / 32; ++i) {
-                float x[8] = {};
-                if (valid) c4_load8(src + B + W / 4 * h4 + 8 * i, x);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    __bf16 terms[TERMS];
-                    split_terms<TERMS>(x[e], terms);
-#pragma unroll
-                    for (int n = 0; n < TERMS; ++n) q[u][n][B / 32 + i][e] = terms[n];
-                }
-            }
-        });
+        load_q<D, TERMS>(static_cast<const T*>(a.q) + (t.s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head, valid, lane, q[u]);
     }
 
     f32x4 o[QT][J];
@@ -491,12 +502,290 @@ __global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ?
     }
 }
 
+// Many rows: a workgroup's four waves have 16 * QT rows each and share keys.  KEYS keys at a time are converted once for all, each wave a part, and left in LDS as finished
+// operands (a lane's 16 bytes side by side: reads and writes without conflicts), two lots in turn, one barrier a lot; the codes of the lot after next are on
+// their way meanwhile.  Against the kernel above, where every wave converts for itself, this takes a third off the vector instructions. 
+// KEYS = 64: wave w converts the 16 keys of half w.  32 (heads wider than 128, whose operands take as much LDS then): waves 0 and 2 convert K, 1 and 3 V.
+template <int D, int DTYPE, int QT>
+__global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
+    using T = typename C4Type<DTYPE>::type;
+    constexpr int TERMS = C4Type<DTYPE>::terms;
+    constexpr int KEYS = D > 128 ? 32 : 64, HALVES = KEYS / 16;
+    constexpr int ROWS = 64 * QT, M = D / 32, J = D / 16;
+    using P = Pieces<D>;
+    __shared__ u32x4 k_ops[2][HALVES][M][64];
+    __shared__ u32x4 v_ops[2][HALVES / 2][J][64];
+    __shared__ int states[2][HALVES];        // 1: the half is in no page; 2: it has NaN values, which were taken as finite
+
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int c = lane & 15, h4 = lane >> 4;
+    const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads;
+    const int tile = fast_div(rest, a.div_splits), split = rest - tile * a.splits;
+    const Tile4 t = find_tile<ROWS, false>(a, tile);
+    if (t.rows <= 0) return;
+    const Range4 range = tile_steps<false>(a, t);
+    const int begin = split * a.chunk, end = min(range.count, begin + a.chunk);       // steps of 32 keys; a.chunk is a multiple of 4
+    if (split > 0 && begin >= end) return;
+    const bool whole = range.count <= a.chunk;
+    const int lots = (32 * (end - begin) + KEYS - 1) / KEYS, key_first = 32 * (range.first + begin);
+    const int half_own = HALVES == 4 ? wave : wave >> 1;
+    const bool does_k = HALVES == 4 || (wave & 1) == 0, does_v = HALVES == 4 || (wave & 1) == 1;
+
+    // Where this wave's halves of the next 64 lots lie, a lane each.
+    uint32_t low = 0, high = 0;
+    unsigned long long present = 0;
+    auto fetch = [&](int lot, Half4& half) {
+        if (lot % 64 == 0) {
+            const int key = key_first + (lot + lane) * KEYS + 16 * half_own;
+            const int page = c4_page(a.r, a.c, t.b, key);
+            present = __ballot(page >= 0);
+            const uint64_t at = (uint64_t)(c4_record(a.c, max(page, 0), head) - a.c.data);
+            low = (uint32_t)at;
+            high = (uint32_t)(at >> 32);
+        }
+        half.record = a.c.data + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)high, lot % 64) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)low, lot % 64));
+        half.key = key_first + lot * KEYS + 16 * half_own;
+        half.offset = half.key & (a.c.page - 1);
+        half.there = present >> (lot % 64) & 1;
+    };
+    uint32_t k_codes[M], k_exp[P::count], v_codes[P::count][4], v_exp[P::count][1];
+    auto load = [&](const Half4& half) {
+        if (does_k) load_k_half<D>(a.c, half, lane, k_codes, k_exp);
+        if (does_v) load_v_half<D, 4>(a.c, half, lane, v_codes, v_exp, 0);
+    };
+
+    const int base = t.s.length - t.s.rows;
+    // The keys that every row of the workgroup sees: [low_last, top_first]; those that some row of this wave sees: [wave_low, wave_top]
+    const int top_first = a.causal ? base + fast_div(t.row0, a.div_group) : t.s.length - 1;
+    const int low_last = a.window > 0 ? base + fast_div(t.row0 + t.rows - 1, a.div_group) - a.window + 1 : 0;
+    const int wave_rows = min(16 * QT, t.rows - 16 * QT * wave), wave_row0 = t.row0 + 16 * QT * wave;
+    const int wave_first = base + fast_div(wave_row0, a.div_group), wave_last = base + fast_div(wave_row0 + max(wave_rows, 1) - 1, a.div_group);
+    const int wave_top = wave_rows <= 0 ? -1 : a.causal ? wave_last : t.s.length - 1, wave_low = a.window > 0 ? wave_first - a.window + 1 : 0;
+    const int full_top = a.causal ? wave_first : t.s.length - 1, full_low = a.window > 0 ? wave_last - a.window + 1 : 0;
+
+    // Finished operands of the half that was loaded.  There are no keys beyond the last page: what is converted for them is masked.
+    auto convert = [&](const Half4& half, int lot) {
+        const int buffer = lot & 1;
+        const int first = key_first + lot * KEYS;
+        const bool masks = !(first + KEYS - 1 <= top_first && first >= low_last && half.there);
+        if (does_k) {
+            static_for<P::count>([&](auto pc) {
+                constexpr int p = pc.value, W = P::width(p), B = P::base(p);
+                const float scale = c4_scale(k_exp[p]);
+#pragma unroll
+                for (int i = 0; i < W / 32; ++i) k_ops[buffer][half_own][B / 32 + i][lane] = __builtin_bit_cast(u32x4, eight_of(k_codes[B / 32 + i], scale));
+            });
+        }
+        if (does_v) {
+            bool bad = false;
+            if (masks) {
+#pragma unroll
+                for (int p = 0; p < P::count; ++p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if ((v_exp[p][0] >> 8 * i & 255u) > C4_EXP_MAX) {
+                            bad = true;
+                            v_exp[p][0] &= ~(255u << 8 * i);
+                        }
+            }
+            const bool any = __ballot(bad) != 0;
+            if (lane == 0) states[buffer][half_own] = (half.there ? 0 : 1) + (any ? 2 : 0);
+            static_for<P::count>([&](auto pc) {
+                constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;
+                float scale[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) scale[i] = c4_scale(v_exp[p][0] >> 8 * i & 255u);
+                static_for<E / 2>([&](auto ec) {
+                    constexpr int e = ec.value;
+                    uint32_t v[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v[i] = pair_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v_codes[p][i], scale[i], e));
+                    u32x2* even = reinterpret_cast<u32x2*>(&v_ops[buffer][half_own >> 1][B / 16 + 2 * e][lane]) + (half_own & 1);
+                    u32x2* odd = reinterpret_cast<u32x2*>(&v_ops[buffer][half_own >> 1][B / 16 + 2 * e + 1][lane]) + (half_own & 1);
+                    *even = u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u)};
+                    *odd = u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u)};
+                });
+            });
+        }
+    };
+
+    Half4 half = {};
+    if (lots > 0) {
+        fetch(0, half);
+        load(half);
+    }
+    bf16x8 q[QT][TERMS][M];
+    int pos[QT];                             // position of the lane's row; -1: no row
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        const int row = wave_row0 + 16 * u + c;
+        const int token = fast_div(row, a.div_group), g = row - token * a.group;
+        const bool valid = 16 * u + c < wave_rows;
+        pos[u] = valid ? base + token : -1;
+        load_q<D, TERMS>(static_cast<const T*>(a.q) + (t.s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head, valid, lane, q[u]);
+    }
+    f32x4 o[QT][J];
+    float m[QT], l[QT];
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        m[u] = C4_LOW;
+        l[u] = 0.f;
+#pragma unroll
+        for (int j = 0; j < J; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    if (lots > 0) {
+        convert(half, 0);
+        if (lots > 1) {
+            fetch(1, half);
+            load(half);
+        }
+    }
+    __syncthreads();
+
+    for (int lot = 0; lot < lots; ++lot) {
+        if (lot + 1 < lots) {
+            convert(half, lot + 1);
+            if (lot + 2 < lots) {
+                fetch(lot + 2, half);
+                load(half);
+            }
+        }
+        const int buffer = lot & 1;
+#pragma unroll
+        for (int st = 0; st < HALVES / 2; ++st) {
+            const int key0 = key_first + lot * KEYS + 32 * st;
+            if (key0 > wave_top || key0 + 31 < wave_low) continue;
+            int state[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) state[s] = __builtin_amdgcn_readfirstlane(states[buffer][2 * st + s]);
+            const bool full = key0 + 31 <= full_top && key0 >= full_low && ((state[0] | state[1]) & 1) == 0;
+            f32x4 score[QT][2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+#pragma unroll
+                for (int u = 0; u < QT; ++u) score[u][s] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < M; ++i) {
+                    const bf16x8 k = __builtin_bit_cast(bf16x8, k_ops[buffer][2 * st + s][i][lane]);
+#pragma unroll
+                    for (int u = 0; u < QT; ++u)
+#pragma unroll
+                        for (int n = 0; n < TERMS; ++n) score[u][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[u][n][i], score[u][s], 0, 0, 0);
+                }
+            }
+            if (!full) {
+#pragma unroll
+                for (int u = 0; u < QT; ++u) {
+                    const int top = a.causal ? pos[u] : t.s.length - 1, bottom = a.window > 0 ? pos[u] - a.window + 1 : 0;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = key0 + 16 * s + 4 * h4 + i;
+                            if (!((state[s] & 1) == 0 && key <= top && key >= bottom)) score[u][s][i] = -__builtin_inff();
+                        }
+                }
+            }
+            if (((state[0] | state[1]) & 2) != 0) {          // seldom: NaN values, which must reach the rows that see them (as in the kernel above)
+                static_for<P::count>([&](auto pc) {
+                    constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;
+                    bf16x8 marks;
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) {
+                        const int page = c4_page(a.r, a.c, t.b, key0 + 16 * s);
+                        const uint8_t* exps = c4_record(a.c, max(page, 0), head) + a.c.v_exps + (key0 + 16 * s & (a.c.page - 1));
+                        const uint32_t bytes = *reinterpret_cast<const uint32_t*>(exps + ((B / 32 + c * E / 32) * a.c.page + 4 * h4));
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) marks[4 * s + i] = (bytes >> 8 * i & 255u) > C4_EXP_MAX ? (__bf16)1.f : (__bf16)0.f;
+                    }
+#pragma unroll
+                    for (int u = 0; u < QT; ++u) {
+                        bf16x8 seen;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) seen[i] = score[u][i >> 2][i & 3] == -__builtin_inff() ? (__bf16)0.f : (__bf16)1.f;
+                        const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(marks, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                        for (int j = 0; j < E; ++j)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i)
+                                if (count[i] > 0.f) o[u][B / 16 + j][i] = __builtin_nanf("");
+                    }
+                });
+            }
+            bf16x8 w[QT][TERMS];
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                float top = score[u][0][0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) top = fmaxf(top, score[u][i >> 2][i & 3]);
+                if (__ballot(top * a.scale > m[u] + C4_SLACK) != 0) {
+                    const float raised = fmaxf(m[u], row_max(top) * a.scale);
+                    const float factor = __builtin_amdgcn_exp2f(m[u] - raised);
+                    m[u] = raised;
+                    l[u] *= factor;
+#pragma unroll
+                    for (int j = 0; j < J; ++j) o[u][j] *= factor;
+                }
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(score[u][i >> 2][i & 3], a.scale, -m[u]));
+                    l[u] += x;
+                    __bf16 terms[TERMS];
+                    split_terms<TERMS>(x, terms);
+#pragma unroll
+                    for (int n = 0; n < TERMS; ++n) w[u][n][i] = terms[n];
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                const bf16x8 v = __builtin_bit_cast(bf16x8, v_ops[buffer][st][j][lane]);
+#pragma unroll
+                for (int u = 0; u < QT; ++u)
+#pragma unroll
+                    for (int n = 0; n < TERMS; ++n) o[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[u][n], o[u][j], 0, 0, 0);
+            }
+        }
+        __syncthreads();
+    }
+
+    const long long slot = ((long long)tile * a.c.kv_heads + head) * a.splits + split;
+#pragma unroll
+    for (int u = 0; u < QT; ++u) {
+        const float total = row_sum(l[u]);
+        if (16 * u + c >= wave_rows) continue;
+        const float f = !whole ? 1.f : total == 0.f ? 0.f : 1.f / total;
+        const int row = wave_row0 + 16 * u + c, r = 16 * QT * wave + 16 * u + c;
+        const int token = fast_div(row, a.div_group), g = row - token * a.group;
+        const long long at = ((long long)(t.s.first + token) * a.c.kv_heads + head) * a.group + g;
+        static_for<P::count>([&](auto pc) {
+            constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;       // E elements in a row
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int d = B + E * (4 * h4 + i);
+                float y[E];
+#pragma unroll
+                for (int j = 0; j < E; ++j) y[j] = whole && total == 0.f ? 0.f : o[u][B / 16 + j][i] * f;
+                if (whole) c4_store<E>(static_cast<T*>(a.out) + at * D + d, y);
+                else c4_store<E>(a.part + (slot * ROWS + r) * D + d, y);
+            }
+        });
+        if (h4 == 0) {
+            if (!whole) {
+                a.part_ml[(slot * ROWS + r) * 2] = m[u];
+                a.part_ml[(slot * ROWS + r) * 2 + 1] = total;
+            } else if (a.lse != nullptr) {
+                a.lse[at] = total == 0.f ? -__builtin_inff() : (m[u] + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+            }
+        }
+    }
+}
+
 // Joins the parts of the tiles whose keys were cut up: a workgroup per row of a tile.  D / 8 lanes hold a row's elements, eight each; the groups of so many lanes take
 // the parts in turn and meet in LDS.
-template <int D, int DTYPE, int QT, bool SPARSE>
+template <int D, int DTYPE, int ROWS, bool SPARSE>
 __global__ __launch_bounds__(256) void join_kernel(Attend4 a) {
     using T = typename C4Type<DTYPE>::type;
-    constexpr int ROWS = 16 * QT, LANES = D / 8, GROUPS = 256 / LANES;
+    constexpr int LANES = D / 8, GROUPS = 256 / LANES;
     __shared__ __align__(16) float sums[GROUPS][D + 4];
     __shared__ float totals[GROUPS];
     const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads, tile = rest, r = (int)blockIdx.y;
@@ -544,29 +833,31 @@ __global__ __launch_bounds__(256) void join_kernel(Attend4 a) {
     if (a.lse != nullptr && d == 0) a.lse[at] = total == 0.f ? -__builtin_inff() : (high + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
 }
 
-template <int D, int DTYPE, int QT, bool SPARSE>
-int launch_attend(const Attend4& a, hipStream_t s) {
+// kernel: attend_kernel or attend_rows_kernel, whose workgroups carry ROWS rows.
+template <int D, int DTYPE, int ROWS, bool SPARSE>
+int launch_attend(void (*kernel)(Attend4), const Attend4& a, hipStream_t s) {
     const unsigned heads = (unsigned)a.c.kv_heads;
-    launch(attend_kernel<D, DTYPE, QT, SPARSE>, dim3((unsigned)a.tiles * (unsigned)a.splits * heads), dim3(256), 0, s, a);
-    const unsigned rows = (unsigned)(SPARSE && a.group < 16 ? a.group : 16 * QT);
-    if (a.splits > 1) launch(join_kernel<D, DTYPE, QT, SPARSE>, dim3((unsigned)a.tiles * heads, rows), dim3(256), 0, s, a);
+    launch(kernel, dim3((unsigned)a.tiles * (unsigned)a.splits * heads), dim3(256), 0, s, a);
+    const unsigned rows = (unsigned)(SPARSE && a.group < ROWS ? a.group : ROWS);
+    if (a.splits > 1) launch(join_kernel<D, DTYPE, ROWS, SPARSE>, dim3((unsigned)a.tiles * heads, rows), dim3(256), 0, s, a);
     return check_launch();
 }
 
 template <int D, int DTYPE>
-int launch_attend_rows(const Attend4& a, int qtiles, hipStream_t s) {
-    if (a.blocks != nullptr) return launch_attend<D, DTYPE, 1, true>(a, s);
-    if (qtiles == 1) return launch_attend<D, DTYPE, 1, false>(a, s);
-    if constexpr (cache4_qtiles(D, DTYPE) >= 2) if (qtiles == 2) return launch_attend<D, DTYPE, 2, false>(a, s);
-    if constexpr (cache4_qtiles(D, DTYPE) >= 4) if (qtiles == 4) return launch_attend<D, DTYPE, 4, false>(a, s);
+int launch_attend_rows(const Attend4& a, int rows, hipStream_t s) {
+    if (a.blocks != nullptr) return launch_attend<D, DTYPE, 16, true>(attend_kernel<D, DTYPE, 1, true>, a, s);
+    constexpr int QT = cache4_wide_qtiles(D, DTYPE);
+    if (rows == 64 * QT) return launch_attend<D, DTYPE, 64 * QT, false>(attend_rows_kernel<D, DTYPE, QT>, a, s);
+    if (rows == 16) return launch_attend<D, DTYPE, 16, false>(attend_kernel<D, DTYPE, 1, false>, a, s);
+    if constexpr (cache4_qtiles(D, DTYPE) >= 2) if (rows == 32) return launch_attend<D, DTYPE, 32, false>(attend_kernel<D, DTYPE, 2, false>, a, s);
     return BNN_ERR_UNSUPPORTED;
 }
 
 template <int D>
-int launch_attend_type(const Attend4& a, int dtype, int qtiles, hipStream_t s) {
-    if (dtype == BNN_BF16) return launch_attend_rows<D, BNN_BF16>(a, qtiles, s);
-    if (dtype == BNN_F16) return launch_attend_rows<D, BNN_F16>(a, qtiles, s);
-    return launch_attend_rows<D, BNN_F32>(a, qtiles, s);
+int launch_attend_type(const Attend4& a, int dtype, int rows, hipStream_t s) {
+    if (dtype == BNN_BF16) return launch_attend_rows<D, BNN_BF16>(a, rows, s);
+    if (dtype == BNN_F16) return launch_attend_rows<D, BNN_F16>(a, rows, s);
+    return launch_attend_rows<D, BNN_F32>(a, rows, s);
 }
 
 }  // namespace

@@ -2,5 +2,5 @@
 #include "bnn_cache4_attend.h"
 
 namespace bnn {
-int launch_cache4_attend192(const Attend4& a, int dtype, int qtiles, hipStream_t s) { return launch_attend_type<192>(a, dtype, qtiles, s); }
+int launch_cache4_attend192(const Attend4& a, int dtype, int rows, hipStream_t s) { return launch_attend_type<192>(a, dtype, rows, s); }
 }  // namespace bnn

@@ -180,11 +180,15 @@ struct AttendPlan4 {
     size_t part_bytes, workspace_bytes;
 };
 
-// Groups of 16 rows that a wave carries, by what fits 256 registers: per group a lane keeps D / 4 of sums and D / 8 of every term of Q.  (With twice as many, at one
-// wave a SIMD, nothing runs while a wave waits: two prompts of 4096 tokens 631 us instead of 416.)
-constexpr int cache4_row_registers(int dim, int dtype) { return dim / 4 + (dtype == BNN_BF16 ? 1 : dtype == BNN_F16 ? 2 : 3) * (dim / 8); }
-constexpr int cache4_qtiles(int dim, int dtype) { return 2 * cache4_row_registers(dim, dtype) <= 150 ? 2 : 1; }          // a workgroup's rows, each wave has all
-constexpr int cache4_wide_qtiles(int dim, int dtype) { return 2 * cache4_row_registers(dim, dtype) <= 130 ? 2 : 1; }     // a wave's, of four with different rows
+// Groups of 16 rows that a wave carries, by what fits 256 registers: per group a lane keeps D / 4 of sums, D / 8 of every term of Q, and scores and weights.  (With twice as
+// many, at one wave a SIMD, nothing runs while a wave waits: two prompts of 4096 tokens 631 us instead of 416.)
+constexpr int cache4_terms(int dtype) { return dtype == BNN_BF16 ? 1 : dtype == BNN_F16 ? 2 : 3; }
+constexpr int cache4_qtiles(int dim, int dtype) {            // a workgroup's rows, each wave has all
+    return 2 * (dim / 4 + cache4_terms(dtype) * (dim / 8) + 4 * cache4_terms(dtype)) < 144 ? 2 : 1;
+}
+constexpr int cache4_wide_qtiles(int dim, int dtype) {       // a wave's, of four with different rows
+    return 2 * (dim / 4 + cache4_terms(dtype) * (dim / 8) + 8 * cache4_terms(dtype) + 16) <= 170 ? 2 : 1;
+}
 
 int launch_cache4_attend64(const Attend4& a, int dtype, int rows, hipStream_t s);
 int launch_cache4_attend96(const Attend4& a, int dtype, int rows, hipStream_t s);

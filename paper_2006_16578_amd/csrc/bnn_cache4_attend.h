@@ -11,8 +11,8 @@
 // a key side by side; lane l loads, for its eight keys, the elements 8 (l % 16) .. + 7, converts pairs and interleaves the halves of registers.
 // Element 8 i + j is then row i of product j.  64 and 32 elements that are left over of a head dimension work alike with 4 and 2 elements.
 //
-// The maximum follows the scores in steps: it is raised (and the sums rescaled) only when a score passes it by more than 8 (as powers of two), which a wave tests without
-// any exchange between lanes; weights are at most 2^8 then, and nothing is lost, as weights and sums scale alike.
+// The reference point of the weights follows the maximum in steps: it is raised, to 8 (as powers of two) above the highest score, and the sums rescaled, only when a score
+// passes it by more than 8, which a wave tests without any exchange between lanes; weights are at most 2^8 then, and nothing is lost, as weights and sums scale alike.
 //
 // Queries and weights enter the products as sums of 1 (bf16), 2 (fp16) or 3 (fp32) bf16 terms: queries exactly; weights to 8, 16 and 24 bits.
 #ifndef BNN_CACHE4_ATTEND_H
@@ -30,8 +30,6 @@ template <int DTYPE> struct C4Type { using type = float; static constexpr int te
 template <> struct C4Type<BNN_BF16> { using type = __bf16; static constexpr int terms = 1; };
 template <> struct C4Type<BNN_F16> { using type = _Float16; static constexpr int terms = 2; };
 
-template <int DTYPE> constexpr int TERMS4 = C4Type<DTYPE>::terms;
-
 // The largest over the four lanes of a row (lanes l, l + 16, l + 32, l + 48).
 __device__ __forceinline__ float row_max(float v) {
     auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -44,6 +42,22 @@ __device__ __forceinline__ float row_sum(float v) {
     v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
     auto b = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
     return __uint_as_float(b[0]) + __uint_as_float(b[1]);
+}
+
+// The largest of a lane's eight scores; NaN if there is one.  (fmaxf passes over NaN, for which every result of a matrix instruction takes an instruction more.)
+__device__ __forceinline__ float max8(const f32x4& a, const f32x4& b) {
+    const float v = __builtin_elementwise_maximum(__builtin_elementwise_maximum(a[0], a[1]), a[2]);
+    const float w = __builtin_elementwise_maximum(__builtin_elementwise_maximum(v, a[3]), b[0]);
+    return __builtin_elementwise_maximum(__builtin_elementwise_maximum(__builtin_elementwise_maximum(w, b[1]), b[2]), b[3]);
+}
+
+// The reference point of a row's weights, 2^(score - m): raised to C4_SLACK above the highest score when one has passed it by more than C4_SLACK.  Returns what sums are
+// scaled by.
+__device__ __forceinline__ float raise_maximum(float& m, float high) {
+    const float to = high > m + C4_SLACK ? high + C4_SLACK : m;
+    const float factor = __builtin_amdgcn_exp2f(m - to);
+    m = to;
+    return factor;
 }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -229,7 +243,7 @@ __device__ __forceinline__ void load_q(const T* src, bool valid, int lane, bf16x
 }
 
 template <int D, int DTYPE, int QT, bool SPARSE>
-__global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ? 1 : 2) void attend_kernel(Attend4 a) {
+__global__ __launch_bounds__(256, D == 256 && DTYPE == BNN_F32 ? 1 : 2) void attend_kernel(Attend4 a) {
     using T = typename C4Type<DTYPE>::type;
     constexpr int TERMS = C4Type<DTYPE>::terms;
     constexpr int ROWS = 16 * QT, M = D / 32, J = D / 16;
@@ -369,13 +383,9 @@ __global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ?
         bf16x8 w[QT][TERMS];
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
-            float high = score[u][0][0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) high = fmaxf(high, score[u][i >> 2][i & 3]);
+            const float high = max8(score[u][0], score[u][1]);
             if (__ballot(high * a.scale > m[u] + C4_SLACK) != 0) {
-                const float raised = fmaxf(m[u], row_max(high) * a.scale);
-                const float factor = __builtin_amdgcn_exp2f(m[u] - raised);
-                m[u] = raised;
+                const float factor = raise_maximum(m[u], row_max(high) * a.scale);
                 l[u] *= factor;
 #pragma unroll
                 for (int j = 0; j < J; ++j) o[u][j] *= factor;
@@ -502,20 +512,19 @@ __global__ __launch_bounds__(256, QT * (D / 4 + TERMS4<DTYPE> * (D / 8)) > 150 ?
     }
 }
 
-// Many rows: a workgroup's four waves have 16 * QT rows each and share keys.  KEYS keys at a time are converted once for all, each wave a part, and left in LDS as finished
-// operands (a lane's 16 bytes side by side: reads and writes without conflicts), two lots in turn, one barrier a lot; the codes of the lot after next are on
-// their way meanwhile.  Against the kernel above, where every wave converts for itself, this takes a third off the vector instructions. 
-// KEYS = 64: wave w converts the 16 keys of half w.  32 (heads wider than 128, whose operands take as much LDS then): waves 0 and 2 convert K, 1 and 3 V.
+// Many rows: a workgroup's four waves have 16 * QT rows each and share keys.  32 keys at a time are converted once for all and left in LDS as finished operands (a
+// lane's 16 bytes side by side: reads and writes without conflicts): waves 0 and 2 convert K, two steps ahead of its use, 1 and 3 V; one barrier a step.
+// In step i a wave forms the scores of step i + 1, the weights of step i and the sums of step i - 1: three pieces of work that do not wait for each other, so that matrix
+// and vector instructions of one wave alternate.  A maximum that is raised in step i scales the sums at the step's end, when those of step i - 1 are in.
 template <int D, int DTYPE, int QT>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     using T = typename C4Type<DTYPE>::type;
     constexpr int TERMS = C4Type<DTYPE>::terms;
-    constexpr int KEYS = D > 128 ? 32 : 64, HALVES = KEYS / 16;
     constexpr int ROWS = 64 * QT, M = D / 32, J = D / 16;
     using P = Pieces<D>;
-    __shared__ u32x4 k_ops[2][HALVES][M][64];
-    __shared__ u32x4 v_ops[2][HALVES / 2][J][64];
-    __shared__ int states[2][HALVES];        // 1: the half is in no page; 2: it has NaN values, which were taken as finite
+    __shared__ u32x4 k_ops[2][2][M][64];     // [step % 2][half][..]
+    __shared__ u32x4 v_ops[2][J][64];
+    __shared__ int nans[2][2];               // [step % 2][half]: values that are NaN and were taken as finite
 
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int c = lane & 15, h4 = lane >> 4;
@@ -524,96 +533,102 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     const Tile4 t = find_tile<ROWS, false>(a, tile);
     if (t.rows <= 0) return;
     const Range4 range = tile_steps<false>(a, t);
-    const int begin = split * a.chunk, end = min(range.count, begin + a.chunk);       // steps of 32 keys; a.chunk is a multiple of 4
+    const int begin = split * a.chunk, end = min(range.count, begin + a.chunk);
     if (split > 0 && begin >= end) return;
     const bool whole = range.count <= a.chunk;
-    const int lots = (32 * (end - begin) + KEYS - 1) / KEYS, key_first = 32 * (range.first + begin);
-    const int half_own = HALVES == 4 ? wave : wave >> 1;
-    const bool does_k = HALVES == 4 || (wave & 1) == 0, does_v = HALVES == 4 || (wave & 1) == 1;
+    const int steps = max(end - begin, 0), key_first = 32 * (range.first + begin);
+    const int own = wave >> 1;               // the half of every step that this wave converts, K and V in turn with its neighbour
 
-    // Where this wave's halves of the next 64 lots lie, a lane each.
-    uint32_t low = 0, high = 0;
-    unsigned long long present = 0;
-    auto fetch = [&](int lot, Half4& half) {
-        if (lot % 64 == 0) {
-            const int key = key_first + (lot + lane) * KEYS + 16 * half_own;
-            const int page = c4_page(a.r, a.c, t.b, key);
-            present = __ballot(page >= 0);
-            const uint64_t at = (uint64_t)(c4_record(a.c, max(page, 0), head) - a.c.data);
-            low = (uint32_t)at;
-            high = (uint32_t)(at >> 32);
-        }
-        half.record = a.c.data + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)high, lot % 64) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)low, lot % 64));
-        half.key = key_first + lot * KEYS + 16 * half_own;
-        half.offset = half.key & (a.c.page - 1);
-        half.there = present >> (lot % 64) & 1;
+    // Where the halves of 32 steps lie, a lane each (2 * step + half), and which are in a page; K's turn is ahead of V's.
+    struct Pages {
+        uint32_t low, high;
+        unsigned long long present;
     };
-    uint32_t k_codes[M], k_exp[P::count], v_codes[P::count][4], v_exp[P::count][1];
-    auto load = [&](const Half4& half) {
-        if (does_k) load_k_half<D>(a.c, half, lane, k_codes, k_exp);
-        if (does_v) load_v_half<D, 4>(a.c, half, lane, v_codes, v_exp, 0);
+    auto locate = [&](Pages& p, int step) {  // step: a multiple of 32
+        const int page = c4_page(a.r, a.c, t.b, key_first + 32 * step + 16 * lane);
+        p.present = __ballot(page >= 0);
+        const uint64_t at = (uint64_t)(c4_record(a.c, max(page, 0), head) - a.c.data);
+        p.low = (uint32_t)at;
+        p.high = (uint32_t)(at >> 32);
+    };
+    auto place = [&](const Pages& p, int step) {                     // of this wave's half
+        const int at = 2 * (step % 32) + own;
+        Half4 half;
+        half.record = a.c.data + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)p.high, at) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)p.low, at));
+        half.key = key_first + 32 * step + 16 * own;
+        half.offset = half.key & (a.c.page - 1);
+        half.there = true;
+        return half;
     };
 
     const int base = t.s.length - t.s.rows;
-    // The keys that every row of the workgroup sees: [low_last, top_first]; those that some row of this wave sees: [wave_low, wave_top]
+    // The keys that every row of the workgroup sees, [low_last, top_first], that every row of this wave sees, [full_low, full_top], and that some row of it sees
     const int top_first = a.causal ? base + fast_div(t.row0, a.div_group) : t.s.length - 1;
     const int low_last = a.window > 0 ? base + fast_div(t.row0 + t.rows - 1, a.div_group) - a.window + 1 : 0;
     const int wave_rows = min(16 * QT, t.rows - 16 * QT * wave), wave_row0 = t.row0 + 16 * QT * wave;
     const int wave_first = base + fast_div(wave_row0, a.div_group), wave_last = base + fast_div(wave_row0 + max(wave_rows, 1) - 1, a.div_group);
-    const int wave_top = wave_rows <= 0 ? -1 : a.causal ? wave_last : t.s.length - 1, wave_low = a.window > 0 ? wave_first - a.window + 1 : 0;
     const int full_top = a.causal ? wave_first : t.s.length - 1, full_low = a.window > 0 ? wave_last - a.window + 1 : 0;
 
-    // Finished operands of the half that was loaded.  There are no keys beyond the last page: what is converted for them is masked.
-    auto convert = [&](const Half4& half, int lot) {
-        const int buffer = lot & 1;
-        const int first = key_first + lot * KEYS;
-        const bool masks = !(first + KEYS - 1 <= top_first && first >= low_last && half.there);
-        if (does_k) {
-            static_for<P::count>([&](auto pc) {
-                constexpr int p = pc.value, W = P::width(p), B = P::base(p);
-                const float scale = c4_scale(k_exp[p]);
+    uint32_t k_codes[M], k_exp[P::count], v_codes[P::count][4], v_exp[P::count][1];
+    Pages k_pages = {}, v_pages = {};
+    // Whether masks are at work in the step (for any row of the workgroup; asked while V's pages are at hand): NaN must not spread then.
+    auto masked = [&](int step) {
+        const int first = key_first + 32 * step;
+        return !(first + 31 <= top_first && first >= low_last && (v_pages.present >> 2 * (step % 32) & 3) == 3);
+    };
+    auto convert_k = [&](int step) {         // what was loaded
+        static_for<P::count>([&](auto pc) {
+            constexpr int p = pc.value, W = P::width(p), B = P::base(p);
+            const float scale = c4_scale(k_exp[p]);
 #pragma unroll
-                for (int i = 0; i < W / 32; ++i) k_ops[buffer][half_own][B / 32 + i][lane] = __builtin_bit_cast(u32x4, eight_of(k_codes[B / 32 + i], scale));
-            });
-        }
-        if (does_v) {
+            for (int i = 0; i < W / 32; ++i) k_ops[step & 1][own][B / 32 + i][lane] = __builtin_bit_cast(u32x4, eight_of(k_codes[B / 32 + i], scale));
+        });
+    };
+    auto convert_v = [&](int step) {
+        if (masked(step)) {
             bool bad = false;
-            if (masks) {
 #pragma unroll
-                for (int p = 0; p < P::count; ++p)
+            for (int p = 0; p < P::count; ++p)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if ((v_exp[p][0] >> 8 * i & 255u) > C4_EXP_MAX) {
-                            bad = true;
-                            v_exp[p][0] &= ~(255u << 8 * i);
-                        }
-            }
+                for (int i = 0; i < 4; ++i)
+                    if ((v_exp[p][0] >> 8 * i & 255u) > C4_EXP_MAX) {
+                        bad = true;
+                        v_exp[p][0] &= ~(255u << 8 * i);
+                    }
             const bool any = __ballot(bad) != 0;
-            if (lane == 0) states[buffer][half_own] = (half.there ? 0 : 1) + (any ? 2 : 0);
-            static_for<P::count>([&](auto pc) {
-                constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;
-                float scale[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) scale[i] = c4_scale(v_exp[p][0] >> 8 * i & 255u);
-                static_for<E / 2>([&](auto ec) {
-                    constexpr int e = ec.value;
-                    uint32_t v[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v[i] = pair_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v_codes[p][i], scale[i], e));
-                    u32x2* even = reinterpret_cast<u32x2*>(&v_ops[buffer][half_own >> 1][B / 16 + 2 * e][lane]) + (half_own & 1);
-                    u32x2* odd = reinterpret_cast<u32x2*>(&v_ops[buffer][half_own >> 1][B / 16 + 2 * e + 1][lane]) + (half_own & 1);
-                    *even = u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u)};
-                    *odd = u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u)};
-                });
-            });
+            if (lane == 0) nans[step & 1][own] = any;
         }
+        static_for<P::count>([&](auto pc) {
+            constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;
+            float scale[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) scale[i] = c4_scale(v_exp[p][0] >> 8 * i & 255u);
+            static_for<E / 2>([&](auto ec) {
+                constexpr int e = ec.value;
+                uint32_t v[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = pair_bits(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(v_codes[p][i], scale[i], e));
+                u32x2* even = reinterpret_cast<u32x2*>(&v_ops[step & 1][B / 16 + 2 * e][lane]) + own;
+                u32x2* odd = reinterpret_cast<u32x2*>(&v_ops[step & 1][B / 16 + 2 * e + 1][lane]) + own;
+                *even = u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x05040100u), __builtin_amdgcn_perm(v[3], v[2], 0x05040100u)};
+                *odd = u32x2{__builtin_amdgcn_perm(v[1], v[0], 0x07060302u), __builtin_amdgcn_perm(v[3], v[2], 0x07060302u)};
+            });
+        });
+    };
+    // The page table is read at every 32nd step, whichever wave's turn it is.
+    auto load_k_step = [&](int step, bool mine) {
+        if (step >= steps) return;
+        if (step % 32 == 0) locate(k_pages, step);
+        if (mine) load_k_half<D>(a.c, place(k_pages, step), lane, k_codes, k_exp);
+    };
+    auto load_v_step = [&](int step, bool mine) {
+        if (step >= steps) return;
+        if (step % 32 == 0) locate(v_pages, step);
+        if (mine) load_v_half<D, 4>(a.c, place(v_pages, step), lane, v_codes, v_exp, 0);
     };
 
-    Half4 half = {};
-    if (lots > 0) {
-        fetch(0, half);
-        load(half);
-    }
+    load_k_step(0, (wave & 1) == 0);
+    load_k_step(1, (wave & 1) == 1);
     bf16x8 q[QT][TERMS][M];
     int pos[QT];                             // position of the lane's row; -1: no row
 #pragma unroll
@@ -633,119 +648,182 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
 #pragma unroll
         for (int j = 0; j < J; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    if (lots > 0) {
-        convert(half, 0);
-        if (lots > 1) {
-            fetch(1, half);
-            load(half);
-        }
-    }
-    __syncthreads();
 
-    for (int lot = 0; lot < lots; ++lot) {
-        if (lot + 1 < lots) {
-            convert(half, lot + 1);
-            if (lot + 2 < lots) {
-                fetch(lot + 2, half);
-                load(half);
-            }
-        }
-        const int buffer = lot & 1;
+    constexpr int SHARE = (QT * 8 * (2 + 2 * TERMS) + J + 2 * M - 1) / (J + 2 * M);
+    using Scores = f32x4[QT][2];
+    using Weights = bf16x8[QT][TERMS];
+    auto visible = [&](int u, int key, bool there) {
+        const int top = a.causal ? pos[u] : t.s.length - 1, bottom = a.window > 0 ? pos[u] - a.window + 1 : 0;
+        return there && key <= top && key >= bottom;
+    };
+    auto products = [&](Scores& score, int step) {
 #pragma unroll
-        for (int st = 0; st < HALVES / 2; ++st) {
-            const int key0 = key_first + lot * KEYS + 32 * st;
-            if (key0 > wave_top || key0 + 31 < wave_low) continue;
-            int state[2];
+        for (int s = 0; s < 2; ++s) {
 #pragma unroll
-            for (int s = 0; s < 2; ++s) state[s] = __builtin_amdgcn_readfirstlane(states[buffer][2 * st + s]);
-            const bool full = key0 + 31 <= full_top && key0 >= full_low && ((state[0] | state[1]) & 1) == 0;
-            f32x4 score[QT][2];
+            for (int u = 0; u < QT; ++u) score[u][s] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-#pragma unroll
-                for (int u = 0; u < QT; ++u) score[u][s] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < M; ++i) {
-                    const bf16x8 k = __builtin_bit_cast(bf16x8, k_ops[buffer][2 * st + s][i][lane]);
-#pragma unroll
-                    for (int u = 0; u < QT; ++u)
-#pragma unroll
-                        for (int n = 0; n < TERMS; ++n) score[u][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[u][n][i], score[u][s], 0, 0, 0);
-                }
-            }
-            if (!full) {
-#pragma unroll
-                for (int u = 0; u < QT; ++u) {
-                    const int top = a.causal ? pos[u] : t.s.length - 1, bottom = a.window > 0 ? pos[u] - a.window + 1 : 0;
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int key = key0 + 16 * s + 4 * h4 + i;
-                            if (!((state[s] & 1) == 0 && key <= top && key >= bottom)) score[u][s][i] = -__builtin_inff();
-                        }
-                }
-            }
-            if (((state[0] | state[1]) & 2) != 0) {          // seldom: NaN values, which must reach the rows that see them (as in the kernel above)
-                static_for<P::count>([&](auto pc) {
-                    constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;
-                    bf16x8 marks;
-#pragma unroll
-                    for (int s = 0; s < 2; ++s) {
-                        const int page = c4_page(a.r, a.c, t.b, key0 + 16 * s);
-                        const uint8_t* exps = c4_record(a.c, max(page, 0), head) + a.c.v_exps + (key0 + 16 * s & (a.c.page - 1));
-                        const uint32_t bytes = *reinterpret_cast<const uint32_t*>(exps + ((B / 32 + c * E / 32) * a.c.page + 4 * h4));
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) marks[4 * s + i] = (bytes >> 8 * i & 255u) > C4_EXP_MAX ? (__bf16)1.f : (__bf16)0.f;
-                    }
-#pragma unroll
-                    for (int u = 0; u < QT; ++u) {
-                        bf16x8 seen;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) seen[i] = score[u][i >> 2][i & 3] == -__builtin_inff() ? (__bf16)0.f : (__bf16)1.f;
-                        const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(marks, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                        for (int j = 0; j < E; ++j)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i)
-                                if (count[i] > 0.f) o[u][B / 16 + j][i] = __builtin_nanf("");
-                    }
-                });
-            }
-            bf16x8 w[QT][TERMS];
-#pragma unroll
-            for (int u = 0; u < QT; ++u) {
-                float top = score[u][0][0];
-#pragma unroll
-                for (int i = 1; i < 8; ++i) top = fmaxf(top, score[u][i >> 2][i & 3]);
-                if (__ballot(top * a.scale > m[u] + C4_SLACK) != 0) {
-                    const float raised = fmaxf(m[u], row_max(top) * a.scale);
-                    const float factor = __builtin_amdgcn_exp2f(m[u] - raised);
-                    m[u] = raised;
-                    l[u] *= factor;
-#pragma unroll
-                    for (int j = 0; j < J; ++j) o[u][j] *= factor;
-                }
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(score[u][i >> 2][i & 3], a.scale, -m[u]));
-                    l[u] += x;
-                    __bf16 terms[TERMS];
-                    split_terms<TERMS>(x, terms);
-#pragma unroll
-                    for (int n = 0; n < TERMS; ++n) w[u][n][i] = terms[n];
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const bf16x8 v = __builtin_bit_cast(bf16x8, v_ops[buffer][st][j][lane]);
+            for (int i = 0; i < M; ++i) {
+                const bf16x8 k = __builtin_bit_cast(bf16x8, k_ops[step & 1][s][i][lane]);
 #pragma unroll
                 for (int u = 0; u < QT; ++u)
 #pragma unroll
-                    for (int n = 0; n < TERMS; ++n) o[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[u][n], o[u][j], 0, 0, 0);
+                    for (int n = 0; n < TERMS; ++n) score[u][s] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[u][n][i], score[u][s], 0, 0, 0);
             }
         }
+    };
+    auto sums = [&](const Weights& w, int step) {
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const bf16x8 v = __builtin_bit_cast(bf16x8, v_ops[step & 1][j][lane]);
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+#pragma unroll
+                for (int n = 0; n < TERMS; ++n) o[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[u][n], o[u][j], 0, 0, 0);
+        }
+    };
+    // Step i of the loop; there: which of its halves are in a page; now: its scores, next: where those of step i + 1 go; before: the weights of step i - 1, after: where its own go.
+    auto turn = [&](auto first, int i, int there, Scores& now, Scores& next, const Weights& before, Weights& after) {
+        const int key0 = key_first + 32 * i;
+        if (!(key0 + 31 <= full_top && key0 >= full_low && there == 3)) {
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    if (!visible(u, key0 + 16 * (x >> 2) + 4 * h4 + (x & 3), there >> (x >> 2) & 1)) now[u][x >> 2][x & 3] = -__builtin_inff();
+        }
+        float factor[QT];
+        bool raise = false;
+#pragma unroll
+        for (int u = 0; u < QT; ++u) {
+            const float top = max8(now[u][0], now[u][1]);
+            factor[u] = top;
+            raise = raise || top * a.scale > m[u] + C4_SLACK;
+        }
+        const bool raised = __ballot(raise) != 0;
+        if (raised) {
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                factor[u] = raise_maximum(m[u], row_max(factor[u]) * a.scale);
+                l[u] *= factor[u];
+            }
+        }
+        if constexpr (!first.value) sums(before, i - 1);
+#pragma unroll
+        for (int u = 0; u < QT; ++u)
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                const float y = __builtin_amdgcn_exp2f(fmaf(now[u][x >> 2][x & 3], a.scale, -m[u]));
+                l[u] += y;
+                __bf16 terms[TERMS];
+                split_terms<TERMS>(y, terms);
+#pragma unroll
+                for (int n = 0; n < TERMS; ++n) after[u][n][x] = terms[n];
+            }
+        products(next, i + 1);               // (of the last step: what is left in LDS, and not used)
+#pragma unroll
+        for (int u = 0; u < QT; ++u)         // the weights are wanted here, among the products, not where they are used
+#pragma unroll
+            for (int n = 0; n < TERMS; ++n) {
+                u32x4 bits = __builtin_bit_cast(u32x4, after[u][n]);
+                asm volatile("" : "+v"(bits));
+                after[u][n] = __builtin_bit_cast(bf16x8, bits);
+            }
+        // One read of LDS, two ahead of its use, QT * TERMS matrix and a share of the vector instructions at a time
+        __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+        for (int x = 0; x < J + 2 * M; ++x) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, QT * TERMS, 0);
+            __builtin_amdgcn_sched_group_barrier(0x402, SHARE, 0);
+        }
+        if (raised) {
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+#pragma unroll
+                for (int j = 0; j < J; ++j) o[u][j] *= factor[u];
+        }
+    };
+    // Seldom: NaN values, which must reach the rows that see them (as in the kernel above).
+    auto spread_nans = [&](int i, bool was_masked) {
+        if (!was_masked || (__builtin_amdgcn_readfirstlane(nans[i & 1][0]) | __builtin_amdgcn_readfirstlane(nans[i & 1][1])) == 0) return;
+        const int key0 = key_first + 32 * i;
+        static_for<P::count>([&](auto pc) {
+            constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;
+            bf16x8 marks;
+            bool there[2];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int page = c4_page(a.r, a.c, t.b, key0 + 16 * s);
+                there[s] = page >= 0;
+                const uint8_t* exps = c4_record(a.c, max(page, 0), head) + a.c.v_exps + ((key0 + 16 * s) & (a.c.page - 1));
+                const uint32_t bytes = *reinterpret_cast<const uint32_t*>(exps + ((B / 32 + c * E / 32) * a.c.page + 4 * h4));
+#pragma unroll
+                for (int x = 0; x < 4; ++x) marks[4 * s + x] = (bytes >> 8 * x & 255u) > C4_EXP_MAX ? (__bf16)1.f : (__bf16)0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                bf16x8 seen;
+#pragma unroll
+                for (int x = 0; x < 8; ++x) seen[x] = visible(u, key0 + 16 * (x >> 2) + 4 * h4 + (x & 3), there[x >> 2]) ? (__bf16)1.f : (__bf16)0.f;
+                const f32x4 count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(marks, seen, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                for (int j = 0; j < E; ++j)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        if (count[x] > 0.f) o[u][B / 16 + j][x] = __builtin_nanf("");
+            }
+        });
+    };
+
+    Scores s0, s1;
+    Weights w0, w1;
+    // K of steps 0 and 1 before the loop.  Within step i: K of step i + 2 and V of step i, loaded a step earlier, by the two waves of a half in turn.
+    auto does_v = [&](int i) { return ((wave ^ i) & 1) == 1; };
+    auto load_for = [&](int i) {
+        load_k_step(i + 2, !does_v(i));
+        load_v_step(i, does_v(i));
+    };
+    if (steps > 0) {
+        if ((wave & 1) == 0) convert_k(0);
+        else if (steps > 1) convert_k(1);
+        load_for(0);
         __syncthreads();
+        products(s0, 0);
+        __syncthreads();                     // step 2's K may take step 0's place
+    }
+    auto prepare = [&](int i) {
+        if (does_v(i)) convert_v(i);
+        else if (i + 2 < steps) convert_k(i + 2);
+        if (i + 1 < steps) load_for(i + 1);
+    };
+    if (steps > 0) {
+        // (what prepare() asks of step i's pages is asked before it goes on to those of step i + 1)
+        bool was_masked = masked(0);
+        int there = (int)(v_pages.present & 3);
+        prepare(0);
+        turn(std::true_type{}, 0, there, s0, s1, w1, w0);
+        __syncthreads();
+        for (int i = 1; i < steps; i += 2) {
+            bool is_masked = masked(i);
+            there = (int)(v_pages.present >> 2 * (i % 32) & 3);
+            prepare(i);
+            spread_nans(i - 1, was_masked);
+            turn(std::false_type{}, i, there, s1, s0, w0, w1);
+            __syncthreads();
+            was_masked = is_masked;
+            if (i + 1 < steps) {
+                is_masked = masked(i + 1);
+                there = (int)(v_pages.present >> 2 * ((i + 1) % 32) & 3);
+                prepare(i + 1);
+                spread_nans(i, was_masked);
+                turn(std::false_type{}, i + 1, there, s0, s1, w1, w0);
+                __syncthreads();
+                was_masked = is_masked;
+            }
+        }
+        spread_nans(steps - 1, was_masked);
+        if (steps % 2 == 1) sums(w0, steps - 1);
+        else sums(w1, steps - 1);
     }
 
     const long long slot = ((long long)tile * a.c.kv_heads + head) * a.splits + split;

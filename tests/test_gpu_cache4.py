@@ -233,6 +233,18 @@ def test_attend_many_tokens(bnn, dtype, dim, page, heads, group):
     check_attend(su, su.queries(heads * group, 3.0))
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+def test_attend_chunks_of_a_long_cache(bnn, dim, dtype):
+    # many rows at the end of a few hundred keys: several steps before any mask, pages given back, a window that starts in the middle; and keys cut into parts
+    su = Setup(bnn, 19, [700, 333, 65], [40, 70, 65], 1, dim, 64, dtype=dtype, width=80)
+    su.table[0, 3] = su.table[1, 0] = -1
+    su.replan()
+    q = su.queries(3, 2.0)
+    check_attend(su, q)
+    check_attend(su, q, window=150)
+
+
 def test_attend_ragged_batch_of_many_sequences(bnn):
     # more sequences than lanes of a wave
     rng = np.random.default_rng(0)
@@ -272,7 +284,7 @@ def test_attend_over_blocks(bnn, dtype, dim, page, heads, group):
     check_attend(su, q, blocks=blocks, causal=False)
 
 
-@pytest.mark.parametrize("counts", [[1, 1, 1], [20, 20, 20], [40, 3, 1]])
+@pytest.mark.parametrize("counts", [[1, 1, 1], [20, 20, 20], [40, 3, 1], [44, 44, 44], [60, 41, 44]])
 def test_what_is_masked_does_not_arrive(bnn, counts):
     # NaN keys and values: rows that see them become NaN, rows before them and other heads and sequences do not
     lens = [60, 50, 44]

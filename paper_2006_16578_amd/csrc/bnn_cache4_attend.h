@@ -3,7 +3,7 @@
 // Rows of queries that share a kv head -- its query heads, for one token or for several -- are the columns of the products, keys their rows:
 //   S^T [keys][rows] = K Q^T,   O^T [dim][rows] += V^T P^T   (v_mfma_f32_16x16x32_bf16).
 // A lane then holds, of 32 keys, the scores of ONE row at 8 keys, and exactly those eight are its operand of the second product: softmax weights never cross
-// lanes.  Four waves share the 16 * QT rows of a workgroup and take steps of 32 keys in turn, each with a running maximum and sum of its own; they meet in LDS once, at the end.
+// lanes.  Eight or four waves share the 16 * QT rows of a workgroup and take steps of 32 keys in turn, each with a running maximum and sum of its own; they meet in LDS once, at the end.
 // The cache's values are exact in bf16: the conversion instruction applies the scale.
 //
 // K: lane l supplies key l % 16 of a step's half and, of every 128 elements, the 32 of group l / 16: one 16-byte load and one scale.  Which elements a matrix
@@ -243,14 +243,14 @@ __device__ __forceinline__ void load_q(const T* src, bool valid, int lane, bf16x
 }
 
 template <int D, int DTYPE, int QT, bool SPARSE>
-__global__ __launch_bounds__(256, D == 256 && DTYPE == BNN_F32 ? 1 : 2) void attend_kernel(Attend4 a) {
+__global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE == BNN_F32 ? 1 : 2) void attend_kernel(Attend4 a) {
     using T = typename C4Type<DTYPE>::type;
     constexpr int TERMS = C4Type<DTYPE>::terms;
-    constexpr int ROWS = 16 * QT, M = D / 32, J = D / 16;
+    constexpr int ROWS = 16 * QT, M = D / 32, J = D / 16, WAVES = cache4_waves(D, DTYPE, QT);
     constexpr int LD = D + 4;                // floats of a row in LDS: rows of the 16 lanes fall on different banks
     using P = Pieces<D>;
-    __shared__ __align__(16) float sums[4][16][LD];
-    __shared__ float stats[4][ROWS][2];
+    __shared__ __align__(16) float sums[WAVES][16][LD];
+    __shared__ float stats[WAVES][ROWS][2];
 
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int c = lane & 15, h4 = lane >> 4;
@@ -269,12 +269,12 @@ __global__ __launch_bounds__(256, D == 256 && DTYPE == BNN_F32 ? 1 : 2) void att
     const int32_t* list = SPARSE ? a.blocks + ((long long)(t.s.first + fast_div(t.row0, a.div_group)) * a.c.kv_heads + head) * a.keep : nullptr;
     const int per_shift = a.c.page_shift - 4;                        // halves of steps in a page
     // Where the halves of this wave's next 32 steps lie, a lane each: the record's offset in the cache, the first key's number (sparse), whether there is a page.
-    const int turns = (end - begin - wave + 3) / 4;                  // steps of this wave
+    const int turns = (end - begin - wave + WAVES - 1) / WAVES;                  // steps of this wave
     uint32_t low = 0, high = 0;
     int keys = 0;
     unsigned long long present = 0;
     auto locate = [&](int turn) {                                    // turn: a multiple of 32
-        const int i = 2 * (range.first + begin + wave + 4 * (turn + (lane >> 1))) + (lane & 1);
+        const int i = 2 * (range.first + begin + wave + WAVES * (turn + (lane >> 1))) + (lane & 1);
         bool listed = true;
         if constexpr (SPARSE) {
             const int entry = i >> per_shift;
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(256, D == 256 && DTYPE == BNN_F32 ? 1 : 2) void att
         for (int s = 0; s < 2; ++s) {
             const int at = 2 * (turn % 32) + s;
             half[s].record = a.c.data + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)high, at) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)low, at));
-            half[s].key = SPARSE ? __builtin_amdgcn_readlane(keys, at) : 32 * (range.first + begin + wave + 4 * turn) + 16 * s;
+            half[s].key = SPARSE ? __builtin_amdgcn_readlane(keys, at) : 32 * (range.first + begin + wave + WAVES * turn) + 16 * s;
             half[s].offset = half[s].key & (a.c.page - 1);
             half[s].there = present >> at & 1;
         }
@@ -480,14 +480,14 @@ __global__ __launch_bounds__(256, D == 256 && DTYPE == BNN_F32 ? 1 : 2) void att
                 for (int j = 0; j < E; ++j) sums[wave][c][B + E * (4 * h4 + i) + j] = o[u][B / 16 + j][i];
         });
         __syncthreads();
-        for (int x = (int)threadIdx.x; x < 16 * (D / 8); x += 256) {
+        for (int x = (int)threadIdx.x; x < 16 * (D / 8); x += 64 * WAVES) {
             const int row = x / (D / 8), d = x % (D / 8) * 8, r = 16 * u + row;
             if (r >= t.rows) continue;
             float high = C4_LOW, total = 0.f, y[8] = {};
 #pragma unroll
-            for (int v = 0; v < 4; ++v) high = fmaxf(high, stats[v][r][0]);
+            for (int v = 0; v < WAVES; ++v) high = fmaxf(high, stats[v][r][0]);
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
+            for (int v = 0; v < WAVES; ++v) {
                 const float f = __builtin_amdgcn_exp2f(stats[v][r][0] - high);
                 total = fmaf(stats[v][r][1], f, total);
 #pragma unroll
@@ -913,9 +913,9 @@ __global__ __launch_bounds__(256) void join_kernel(Attend4 a) {
 
 // kernel: attend_kernel or attend_rows_kernel, whose workgroups carry ROWS rows.
 template <int D, int DTYPE, int ROWS, bool SPARSE>
-int launch_attend(void (*kernel)(Attend4), const Attend4& a, hipStream_t s) {
+int launch_attend(void (*kernel)(Attend4), int threads, const Attend4& a, hipStream_t s) {
     const unsigned heads = (unsigned)a.c.kv_heads;
-    launch(kernel, dim3((unsigned)a.tiles * (unsigned)a.splits * heads), dim3(256), 0, s, a);
+    launch(kernel, dim3((unsigned)a.tiles * (unsigned)a.splits * heads), dim3((unsigned)threads), 0, s, a);
     const unsigned rows = (unsigned)(SPARSE && a.group < ROWS ? a.group : ROWS);
     if (a.splits > 1) launch(join_kernel<D, DTYPE, ROWS, SPARSE>, dim3((unsigned)a.tiles * heads, rows), dim3(256), 0, s, a);
     return check_launch();
@@ -923,11 +923,11 @@ int launch_attend(void (*kernel)(Attend4), const Attend4& a, hipStream_t s) {
 
 template <int D, int DTYPE>
 int launch_attend_rows(const Attend4& a, int rows, hipStream_t s) {
-    if (a.blocks != nullptr) return launch_attend<D, DTYPE, 16, true>(attend_kernel<D, DTYPE, 1, true>, a, s);
+    if (a.blocks != nullptr) return launch_attend<D, DTYPE, 16, true>(attend_kernel<D, DTYPE, 1, true>, 64 * cache4_waves(D, DTYPE, 1), a, s);
     constexpr int QT = cache4_wide_qtiles(D, DTYPE);
-    if (rows == 64 * QT) return launch_attend<D, DTYPE, 64 * QT, false>(attend_rows_kernel<D, DTYPE, QT>, a, s);
-    if (rows == 16) return launch_attend<D, DTYPE, 16, false>(attend_kernel<D, DTYPE, 1, false>, a, s);
-    if constexpr (cache4_qtiles(D, DTYPE) >= 2) if (rows == 32) return launch_attend<D, DTYPE, 32, false>(attend_kernel<D, DTYPE, 2, false>, a, s);
+    if (rows == 64 * QT) return launch_attend<D, DTYPE, 64 * QT, false>(attend_rows_kernel<D, DTYPE, QT>, 256, a, s);
+    if (rows == 16) return launch_attend<D, DTYPE, 16, false>(attend_kernel<D, DTYPE, 1, false>, 64 * cache4_waves(D, DTYPE, 1), a, s);
+    if constexpr (cache4_qtiles(D, DTYPE) >= 2) if (rows == 32) return launch_attend<D, DTYPE, 32, false>(attend_kernel<D, DTYPE, 2, false>, 64 * cache4_waves(D, DTYPE, 2), a, s);
     return BNN_ERR_UNSUPPORTED;
 }
 

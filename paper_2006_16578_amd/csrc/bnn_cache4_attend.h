@@ -149,9 +149,16 @@ struct Pieces {
     static constexpr int base(int p) { return p < n128 ? 128 * p : p < n128 + n64 ? 128 * n128 : 128 * n128 + 64 * n64; }
 };
 
+// Memory of the cache by an address that lanes hold and hand over as two 32-bit halves.
+typedef const uint8_t __attribute__((address_space(1))) * Global4;
+template <class T>
+__device__ __forceinline__ T load_at(Global4 base, uint32_t offset) {
+    return *reinterpret_cast<const T __attribute__((address_space(1))) *>(base + offset);
+}
+
 // Where the 16 keys of half a step lie, all in one page.  Uniform over a wave.
 struct Half4 {
-    const uint8_t* record;
+    Global4 record;
     int offset;                              // of the first key in the page
     int key;                                 // its number in the sequence
     bool there;
@@ -167,27 +174,26 @@ struct Raw4 {
     uint32_t v_exp[P::count][2];
 };
 
-// (The parts of an address that differ between lanes are 32-bit numbers that no step changes; the rest is scalar.)
+// (Scalar: the record; a lane's offset in it is one addition to a number that no step changes.)
 template <int D>
 __device__ __forceinline__ void load_k_half(const Cache4& c, const Half4& half, int lane, uint32_t (&codes)[D / 32], uint32_t (&exp)[Pieces<D>::count]) {
     using P = Pieces<D>;
     const uint32_t col = lane & 15, h4 = lane >> 4;
-    const uint8_t* row = half.record + half.offset * (D / 2);
-    const uint8_t* exps = half.record + c.k_exps + half.offset;
+    const uint32_t row = col * (D / 2) + (uint32_t)half.offset * (D / 2);
     static_for<P::count>([&](auto pc) {
         constexpr int p = pc.value, W = P::width(p), B = P::base(p);
         if constexpr (W == 128) {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(row + (col * (D / 2) + B / 2 + 16 * h4));
+            const u32x4 v = load_at<u32x4>(half.record, row + 16 * h4 + B / 2);
 #pragma unroll
             for (int i = 0; i < 4; ++i) codes[B / 32 + i] = v[i];
         } else if constexpr (W == 64) {
-            const u32x2 v = *reinterpret_cast<const u32x2*>(row + (col * (D / 2) + B / 2 + 8 * h4));
+            const u32x2 v = load_at<u32x2>(half.record, row + 8 * h4 + B / 2);
             codes[B / 32] = v[0];
             codes[B / 32 + 1] = v[1];
         } else {
-            codes[B / 32] = *reinterpret_cast<const uint32_t*>(row + (col * (D / 2) + B / 2 + 4 * h4));
+            codes[B / 32] = load_at<uint32_t>(half.record, row + 4 * h4 + B / 2);
         }
-        exp[p] = exps[(B / 32 + h4 * W / 128) * (uint32_t)c.page + col];
+        exp[p] = load_at<uint8_t>(half.record, (uint32_t)c.k_exps + (B / 32 + h4 * W / 128) * (uint32_t)c.page + col + (uint32_t)half.offset);
     });
 }
 // codes[p][0..3] and exp[p]: of the keys 4 (lane / 16) .. + 3 of the half.
@@ -196,20 +202,22 @@ __device__ __forceinline__ void load_v_half(const Cache4& c, const Half4& half, 
                                             int s) {
     using P = Pieces<D>;
     const uint32_t col = lane & 15, h4 = lane >> 4;
-    const uint8_t* from = half.record + c.v_codes + half.offset * (D / 2);
-    const uint8_t* exps = half.record + c.v_exps + half.offset;
     static_for<P::count>([&](auto pc) {
         constexpr int p = pc.value, W = P::width(p), B = P::base(p), E = W / 16;           // E elements of each of 4 keys
+        const uint32_t from = (uint32_t)c.v_codes + 4 * h4 * (D / 2) + B / 2 + E / 2 * col + (uint32_t)half.offset * (D / 2);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint8_t* at = from + ((4 * h4 + i) * (D / 2) + B / 2 + E / 2 * col);
-            if constexpr (E == 8) codes[p][4 * s + i] = *reinterpret_cast<const uint32_t*>(at);
-            else if constexpr (E == 4) codes[p][4 * s + i] = *reinterpret_cast<const uint16_t*>(at);
-            else codes[p][4 * s + i] = *at;
+            if constexpr (E == 8) codes[p][4 * s + i] = load_at<uint32_t>(half.record, from + i * (D / 2));
+            else if constexpr (E == 4) codes[p][4 * s + i] = load_at<uint16_t>(half.record, from + i * (D / 2));
+            else codes[p][4 * s + i] = load_at<uint8_t>(half.record, from + i * (D / 2));
         }
-        exp[p][s] = *reinterpret_cast<const uint32_t*>(exps + ((B / 32 + col * E / 32) * (uint32_t)c.page + 4 * h4));
+        exp[p][s] = load_at<uint32_t>(half.record, (uint32_t)c.v_exps + (B / 32 + col * E / 32) * (uint32_t)c.page + 4 * h4 + (uint32_t)half.offset);
     });
 }
+__device__ __forceinline__ Global4 record_of(uint32_t low, uint32_t high, int lane) {
+    return reinterpret_cast<Global4>((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)high, lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)low, lane));
+}
+
 template <int D>
 __device__ __forceinline__ void load_k(const Cache4& c, const Half4 (&half)[2], int lane, Raw4<D>& raw) {
 #pragma unroll
@@ -268,7 +276,7 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
     const int base = t.s.length - t.s.rows;
     const int32_t* list = SPARSE ? a.blocks + ((long long)(t.s.first + fast_div(t.row0, a.div_group)) * a.c.kv_heads + head) * a.keep : nullptr;
     const int per_shift = a.c.page_shift - 4;                        // halves of steps in a page
-    // Where the halves of this wave's next 32 steps lie, a lane each: the record's offset in the cache, the first key's number (sparse), whether there is a page.
+    // Where the halves of this wave's next 32 steps lie, a lane each: the record's address, the first key's number (sparse), whether there is a page.
     const int turns = (end - begin - wave + WAVES - 1) / WAVES;                  // steps of this wave
     uint32_t low = 0, high = 0;
     int keys = 0;
@@ -286,7 +294,7 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
         }
         const int page = c4_page(a.r, a.c, t.b, keys);
         present = __ballot(listed && page >= 0);
-        const uint64_t at = (uint64_t)(c4_record(a.c, max(page, 0), head) - a.c.data);
+        const uint64_t at = (uint64_t)(uintptr_t)c4_record(a.c, max(page, 0), head);
         low = (uint32_t)at;
         high = (uint32_t)(at >> 32);
     };
@@ -295,7 +303,7 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
             const int at = 2 * (turn % 32) + s;
-            half[s].record = a.c.data + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)high, at) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)low, at));
+            half[s].record = record_of(low, high, at);
             half[s].key = SPARSE ? __builtin_amdgcn_readlane(keys, at) : 32 * (range.first + begin + wave + WAVES * turn) + 16 * s;
             half[s].offset = half[s].key & (a.c.page - 1);
             half[s].there = present >> at & 1;
@@ -539,22 +547,22 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     const int steps = max(end - begin, 0), key_first = 32 * (range.first + begin);
     const int own = wave >> 1;               // the half of every step that this wave converts, K and V in turn with its neighbour
 
-    // Where the halves of 32 steps lie, a lane each (2 * step + half), and which are in a page; K's turn is ahead of V's.
+    // Where the halves of 32 steps lie, a lane each (2 * step + half); whole: all that are asked for are in pages.  K's turn is ahead of V's.
     struct Pages {
         uint32_t low, high;
-        unsigned long long present;
+        bool whole;
     };
     auto locate = [&](Pages& p, int step) {  // step: a multiple of 32
         const int page = c4_page(a.r, a.c, t.b, key_first + 32 * step + 16 * lane);
-        p.present = __ballot(page >= 0);
-        const uint64_t at = (uint64_t)(c4_record(a.c, max(page, 0), head) - a.c.data);
+        p.whole = __ballot(page < 0 && step + lane / 2 < steps) == 0;
+        const uint64_t at = (uint64_t)(uintptr_t)c4_record(a.c, max(page, 0), head);
         p.low = (uint32_t)at;
         p.high = (uint32_t)(at >> 32);
     };
     auto place = [&](const Pages& p, int step) {                     // of this wave's half
         const int at = 2 * (step % 32) + own;
         Half4 half;
-        half.record = a.c.data + ((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)p.high, at) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)p.low, at));
+        half.record = record_of(p.low, p.high, at);
         half.key = key_first + 32 * step + 16 * own;
         half.offset = half.key & (a.c.page - 1);
         half.there = true;
@@ -562,20 +570,25 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     };
 
     const int base = t.s.length - t.s.rows;
-    // The keys that every row of the workgroup sees, [low_last, top_first], that every row of this wave sees, [full_low, full_top], and that some row of it sees
-    const int top_first = a.causal ? base + fast_div(t.row0, a.div_group) : t.s.length - 1;
-    const int low_last = a.window > 0 ? base + fast_div(t.row0 + t.rows - 1, a.div_group) - a.window + 1 : 0;
     const int wave_rows = min(16 * QT, t.rows - 16 * QT * wave), wave_row0 = t.row0 + 16 * QT * wave;
-    const int wave_first = base + fast_div(wave_row0, a.div_group), wave_last = base + fast_div(wave_row0 + max(wave_rows, 1) - 1, a.div_group);
-    const int full_top = a.causal ? wave_first : t.s.length - 1, full_low = a.window > 0 ? wave_last - a.window + 1 : 0;
+    // Steps whose keys every row of some rows sees, [from, from + count), if all are in pages: of the workgroup's rows, and of this wave's
+    struct Steps {
+        int from;
+        unsigned count;
+        __device__ bool operator()(int step) const { return (unsigned)(step - from) < count; }
+    };
+    auto seen_by_all = [&](int row0, int rows) {
+        const int first = base + fast_div(row0, a.div_group), last = base + fast_div(row0 + max(rows, 1) - 1, a.div_group);
+        const int top = a.causal ? first : t.s.length - 1, bottom = a.window > 0 ? max(last - a.window + 1, 0) : 0;
+        Steps r;
+        r.from = max((bottom - key_first + 31) >> 5, 0);
+        r.count = (unsigned)max(((top + 1 - key_first) >> 5) - r.from, 0);
+        return r;
+    };
+    const Steps clear = seen_by_all(t.row0, t.rows), wave_clear = seen_by_all(wave_row0, wave_rows);
 
     uint32_t k_codes[M], k_exp[P::count], v_codes[P::count][4], v_exp[P::count][1];
     Pages k_pages = {}, v_pages = {};
-    // Whether masks are at work in the step (for any row of the workgroup; asked while V's pages are at hand): NaN must not spread then.
-    auto masked = [&](int step) {
-        const int first = key_first + 32 * step;
-        return !(first + 31 <= top_first && first >= low_last && (v_pages.present >> 2 * (step % 32) & 3) == 3);
-    };
     auto convert_k = [&](int step) {         // what was loaded
         static_for<P::count>([&](auto pc) {
             constexpr int p = pc.value, W = P::width(p), B = P::base(p);
@@ -584,8 +597,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
             for (int i = 0; i < W / 32; ++i) k_ops[step & 1][own][B / 32 + i][lane] = __builtin_bit_cast(u32x4, eight_of(k_codes[B / 32 + i], scale));
         });
     };
-    auto convert_v = [&](int step) {
-        if (masked(step)) {
+    auto convert_v = [&](int step, bool masked) {                    // masked: some row of the workgroup does not see some key
+        if (masked) {
             bool bad = false;
 #pragma unroll
             for (int p = 0; p < P::count; ++p)
@@ -681,15 +694,16 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
                 for (int n = 0; n < TERMS; ++n) o[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, w[u][n], o[u][j], 0, 0, 0);
         }
     };
-    // Step i of the loop; there: which of its halves are in a page; now: its scores, next: where those of step i + 1 go; before: the weights of step i - 1, after: where its own go.
-    auto turn = [&](auto first, int i, int there, Scores& now, Scores& next, const Weights& before, Weights& after) {
-        const int key0 = key_first + 32 * i;
-        if (!(key0 + 31 <= full_top && key0 >= full_low && there == 3)) {
+    // Step i of the loop; whole: its keys are all in pages; now: its scores, next: where those of step i + 1 go; before: the weights of step i - 1, after: where its own go.
+    auto turn = [&](auto first, int i, bool whole, Scores& now, Scores& next, const Weights& before, Weights& after) {
+        if (!(whole && wave_clear(i))) {
+            const int key0 = key_first + 32 * i;
+            const bool there[2] = {c4_page(a.r, a.c, t.b, key0) >= 0, c4_page(a.r, a.c, t.b, key0 + 16) >= 0};
 #pragma unroll
             for (int u = 0; u < QT; ++u)
 #pragma unroll
                 for (int x = 0; x < 8; ++x)
-                    if (!visible(u, key0 + 16 * (x >> 2) + 4 * h4 + (x & 3), there >> (x >> 2) & 1)) now[u][x >> 2][x & 3] = -__builtin_inff();
+                    if (!visible(u, key0 + 16 * (x >> 2) + 4 * h4 + (x & 3), there[x >> 2])) now[u][x >> 2][x & 3] = -__builtin_inff();
         }
         float factor[QT];
         bool raise = false;
@@ -778,50 +792,47 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     Scores s0, s1;
     Weights w0, w1;
     // K of steps 0 and 1 before the loop.  Within step i: K of step i + 2 and V of step i, loaded a step earlier, by the two waves of a half in turn.
-    auto does_v = [&](int i) { return ((wave ^ i) & 1) == 1; };
-    auto load_for = [&](int i) {
-        load_k_step(i + 2, !does_v(i));
-        load_v_step(i, does_v(i));
+    const bool odd = (wave & 1) == 1;        // a wave that converts V in even steps
+    auto load_for = [&](int i, bool v) {
+        load_k_step(i + 2, !v);
+        load_v_step(i, v);
+    };
+    auto prepare = [&](int i, bool v, bool masked) {
+        if (v) convert_v(i, masked);
+        else if (i + 2 < steps) convert_k(i + 2);
+        if (i + 1 < steps) load_for(i + 1, !v);
     };
     if (steps > 0) {
-        if ((wave & 1) == 0) convert_k(0);
+        if (!odd) convert_k(0);
         else if (steps > 1) convert_k(1);
-        load_for(0);
+        load_for(0, odd);
         __syncthreads();
         products(s0, 0);
         __syncthreads();                     // step 2's K may take step 0's place
-    }
-    auto prepare = [&](int i) {
-        if (does_v(i)) convert_v(i);
-        else if (i + 2 < steps) convert_k(i + 2);
-        if (i + 1 < steps) load_for(i + 1);
-    };
-    if (steps > 0) {
-        // (what prepare() asks of step i's pages is asked before it goes on to those of step i + 1)
-        bool was_masked = masked(0);
-        int there = (int)(v_pages.present & 3);
-        prepare(0);
-        turn(std::true_type{}, 0, there, s0, s1, w1, w0);
+        // (whether step i's keys are in pages is asked before prepare() goes on to the pages of step i + 1)
+        bool whole = v_pages.whole, masked = !(whole && clear(0));
+        prepare(0, odd, masked);
+        turn(std::true_type{}, 0, whole, s0, s1, w1, w0);
         __syncthreads();
         for (int i = 1; i < steps; i += 2) {
-            bool is_masked = masked(i);
-            there = (int)(v_pages.present >> 2 * (i % 32) & 3);
-            prepare(i);
+            bool was_masked = masked;
+            whole = v_pages.whole;
+            masked = !(whole && clear(i));
+            prepare(i, !odd, masked);
             spread_nans(i - 1, was_masked);
-            turn(std::false_type{}, i, there, s1, s0, w0, w1);
+            turn(std::false_type{}, i, whole, s1, s0, w0, w1);
             __syncthreads();
-            was_masked = is_masked;
             if (i + 1 < steps) {
-                is_masked = masked(i + 1);
-                there = (int)(v_pages.present >> 2 * ((i + 1) % 32) & 3);
-                prepare(i + 1);
+                was_masked = masked;
+                whole = v_pages.whole;
+                masked = !(whole && clear(i + 1));
+                prepare(i + 1, odd, masked);
                 spread_nans(i, was_masked);
-                turn(std::false_type{}, i + 1, there, s0, s1, w1, w0);
+                turn(std::false_type{}, i + 1, whole, s0, s1, w1, w0);
                 __syncthreads();
-                was_masked = is_masked;
             }
         }
-        spread_nans(steps - 1, was_masked);
+        spread_nans(steps - 1, masked);
         if (steps % 2 == 1) sums(w0, steps - 1);
         else sums(w1, steps - 1);
     }

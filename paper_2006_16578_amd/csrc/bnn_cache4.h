@@ -171,7 +171,7 @@ struct Attend4 {
     int splits, chunk;                       // parts the keys are cut into: of `chunk` steps of 32 keys
     FastDiv div_splits, div_heads;
     float* part;                             // [tiles][kv_heads][splits][rows of a tile][dim]
-    float* part_ml;                          // ... [2]: maximum and sum
+    f32x4* part_sums;                        // [tiles][kv_heads][splits][rows of a tile]: reference point, sum of the weights, sum of the rounded weights
 };
 
 // How a call is cut up.  rows: of a workgroup.

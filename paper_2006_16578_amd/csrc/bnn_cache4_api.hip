@@ -89,7 +89,7 @@ AttendPlan4 plan_attend(const Cache4& c, const Rows4& r, int dtype, int group, i
     if (p.splits > 1) {
         const size_t rows = (size_t)tiles * c.kv_heads * p.splits * p.rows;
         p.part_bytes = rows * c.dim * 4;
-        p.workspace_bytes = p.part_bytes + rows * 8;
+        p.workspace_bytes = p.part_bytes + rows * sizeof(f32x4);
     }
     return p;
 }
@@ -194,7 +194,7 @@ int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
     a.div_splits = make_fastdiv((uint32_t)p.splits);
     a.div_heads = make_fastdiv((uint32_t)a.c.kv_heads);
     a.part = static_cast<float*>(workspace);
-    a.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + p.part_bytes);
+    a.part_sums = reinterpret_cast<f32x4*>(static_cast<char*>(workspace) + p.part_bytes);
     hipStream_t s = static_cast<hipStream_t>(stream);
     switch (a.c.dim) {
         case 64: return launch_cache4_attend64(a, dtype, p.rows, s);

@@ -14,6 +14,8 @@
 // The reference point of the weights follows the maximum in steps: it is raised, to 8 (as powers of two) above the highest score, and the sums rescaled, only when a score
 // passes it by more than 8, which a wave tests without any exchange between lanes; weights are at most 2^8 then, and nothing is lost, as weights and sums scale alike.
 //
+// Weights of one bf16 term are divided by the sum of the rounded weights, a product with ones, so that where one key has nearly all the weight its rounding cancels
+// (error against 64 bits 0.0016 of the result's size, 0.0015 from rounding the result; 0.0022 without); the logarithm of the sum is of the unrounded ones.
 // Queries and weights enter the products as sums of 1 (bf16), 2 (fp16) or 3 (fp32) bf16 terms: queries exactly; weights to 8, 16 and 24 bits.
 #ifndef BNN_CACHE4_ATTEND_H
 #define BNN_CACHE4_ATTEND_H
@@ -64,6 +66,7 @@ __device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, 
     const u32x4 v = {a, b, c, d};
     return __builtin_bit_cast(bf16x8, v);
 }
+__device__ __forceinline__ bf16x8 ones() { return as_bf16x8(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u); }
 __device__ __forceinline__ uint32_t pair_bits(bf16x2 v) { return __builtin_bit_cast(uint32_t, v); }
 
 // x as a sum of TERMS bf16 numbers, the largest first.
@@ -258,7 +261,7 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
     constexpr int LD = D + 4;                // floats of a row in LDS: rows of the 16 lanes fall on different banks
     using P = Pieces<D>;
     __shared__ __align__(16) float sums[WAVES][16][LD];
-    __shared__ float stats[WAVES][ROWS][2];
+    __shared__ float stats[WAVES][ROWS][3];  // reference point, sum of the weights, sum of the rounded weights
 
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int c = lane & 15, h4 = lane >> 4;
@@ -332,12 +335,13 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
         load_q<D, TERMS>(static_cast<const T*>(a.q) + (t.s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head, valid, lane, q[u]);
     }
 
-    f32x4 o[QT][J];
+    f32x4 o[QT][J], rounded[QT];
     float m[QT], l[QT];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         m[u] = C4_LOW;
         l[u] = 0.f;
+        rounded[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < J; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -395,6 +399,7 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
             if (__ballot(high * a.scale > m[u] + C4_SLACK) != 0) {
                 const float factor = raise_maximum(m[u], row_max(high) * a.scale);
                 l[u] *= factor;
+                rounded[u] *= factor;
 #pragma unroll
                 for (int j = 0; j < J; ++j) o[u][j] *= factor;
             }
@@ -407,6 +412,7 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
 #pragma unroll
                 for (int n = 0; n < TERMS; ++n) w[u][n][i] = terms[n];
             }
+            if constexpr (TERMS == 1) rounded[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones(), w[u][0], rounded[u], 0, 0, 0);
         }
 
         // V
@@ -473,6 +479,7 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
         if (h4 == 0) {
             stats[wave][16 * u + c][0] = m[u];
             stats[wave][16 * u + c][1] = sum;
+            stats[wave][16 * u + c][2] = TERMS == 1 ? rounded[u][0] : sum;
         }
     }
     const long long slot = ((long long)tile * a.c.kv_heads + head) * a.splits + split;
@@ -491,30 +498,28 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
         for (int x = (int)threadIdx.x; x < 16 * (D / 8); x += 64 * WAVES) {
             const int row = x / (D / 8), d = x % (D / 8) * 8, r = 16 * u + row;
             if (r >= t.rows) continue;
-            float high = C4_LOW, total = 0.f, y[8] = {};
+            float high = C4_LOW, total = 0.f, divisor = 0.f, y[8] = {};
 #pragma unroll
             for (int v = 0; v < WAVES; ++v) high = fmaxf(high, stats[v][r][0]);
 #pragma unroll
             for (int v = 0; v < WAVES; ++v) {
                 const float f = __builtin_amdgcn_exp2f(stats[v][r][0] - high);
                 total = fmaf(stats[v][r][1], f, total);
+                divisor = fmaf(stats[v][r][2], f, divisor);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) y[e] = fmaf(sums[v][row][d + e], f, y[e]);
             }
             if (whole) {
                 const int token = fast_div(t.row0 + r, a.div_group), g = t.row0 + r - token * a.group;
                 const long long at = ((long long)(t.s.first + token) * a.c.kv_heads + head) * a.group + g;
-                const float f = total == 0.f ? 0.f : 1.f / total;
+                const float f = 1.f / divisor;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = total == 0.f ? 0.f : y[e] * f;
+                for (int e = 0; e < 8; ++e) y[e] = divisor == 0.f ? 0.f : y[e] * f;
                 c4_store8(static_cast<T*>(a.out) + at * D + d, y);
                 if (a.lse != nullptr && d == 0) a.lse[at] = total == 0.f ? -__builtin_inff() : (high + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
             } else {
                 c4_store8(a.part + (slot * ROWS + r) * D + d, y);
-                if (d == 0) {
-                    a.part_ml[(slot * ROWS + r) * 2] = high;
-                    a.part_ml[(slot * ROWS + r) * 2 + 1] = total;
-                }
+                if (d == 0) a.part_sums[slot * ROWS + r] = f32x4{high, total, divisor, 0.f};
             }
         }
     }
@@ -652,12 +657,13 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
         pos[u] = valid ? base + token : -1;
         load_q<D, TERMS>(static_cast<const T*>(a.q) + (t.s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head, valid, lane, q[u]);
     }
-    f32x4 o[QT][J];
+    f32x4 o[QT][J], rounded[QT];
     float m[QT], l[QT];
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         m[u] = C4_LOW;
         l[u] = 0.f;
+        rounded[u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < J; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -685,6 +691,9 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
         }
     };
     auto sums = [&](const Weights& w, int step) {
+        if constexpr (TERMS == 1)
+#pragma unroll
+            for (int u = 0; u < QT; ++u) rounded[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones(), w[u][0], rounded[u], 0, 0, 0);
 #pragma unroll
         for (int j = 0; j < J; ++j) {
             const bf16x8 v = __builtin_bit_cast(bf16x8, v_ops[step & 1][j][lane]);
@@ -752,9 +761,11 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
         }
         if (raised) {
 #pragma unroll
-            for (int u = 0; u < QT; ++u)
+            for (int u = 0; u < QT; ++u) {
+                rounded[u] *= factor[u];
 #pragma unroll
                 for (int j = 0; j < J; ++j) o[u][j] *= factor[u];
+            }
         }
     };
     // Seldom: NaN values, which must reach the rows that see them (as in the kernel above).
@@ -840,9 +851,9 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     const long long slot = ((long long)tile * a.c.kv_heads + head) * a.splits + split;
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
-        const float total = row_sum(l[u]);
+        const float total = row_sum(l[u]), divisor = TERMS == 1 ? rounded[u][0] : total;
         if (16 * u + c >= wave_rows) continue;
-        const float f = !whole ? 1.f : total == 0.f ? 0.f : 1.f / total;
+        const float f = whole ? 1.f / divisor : 1.f;
         const int row = wave_row0 + 16 * u + c, r = 16 * QT * wave + 16 * u + c;
         const int token = fast_div(row, a.div_group), g = row - token * a.group;
         const long long at = ((long long)(t.s.first + token) * a.c.kv_heads + head) * a.group + g;
@@ -853,15 +864,14 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
                 const int d = B + E * (4 * h4 + i);
                 float y[E];
 #pragma unroll
-                for (int j = 0; j < E; ++j) y[j] = whole && total == 0.f ? 0.f : o[u][B / 16 + j][i] * f;
+                for (int j = 0; j < E; ++j) y[j] = whole && divisor == 0.f ? 0.f : o[u][B / 16 + j][i] * f;
                 if (whole) c4_store<E>(static_cast<T*>(a.out) + at * D + d, y);
                 else c4_store<E>(a.part + (slot * ROWS + r) * D + d, y);
             }
         });
         if (h4 == 0) {
             if (!whole) {
-                a.part_ml[(slot * ROWS + r) * 2] = m[u];
-                a.part_ml[(slot * ROWS + r) * 2 + 1] = total;
+                a.part_sums[slot * ROWS + r] = f32x4{m[u], total, divisor, 0.f};
             } else if (a.lse != nullptr) {
                 a.lse[at] = total == 0.f ? -__builtin_inff() : (m[u] + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
             }
@@ -876,7 +886,7 @@ __global__ __launch_bounds__(256) void join_kernel(Attend4 a) {
     using T = typename C4Type<DTYPE>::type;
     constexpr int LANES = D / 8, GROUPS = 256 / LANES;
     __shared__ __align__(16) float sums[GROUPS][D + 4];
-    __shared__ float totals[GROUPS];
+    __shared__ float totals[GROUPS][2];
     const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads, tile = rest, r = (int)blockIdx.y;
     const Tile4 t = find_tile<ROWS, SPARSE>(a, tile);
     if (r >= t.rows) return;
@@ -885,23 +895,28 @@ __global__ __launch_bounds__(256) void join_kernel(Attend4 a) {
     const int parts = (range.count + a.chunk - 1) / a.chunk;
     const long long slot = (((long long)tile * a.c.kv_heads + head) * a.splits) * ROWS + r;
     const int group = (int)threadIdx.x / LANES, d = (int)threadIdx.x % LANES * 8;
-    const float* ml = a.part_ml + slot * 2;
-    float high = C4_LOW, total = 0.f, y[8] = {};
-    for (int p = (int)threadIdx.x & 63; p < parts; p += 64) high = fmaxf(high, ml[(long long)p * ROWS * 2]);
+    const f32x4* ml = a.part_sums + slot;
+    float high = C4_LOW, total = 0.f, divisor = 0.f, y[8] = {};
+    for (int p = (int)threadIdx.x & 63; p < parts; p += 64) high = fmaxf(high, ml[(long long)p * ROWS][0]);
     high = row_max(high);
 #pragma unroll
     for (int x = 1; x < 16; x <<= 1) high = fmaxf(high, __shfl_xor(high, x));
     if (group < GROUPS) {
         for (int p = group; p < parts; p += GROUPS) {
-            const float f = __builtin_amdgcn_exp2f(ml[(long long)p * ROWS * 2] - high);
-            total = fmaf(ml[(long long)p * ROWS * 2 + 1], f, total);
+            const f32x4 v = ml[(long long)p * ROWS];
+            const float f = __builtin_amdgcn_exp2f(v[0] - high);
+            total = fmaf(v[1], f, total);
+            divisor = fmaf(v[2], f, divisor);
             float part[8];
             c4_load8(a.part + (slot + (long long)p * ROWS) * D + d, part);
 #pragma unroll
             for (int e = 0; e < 8; ++e) y[e] = fmaf(part[e], f, y[e]);
         }
         c4_store8(&sums[group][d], y);
-        if (d == 0) totals[group] = total;
+        if (d == 0) {
+            totals[group][0] = total;
+            totals[group][1] = divisor;
+        }
     }
     __syncthreads();
     if (group > 0) return;
@@ -909,15 +924,16 @@ __global__ __launch_bounds__(256) void join_kernel(Attend4 a) {
     for (int g = 1; g < groups; ++g) {
         float part[8];
         c4_load8(&sums[g][d], part);
-        total += totals[g];
+        total += totals[g][0];
+        divisor += totals[g][1];
 #pragma unroll
         for (int e = 0; e < 8; ++e) y[e] += part[e];
     }
     const int token = fast_div(t.row0 + r, a.div_group), g = t.row0 + r - token * a.group;
     const long long at = ((long long)(t.s.first + token) * a.c.kv_heads + head) * a.group + g;
-    const float f = total == 0.f ? 0.f : 1.f / total;
+    const float f = 1.f / divisor;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = total == 0.f ? 0.f : y[e] * f;
+    for (int e = 0; e < 8; ++e) y[e] = divisor == 0.f ? 0.f : y[e] * f;
     c4_store8(static_cast<T*>(a.out) + at * D + d, y);
     if (a.lse != nullptr && d == 0) a.lse[at] = total == 0.f ? -__builtin_inff() : (high + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
 }

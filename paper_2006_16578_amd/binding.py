@@ -834,8 +834,12 @@ class Cache4:
         _dev(data, torch.uint8, 3, "data")
         if data.shape[1] != kv_heads or data.shape[2] != record or pages not in (None, data.shape[0]):
             raise ValueError("data must be [pages][kv_heads][%d]" % record)
-        self.data, self.kv_heads, self.head_dim, self.page, self.signs = data, int(kv_heads), int(head_dim), int(page), bool(signs)
+        self.kv_heads, self.head_dim, self.page, self.signs = int(kv_heads), int(head_dim), int(page), bool(signs)
         self._plain = (data, self.kv_heads, self.head_dim, self.page, int(self.signs))         # what the native module takes
+
+    @property
+    def data(self):
+        return self._plain[0]
 
     def _struct(self):
         return ctypes.byref(_Cache4Struct(self.data.data_ptr(), self.data.shape[0], self.kv_heads, self.head_dim, self.page, int(self.signs)))
@@ -864,7 +868,7 @@ class Cache4:
             raise ValueError("%s must be on the cache's device" % name)
         if x.stride(2) != 1 and x.numel() != 0:
             raise ValueError("the elements of a head of %s must be contiguous" % name)
-        return _ELEMENTS[x.dtype], ctypes.c_int64(x.stride(0)), ctypes.c_int64(x.stride(1))
+        return _ELEMENTS[x.dtype], *(ctypes.c_int64(x.stride(i) if x.shape[i] > 1 else 0) for i in (0, 1))
 
     def write(self, k, v, table, lens, start=None):
         """Quantises k, v [tokens][kv_heads][head_dim], the newest tokens of every sequence, into the cache."""

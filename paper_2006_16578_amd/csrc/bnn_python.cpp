@@ -64,6 +64,8 @@ struct Call {
         ok = type == at::kFloat || type == at::kBFloat16 || type == at::kHalf;
         return &t;
     }
+    // Elements between neighbours of a dimension; of one of a single entry there are none.
+    static int64_t distance(const Tensor& t, int dim) { return t.size(dim) > 1 ? t.stride(dim) : 0; }
     bool truth(PyObject* o) {
         ok = ok && (o == Py_True || o == Py_False);
         return o == Py_True;
@@ -380,7 +382,8 @@ PyObject* cache4_write(PyObject*, PyObject* const* a, Py_ssize_t nargs) {    // 
         PLAIN(c);
         if (code != code_v || k.size(0) != v.size(0) || k.size(1) != p.cache.kv_heads || v.size(1) != p.cache.kv_heads) Py_RETURN_NONE;
         p.finish((int)k.size(0));
-        if (!run(c, "bnn_cache4_write", p_bnn_cache4_write, &p.cache, &p.rows, k.data_ptr(), v.data_ptr(), code, k.stride(0), k.stride(1), v.stride(0), v.stride(1)))
+        if (!run(c, "bnn_cache4_write", p_bnn_cache4_write, &p.cache, &p.rows, k.data_ptr(), v.data_ptr(), code, Call::distance(k, 0), Call::distance(k, 1),
+                 Call::distance(v, 0), Call::distance(v, 1)))
             return nullptr;
         Py_RETURN_TRUE;
     });
@@ -413,7 +416,7 @@ PyObject* cache4_select(PyObject*, PyObject* const* a, Py_ssize_t nargs) {   // 
         p.finish((int)q.size(0));
         const Tensor blocks = empty(q, {q.size(0), p.cache.kv_heads, keep}, at::kInt);
         const Tensor work = empty(q, {std::max<int64_t>((int64_t)p_bnn_cache4_select_workspace_bytes(&p.cache, &p.rows), 16)}, at::kByte);
-        const bool done = run(c, "bnn_cache4_select", p_bnn_cache4_select, &p.cache, &p.rows, q.data_ptr(), code, q.stride(0), q.stride(1), (int)q.size(1), keep, first, last,
+        const bool done = run(c, "bnn_cache4_select", p_bnn_cache4_select, &p.cache, &p.rows, q.data_ptr(), code, Call::distance(q, 0), Call::distance(q, 1), (int)q.size(1), keep, first, last,
                               ptr<int32_t>(blocks), work.data_ptr(), (size_t)work.numel());
         return done ? THPVariable_Wrap(blocks) : nullptr;
     });
@@ -440,7 +443,7 @@ PyObject* cache4_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs) {   // 
         if (want_lse) lse = empty(q, {q.size(0), heads}, at::kFloat);
         const size_t need = p_bnn_cache4_attend_workspace_bytes(&p.cache, &p.rows, code, heads, window, keep);
         if (need) work = empty(q, {(int64_t)need}, at::kByte);
-        const bool done = run(c, "bnn_cache4_attend", p_bnn_cache4_attend, &p.cache, &p.rows, q.data_ptr(), code, q.stride(0), q.stride(1), heads, scale, (int)causal, window,
+        const bool done = run(c, "bnn_cache4_attend", p_bnn_cache4_attend, &p.cache, &p.rows, q.data_ptr(), code, Call::distance(q, 0), Call::distance(q, 1), heads, scale, (int)causal, window,
                               blocks ? ptr<int32_t>(*blocks) : nullptr, keep, out.data_ptr(), want_lse ? ptr<float>(lse) : nullptr, need ? work.data_ptr() : nullptr, need);
         if (!done) return nullptr;
         return want_lse ? pair(out, lse) : THPVariable_Wrap(out);

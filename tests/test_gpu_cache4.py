@@ -166,6 +166,10 @@ def test_strided_inputs_and_no_signs(bnn):
     assert torch.equal(a, su.gpu.attend(q.contiguous(), **su.plan))
     assert torch.equal(a, su.gpu.attend(q.transpose(0, 1).contiguous().transpose(0, 1), **su.plan))
     check_attend(su, host(q))
+    # a dimension of one entry, whatever its stride says
+    one = torch.as_strided(q[:1].contiguous(), (1, 4, 64), (3, 64, 1))
+    plan = dict(table=su.plan["table"][:1], lens=su.plan["lens"][:1])
+    assert torch.equal(su.gpu.attend(one, **plan), su.gpu.attend(q[:1].contiguous(), **plan))
     with pytest.raises(ValueError):
         su.gpu.write(k.transpose(1, 2), v, **su.plan)
     with pytest.raises(bnn.BnnError) as e:                           # no signs were kept
@@ -189,7 +193,7 @@ def test_select(bnn, dim, page, heads, group, dtype):
         assert (got == want).all(), (keep, first, last)
 
 
-@pytest.mark.parametrize("blocks,keep", [(255, 17), (256, 100), (257, 256), (700, 64), (1030, 3)])
+@pytest.mark.parametrize("blocks,keep", [(255, 17), (256, 100), (257, 256), (700, 64), (1030, 3), (2100, 40)])
 def test_select_among_many_with_ties(bnn, blocks, keep):
     # keys from a few patterns only: long ties, broken by the lowest index
     def values(rng, n):

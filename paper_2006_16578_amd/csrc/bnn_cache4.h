@@ -71,10 +71,9 @@ __device__ __forceinline__ uint8_t* c4_record(const Cache4& c, int page, int hea
     return c.data + ((long long)page * c.kv_heads + head) * c.record;
 }
 
-// Tiles of ROWS rows (units: rows of a token) that never span sequences: the sequence of `tile`, and its number in it; false: there are fewer tiles.
+// Tiles of `rows` rows (units: rows of a token) that never span sequences: the sequence of `tile`, and its number in it; false: there are fewer tiles.
 // With start == nullptr every sequence has seq_tiles; else a wave counts the tiles of 64 sequences at a time.
-template <int ROWS>
-__device__ __forceinline__ bool c4_find_tile(const Rows4& r, int units, int tile, int seq_tiles, const FastDiv& div_seq_tiles, int& b, int& local) {
+__device__ __forceinline__ bool c4_find_tile(const Rows4& r, int units, int rows, int tile, int seq_tiles, const FastDiv& div_seq_tiles, int& b, int& local) {
     if (r.start == nullptr) {
         b = fast_div(tile, div_seq_tiles);
         local = tile - b * seq_tiles;
@@ -86,7 +85,7 @@ __device__ __forceinline__ bool c4_find_tile(const Rows4& r, int units, int tile
         int n = 0;
         if (b0 + lane < r.batch) {
             const int first = min(max(r.start[b0 + lane], 0), r.tokens);
-            n = (int)(((long long)(min(max(r.start[b0 + lane + 1], first), r.tokens) - first) * units + ROWS - 1) / ROWS);
+            n = (int)(((long long)(min(max(r.start[b0 + lane + 1], first), r.tokens) - first) * units + rows - 1) / rows);
         }
         int sum = n;
 #pragma unroll
@@ -210,7 +209,8 @@ struct Select4 {
     int32_t* blocks;                         // [tokens][kv_heads][keep]
     uint16_t* scores;                        // [tokens][kv_heads][table_pages]: score + 1, 0 where the row sees no key of the block
     // of the launch that scores
-    int columns_shift;                       // a token has 2^columns_shift of the 32 columns: its query heads, rounded up
+    int columns, tile_tokens;                // columns of a token, its query heads, and tokens in 32 columns
+    FastDiv div_columns;
     int tiles, seq_tiles, parts;
     FastDiv div_seq_tiles, div_parts, div_heads;
 };

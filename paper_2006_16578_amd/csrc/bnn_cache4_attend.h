@@ -1,9 +1,13 @@
-// Attention over the 4-bit cache, one template for single tokens, drafts, chunks and whole prompts; instantiated per head dimension in bnn_cache4_attend*.hip.
+// Attention over the 4-bit cache; instantiated per head dimension in bnn_cache4_attend*.hip.  attend_kernel: single tokens, drafts, selected blocks (up to 32 rows of queries a
+// workgroup, whose waves share the keys); attend_rows_kernel, further down: chunks and prompts (64 or 128 rows, whose waves share what is converted).
 //
 // Rows of queries that share a kv head -- its query heads, for one token or for several -- are the columns of the products, keys their rows:
 //   S^T [keys][rows] = K Q^T,   O^T [dim][rows] += V^T P^T   (v_mfma_f32_16x16x32_bf16).
 // A lane then holds, of 32 keys, the scores of ONE row at 8 keys, and exactly those eight are its operand of the second product: softmax weights never cross
 // lanes.  Eight or four waves share the 16 * QT rows of a workgroup and take steps of 32 keys in turn, each with a running maximum and sum of its own; they meet in LDS once, at the end.
+// What bounds it is memory: the next step's codes are under way while one is computed, and page addresses are read 32 steps ahead, a lane each.  Two documents of 100001 and
+// 131072 tokens (8 kv heads of 128, 251 MB): 42 us, 5.9 TB/s; 64 conversations of 500 to 8192 tokens (304 MB): 58 us, 5.3 TB/s.  A step is about 195 vector instructions, half
+// of them conversions, and 17 MFMAs of 16 cycles.
 // The cache's values are exact in bf16: the conversion instruction applies the scale.
 //
 // K: lane l supplies key l % 16 of a step's half and, of every 128 elements, the 32 of group l / 16: one 16-byte load and one scale.  Which elements a matrix
@@ -15,7 +19,7 @@
 // passes it by more than 8, which a wave tests without any exchange between lanes; weights are at most 2^8 then, and nothing is lost, as weights and sums scale alike.
 //
 // Weights of one bf16 term are divided by the sum of the rounded weights, a product with ones, so that where one key has nearly all the weight its rounding cancels
-// (error against 64 bits 0.0016 of the result's size, 0.0015 from rounding the result; 0.0022 without); the logarithm of the sum is of the unrounded ones.
+// (error against 64 bits 0.0016 of the result's size, 0.0015 from rounding the result; 0.0021 without); the logarithm of the sum is of the unrounded ones.
 // Queries and weights enter the products as sums of 1 (bf16), 2 (fp16) or 3 (fp32) bf16 terms: queries exactly; weights to 8, 16 and 24 bits.
 #ifndef BNN_CACHE4_ATTEND_H
 #define BNN_CACHE4_ATTEND_H
@@ -100,7 +104,7 @@ __device__ __forceinline__ Tile4 find_tile(const Attend4& a, int tile) {
         return t;
     } else {
         int local;
-        if (!c4_find_tile<ROWS>(a.r, a.group, tile, a.seq_tiles, a.div_seq_tiles, t.b, local)) return t;
+        if (!c4_find_tile(a.r, a.group, ROWS, tile, a.seq_tiles, a.div_seq_tiles, t.b, local)) return t;
         t.s = c4_sequence(a.r, a.c, t.b);
         const int all = t.s.rows * a.group;
         t.row0 = local * ROWS;
@@ -526,9 +530,12 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
 }
 
 // Many rows: a workgroup's four waves have 16 * QT rows each and share keys.  32 keys at a time are converted once for all and left in LDS as finished operands (a
-// lane's 16 bytes side by side: reads and writes without conflicts): waves 0 and 2 convert K, two steps ahead of its use, 1 and 3 V; one barrier a step.
+// lane's 16 bytes side by side: reads and writes without conflicts): two waves have a half each of the keys, K two steps ahead of its use and V in turn; one barrier a step.
 // In step i a wave forms the scores of step i + 1, the weights of step i and the sums of step i - 1: three pieces of work that do not wait for each other, so that matrix
 // and vector instructions of one wave alternate.  A maximum that is raised in step i scales the sums at the step's end, when those of step i - 1 are in.
+// Two prompts of 4096 tokens (32 heads of 128 on 8 kv heads, bf16): 332 to 350 us, 0.8 PFLOP/s; every wave converting for itself 416.  Bounded by waits at two waves a SIMD, which 32 rows of
+// sums, queries, scores and weights allow (231 registers): the matrix pipe is busy 36 % of the time and the vector ALU 46 %.  16 rows a wave at three or four waves a SIMD read twice
+// the operands from LDS for a row: 424 us.
 template <int D, int DTYPE, int QT>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     using T = typename C4Type<DTYPE>::type;
@@ -880,7 +887,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
 }
 
 // Joins the parts of the tiles whose keys were cut up: a workgroup per row of a tile.  D / 8 lanes hold a row's elements, eight each; the groups of so many lanes take
-// the parts in turn and meet in LDS.
+// the parts in turn and meet in LDS.  32 parts of 16 rows x 16 heads (1 MB): 4.9 us, a launch and three dependent loads; one workgroup for all rows of a tile took 42 with 64 parts.
 template <int D, int DTYPE, int ROWS, bool SPARSE>
 __global__ __launch_bounds__(256) void join_kernel(Attend4 a) {
     using T = typename C4Type<DTYPE>::type;

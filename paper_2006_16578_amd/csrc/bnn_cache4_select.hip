@@ -4,8 +4,10 @@
 // bits count as {0, 1}, a query's as -1 / +1: sum_d k_d q_d over them is the number of agreeing bits less the query's 0 bits, a constant of the column,
 // so it has the same maximum, and a key's word becomes an operand by four ANDs and one shift: product j takes bit j of every nibble, as 0.5, 1, 2 and
 // (shifted) 2, and the query's factor, 2, 1, 0.5 and 0.5, makes them count alike.  A lane holds the products of one column with 16 keys of each tile of 32:
-// the maximum over a block is taken in registers, then across two half waves, and the sum over the heads of a token across lanes.  All numbers are whole and exact.
+// the maximum over a block is taken in registers, then across two half waves, and the sum over the heads of a token as a difference of running sums across lanes.  All numbers are whole and exact.
 // A wave takes 128 keys (or a block of 256) at a time and has loaded the next two lots.
+// 8 sequences of 50001 to 65536 tokens, 64 query heads on 8 kv heads of 128: 59 MB of signs in 14 to 16 us, where counting with xor and popcount on the vector ALU took 20; 666 query tokens with 20
+// heads on 4 of 64 over up to 10007 keys: 20 us (61).  Bounded by issue slots: 5 instructions a word of 32 signs, 8 for the maxima of 32 keys x 32 columns.
 // pick_kernel: a workgroup per (token, kv head) counts the scores into bins, finds the score at which the places run out, and writes the blocks in order;
 // of those at that score the lowest.  Everything is whole numbers, so the result does not depend on any order.
 #include "bnn_cache4.h"
@@ -51,21 +53,21 @@ __device__ __forceinline__ uint32_t sign_word(const T* p) {
     return w;
 }
 
-template <int CTRL>
-__device__ __forceinline__ float dpp(float v) {
-    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, 0xf, 0xf, true));
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ float dpp(float v) {              // 0 where the lane has no source, or its row of 16 is not in ROWS
+    return __uint_as_float((uint32_t)__builtin_amdgcn_update_dpp(0, (int)__float_as_uint(v), CTRL, ROWS, 0xf, true));
 }
-// Sums over groups of 2^shift lanes, in every lane of them.
-__device__ __forceinline__ float sum_columns(float v, int shift) {
-    if (shift > 0) v += dpp<0xB1>(v);                            // lanes 1,0,3,2
-    if (shift > 1) v += dpp<0x4E>(v);                            // lanes 2,3,0,1
-    if (shift > 2) v += dpp<0x141>(v);                           // mirrored within 8
-    if (shift > 3) v += dpp<0x140>(v);                           // mirrored within 16
-    if (shift > 4) {
-        auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-    }
-    return v;
+// Sum over the `group` columns up to the lane's own, for the last lane of each group; columns are the 32 lanes of a half wave.
+__device__ __forceinline__ float sum_columns(float v, int group) {
+    if (group == 1) return v;
+    v += dpp<0x111>(v);                                          // running sums in rows of 16: lanes 1, 2, 4, 8 below
+    v += dpp<0x112>(v);
+    v += dpp<0x114>(v);
+    v += dpp<0x118>(v);
+    v += dpp<0x142, 0xa>(v);                                     // the last of a half wave's first row to its second
+    const int lane = (int)threadIdx.x & 63, from = lane - group;
+    const float before = __uint_as_float((uint32_t)__builtin_amdgcn_ds_bpermute(4 * from, (int)__float_as_uint(v)));
+    return v - ((lane & 31) < group ? 0.f : before);
 }
 // Lower half wave: the larger of x's halves; upper: of y's.
 __device__ __forceinline__ float max_halves(float x, float y) {
@@ -82,10 +84,9 @@ __global__ __launch_bounds__(256, PAGE == 256 && D > 64 ? 2 : D >= 192 || PAGE =
     const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads;
     const int tile = fast_div(rest, a.div_parts), part = rest - tile * a.parts;
     int b, local;
-    if (!c4_find_tile<32>(a.r, 1 << a.columns_shift, tile, a.seq_tiles, a.div_seq_tiles, b, local)) return;
+    if (!c4_find_tile(a.r, 1, a.tile_tokens, tile, a.seq_tiles, a.div_seq_tiles, b, local)) return;
     const Sequence4 s = c4_sequence(a.r, a.c, b);
-    const int per_tile = 32 >> a.columns_shift;                  // tokens
-    const int i0 = local * per_tile, tokens = min(per_tile, s.rows - i0);
+    const int i0 = local * a.tile_tokens, tokens = min(a.tile_tokens, s.rows - i0);
     if (tokens <= 0) return;
     const int base = s.length - s.rows + i0;                     // position of the first
     const int last = base + tokens - 1;
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(256, PAGE == 256 && D > 64 ? 2 : D >= 192 || PAGE =
     const int share = (steps + a.parts - 1) / a.parts, begin = part * share, end = min(steps, begin + share);
     if (begin >= end) return;
 
-    const int i = col >> a.columns_shift, g1 = col & ((1 << a.columns_shift) - 1);
+    const int i = fast_div(col, a.div_columns), g1 = col - i * a.columns;
     const bool row = i < tokens;
     const int pos = base + i;
     const long long token = s.first + i0 + (row ? i : 0);
@@ -196,9 +197,9 @@ __global__ __launch_bounds__(256, PAGE == 256 && D > 64 ? 2 : D >= 192 || PAGE =
             for (int n = 0; n < NB; n += 2) {
                 const int other = n + 1 < NB ? n + 1 : n;
                 float v = max_halves(best[n], best[other]) + zeros;
-                v = sum_columns(there ? v : 0.f, a.columns_shift);
+                v = sum_columns(there && v >= 0.f ? v : 0.f, a.columns);             // (below 0: the token sees none of the keys)
                 const int block = step * NB + (upper ? other : n);
-                if (row && g1 == 0 && block < blocks) {
+                if (row && g1 == a.columns - 1 && block < blocks) {
                     const bool seen = (in >> (upper ? other : n) & 1) && block << a.c.page_shift <= pos;
                     scores[block] = (uint16_t)(!seen ? 0 : (int)v + (g0 == 0 ? 1 : scores[block]));
                 }
@@ -211,7 +212,8 @@ __global__ __launch_bounds__(256, PAGE == 256 && D > 64 ? 2 : D >= 192 || PAGE =
     }
 }
 
-// Sums over the lanes of the workgroup before this one, and over all; scratch: 8 ints.
+// Sums over the lanes of the workgroup before this one, and over all.
+template <int WAVES>
 __device__ __forceinline__ int2 scan2(int2 v, int2* scratch, int2& all) {
     const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6;
     int2 sum = v;
@@ -226,7 +228,7 @@ __device__ __forceinline__ int2 scan2(int2 v, int2* scratch, int2& all) {
     int2 before = make_int2(sum.x - v.x, sum.y - v.y);
     all = make_int2(0, 0);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < WAVES; ++w) {
         const int2 x = scratch[w];
         if (w < wave) { before.x += x.x; before.y += x.y; }
         all.x += x.x; all.y += x.y;
@@ -234,17 +236,18 @@ __device__ __forceinline__ int2 scan2(int2 v, int2* scratch, int2& all) {
     return before;
 }
 
-// A thread owns `each` consecutive blocks (at most EACH, held in registers, or, with EACH == 0, read again in every pass) and, from the highest down, bins / 256 consecutive
+// A thread owns `each` consecutive blocks (at most EACH, held in registers, or, with EACH == 0, read again in every pass) and, from the highest down, an even share of the
 // bins.  The scores are asked for before it is known how many blocks there are: 1024 of them picked in 4.8 us, in 5.5 when every pass read its own.
-template <int EACH>
-__global__ __launch_bounds__(256) void pick_kernel(Select4 a, int bins) {
+template <int EACH, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void pick_kernel(Select4 a, int bins) {
+    constexpr int THREADS = 64 * WAVES;
     extern __shared__ int count[];           // [bins]
-    __shared__ int2 scratch[4];
+    __shared__ int2 scratch[WAVES];
     __shared__ int found[2];                 // score at the edge, places for it
     const int token = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - token * a.c.kv_heads;
     const long long at = (long long)token * a.c.kv_heads + head;
     const uint16_t* scores = a.scores + at * a.r.table_pages;
-    const int each = (a.r.table_pages + 255) >> 8, x0 = (int)threadIdx.x * each;
+    const int each = (a.r.table_pages + THREADS - 1) / THREADS, x0 = (int)threadIdx.x * each;
     uint16_t held[EACH > 0 ? EACH : 1];
 #pragma unroll
     for (int i = 0; i < EACH; ++i) held[i] = scores[min(x0 + i, a.r.table_pages - 1)];
@@ -269,7 +272,7 @@ __global__ __launch_bounds__(256) void pick_kernel(Select4 a, int bins) {
             }
         }
     };
-    for (int x = (int)threadIdx.x; x < bins; x += 256) count[x] = 0;
+    for (int x = (int)threadIdx.x; x < bins; x += THREADS) count[x] = 0;
     if (threadIdx.x < 2) found[threadIdx.x] = 0;
     __syncthreads();
     int2 forced = make_int2(0, 0);
@@ -278,13 +281,13 @@ __global__ __launch_bounds__(256) void pick_kernel(Select4 a, int bins) {
         else atomicAdd(&count[v], 1);
     });
     int2 all;
-    scan2(forced, scratch, all);
+    scan2<WAVES>(forced, scratch, all);
     const int places = a.keep - all.x;       // >= 0: keep >= first + last
     // The edge: the highest score at which `places` blocks are reached (0: never)
-    const int span = (bins + 255) >> 8, top = bins - 1 - (int)threadIdx.x * span;
+    const int span = (bins + THREADS - 1) / THREADS, top = bins - 1 - (int)threadIdx.x * span;
     int2 mine = make_int2(0, 0);
     for (int v = top; v > top - span && v >= 1; --v) mine.x += count[v];
-    int above = scan2(mine, scratch, all).x;
+    int above = scan2<WAVES>(mine, scratch, all).x;
     if (above < places && above + mine.x >= places) {
         for (int v = top; v > top - span && v >= 1; --v) {
             if (above + count[v] >= places) {
@@ -303,7 +306,7 @@ __global__ __launch_bounds__(256) void pick_kernel(Select4 a, int bins) {
         if (kept(x, v)) ++chosen.x;
         else if (v == edge) ++chosen.y;
     });
-    const int2 before = scan2(chosen, scratch, all);
+    const int2 before = scan2<WAVES>(chosen, scratch, all);
     int place = before.x + min(before.y, left), ties = before.y;
     for_each([&](int x, int v) {
         const bool above_edge = kept(x, v);
@@ -313,7 +316,7 @@ __global__ __launch_bounds__(256) void pick_kernel(Select4 a, int bins) {
         }
         if (!above_edge && v == edge) ++ties;
     });
-    for (int x = all.x + min(all.y, left) + (int)threadIdx.x; x < a.keep; x += 256) out[x] = -1;
+    for (int x = all.x + min(all.y, left) + (int)threadIdx.x; x < a.keep; x += THREADS) out[x] = -1;
 }
 
 template <int D>
@@ -331,9 +334,10 @@ void launch_score(const Select4& a, int dtype, hipStream_t s) {
 }  // namespace
 
 int launch_cache4_select(Select4 a, int dtype, hipStream_t s) {
-    a.columns_shift = 0;
-    while (a.columns_shift < 5 && (1 << a.columns_shift) < a.group) ++a.columns_shift;
-    const long long tiles = c4_tiles(a.r, 1 << a.columns_shift, 32, &a.seq_tiles);
+    a.columns = std::min(a.group, 32);
+    a.div_columns = make_fastdiv((uint32_t)a.columns);
+    a.tile_tokens = 32 / a.columns;
+    const long long tiles = c4_tiles(a.r, 1, a.tile_tokens, &a.seq_tiles);
     // parts of the keys: 1024 workgroups if there are so many steps, of which a workgroup takes four at a time
     const long long steps = cdiv((long long)a.r.table_pages * a.c.page, a.c.page > 128 ? 256 : 128);
     const long long parts = std::max(1LL, std::min(cdiv(1024, tiles * a.c.kv_heads), cdiv(steps, 4)));
@@ -353,8 +357,10 @@ int launch_cache4_select(Select4 a, int dtype, hipStream_t s) {
     const int rc = check_launch();
     if (rc != BNN_OK) return rc;
     const int bins = a.group * a.c.dim + 2;
-    const int each = (a.r.table_pages + 255) >> 8;
-    launch(each <= 2 ? pick_kernel<2> : each <= 8 ? pick_kernel<8> : pick_kernel<0>, dim3((unsigned)a.r.tokens * (unsigned)a.c.kv_heads), dim3(256), (size_t)bins * 4, s, a, bins);
+    // A wave a row where rows fill the chip without more (2664 rows of 313 blocks: 6.0 us, 7.7 with four waves each); else four, up to 2048 blocks in registers
+    const long long rows = (long long)a.r.tokens * a.c.kv_heads;
+    const bool single = rows >= 1024 && a.r.table_pages <= 512;
+    launch(single ? pick_kernel<8, 1> : a.r.table_pages <= 2048 ? pick_kernel<8, 4> : pick_kernel<0, 4>, dim3((unsigned)rows), dim3(single ? 64u : 256u), (size_t)bins * 4, s, a, bins);
     return check_launch();
 }
 

@@ -179,7 +179,8 @@ def test_strided_inputs_and_no_signs(bnn):
 
 # ------------------------------------------------------------------------------------------ selection
 
-@pytest.mark.parametrize("dim,page,heads,group,dtype", [(64, 16, 2, 5, "f32"), (96, 32, 1, 1, "bf16"), (128, 64, 2, 8, "bf16"), (192, 16, 1, 9, "f16"), (256, 128, 1, 17, "f32")])
+@pytest.mark.parametrize("dim,page,heads,group,dtype", [(64, 16, 2, 5, "f32"), (96, 32, 1, 1, "bf16"), (128, 64, 2, 8, "bf16"), (192, 16, 1, 9, "f16"), (256, 128, 1, 17, "f32"), (64, 32, 1, 40, "bf16"),
+                                                        (96, 16, 1, 3, "f16")])
 def test_select(bnn, dim, page, heads, group, dtype):
     su = Setup(bnn, 4, [page * 9 + 3, page * 4, 1, 0, page * 20 + 1], [3, 2, 1, 1, 4], heads, dim, page, dtype=dtype)
     su.table[4, 3] = su.table[4, 11] = -1
@@ -210,6 +211,15 @@ def test_select_among_many_with_ties(bnn, blocks, keep):
     su.upload()
     want = oc.select(su.cache, q, su.table, su.lens, keep, first=0, last=0)
     assert (su.gpu.select(dev(q, "bf16"), keep=keep, first=0, last=0, **su.plan).cpu().numpy() == want).all() and want[0, 0, 0] == 0
+
+
+def test_select_for_many_tokens(bnn):
+    # chunks whose tokens see different numbers of blocks, several tokens to a tile of the products
+    su = Setup(bnn, 20, [610, 700, 33], [600, 590, 33], 1, 64, 16)
+    for heads, keep in ((3, 7), (1, 20), (6, 3)):
+        q = su.queries(heads)
+        want = oc.select(su.cache, q, su.table, su.lens, keep, su.start)
+        assert (su.gpu.select(dev(q, "bf16"), keep=keep, **su.plan).cpu().numpy() == want).all(), heads
 
 
 # ------------------------------------------------------------------------------------------ attention

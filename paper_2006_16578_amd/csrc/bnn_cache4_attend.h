@@ -181,7 +181,8 @@ struct Raw4 {
     uint32_t v_exp[P::count][2];
 };
 
-// (Scalar: the record; a lane's offset in it is one addition to a number that no step changes.)
+// (Scalar: the record; a lane's offset in it is one addition to a number that no step changes.  Exponents come four keys at a time, and k_scale() takes the lane's: a byte loaded
+// alone is widened where it arrives, not where it is used, and that waits for the next step's loads within this one.)
 template <int D>
 __device__ __forceinline__ void load_k_half(const Cache4& c, const Half4& half, int lane, uint32_t (&codes)[D / 32], uint32_t (&exp)[Pieces<D>::count]) {
     using P = Pieces<D>;
@@ -200,8 +201,11 @@ __device__ __forceinline__ void load_k_half(const Cache4& c, const Half4& half, 
         } else {
             codes[B / 32] = load_at<uint32_t>(half.record, row + 4 * h4 + B / 2);
         }
-        exp[p] = load_at<uint8_t>(half.record, (uint32_t)c.k_exps + (B / 32 + h4 * W / 128) * (uint32_t)c.page + col + (uint32_t)half.offset);
+        exp[p] = load_at<uint32_t>(half.record, (uint32_t)c.k_exps + (B / 32 + h4 * W / 128) * (uint32_t)c.page + (col & 12u) + (uint32_t)half.offset);
     });
+}
+__device__ __forceinline__ float k_scale(uint32_t exp, int lane) {
+    return __uint_as_float(__builtin_amdgcn_perm(exp, exp, (uint32_t)(lane & 3) << 24 | 0x0c0c0cu) >> 1);
 }
 // codes[p][0..3] and exp[p]: of the keys 4 (lane / 16) .. + 3 of the half.
 template <int D, int N>
@@ -366,7 +370,7 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
             for (int u = 0; u < QT; ++u) score[u][s] = f32x4{0.f, 0.f, 0.f, 0.f};
             static_for<P::count>([&](auto pc) {
                 constexpr int p = pc.value, W = P::width(p), B = P::base(p);
-                const float scale = c4_scale(raw.k_exp[s][p]);
+                const float scale = k_scale(raw.k_exp[s][p], lane);
 #pragma unroll
                 for (int i = 0; i < W / 32; ++i) {
                     const bf16x8 k = eight_of(raw.k[s][B / 32 + i], scale);
@@ -604,7 +608,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     auto convert_k = [&](int step) {         // what was loaded
         static_for<P::count>([&](auto pc) {
             constexpr int p = pc.value, W = P::width(p), B = P::base(p);
-            const float scale = c4_scale(k_exp[p]);
+            const float scale = k_scale(k_exp[p], lane);
 #pragma unroll
             for (int i = 0; i < W / 32; ++i) k_ops[step & 1][own][B / 32 + i][lane] = __builtin_bit_cast(u32x4, eight_of(k_codes[B / 32 + i], scale));
         });

@@ -186,7 +186,7 @@ constexpr int cache4_qtiles(int dim, int dtype) {            // a workgroup's ro
     return 2 * (dim / 4 + cache4_terms(dtype) * (dim / 8) + 4 * cache4_terms(dtype)) < 144 ? 2 : 1;
 }
 // Waves that share the keys of 16 rows, or of 32 (and of wide heads in fp32, which take more than the 256 registers that eight waves leave each other).  Eight make for half
-// as many parts to be joined as four: two long documents 50 -> 48 us, 64 conversations 76 -> 66.
+// as many parts to be joined as four: two long documents 50 -> 48 us, 64 conversations 76 -> 66 (now 60; with sixteen 77).
 constexpr int cache4_waves(int dim, int dtype, int qtiles) { return qtiles == 1 && !(dim == 256 && dtype == BNN_F32) ? 8 : 4; }
 constexpr int cache4_wide_qtiles(int dim, int dtype) {       // a wave's, of four with different rows
     return 2 * (dim / 4 + cache4_terms(dtype) * (dim / 8) + 8 * cache4_terms(dtype) + 16) <= 170 ? 2 : 1;

@@ -17,6 +17,8 @@
 //
 // The reference point of the weights follows the maximum in steps: it is raised, to 8 (as powers of two) above the highest score, and the sums rescaled, only when a score
 // passes it by more than 8, which a wave tests without any exchange between lanes; weights are at most 2^8 then, and nothing is lost, as weights and sums scale alike.
+// A weight's exponent is one multiply-add of the score, exact up to its own rounding, while the reference point is rounded: from 2^26 on by enough for the weights of a
+// row to overflow or to vanish together.  A wave that meets such a point multiplies its scores first from then on, which rounds them as it rounded the point.
 //
 // Weights of one bf16 term are divided by the sum of the rounded weights, a product with ones, so that where one key has nearly all the weight its rounding cancels
 // (error against 64 bits 0.0016 of the result's size, 0.0015 from rounding the result; 0.0021 without); the logarithm of the sum is of the unrounded ones.
@@ -31,6 +33,7 @@ namespace {
 
 constexpr float C4_LOW = -3.0e38f;           // below every score: a row that has seen nothing
 constexpr float C4_SLACK = 8.f;
+constexpr float C4_FAR = 67108864.f;         // 2^26: fp32 numbers lie 8 apart from here on
 
 template <int DTYPE> struct C4Type { using type = float; static constexpr int terms = 3; };
 template <> struct C4Type<BNN_BF16> { using type = __bf16; static constexpr int terms = 1; };
@@ -65,6 +68,18 @@ __device__ __forceinline__ float raise_maximum(float& m, float high) {
     m = to;
     return factor;
 }
+
+// Products that stay products: fused with the subtraction that follows they would not be rounded as the reference point is.
+__device__ __forceinline__ float product(float a, float b) {
+#pragma clang fp contract(off)
+    return a * b;
+}
+__device__ __forceinline__ void multiply(f32x4& score, float scale) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) score[i] = product(score[i], scale);
+}
+// Whether some row of the wave has a reference point (not that of a row that has seen nothing) beside which scores have to be multiplied before it is subtracted.
+__device__ __forceinline__ bool any_far(float m) { return __ballot(fabsf(m) > C4_FAR && m > C4_LOW) != 0; }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     const u32x4 v = {a, b, c, d};
@@ -345,6 +360,8 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
 
     f32x4 o[QT][J], rounded[QT];
     float m[QT], l[QT];
+    bool far = false;                        // scores are multiplied by the scale first, and `times` is 1
+    float times = a.scale;
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         m[u] = C4_LOW;
@@ -399,21 +416,36 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
             }
         }
 
+        if (far) {
+#pragma unroll
+            for (int u = 0; u < QT; ++u)
+#pragma unroll
+                for (int s = 0; s < 2; ++s) multiply(score[u][s], a.scale);
+        }
+
         // weights
         bf16x8 w[QT][TERMS];
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
             const float high = max8(score[u][0], score[u][1]);
-            if (__ballot(high * a.scale > m[u] + C4_SLACK) != 0) {
-                const float factor = raise_maximum(m[u], row_max(high) * a.scale);
+            if (__ballot(high * times > m[u] + C4_SLACK) != 0) {
+                const float factor = raise_maximum(m[u], product(row_max(high), times));
                 l[u] *= factor;
                 rounded[u] *= factor;
 #pragma unroll
                 for (int j = 0; j < J; ++j) o[u][j] *= factor;
+                if (!far && any_far(m[u])) {
+                    far = true;
+                    times = 1.f;
+#pragma unroll
+                    for (int v = u; v < QT; ++v)
+#pragma unroll
+                        for (int s = 0; s < 2; ++s) multiply(score[v][s], a.scale);
+                }
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float x = __builtin_amdgcn_exp2f(fmaf(score[u][i >> 2][i & 3], a.scale, -m[u]));
+                const float x = __builtin_amdgcn_exp2f(fmaf(score[u][i >> 2][i & 3], times, -m[u]));
                 l[u] += x;
                 __bf16 terms[TERMS];
                 split_terms<TERMS>(x, terms);
@@ -680,6 +712,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
         for (int j = 0; j < J; ++j) o[u][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
+    bool far = false;                        // scores are multiplied by the scale first, and `times` is 1
+    float times = a.scale;
     constexpr int SHARE = (QT * 8 * (2 + 2 * TERMS) + J + 2 * M - 1) / (J + 2 * M);
     using Scores = f32x4[QT][2];
     using Weights = bf16x8[QT][TERMS];
@@ -717,28 +751,48 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     };
     // Step i of the loop; whole: its keys are all in pages; now: its scores, next: where those of step i + 1 go; before: the weights of step i - 1, after: where its own go.
     auto turn = [&](auto first, int i, bool whole, Scores& now, Scores& next, const Weights& before, Weights& after) {
-        if (!(whole && wave_clear(i))) {
-            const int key0 = key_first + 32 * i;
-            const bool there[2] = {c4_page(a.r, a.c, t.b, key0) >= 0, c4_page(a.r, a.c, t.b, key0 + 16) >= 0};
-#pragma unroll
-            for (int u = 0; u < QT; ++u)
-#pragma unroll
-                for (int x = 0; x < 8; ++x)
-                    if (!visible(u, key0 + 16 * (x >> 2) + 4 * h4 + (x & 3), there[x >> 2])) now[u][x >> 2][x & 3] = -__builtin_inff();
-        }
         float factor[QT];
-        bool raise = false;
+        bool raise = false, raised = false;
 #pragma unroll
         for (int u = 0; u < QT; ++u) {
-            const float top = max8(now[u][0], now[u][1]);
-            factor[u] = top;
-            raise = raise || top * a.scale > m[u] + C4_SLACK;
+            factor[u] = max8(now[u][0], now[u][1]);
+            raise = raise || factor[u] * times > m[u] + C4_SLACK;
         }
-        const bool raised = __ballot(raise) != 0;
-        if (raised) {
+        const bool masked = !(whole && wave_clear(i));
+        if (__ballot(raise) != 0 || masked || far) {
+            if (masked) {
+                const int key0 = key_first + 32 * i;
+                const bool there[2] = {c4_page(a.r, a.c, t.b, key0) >= 0, c4_page(a.r, a.c, t.b, key0 + 16) >= 0};
+#pragma unroll
+                for (int u = 0; u < QT; ++u)
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        if (!visible(u, key0 + 16 * (x >> 2) + 4 * h4 + (x & 3), there[x >> 2])) now[u][x >> 2][x & 3] = -__builtin_inff();
+            }
+            raise = false;
+            float most = 0.f;                // of the new reference points' magnitudes
 #pragma unroll
             for (int u = 0; u < QT; ++u) {
-                factor[u] = raise_maximum(m[u], row_max(factor[u]) * a.scale);
+                factor[u] = product(row_max(max8(now[u][0], now[u][1])), a.scale);
+                if (factor[u] > m[u] + C4_SLACK) {
+                    raise = true;
+                    most = fmaxf(most, fabsf(factor[u]));
+                }
+            }
+            raised = __ballot(raise) != 0;
+            if (any_far(most)) {
+                far = true;
+                times = 1.f;
+            }
+            if (far) {
+#pragma unroll
+                for (int u = 0; u < QT; ++u)
+#pragma unroll
+                    for (int s = 0; s < 2; ++s) multiply(now[u][s], a.scale);
+            }
+#pragma unroll
+            for (int u = 0; u < QT; ++u) {
+                factor[u] = raise_maximum(m[u], factor[u]);
                 l[u] *= factor[u];
             }
         }
@@ -747,7 +801,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
         for (int u = 0; u < QT; ++u)
 #pragma unroll
             for (int x = 0; x < 8; ++x) {
-                const float y = __builtin_amdgcn_exp2f(fmaf(now[u][x >> 2][x & 3], a.scale, -m[u]));
+                const float y = __builtin_amdgcn_exp2f(fmaf(now[u][x >> 2][x & 3], times, -m[u]));
                 l[u] += y;
                 __bf16 terms[TERMS];
                 split_terms<TERMS>(y, terms);

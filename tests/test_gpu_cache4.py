@@ -452,3 +452,46 @@ def test_refusals(bnn):
         with pytest.raises(error):
             fn()
     assert (su.gpu.data.cpu().numpy() == su.data).all()
+
+
+def check_far_scores(su, q, scale, blocks=None):
+    """Attention where scores lie so far apart that a row has the value of its best key, or the mean over keys that equal it.  Rows whose best and next score are
+    nearer than twice the error of a score (D + 8 units of fp32 of the sum of magnitudes, 4 of itself) plus 60 are left out; returns the share of the others."""
+    u, dim, heads = 2.0 ** -24, su.cache.dim, su.cache.heads
+    got, got_lse = su.gpu.attend(dev(q, su.dtype), scale=scale, want_lse=True, blocks=None if blocks is None else torch.from_numpy(blocks).cuda(), **su.plan)
+    got, got_lse = got.double().cpu().numpy(), got_lse.double().cpu().numpy()
+    weight = {"bf16": 2.0 ** -8, "f16": 2.0 ** -16, "f32": 2.0 ** -24}[su.dtype]
+    out = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": u}[su.dtype]
+    group, sure = q.shape[1] // heads, []
+    for t, (b, pos) in enumerate(oc.row_places(su.cache, su.table, su.lens, su.start, su.tokens)):
+        for h in range(heads):
+            keys = [p for p in range(pos + 1) if blocks is None or p // su.cache.page in blocks[t, h]]
+            if not keys:
+                continue
+            k, v = (np.stack([su.cache.record(su.table, b, p, h).get(name, p % su.cache.page) for p in keys]) for name in "kv")
+            for g in range(h * group, (h + 1) * group):
+                s = scale * (k @ q[t, g])
+                error = (dim + 8) * u * scale * (np.abs(k) @ np.abs(q[t, g])).max() + 4 * u * np.abs(s).max()
+                best = np.flatnonzero(s > s.max() - 2 * error - 60)
+                sure.append((k[best] == k[best[0]]).all())
+                if sure[-1]:
+                    want, size = v[best].mean(0), np.abs(v[best]).mean(0)
+                    assert (np.abs(got[t, g] - want) <= (weight + (8 + len(best)) * u) * size * 1.02 + out * np.abs(want) * 1.01 + 2.0 ** -25).all(), (t, g)
+                    assert abs(got_lse[t, g] - s.max() - np.log(len(best))) <= error + 8 * u * abs(s.max()), (t, g)
+    return np.mean(sure)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_scores_beyond_what_fp32_resolves(bnn, dtype):
+    same = lambda rng, n: (np.repeat(rng.standard_normal((1, 1, 64)), n, 0), rng.standard_normal((n, 1, 64)))
+    for values in (None, same):
+        single = Setup(bnn, 21, [1, 40, 700], None, 1, 64, 16, dtype=dtype, values=values)
+        parts = Setup(bnn, 22, [2100, 300], None, 1, 64, 64, dtype=dtype, width=100, values=values)
+        many = Setup(bnn, 23, [75, 130], [75, 40], 1, 64, 32, dtype=dtype, values=values)
+        q = parts.queries(3)
+        blocks = oc.select(parts.cache, q, parts.table, parts.lens, 3)
+        for power in (20, 33, 70):
+            assert check_far_scores(single, single.queries(5), 2.0 ** power) > 0.8
+            assert check_far_scores(parts, q, 2.0 ** power) > 0.8
+            assert check_far_scores(parts, q, 2.0 ** power, blocks) > 0.8
+            assert check_far_scores(many, many.queries(2), 2.0 ** power) > 0.8

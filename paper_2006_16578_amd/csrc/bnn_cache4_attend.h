@@ -255,7 +255,8 @@ __device__ __forceinline__ void load_v(const Cache4& c, const Half4 (&half)[2], 
     for (int s = 0; s < 2; ++s) load_v_half<D, 8>(c, half[s], lane, raw.v, raw.v_exp, s);
 }
 
-// Q of the lane's row, in the order of elements that K's loads give, as a sum of TERMS bf16 numbers; zero without a row.
+// Q of the lane's row, in the order of elements that K's loads give, as a sum of TERMS bf16 numbers; zero without a row.  An infinite element becomes NaN (a sum of several
+// terms makes it one by itself): its products are infinite or NaN for every key, so no weights are defined, also where all scores are -infinity, the mark of keys not seen.
 template <int D, int TERMS, class T>
 __device__ __forceinline__ void load_q(const T* src, bool valid, int lane, bf16x8 (&q)[TERMS][D / 32]) {
     using P = Pieces<D>;
@@ -268,7 +269,7 @@ __device__ __forceinline__ void load_q(const T* src, bool valid, int lane, bf16x
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 __bf16 terms[TERMS];
-                split_terms<TERMS>(x[e], terms);
+                split_terms<TERMS>(TERMS == 1 ? fmaf(x[e], 0.f, x[e]) : x[e], terms);
 #pragma unroll
                 for (int n = 0; n < TERMS; ++n) q[n][B / 32 + i][e] = terms[n];
             }

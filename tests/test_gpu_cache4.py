@@ -495,3 +495,17 @@ def test_scores_beyond_what_fp32_resolves(bnn, dtype):
             assert check_far_scores(parts, q, 2.0 ** power) > 0.8
             assert check_far_scores(parts, q, 2.0 ** power, blocks) > 0.8
             assert check_far_scores(many, many.queries(2), 2.0 ** power) > 0.8
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_infinite_queries(bnn, dtype):
+    # scores that are all -infinity, all +infinity, or some of each: no weights are defined, the row is NaN; others are not touched
+    def values(rng, n):
+        k = rng.standard_normal((n, 1, 64))
+        k[..., 0] = -2 - rng.random((n, 1))
+        return k, rng.standard_normal((n, 1, 64))
+    for lens, counts in (([1, 40, 700], None), ([75, 130], [75, 40])):
+        su = Setup(bnn, 24, lens, counts, 1, 64, 32, dtype=dtype, values=values)
+        q = su.queries(4)
+        q[0, 0, 0], q[1, 1, 0], q[-1, 2, 5], q[-1, 0, 0] = np.inf, -np.inf, np.inf, np.inf
+        check_attend(su, q)

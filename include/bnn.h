@@ -402,8 +402,8 @@ int bnn_net_layer_bits(const bnn_net* net, int layer, const uint32_t** bits, int
  * Rows of a call: sequence b contributes its newest tokens, as start[b + 1] - start[b] consecutive rows (start[0] = 0, start[batch] = tokens); row i
  * of n is the token at position lens[b] - n + i.  With start == NULL every sequence has tokens / batch rows.  lens[b] counts the tokens that sequence b
  * has after this call's are in.  Token i lies in page table[b][i / page], at i % page; a table entry that is no page (such as -1: given back, or
- * not needed) holds nothing: writes to it are dropped, reads give 0, and attention and selection pass it over.  The three arrays are on the device and
- * are read by the kernels; whatever they hold, no access leaves the cache or the call's arrays, but rows outside every sequence keep what they held.
+ * not needed) and what lies past the table's end hold nothing: writes there are dropped, reads give 0, and attention and selection pass them over.  The three arrays are
+ * on the device and are read by the kernels; whatever they hold, no access leaves the cache or the call's arrays, but rows outside every sequence keep what they held.
  * ---------------------------------------------------------------------------------------- */
 #define BNN_F32 0
 #define BNN_BF16 1

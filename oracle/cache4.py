@@ -86,8 +86,7 @@ def row_places(cache, table, lens, start, tokens):
     out = []
     for b in range(batch):
         n = start[b + 1] - start[b]
-        length = min(int(lens[b]), table.shape[1] * cache.page)
-        out += [(b, length - n + i) for i in range(n)]
+        out += [(b, int(lens[b]) - n + i) for i in range(n)]
     return out
 
 
@@ -140,8 +139,7 @@ def attend(cache, q, table, lens, start=None, scale=1.0, causal=True, window=0, 
     places = row_places(cache, table, lens, start, tokens)
     values = {}
     for t, (b, pos) in enumerate(places):
-        length = min(int(lens[b]), table.shape[1] * cache.page)
-        top = pos if causal else length - 1
+        top = pos if causal else int(lens[b]) - 1
         low = max(0, pos - window + 1) if window else 0
         for h in range(cache.heads):
             keys = []

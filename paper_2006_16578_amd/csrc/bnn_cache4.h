@@ -30,12 +30,12 @@ struct Rows4 {
     FastDiv div_each;
 };
 
-// One sequence of a call: its first row, its number of rows, its length.  Row i (of the sequence) is the token at length - rows + i.
+// One sequence of a call: its first row, its number of rows, its length, which may pass the end of its table.  Row i (of the sequence) is the token at length - rows + i.
 struct Sequence4 {
     int first, rows, length;
 };
 
-__device__ __forceinline__ Sequence4 c4_sequence(const Rows4& r, const Cache4& c, int b) {
+__device__ __forceinline__ Sequence4 c4_sequence(const Rows4& r, int b) {
     Sequence4 s;
     if (r.start == nullptr) {
         s.first = b * r.each;
@@ -44,11 +44,12 @@ __device__ __forceinline__ Sequence4 c4_sequence(const Rows4& r, const Cache4& c
         s.first = min(max(r.start[b], 0), r.tokens);
         s.rows = min(max(r.start[b + 1], s.first), r.tokens) - s.first;
     }
-    const long long most = (long long)r.table_pages << c.page_shift;
     s.length = max(r.lens[b], 0);
-    if (s.length > most) s.length = (int)most;
     return s;
 }
+
+// Tokens that a table has room for.
+__device__ __forceinline__ int c4_room(const Rows4& r, const Cache4& c) { return (int)((long long)r.table_pages << c.page_shift); }
 
 // The sequence that row t belongs to: the last one that starts at or before t.
 __device__ __forceinline__ int c4_sequence_of(const Rows4& r, int t) {

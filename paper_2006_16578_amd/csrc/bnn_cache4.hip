@@ -26,7 +26,7 @@ struct Place {
 
 __device__ __forceinline__ Place place_of_row(const Cache4& c, const Rows4& r, int t) {
     const int b = c4_sequence_of(r, t);
-    const Sequence4 s = c4_sequence(r, c, b);
+    const Sequence4 s = c4_sequence(r, b);
     const int i = t - s.first;
     const int token = s.length - s.rows + i;
     Place p;

@@ -111,7 +111,7 @@ __device__ __forceinline__ Tile4 find_tile(const Attend4& a, int tile) {
     if constexpr (SPARSE) {
         const int per = (a.group + ROWS - 1) / ROWS, token = per == 1 ? tile : tile / per, part = tile - token * per;
         t.b = c4_sequence_of(a.r, token);
-        t.s = c4_sequence(a.r, a.c, t.b);
+        t.s = c4_sequence(a.r, t.b);
         const int i = token - t.s.first;
         if (i < 0 || i >= t.s.rows) return t;
         t.row0 = i * a.group + part * ROWS;
@@ -120,7 +120,7 @@ __device__ __forceinline__ Tile4 find_tile(const Attend4& a, int tile) {
     } else {
         int local;
         if (!c4_find_tile(a.r, a.group, ROWS, tile, a.seq_tiles, a.div_seq_tiles, t.b, local)) return t;
-        t.s = c4_sequence(a.r, a.c, t.b);
+        t.s = c4_sequence(a.r, t.b);
         const int all = t.s.rows * a.group;
         t.row0 = local * ROWS;
         t.rows = max(0, min(ROWS, all - t.row0));
@@ -147,11 +147,11 @@ __device__ __forceinline__ Range4 tile_steps(const Attend4& a, const Tile4& t) {
         return r;
     } else {
         const int base = t.s.length - t.s.rows;
-        const int top = a.causal ? base + fast_div(t.row0 + t.rows - 1, a.div_group) + 1 : t.s.length;      // keys below it are visited
+        const int top = min(a.causal ? base + fast_div(t.row0 + t.rows - 1, a.div_group) + 1 : t.s.length, c4_room(a.r, a.c));      // keys below it are visited
         const int low = a.window > 0 ? max(0, base + fast_div(t.row0, a.div_group) - a.window + 1) : 0;
         if (top <= low) return r;
         r.first = low >> 5;
-        r.count = ((top + 31) >> 5) - r.first;
+        r.count = ((top - 1) >> 5) + 1 - r.first;
         return r;
     }
 }

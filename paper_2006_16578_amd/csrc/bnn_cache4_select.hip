@@ -85,12 +85,12 @@ __global__ __launch_bounds__(256, PAGE == 256 && D > 64 ? 2 : D >= 192 || PAGE =
     const int tile = fast_div(rest, a.div_parts), part = rest - tile * a.parts;
     int b, local;
     if (!c4_find_tile(a.r, 1, a.tile_tokens, tile, a.seq_tiles, a.div_seq_tiles, b, local)) return;
-    const Sequence4 s = c4_sequence(a.r, a.c, b);
+    const Sequence4 s = c4_sequence(a.r, b);
     const int i0 = local * a.tile_tokens, tokens = min(a.tile_tokens, s.rows - i0);
     if (tokens <= 0) return;
     const int base = s.length - s.rows + i0;                     // position of the first
     const int last = base + tokens - 1;
-    const int blocks = last < 0 ? 0 : (last >> a.c.page_shift) + 1;
+    const int blocks = last < 0 ? 0 : min((last >> a.c.page_shift) + 1, a.r.table_pages);
     const int steps = (blocks + NB - 1) / NB;
     // a share of the steps for every part, each wave every fourth of it
     const int share = (steps + a.parts - 1) / a.parts, begin = part * share, end = min(steps, begin + share);
@@ -252,13 +252,13 @@ __global__ __launch_bounds__(64 * WAVES) void pick_kernel(Select4 a, int bins) {
 #pragma unroll
     for (int i = 0; i < EACH; ++i) held[i] = scores[min(x0 + i, a.r.table_pages - 1)];
     const int b = c4_sequence_of(a.r, token);
-    const Sequence4 s = c4_sequence(a.r, a.c, b);
+    const Sequence4 s = c4_sequence(a.r, b);
     const int i = token - s.first;
     if (i < 0 || i >= s.rows) return;
     const int pos = s.length - s.rows + i;
-    const int blocks = pos < 0 ? 0 : (pos >> a.c.page_shift) + 1, x1 = min(blocks, x0 + each);
+    const int own = pos >> a.c.page_shift, blocks = pos < 0 ? 0 : min(own + 1, a.r.table_pages), x1 = min(blocks, x0 + each);
     int32_t* out = a.blocks + at * a.keep;
-    const int tail = blocks - a.last;        // blocks from here on are kept
+    const int tail = own + 1 - a.last;       // blocks from here on are kept
     // f(block, score + 1) for this thread's blocks that can be selected
     auto for_each = [&](auto f) {
         if constexpr (EACH > 0) {

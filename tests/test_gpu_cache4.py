@@ -509,3 +509,26 @@ def test_infinite_queries(bnn, dtype):
         q = su.queries(4)
         q[0, 0, 0], q[1, 1, 0], q[-1, 2, 5], q[-1, 0, 0] = np.inf, -np.inf, np.inf, np.inf
         check_attend(su, q)
+
+
+@pytest.mark.parametrize("counts", [[8, 8], [70, 66]])
+def test_more_tokens_than_the_table_holds(bnn, counts):
+    # the newest tokens of the first sequence lie past the end of its table: they are dropped, and nothing that the table holds is touched
+    su = Setup(bnn, 26, [64, 66], counts, 2, 64, 16, dtype="f32", width=5)
+    su.table = np.ascontiguousarray(su.table[:, :4])
+    su.lens[:] = 73, 66
+    su.replan()
+    k, v = (rounded(su.rng.standard_normal((su.tokens, 2, 64)), "f32") for _ in range(2))
+    oc.write(su.cache, k, v, su.table, su.lens, su.start)
+    su.gpu.write(dev(k, "f32"), dev(v, "f32"), **su.plan)
+    assert (su.gpu.data.cpu().numpy() == su.data).all()
+    want = oc.read(su.cache, su.table, su.lens, su.start, su.tokens)
+    assert all(torch.equal(a, dev(b, "f32")) for a, b in zip(su.gpu.read(tokens=su.tokens, dtype=torch.float32, **su.plan), want)) and (want[0][counts[0] - 1] == 0).all()
+    q = su.queries(6)
+    check_attend(su, q)
+    check_attend(su, q, window=20)
+    check_attend(su, q, causal=False)
+    for keep, first, last in ((2, 1, 1), (3, 0, 2), (6, 1, 1)):
+        blocks = oc.select(su.cache, q, su.table, su.lens, keep, su.start, first, last)
+        assert (su.gpu.select(dev(q, "f32"), keep=keep, first=first, last=last, **su.plan).cpu().numpy() == blocks).all(), (keep, first, last)
+        check_attend(su, q, blocks=blocks)

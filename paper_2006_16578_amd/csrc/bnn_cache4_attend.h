@@ -148,7 +148,7 @@ __device__ __forceinline__ Range4 tile_steps(const Attend4& a, const Tile4& t) {
     } else {
         const int base = t.s.length - t.s.rows;
         const int top = min(a.causal ? base + fast_div(t.row0 + t.rows - 1, a.div_group) + 1 : t.s.length, c4_room(a.r, a.c));      // keys below it are visited
-        const int low = a.window > 0 ? max(0, base + fast_div(t.row0, a.div_group) - a.window + 1) : 0;
+        const int low = a.window > 0 ? max(0, max(base + fast_div(t.row0, a.div_group), 0) - a.window + 1) : 0;      // (rows before token 0 see nothing; any window may be theirs)
         if (top <= low) return r;
         r.first = low >> 5;
         r.count = ((top - 1) >> 5) + 1 - r.first;
@@ -349,13 +349,13 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
 
     // Q, in the order of elements that K's loads give
     bf16x8 q[QT][TERMS][M];
-    int pos[QT];                             // position of the lane's row; -1: no row
+    int pos[QT];                             // position of the lane's row; -1: no row, or one before the first token
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         const int row = t.row0 + 16 * u + c;
         const int token = fast_div(row, a.div_group), g = row - token * a.group;
         const bool valid = 16 * u + c < t.rows;
-        pos[u] = valid ? base + token : -1;
+        pos[u] = valid ? max(base + token, -1) : -1;
         load_q<D, TERMS>(static_cast<const T*>(a.q) + (t.s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head, valid, lane, q[u]);
     }
 
@@ -373,7 +373,7 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
     }
     // keys that every row of the tile sees, if none is missing: [low_last, top_first]
     const int top_first = a.causal ? base + fast_div(t.row0, a.div_group) : t.s.length - 1;
-    const int low_last = a.window > 0 ? base + fast_div(t.row0 + t.rows - 1, a.div_group) - a.window + 1 : 0;
+    const int low_last = a.window > 0 ? max(base + fast_div(t.row0 + t.rows - 1, a.div_group), 0) - a.window + 1 : 0;
 
     for (int turn = 0; turn < turns; ++turn) {
         bool full = true;
@@ -629,7 +629,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     };
     auto seen_by_all = [&](int row0, int rows) {
         const int first = base + fast_div(row0, a.div_group), last = base + fast_div(row0 + max(rows, 1) - 1, a.div_group);
-        const int top = a.causal ? first : t.s.length - 1, bottom = a.window > 0 ? max(last - a.window + 1, 0) : 0;
+        const int top = a.causal ? first : t.s.length - 1, bottom = a.window > 0 ? max(max(last, 0) - a.window + 1, 0) : 0;
         Steps r;
         r.from = max((bottom - key_first + 31) >> 5, 0);
         r.count = (unsigned)max(((top + 1 - key_first) >> 5) - r.from, 0);
@@ -693,13 +693,13 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {
     load_k_step(0, (wave & 1) == 0);
     load_k_step(1, (wave & 1) == 1);
     bf16x8 q[QT][TERMS][M];
-    int pos[QT];                             // position of the lane's row; -1: no row
+    int pos[QT];                             // position of the lane's row; -1: no row, or one before the first token
 #pragma unroll
     for (int u = 0; u < QT; ++u) {
         const int row = wave_row0 + 16 * u + c;
         const int token = fast_div(row, a.div_group), g = row - token * a.group;
         const bool valid = 16 * u + c < wave_rows;
-        pos[u] = valid ? base + token : -1;
+        pos[u] = valid ? max(base + token, -1) : -1;
         load_q<D, TERMS>(static_cast<const T*>(a.q) + (t.s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head, valid, lane, q[u]);
     }
     f32x4 o[QT][J], rounded[QT];

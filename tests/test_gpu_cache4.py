@@ -532,3 +532,13 @@ def test_more_tokens_than_the_table_holds(bnn, counts):
         blocks = oc.select(su.cache, q, su.table, su.lens, keep, su.start, first, last)
         assert (su.gpu.select(dev(q, "f32"), keep=keep, first=first, last=last, **su.plan).cpu().numpy() == blocks).all(), (keep, first, last)
         check_attend(su, q, blocks=blocks)
+
+
+@pytest.mark.parametrize("counts", [[8, 8, 3], [70, 66, 64]])
+def test_windows_of_any_size(bnn, counts):
+    # rows that reach before the first token of their sequence, and a window that no sequence fills
+    su = Setup(bnn, 25, [5, 66, 3], counts, 1, 64, 16, dtype="f32")
+    q = su.queries(2)
+    for window in (2 ** 31 - 1, 2 ** 31 - 60, 2 ** 30):
+        check_attend(su, q, window=window)
+        check_attend(su, q, window=window, blocks=oc.select(su.cache, q, su.table, su.lens, 3, su.start))

@@ -236,6 +236,8 @@ __device__ __forceinline__ int2 scan2(int2 v, int2* scratch, int2& all) {
     return before;
 }
 
+// A score is a bin's number in LDS, so none above the last is taken as it is: where the plan's start falls, rows can be asked for whose scores no workgroup has
+// written, and memory may hold anything.
 // A thread owns `each` consecutive blocks (at most EACH, held in registers, or, with EACH == 0, read again in every pass) and, from the highest down, an even share of the
 // bins.  The scores are asked for before it is known how many blocks there are: 1024 of them picked in 4.8 us, in 5.5 when every pass read its own.
 template <int EACH, int WAVES>
@@ -264,10 +266,10 @@ __global__ __launch_bounds__(64 * WAVES) void pick_kernel(Select4 a, int bins) {
         if constexpr (EACH > 0) {
 #pragma unroll
             for (int i = 0; i < EACH; ++i)
-                if (x0 + i < x1 && held[i] != 0) f(x0 + i, (int)held[i]);
+                if (x0 + i < x1 && held[i] != 0) f(x0 + i, min((int)held[i], bins - 1));
         } else {
             for (int x = x0; x < x1; ++x) {
-                const int v = scores[x];
+                const int v = min((int)scores[x], bins - 1);
                 if (v != 0) f(x, v);
             }
         }

@@ -1,4 +1,6 @@
 """GPU: the 4-bit key/value cache against the oracle in 64 bits: writing and reading, selection (both exact), attention (within bounds worked out below)."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -542,3 +544,45 @@ def test_windows_of_any_size(bnn, counts):
     for window in (2 ** 31 - 1, 2 ** 31 - 60, 2 ** 30):
         check_attend(su, q, window=window)
         check_attend(su, q, window=window, blocks=oc.select(su.cache, q, su.table, su.lens, 3, su.start))
+
+
+@pytest.mark.parametrize("group", [1, 3, 40])
+def test_no_plan_leads_out(bnn, group):
+    # tables, lengths and starts of any content: calls end, and bytes around the cache, the outputs and the workspaces stay as they are
+    rng, dim, page, heads, pages, batch, tokens, width = np.random.default_rng(30), 64, 16, 2, 12, 5, 40, 6
+    record = oc.record_bytes(dim, page)
+    memory = torch.full((pages + 8, heads, record), 0xA5, dtype=torch.uint8, device="cuda")
+    cache = bnn.Cache4(kv_heads=heads, head_dim=dim, page=page, data=memory[4:-4])
+    q = torch.randn(tokens, heads * group, dim, device="cuda")
+    outs = torch.full((tokens + 2, heads * group, dim), 7.0, device="cuda")
+
+    def guarded(need):
+        whole = torch.full((need + 512,), 0xFF, dtype=torch.uint8, device="cuda")
+        return whole, whole[256:-256]
+
+    def untouched(whole):
+        return bool((whole[:256] == 0xFF).all() and (whole[-256:] == 0xFF).all())
+
+    plans = [dict(start=rng.choice([-2 ** 31, -3, 0, 7, 20, 40, 41, 2 ** 31 - 1], batch + 1)) for _ in range(8)] + [dict(start=None) for _ in range(4)]
+    plans.append(dict(start=np.array([0, 20, 0, 40, 40, 40]), lens=np.full(batch, 96)))          # rows whose scores no workgroup writes
+    for plan in plans:
+        plan.setdefault("lens", rng.choice([-2 ** 31, -1, 0, 5, 40, 96, 97, 500, 2 ** 31 - 1], batch))
+        plan["table"] = rng.choice([-2 ** 31, -1, pages, pages + 1, 2 ** 31 - 1, *range(pages), *range(pages)], (batch, width))
+        print(plan, flush=True)
+        plan = {name: None if x is None else torch.from_numpy(x.astype(np.int32)).cuda() for name, x in plan.items()}
+        cache.write(q[:, :heads], q[:, :heads], **plan)
+        cache.read(tokens=tokens, **plan)
+        rows = cache._rows(plan["table"], plan["lens"], plan["start"], tokens)
+        lists = [None, torch.from_numpy(rng.integers(-2, width + 2, (tokens, heads, 3)).astype(np.int32)).cuda()]
+        for keep in (2, 9):
+            whole, work = guarded(int(bnn.load().bnn_cache4_select_workspace_bytes(cache._struct(), ctypes.byref(rows))))
+            lists.append(cache.select(q, keep=keep, workspace=work, **plan))
+            assert untouched(whole)
+        for blocks in lists:
+            for kw in (dict(), dict(window=30), dict(causal=False)):
+                need = int(bnn.load().bnn_cache4_attend_workspace_bytes(cache._struct(), ctypes.byref(rows), 0, heads * group, kw.get("window", 0), 0 if blocks is None else blocks.shape[2]))
+                whole, work = guarded(need)
+                cache.attend(q, blocks=blocks, out=outs[1:-1], workspace=work, **plan, **kw)
+                assert untouched(whole)
+        assert (outs[0] == 7).all() and (outs[-1] == 7).all() and (memory[:4] == 0xA5).all() and (memory[-4:] == 0xA5).all()
+    assert (lists[2] < width).all() and (lists[3] < width).all()

@@ -929,8 +929,8 @@ class Cache4:
         if blocks is not None:
             _dev(blocks, torch.int32, 3, "blocks")
             keep = blocks.shape[2]
-            if blocks.shape[0] != q.shape[0] or blocks.shape[1] != self.kv_heads or blocks.device != q.device:
-                raise ValueError("blocks must be [tokens][kv_heads][keep], on q's device")
+            if blocks.shape[0] != q.shape[0] or blocks.shape[1] != self.kv_heads or keep < 1 or blocks.device != q.device:
+                raise ValueError("blocks must be [tokens][kv_heads][keep], keep >= 1, on q's device")
         if out is None:
             out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         elif _dev(out, q.dtype, 3, "out").shape != q.shape or out.device != q.device:

@@ -435,7 +435,8 @@ PyObject* cache4_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs) {   // 
         const int window = c.number(a[11]);
         const Tensor* blocks = a[12] == Py_None ? nullptr : c.tensor(a[12], at::kInt, 3);
         PLAIN(c);
-        if (blocks && (blocks->size(0) != q.size(0) || blocks->size(1) != p.cache.kv_heads)) Py_RETURN_NONE;
+        // (an empty list has no memory, and without a pointer the library would attend to every key)
+        if (blocks && (blocks->size(0) != q.size(0) || blocks->size(1) != p.cache.kv_heads || blocks->size(2) < 1)) Py_RETURN_NONE;
         p.finish((int)q.size(0));
         const int heads = (int)q.size(1), keep = blocks ? (int)blocks->size(2) : 0;
         const Tensor out = empty(q, q.sizes(), ELEMENTS[code]);

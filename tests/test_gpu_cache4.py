@@ -586,3 +586,17 @@ def test_no_plan_leads_out(bnn, group):
                 assert untouched(whole)
         assert (outs[0] == 7).all() and (outs[-1] == 7).all() and (memory[:4] == 0xA5).all() and (memory[-4:] == 0xA5).all()
     assert (lists[2] < width).all() and (lists[3] < width).all()
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_an_empty_list_of_blocks(bnn, monkeypatch, native):
+    # refused: it is not "no list", which attends to every key
+    from paper_2006_16578_amd import binding
+    if not native:
+        monkeypatch.setattr(binding, "_native", binding._PythonOnly())
+    su = Setup(bnn, 27, [30, 9], None, 2, 64, 16)
+    q = dev(su.queries(4), "bf16")
+    blocks = su.gpu.select(q, keep=2, **su.plan)
+    with pytest.raises(ValueError, match="keep >= 1"):
+        su.gpu.attend(q, blocks=blocks[:, :, :0], **su.plan)
+    assert torch.equal(su.gpu.attend(q, blocks=blocks[:, :, :1].contiguous(), **su.plan), su.gpu.attend(q, blocks=torch.cat([blocks[:, :, :1], torch.full_like(blocks, -1)], 2), **su.plan))

@@ -173,8 +173,9 @@ int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
     int rc = make_cache(cache, a.c);
     if (rc != BNN_OK || (rc = make_rows(rows, a.c, a.r)) != BNN_OK || (rc = check_heads(a.c, heads, a.group)) != BNN_OK) return rc;
     if (element_bytes(dtype) == 0 || !(scale > 0.f) || !isfinite(scale) || window < 0 || (window > 0 && !causal)) return BNN_ERR_INVALID_ARG;
-    if (blocks ? keep < 1 : keep != 0) return BNN_ERR_INVALID_ARG;
+    if (blocks ? keep < 1 : keep < 0) return BNN_ERR_INVALID_ARG;
     if (a.r.tokens == 0) return BNN_OK;
+    if (!blocks && keep != 0) return BNN_ERR_INVALID_ARG;            // (the lists of no rows need no memory)
     if ((rc = check_elements(q, dtype, q_token, q_head)) != BNN_OK || (rc = check_elements(out, dtype, 0, 0)) != BNN_OK) return rc;
     if ((reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(blocks) & 3u)) return BNN_ERR_ALIGNMENT;
     if ((long long)a.r.tokens * a.group >= (1LL << 30) || (long long)keep * a.c.page >= (1LL << 31)) return BNN_ERR_UNSUPPORTED;

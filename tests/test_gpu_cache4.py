@@ -600,3 +600,15 @@ def test_an_empty_list_of_blocks(bnn, monkeypatch, native):
     with pytest.raises(ValueError, match="keep >= 1"):
         su.gpu.attend(q, blocks=blocks[:, :, :0], **su.plan)
     assert torch.equal(su.gpu.attend(q, blocks=blocks[:, :, :1].contiguous(), **su.plan), su.gpu.attend(q, blocks=torch.cat([blocks[:, :, :1], torch.full_like(blocks, -1)], 2), **su.plan))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_blocks_of_no_tokens(bnn, monkeypatch, native):
+    from paper_2006_16578_amd import binding
+    if not native:
+        monkeypatch.setattr(binding, "_native", binding._PythonOnly())
+    su = Setup(bnn, 27, [30, 9], None, 2, 64, 16)
+    q = dev(su.queries(4), "bf16")[:0]
+    blocks = su.gpu.select(q, keep=3, **su.plan)
+    out, lse = su.gpu.attend(q, blocks=blocks, want_lse=True, **su.plan)
+    assert blocks.shape == (0, 2, 3) and out.shape == (0, 4, 64) and lse.shape == (0, 4)

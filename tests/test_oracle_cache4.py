@@ -158,3 +158,10 @@ def test_record_bytes():
     assert lib.bnn_cache4_record_bytes(100, 64, 1) == 0 and lib.bnn_cache4_record_bytes(128, 63, 1) == 0
     with pytest.raises(ValueError):
         b.Cache4(4, kv_heads=2, head_dim=100)
+
+
+def test_no_rows_with_blocks():
+    # select gives an empty list for no rows, whose tensor has no memory; attend takes it
+    import paper_2006_16578_amd as b
+    assert Call(b).attend(tokens=0, keep=3) == 0 and Call(b).attend(tokens=0, keep=3, blocks=4096) == 0
+    assert Call(b).attend(tokens=0, keep=-1) == INVALID and Call(b).attend(tokens=4, keep=3) == INVALID

@@ -870,6 +870,12 @@ class Cache4:
             raise ValueError("the elements of a head of %s must be contiguous" % name)
         return _ELEMENTS[x.dtype], *(ctypes.c_int64(x.stride(i) if x.shape[i] > 1 else 0) for i in (0, 1))
 
+    def _workspace(self, workspace):
+        """The caller's: plain bytes on the cache's device (that they suffice is checked by the library)."""
+        if _dev(workspace, torch.uint8, 1, "workspace").device != self.data.device:
+            raise ValueError("workspace must be on the cache's device")
+        return workspace
+
     def write(self, k, v, table, lens, start=None):
         """Quantises k, v [tokens][kv_heads][head_dim], the newest tokens of every sequence, into the cache."""
         if (_native or _load_native()).cache4_write(*self._plain, table, lens, start, k, v):
@@ -909,6 +915,8 @@ class Cache4:
         if workspace is None:
             need = int(load().bnn_cache4_select_workspace_bytes(self._struct(), ctypes.byref(rows)))
             workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+        else:
+            self._workspace(workspace)
         with _on(q):
             _check(load().bnn_cache4_select(self._struct(), ctypes.byref(rows), _ptr(q), code, qt, qh, q.shape[1], int(keep), int(first), int(last),
                                             _ptr(blocks), _ptr(workspace), ctypes.c_size_t(workspace.numel()), _stream(q)), "bnn_cache4_select")
@@ -939,6 +947,8 @@ class Cache4:
         if workspace is None:
             need = int(load().bnn_cache4_attend_workspace_bytes(self._struct(), ctypes.byref(rows), code, q.shape[1], int(window), keep))
             workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        else:
+            self._workspace(workspace)
         with _on(q):
             _check(load().bnn_cache4_attend(self._struct(), ctypes.byref(rows), _ptr(q), code, qt, qh, q.shape[1], ctypes.c_float(scale),
                                             int(bool(causal)), int(window), _ptr(blocks), keep, _ptr(out), _ptr(lse), _ptr(workspace),

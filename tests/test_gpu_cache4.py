@@ -612,3 +612,24 @@ def test_blocks_of_no_tokens(bnn, monkeypatch, native):
     blocks = su.gpu.select(q, keep=3, **su.plan)
     out, lse = su.gpu.attend(q, blocks=blocks, want_lse=True, **su.plan)
     assert blocks.shape == (0, 2, 3) and out.shape == (0, 4, 64) and lse.shape == (0, 4)
+
+
+def test_workspace_and_out_of_the_caller(bnn):
+    # the same results in memory that the caller gives; what is no memory of the cache's device, or not enough, is refused before anything runs
+    su = Setup(bnn, 31, [5000, 300], None, 1, 64, 64, width=200)
+    q = dev(su.queries(4), "bf16")
+    rows = su.gpu._rows(su.plan["table"], su.plan["lens"], None, 2)
+    need = int(bnn.load().bnn_cache4_select_workspace_bytes(su.gpu._struct(), ctypes.byref(rows)))
+    need_attend = int(bnn.load().bnn_cache4_attend_workspace_bytes(su.gpu._struct(), ctypes.byref(rows), 1, 4, 0, 0))
+    assert need == 2 * 200 * 2 and need_attend > 0                     # (the keys are cut into parts)
+    memory = lambda n, **kw: torch.full((n,), 0xFF, dtype=torch.uint8, **{"device": "cuda", **kw})
+    blocks, out = su.gpu.select(q, keep=4, **su.plan), torch.empty_like(q)
+    assert torch.equal(su.gpu.select(q, keep=4, workspace=memory(need), **su.plan), blocks)
+    assert su.gpu.attend(q, out=out, workspace=memory(need_attend), **su.plan) is out and torch.equal(out, su.gpu.attend(q, **su.plan))
+    for bad, error in ((lambda n: memory(n, device="cpu"), TypeError), (lambda n: memory(1).expand(n), ValueError), (lambda n: memory(2 * n)[::2], ValueError),
+                       (lambda n: memory(n).view(torch.int16), TypeError), (lambda n: memory(n).view(1, n), ValueError), (lambda n: memory(n - 1), bnn.BnnError),
+                       (lambda n: memory(n + 1)[1:], bnn.BnnError), (lambda n: memory(0), bnn.BnnError)):
+        with pytest.raises(error):
+            su.gpu.select(q, keep=4, workspace=bad(need), **su.plan)
+        with pytest.raises(error):
+            su.gpu.attend(q, workspace=bad(need_attend), **su.plan)

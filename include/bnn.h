@@ -404,6 +404,9 @@ int bnn_net_layer_bits(const bnn_net* net, int layer, const uint32_t** bits, int
  * has after this call's are in.  Token i lies in page table[b][i / page], at i % page; a table entry that is no page (such as -1: given back, or
  * not needed) and what lies past the table's end hold nothing: writes there are dropped, reads give 0, and attention and selection pass them over.  The three arrays are
  * on the device and are read by the kernels; whatever they hold, no access leaves the cache or the call's arrays, but rows outside every sequence keep what they held.
+ *
+ * BNN_ERR_UNSUPPORTED: launches of 2^32 threads and more (writing and reading: 2^24 times 2048 / head_dim tokens; attention over blocks: 2^23 workgroups, one for every token,
+ * kv head and 16 of its query heads; else one for 16 to 128 rows), tokens * heads / kv_heads from 2^30 on in attention, tokens * kv_heads from 2^24 on in selection.
  * ---------------------------------------------------------------------------------------- */
 #define BNN_F32 0
 #define BNN_BF16 1
@@ -412,7 +415,7 @@ int bnn_net_layer_bits(const bnn_net* net, int layer, const uint32_t** bits, int
 typedef struct bnn_cache4 {
     void* data;          /* 16-byte aligned */
     int64_t pages;       /* < 2^31 */
-    int kv_heads;
+    int kv_heads;        /* <= 65535 */
     int head_dim;        /* 64, 96, 128, 192 or 256 */
     int page;            /* a power of two, 16 to 256 */
     int signs;           /* 1: with the signs of K, which selection needs */
@@ -448,7 +451,7 @@ int bnn_cache4_select(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
  * window > 0 (causal only) the last `window` of them; without, all lens[b] keys.  blocks, or NULL: [tokens][kv_heads][keep], as
  * bnn_cache4_select gives it, leaves only the keys of the listed blocks (entries below 0 or past the table are passed over; a block listed twice counts twice).
  *   q as in bnn_cache4_select;  out [tokens][heads][head_dim] of `dtype`, contiguous;  lse [tokens][heads] fp32 or NULL: log sum_i exp(scale * q . k_i).
- *   A row that sees no key gets 0, and -infinity in lse.  scale > 0.
+ *   A row that sees no key gets 0, and -infinity in lse.  scale > 0, and scale * log2(e) finite.
  * Products are formed of bf16 terms with fp32 sums; the cache's values are exact in bf16, queries enter exactly, softmax weights with 8 (bf16),
  * 16 (fp16) or 24 bits (fp32).  Keys that a row does not see do not reach it, NaN or not. */
 size_t bnn_cache4_attend_workspace_bytes(const bnn_cache4* cache, const bnn_cache4_rows* rows, int dtype, int heads, int window, int keep);

@@ -174,9 +174,12 @@ struct Attend4 {
     f32x4* part_sums;                        // [tiles][kv_heads][splits][rows of a tile]: reference point, sum of the weights, sum of the rounded weights
 };
 
+// A launch has fewer threads than this (along a dimension of its grid).
+constexpr long long C4_THREADS = 1LL << 32;
+
 // How a call is cut up.  rows: of a workgroup.
 struct AttendPlan4 {
-    int rows, tiles, seq_tiles, splits, chunk;
+    int rows, threads, tiles, seq_tiles, splits, chunk;
     size_t part_bytes, workspace_bytes;
 };
 
@@ -216,6 +219,9 @@ struct Select4 {
     FastDiv div_seq_tiles, div_parts, div_heads;
 };
 int launch_cache4_select(Select4 a, int dtype, hipStream_t s);
+// Workgroups of 256 threads of writing and reading, for a kv head: each has the rows whose elements, eight to a thread, fill it.
+inline int cache4_block_rows(const Cache4& c) { return 256 / (c.dim / 8); }
+inline long long cache4_row_blocks(const Cache4& c, const Rows4& r) { return cdiv(r.tokens, cache4_block_rows(c)); }
 int launch_cache4_write(const Cache4& c, const Rows4& r, const void* k, const void* v, int dtype, long long k_token, long long k_head,
                         long long v_token, long long v_head, hipStream_t s);
 int launch_cache4_read(const Cache4& c, const Rows4& r, void* k, void* v, int dtype, hipStream_t s);

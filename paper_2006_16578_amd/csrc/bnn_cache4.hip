@@ -120,8 +120,8 @@ __global__ __launch_bounds__(256) void read_kernel(Cache4 c, Rows4 r, T* __restr
 
 int launch_cache4_write(const Cache4& c, const Rows4& r, const void* k, const void* v, int dtype, long long k_token, long long k_head, long long v_token,
                         long long v_head, hipStream_t s) {
-    const int lanes = c.dim / 8, rows_block = 256 / lanes;
-    const dim3 grid((unsigned)cdiv(r.tokens, rows_block), (unsigned)c.kv_heads);
+    const int lanes = c.dim / 8, rows_block = cache4_block_rows(c);
+    const dim3 grid((unsigned)cache4_row_blocks(c, r), (unsigned)c.kv_heads);
     auto go = [&](auto type) {
         using T = decltype(type);
         launch(write_kernel<T>, grid, dim3(256), 0, s, c, r, static_cast<const T*>(k), static_cast<const T*>(v), k_token, k_head, v_token, v_head,
@@ -134,8 +134,8 @@ int launch_cache4_write(const Cache4& c, const Rows4& r, const void* k, const vo
 }
 
 int launch_cache4_read(const Cache4& c, const Rows4& r, void* k, void* v, int dtype, hipStream_t s) {
-    const int lanes = c.dim / 8, rows_block = 256 / lanes;
-    const dim3 grid((unsigned)cdiv(r.tokens, rows_block), (unsigned)c.kv_heads);
+    const int lanes = c.dim / 8, rows_block = cache4_block_rows(c);
+    const dim3 grid((unsigned)cache4_row_blocks(c, r), (unsigned)c.kv_heads);
     auto go = [&](auto type) {
         using T = decltype(type);
         launch(read_kernel<T>, grid, dim3(256), 0, s, c, r, static_cast<T*>(k), static_cast<T*>(v), make_fastdiv((uint32_t)lanes), rows_block);

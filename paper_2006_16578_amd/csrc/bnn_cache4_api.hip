@@ -70,12 +70,14 @@ AttendPlan4 plan_attend(const Cache4& c, const Rows4& r, int dtype, int group, i
     long long tiles, steps;
     if (keep > 0) {
         p.rows = 16;
+        p.threads = 64 * cache4_waves(c.dim, dtype, 1);
         tiles = (long long)r.tokens * cdiv(group, 16);
         steps = cdiv((long long)keep * (c.page / 16), 2);
     } else {
         const long long rows = cdiv((long long)r.tokens * group, r.batch);
         const int wide = 64 * cache4_wide_qtiles(c.dim, dtype);
         p.rows = rows >= 64 ? wide : rows > 16 ? 16 * cache4_qtiles(c.dim, dtype) : 16;
+        p.threads = rows >= 64 ? 256 : 64 * cache4_waves(c.dim, dtype, p.rows / 16);
         tiles = c4_tiles(r, group, p.rows, &p.seq_tiles);
         long long keys = (long long)r.table_pages << c.page_shift;
         if (window > 0) keys = std::min(keys, (long long)window + cdiv(p.rows, group) + 64);
@@ -118,6 +120,7 @@ int bnn_cache4_write(const bnn_cache4* cache, const bnn_cache4_rows* rows, const
     if (element_bytes(dtype) == 0) return BNN_ERR_INVALID_ARG;
     if (r.tokens == 0) return BNN_OK;
     if ((rc = check_elements(k, dtype, k_token, k_head)) != BNN_OK || (rc = check_elements(v, dtype, v_token, v_head)) != BNN_OK) return rc;
+    if (cache4_row_blocks(c, r) * 256 >= C4_THREADS) return BNN_ERR_UNSUPPORTED;
     return launch_cache4_write(c, r, k, v, dtype, k_token, k_head, v_token, v_head, static_cast<hipStream_t>(stream));
 }
 
@@ -129,6 +132,7 @@ int bnn_cache4_read(const bnn_cache4* cache, const bnn_cache4_rows* rows, void* 
     if (element_bytes(dtype) == 0) return BNN_ERR_INVALID_ARG;
     if (r.tokens == 0) return BNN_OK;
     if ((rc = check_elements(k, dtype, 0, 0)) != BNN_OK || (rc = check_elements(v, dtype, 0, 0)) != BNN_OK) return rc;
+    if (cache4_row_blocks(c, r) * 256 >= C4_THREADS) return BNN_ERR_UNSUPPORTED;
     return launch_cache4_read(c, r, k, v, dtype, static_cast<hipStream_t>(stream));
 }
 
@@ -172,7 +176,8 @@ int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
     Attend4 a = {};
     int rc = make_cache(cache, a.c);
     if (rc != BNN_OK || (rc = make_rows(rows, a.c, a.r)) != BNN_OK || (rc = check_heads(a.c, heads, a.group)) != BNN_OK) return rc;
-    if (element_bytes(dtype) == 0 || !(scale > 0.f) || !isfinite(scale) || window < 0 || (window > 0 && !causal)) return BNN_ERR_INVALID_ARG;
+    const float scale2 = scale * 1.4426950408889634f;                // for powers of two
+    if (element_bytes(dtype) == 0 || !(scale > 0.f) || !isfinite(scale2) || window < 0 || (window > 0 && !causal)) return BNN_ERR_INVALID_ARG;
     if (blocks ? keep < 1 : keep < 0) return BNN_ERR_INVALID_ARG;
     if (a.r.tokens == 0) return BNN_OK;
     if (!blocks && keep != 0) return BNN_ERR_INVALID_ARG;            // (the lists of no rows need no memory)
@@ -180,12 +185,12 @@ int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
     if ((reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(blocks) & 3u)) return BNN_ERR_ALIGNMENT;
     if ((long long)a.r.tokens * a.group >= (1LL << 30) || (long long)keep * a.c.page >= (1LL << 31)) return BNN_ERR_UNSUPPORTED;
     const AttendPlan4 p = plan_attend(a.c, a.r, dtype, a.group, window, keep);
-    if ((long long)p.tiles * p.splits * a.c.kv_heads >= (1LL << 31)) return BNN_ERR_UNSUPPORTED;
+    if ((long long)p.tiles * p.splits * a.c.kv_heads >= C4_THREADS / p.threads) return BNN_ERR_UNSUPPORTED;
     if (p.workspace_bytes != 0 && (!workspace || workspace_bytes < p.workspace_bytes)) return BNN_ERR_WORKSPACE;
     if (p.workspace_bytes != 0 && !aligned16(workspace)) return BNN_ERR_ALIGNMENT;
     a.q = q; a.q_token = q_token; a.q_head = q_head;
     a.div_group = make_fastdiv((uint32_t)a.group);
-    a.scale = scale * 1.4426950408889634f;
+    a.scale = scale2;
     a.causal = causal ? 1 : 0;
     a.window = window;
     a.blocks = blocks; a.keep = keep;

@@ -343,7 +343,7 @@ int launch_cache4_select(Select4 a, int dtype, hipStream_t s) {
     // parts of the keys: 1024 workgroups if there are so many steps, of which a workgroup takes four at a time
     const long long steps = cdiv((long long)a.r.table_pages * a.c.page, a.c.page > 128 ? 256 : 128);
     const long long parts = std::max(1LL, std::min(cdiv(1024, tiles * a.c.kv_heads), cdiv(steps, 4)));
-    if (tiles * parts * a.c.kv_heads >= (1LL << 31)) return BNN_ERR_UNSUPPORTED;
+    if (tiles * parts * a.c.kv_heads >= C4_THREADS / 256) return BNN_ERR_UNSUPPORTED;
     a.tiles = (int)tiles;
     a.parts = (int)parts;
     a.div_seq_tiles = make_fastdiv((uint32_t)std::max(a.seq_tiles, 1));

@@ -165,3 +165,14 @@ def test_no_rows_with_blocks():
     import paper_2006_16578_amd as b
     assert Call(b).attend(tokens=0, keep=3) == 0 and Call(b).attend(tokens=0, keep=3, blocks=4096) == 0
     assert Call(b).attend(tokens=0, keep=-1) == INVALID and Call(b).attend(tokens=4, keep=3) == INVALID
+
+
+def test_refusals_of_what_a_launch_cannot_hold():
+    # before anything is launched: 2^32 threads, and a scale whose product with log2(e) is infinite
+    import paper_2006_16578_amd as b
+    assert Call(b).attend(tokens=1 << 20, kv_heads=8, heads=8, keep=3, blocks=4096) == UNSUPPORTED
+    assert Call(b).attend(tokens=1 << 25, kv_heads=64, heads=64) == UNSUPPORTED
+    assert Call(b).write(tokens=1 << 28) == UNSUPPORTED and Call(b).read(tokens=1 << 28) == UNSUPPORTED
+    assert Call(b).write(tokens=1 << 27, head_dim=256) == UNSUPPORTED
+    assert Call(b).select(tokens=1 << 23) == UNSUPPORTED and Call(b).select(tokens=2, batch=1 << 23, start=4096) == UNSUPPORTED
+    assert Call(b).attend(scale=3e38) == INVALID

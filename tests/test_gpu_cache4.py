@@ -633,3 +633,26 @@ def test_workspace_and_out_of_the_caller(bnn):
             su.gpu.select(q, keep=4, workspace=bad(need), **su.plan)
         with pytest.raises(error):
             su.gpu.attend(q, workspace=bad(need_attend), **su.plan)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dim,heads,group", [(64, 2, 3), (96, 1, 40), (128, 1, 4), (192, 1, 6), (256, 1, 35)])
+def test_pages_of_256(bnn, dtype, dim, heads, group):
+    su = Setup(bnn, 28, [1100, 256, 1, 257, 0], [3, 1, 1, 2, 0], heads, dim, 256, dtype=dtype)
+    k = rounded(su.rng.standard_normal((su.tokens, heads, dim)), dtype)
+    oc.write(su.cache, k, -k, su.table, su.lens, su.start)
+    su.gpu.write(dev(k, dtype), dev(-k, dtype), **su.plan)
+    assert (su.gpu.data.cpu().numpy() == su.data).all()
+    want = oc.read(su.cache, su.table, su.lens, su.start, su.tokens)
+    assert all(torch.equal(a, dev(b, "f32")) for a, b in zip(su.gpu.read(tokens=su.tokens, dtype=torch.float32, **su.plan), want))
+    q = su.queries(heads * group)
+    for keep, first, last in ((2, 1, 1), (3, 0, 1), (4, 0, 0), (9, 1, 1)):
+        blocks = oc.select(su.cache, q, su.table, su.lens, keep, su.start, first, last)
+        assert (su.gpu.select(dev(q, dtype), keep=keep, first=first, last=last, **su.plan).cpu().numpy() == blocks).all(), (keep, first, last)
+        check_attend(su, q, blocks=blocks)
+    check_attend(su, q)
+    check_attend(su, q, window=300)
+    su = Setup(bnn, 29, [300, 520], [70, 66], heads, dim, 256, dtype=dtype)          # many rows
+    q = su.queries(heads * min(group, 4))
+    check_attend(su, q)
+    assert (su.gpu.select(dev(q, dtype), keep=2, **su.plan).cpu().numpy() == oc.select(su.cache, q, su.table, su.lens, 2, su.start)).all()

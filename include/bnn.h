@@ -397,13 +397,14 @@ int bnn_net_layer_bits(const bnn_net* net, int layer, const uint32_t** bits, int
  *    max|x| <= 6 * 2^e.  A code is the magnitude nearest to x * 2^-e, ties to the even code; what is beyond 6 * 2^100 saturates.  A group
  *    with an infinity or a NaN gets the byte 255 and reads as NaN throughout.
  *  - Sign bits in the library's packed layout (bit = (k >= 0), before rounding).
- * Memory of tokens that were never written need not be initialised.
+ * Memory of tokens that were never written need not be initialised.  There are no gradients: the operators are for serving.
  *
  * Rows of a call: sequence b contributes its newest tokens, as start[b + 1] - start[b] consecutive rows (start[0] = 0, start[batch] = tokens); row i
  * of n is the token at position lens[b] - n + i.  With start == NULL every sequence has tokens / batch rows.  lens[b] counts the tokens that sequence b
  * has after this call's are in.  Token i lies in page table[b][i / page], at i % page; a table entry that is no page (such as -1: given back, or
  * not needed) and what lies past the table's end hold nothing: writes there are dropped, reads give 0, and attention and selection pass them over.  The three arrays are
- * on the device and are read by the kernels; whatever they hold, no access leaves the cache or the call's arrays, but rows outside every sequence keep what they held.
+ * on the device and are read by the kernels; whatever they hold, no access leaves the cache or the call's arrays, but outputs of rows outside every sequence keep what they held (bnn_cache4_read
+ * gives 0 there).
  *
  * BNN_ERR_UNSUPPORTED: launches of 2^32 threads and more (writing and reading: 2^24 times 2048 / head_dim tokens; attention over blocks: 2^23 workgroups, one for every token,
  * kv head and 16 of its query heads; else one for 16 to 128 rows), tokens * heads / kv_heads from 2^30 on in attention, tokens * kv_heads from 2^24 on in selection.
@@ -433,7 +434,8 @@ typedef struct bnn_cache4_rows {
 /* Bytes of a record, a multiple of 16; 0 for a head_dim or page that is not supported. */
 size_t bnn_cache4_record_bytes(int head_dim, int page, int signs);
 /* Quantises the rows' keys and values into the cache.  k, v: [tokens][kv_heads][head_dim] of `dtype` (BNN_F32, BNN_BF16, BNN_F16), the elements of a head side by
- * side, tokens and heads *_token and *_head elements apart; pointers and distances multiples of 16 bytes.  A token that two rows name is written by either. */
+ * side, tokens and heads *_token and *_head elements apart; pointers and distances multiples of 16 bytes.  A token that two rows name is left
+ * with parts of either. */
 int bnn_cache4_write(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* k, const void* v, int dtype,
                      int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, void* stream);
 /* The rows' keys and values as the cache holds them, rounded once to `dtype`: k, v [tokens][kv_heads][head_dim], contiguous. */
@@ -443,7 +445,8 @@ int bnn_cache4_read(const bnn_cache4* cache, const bnn_cache4_rows* rows, void* 
  * heads of the kv head, of the most sign bits in which the query agrees with a key of the block (D - popc(q xor k), the library's product up to a factor),
  * over the keys up to the row's own; ties go to the lower block.
  *   q [tokens][heads][head_dim], elements as in bnn_cache4_write; kv head h serves query heads h * heads / kv_heads and on; heads / kv_heads * head_dim <= 16000.
- *   blocks [tokens][kv_heads][keep];  keep >= first + last, first, last >= 0. */
+ *   blocks [tokens][kv_heads][keep];  keep >= first + last, first, last >= 0.
+ * The workspace has 2 bytes for every row, kv head and page of the table: a long prompt is better selected for in chunks. */
 size_t bnn_cache4_select_workspace_bytes(const bnn_cache4* cache, const bnn_cache4_rows* rows);
 int bnn_cache4_select(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads,
                       int keep, int first, int last, int32_t* blocks, void* workspace, size_t workspace_bytes, void* stream);
@@ -452,8 +455,9 @@ int bnn_cache4_select(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
  * bnn_cache4_select gives it, leaves only the keys of the listed blocks (entries below 0 or past the table are passed over; a block listed twice counts twice).
  *   q as in bnn_cache4_select;  out [tokens][heads][head_dim] of `dtype`, contiguous;  lse [tokens][heads] fp32 or NULL: log sum_i exp(scale * q . k_i).
  *   A row that sees no key gets 0, and -infinity in lse.  scale > 0, and scale * log2(e) finite.
- * Products are formed of bf16 terms with fp32 sums; the cache's values are exact in bf16, queries enter exactly, softmax weights with 8 (bf16),
- * 16 (fp16) or 24 bits (fp32).  Keys that a row does not see do not reach it, NaN or not. */
+ * Products are formed of bf16 terms with fp32 sums; the cache's values are exact in bf16, queries enter exactly (infinite from bf16's largest number, 3.39e38, on), softmax
+ * weights with 8 (bf16), 16 (fp16) or 24 bits (fp32).  Keys that a row does not see do not reach it, NaN or not.  A row that sees keys is NaN if its query holds a NaN or
+ * an infinity, if a key that it sees holds a NaN, or if its highest score, q . k, passes fp32's range; of a value that it sees, NaN elements make its own NaN. */
 size_t bnn_cache4_attend_workspace_bytes(const bnn_cache4* cache, const bnn_cache4_rows* rows, int dtype, int heads, int window, int keep);
 int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads,
                       float scale, int causal, int window, const int32_t* blocks, int keep, void* out, float* lse,

@@ -821,7 +821,7 @@ class Cache4:
     ``data`` (uint8 [pages][kv_heads][record]) is the cache's memory, allocated here unless given; the layout is in include/bnn.h.
     Every call takes the plan of a batch: ``table`` int32 [batch][pages of the longest], ``lens`` int32 [batch], tokens per sequence including
     those of this call, and, where sequences contribute different numbers of rows, ``start`` int32 [batch + 1].  The rows of a sequence are
-    its newest tokens.  Tensors of elements are fp32, bf16 or fp16."""
+    its newest tokens.  Tensors of elements are fp32, bf16 or fp16.  No call has a gradient: results of tensors that require one do not."""
 
     def __init__(self, pages: int | None = None, *, kv_heads: int, head_dim: int, page: int = 64, signs: bool = True, data=None, device="cuda"):
         record = int(load().bnn_cache4_record_bytes(int(head_dim), int(page), int(bool(signs))))

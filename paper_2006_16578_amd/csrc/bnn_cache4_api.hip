@@ -61,8 +61,10 @@ int check_elements(const void* p, int dtype, int64_t token, int64_t head) {
     return BNN_OK;
 }
 
-// How attention is cut up.  Rows of a workgroup: 64 or 128 where the rows of a sequence fill them, else 16, or 32 where that saves a workgroup.  Parts of the keys: as many
-// as fill the chip once, two workgroups to a compute unit, but of 2048 keys at least.  64 conversations of up to 8192 tokens, 8 kv heads: one part 66 us, with two
+// How attention is cut up.  Rows of a workgroup: 64 or 128 where the rows of a sequence fill them, else 16, or 32 where that saves a workgroup; by the mean over the batch, one
+// choice for the launch, so single tokens beside a long chunk go through the kernel for many rows.  Parts of the keys: as many as 512 workgroups make, but of 2048 keys at
+// least, by the table's width (lengths are known on the device only): a table much wider than its sequences leaves them fewer parts.  512 workgroups of eight waves are two to
+// a compute unit for heads of 64 and for bf16 ones of 128; others take more than 128 registers, or more than 80 KB of LDS, and run one after another.  64 conversations of up to 8192 tokens, 8 kv heads: one part 66 us, with two
 // 82 (before K's exponents were loaded four keys at a time, now one part 60); two documents of up to 131072: 32 parts 48 us, 48 parts 56, 64 parts 50; 5 drafted tokens over 1000 keys in one part 15 us, in two 19; one conversation of 777 tokens in
 // one part 8.2 us, in two 10.7.
 AttendPlan4 plan_attend(const Cache4& c, const Rows4& r, int dtype, int group, int window, int keep) {

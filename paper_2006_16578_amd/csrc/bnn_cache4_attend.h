@@ -570,9 +570,9 @@ __global__ __launch_bounds__(64 * cache4_waves(D, DTYPE, QT), D == 256 && DTYPE 
 // lane's 16 bytes side by side: reads and writes without conflicts): two waves have a half each of the keys, K two steps ahead of its use and V in turn; one barrier a step.
 // In step i a wave forms the scores of step i + 1, the weights of step i and the sums of step i - 1: three pieces of work that do not wait for each other, so that matrix
 // and vector instructions of one wave alternate.  A maximum that is raised in step i scales the sums at the step's end, when those of step i - 1 are in.
-// Two prompts of 4096 tokens (32 heads of 128 on 8 kv heads, bf16): 332 to 350 us, 0.8 PFLOP/s; every wave converting for itself 416.  Bounded by what a SIMD issues: an MFMA
+// Two prompts of 4096 tokens (32 heads of 128 on 8 kv heads, bf16): 336 to 350 us, 0.8 PFLOP/s; every wave converting for itself 416.  Bounded by what a SIMD issues: an MFMA
 // takes 16.3 cycles of it, a plain vector instruction beside MFMAs 2.1, an exponential 5.5, a read of LDS 7 (each measured), so a step of 34, 109, 16 and 16 of them 1080 at least, 2160 for two waves, which take
-// 2830.  More than two do not fit: 32 rows of sums, queries, scores and weights are 231 registers.  16 rows a wave at three or four waves a SIMD read twice the operands from LDS for a row: 424 us;
+// 2830.  More than two do not fit: 32 rows of sums, queries, scores and weights are 232 registers.  16 rows a wave at three or four waves a SIMD read twice the operands from LDS for a row: 424 us;
 // eight waves to what is converted, 512 threads: 358.
 template <int D, int DTYPE, int QT>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(Attend4 a) {

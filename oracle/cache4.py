@@ -85,7 +85,7 @@ def row_places(cache, table, lens, start, tokens):
     start = np.arange(batch + 1) * (tokens // batch) if start is None else start
     out = []
     for b in range(batch):
-        n = start[b + 1] - start[b]
+        n = int(start[b + 1]) - int(start[b])
         out += [(b, int(lens[b]) - n + i) for i in range(n)]
     return out
 

@@ -385,6 +385,30 @@ int bnn_net_fc_run(const bnn_net* net, int batch, int recorded, int* layers);
  * length in words, rows the number of rows (batch, or batch*P*Q). */
 int bnn_net_layer_bits(const bnn_net* net, int layer, const uint32_t** bits, int64_t* rows, int* words_per_row);
 
+/* Types of elements, where a call takes several. */
+#define BNN_F32 0
+#define BNN_BF16 1
+#define BNN_F16 2
+
+/* ------------------------------------------------------------------------------------------
+ * Rotary positions.  Pair p of every head, (a, b), becomes magnitude * (a cos t - b sin t, a sin t + b cos t) with t = position * frequencies[p] in 64 bits; the sum of
+ * products is in 64 bits too, rounded to fp32 once.  A pair is the elements p and p + pairs of a head, or with `neighbours` the elements 2 p and 2 p + 1;
+ * the elements from 2 * pairs on stay as they are.  With `inverse` the angles have the other sign: the transposed map, which is the gradient's.
+ * ---------------------------------------------------------------------------------------- */
+typedef struct bnn_rotation {
+    const double* frequencies;    /* [pairs], radians a position; |position * frequency| below 2^53, device memory, 8-byte aligned */
+    const int32_t* positions;     /* [tokens], 4-byte aligned; NULL (bnn_cache4_write_rotary only): a token's place in its sequence */
+    int pairs;                    /* 1 to 1024 */
+    int neighbours;               /* 0 or 1 */
+    int inverse;                  /* 0 or 1 */
+    double magnitude;             /* finite */
+} bnn_rotation;
+/* x, out [tokens][heads][dim] of `dtype` (BNN_F32, BNN_BF16, BNN_F16), the elements of a head side by side, tokens and heads *_token and *_head elements apart.  out may be x,
+ * with the same distances.  Pointers aligned to an element; what is aligned to 16 bytes, with distances, pairs and dim that are multiples of 8, runs fastest.
+ * dim >= 2 * pairs.  tokens or heads 0: nothing is done.  BNN_ERR_UNSUPPORTED: 2^24 times 16 tokens and more, dim from 2^20 on, heads beyond 65535 workgroups' (at least one head each). */
+int bnn_rotary(const void* x, void* out, int dtype, int tokens, int heads, int dim, int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head,
+               const bnn_rotation* rotation, void* stream);
+
 /* ------------------------------------------------------------------------------------------
  * A key/value cache in 4 bits, and attention over it: what a language model of binarized layers needs beside them.
  *
@@ -409,10 +433,6 @@ int bnn_net_layer_bits(const bnn_net* net, int layer, const uint32_t** bits, int
  * BNN_ERR_UNSUPPORTED: launches of 2^32 threads and more (writing and reading: 2^24 times 2048 / head_dim tokens; attention over blocks: 2^23 workgroups, one for every token,
  * kv head and 16 of its query heads; else one for 16 to 128 rows), tokens * heads / kv_heads from 2^30 on in attention, tokens * kv_heads from 2^24 on in selection.
  * ---------------------------------------------------------------------------------------- */
-#define BNN_F32 0
-#define BNN_BF16 1
-#define BNN_F16 2
-
 typedef struct bnn_cache4 {
     void* data;          /* 16-byte aligned */
     int64_t pages;       /* < 2^31 */
@@ -438,6 +458,11 @@ size_t bnn_cache4_record_bytes(int head_dim, int page, int signs);
  * with parts of either. */
 int bnn_cache4_write(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* k, const void* v, int dtype,
                      int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, void* stream);
+/* The same with rotary positions: the rows' keys, rotated, and their values go into the cache, and q [tokens][heads][head_dim], rotated, to q_out, contiguous (which may be q).  A rotated
+ * key's element is rounded to fp32, then quantised.  Rows outside every sequence leave q_out as it is; rows whose token the cache does not hold (bnn_cache4_rows) are rotated all the same.
+ * heads 0: no queries.  rotation->pairs at most head_dim / 2. */
+int bnn_cache4_write_rotary(const bnn_cache4* cache, const bnn_cache4_rows* rows, const bnn_rotation* rotation, const void* q, int64_t q_token, int64_t q_head, int heads, void* q_out,
+                            const void* k, const void* v, int dtype, int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, void* stream);
 /* The rows' keys and values as the cache holds them, rounded once to `dtype`: k, v [tokens][kv_heads][head_dim], contiguous. */
 int bnn_cache4_read(const bnn_cache4* cache, const bnn_cache4_rows* rows, void* k, void* v, int dtype, void* stream);
 /* For every row and kv head the `keep` blocks (pages of its sequence, counted from 0) to attend to, ascending, the rest -1: the first `first` blocks
@@ -462,6 +487,44 @@ size_t bnn_cache4_attend_workspace_bytes(const bnn_cache4* cache, const bnn_cach
 int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads,
                       float scale, int causal, int window, const int32_t* blocks, int keep, void* out, float* lse,
                       void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Eviction: a cache cut back to the tokens that attention used most.  Attention gives the logarithms of its weights' sums (lse); bnn_cache4_weigh adds up, call by call, what
+ * weight every cached token got; bnn_cache4_heaviest chooses the tokens to keep, for every kv head by itself; bnn_cache4_move copies them into other pages, as a shorter sequence.
+ * Weights are fp32 [batch][kv_heads][width], a sequence's tokens in order; width >= table_pages * page.  Sequences of up to 2^30 tokens.
+ * ---------------------------------------------------------------------------------------- */
+/* For every token j of every sequence (those that the table holds, up to lens[b]):
+ *   weights[b][h][j] = decay * previous[b][h][j] (0 for this call's tokens, and with previous == NULL) + the sum, over the rows that see j and the query heads of kv head h, of
+ *   exp(scale * q . k_j - lse).
+ * Weights from lens[b] on, and of tokens past the table's end, are left as they are.  previous may be weights.  What a row sees is as in bnn_cache4_attend without blocks, and lse [tokens][heads]
+ * is what that gave for the same q, scale, causal and window; a row with -infinity there adds nothing, and one whose query holds a NaN or an infinity makes the weights of what it sees NaN.
+ * Tokens on no page get nothing.  Products are of bf16 terms, queries exactly, with fp32 sums; sums are fp32 and in the same order for the same arguments.  decay finite. */
+int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads, const float* lse,
+                     float scale, int causal, int window, const float* previous, float decay, float* weights, int64_t width, void* stream);
+/* tokens [batch][kv_heads][keep]: of the tokens of every sequence that lie on a page, all if they are `keep` at most, else the first `first` and last `last` (of the numbers 0 .. lens[b] - 1)
+ * and of the others those with the largest weights; ascending, the rest -1.  Ties go to the lower token; NaN is below every number.  kept [batch]: how many.  first + last <= keep. */
+int bnn_cache4_heaviest(const bnn_cache4* cache, const int32_t* table, const int32_t* lens, int batch, int table_pages, const float* weights, int64_t width,
+                        int keep, int first, int last, int32_t* tokens, int32_t* kept, void* stream);
+/* Token tokens[b][h][i] of the sequence that `table` describes, kv head h, becomes token i of the one that `into` [batch][into_pages] describes: codes, scales and signs as they are.  The
+ * pages of `into` are others than those of `table` (their contents are not defined else), and not shared.  Entries below 0, what lies on no page, and places past `into`'s end are passed over.
+ * weights, moved: both or neither; moved [batch][kv_heads][into_pages * page] gets the tokens' weights, 0 where there is no token. */
+int bnn_cache4_move(const bnn_cache4* cache, const int32_t* tokens, int keep, const int32_t* table, int table_pages, const int32_t* into, int into_pages, int batch,
+                    const float* weights, int64_t width, float* moved, void* stream);
+
+/* ------------------------------------------------------------------------------------------
+ * What the sums of a model's head say.  z = scale * x over the columns of a row of logits:
+ *   logprobs[r] = z[target] - lse,  entropy[r] = lse - sum_j p_j z_j  (p = exp(z - lse)),  lse[r] = log sum_j exp(z_j),
+ *   top_logprobs, top_tokens [rows][top]: the largest log probabilities, descending, and their columns; ties go to the lower column.
+ *   logits [rows][cols], rows ld elements apart, BNN_F32, BNN_BF16, BNN_F16 or BNN_I32 (the sums of bnn_bmm; as fp32 they are exact up to 2^24).  scale > 0 and finite.
+ *   targets [rows] int64 or NULL (no logprobs then); a target outside [0, cols) gives 0 (no token to be judged).
+ *   logprobs, entropy, lse [rows] fp32, each or NULL; top_logprobs [rows][top] fp32 and top_tokens [rows][top] int32, both (NULL if top is 0).
+ * Columns of -infinity have no probability.  A row without a distribution -- every logit -infinity, or a NaN or +infinity among them -- gets NaN, tokens of -1, and an lse of -infinity in the first case.
+ * Sums are fp32.  The logits are read once.  0 <= top <= 64, top <= cols.  BNN_ERR_UNSUPPORTED: 2^24 and more pieces (of 2048 to 16384 columns of a row each), cols from 2^30 on.
+ * ---------------------------------------------------------------------------------------- */
+#define BNN_I32 3
+size_t bnn_token_logprobs_workspace_bytes(int rows, int cols, int dtype, int top);
+int bnn_token_logprobs(const void* logits, int dtype, int rows, int cols, int64_t ld, float scale, const int64_t* targets, int top,
+                       float* logprobs, float* entropy, float* lse, float* top_logprobs, int32_t* top_tokens, void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -7,9 +7,11 @@ dtypes are checked here, everything else by the library, whose status codes are 
 """
 from __future__ import annotations
 
+import collections
 import contextlib
 import ctypes
 import importlib
+import math
 import os
 import sys
 import warnings
@@ -18,7 +20,7 @@ import torch
 
 __all__ = ["BnnError", "lib_path", "load", "PAD_MINUS_ONE", "PAD_EXCLUDE", "PATH_AUTO", "PATH_VALU", "PATH_MFMA",
            "nwords", "round_up", "bmm", "bmm_thr", "bconv", "bconv_thr", "threshold_pack", "pack_u8", "pack_f32",
-           "unpack_i32", "tile_b", "bmm_tiled", "bmm_thr_tiled", "panels_from_rows", "rows_from_panels", "bmm_panels", "bmm_thr_panels", "probe_load_stride", "probe_pipeline", "probe_pipeline_enqueue", "PROBES", "sign_pack_f32", "bmm_general_f32", "bconv_general_f32", "maxpool_or", "conv_f32_thr", "conv_f32_split_thr", "bwn_conv_thr", "head_f32", "Net", "Cache4", "EXPORTS", "bmm_kernel_name", "bconv_kernel_name"]
+           "unpack_i32", "tile_b", "bmm_tiled", "bmm_thr_tiled", "panels_from_rows", "rows_from_panels", "bmm_panels", "bmm_thr_panels", "probe_load_stride", "probe_pipeline", "probe_pipeline_enqueue", "PROBES", "sign_pack_f32", "bmm_general_f32", "bconv_general_f32", "maxpool_or", "conv_f32_thr", "conv_f32_split_thr", "bwn_conv_thr", "head_f32", "Net", "Cache4", "rotary", "rotary_frequencies", "token_logprobs", "TokenLogprobs", "EXPORTS", "bmm_kernel_name", "bconv_kernel_name"]
 
 PAD_MINUS_ONE, PAD_EXCLUDE = 0, 1
 PATH_AUTO, PATH_VALU, PATH_MFMA = 0, 1, 2
@@ -33,8 +35,9 @@ EXPORTS = ["bnn_status_string", "bnn_version", "bnn_bmm_kernel_name", "bnn_bconv
            "bnn_net_destroy", "bnn_net_input_u8", "bnn_net_input_bits", "bnn_net_input_conv_f32", "bnn_net_input_bwn_f32", "bnn_net_add_fc",
            "bnn_net_add_conv", "bnn_net_add_pool", "bnn_net_add_block", "bnn_net_add_head_f32", "bnn_net_workspace_bytes",
            "bnn_net_forward", "bnn_net_forward_static", "bnn_static_workspace_init", "bnn_net_forward_persistent", "bnn_net_persistent_status", "bnn_net_fc_run", "bnn_net_layer_bits",
-           "bnn_cache4_record_bytes", "bnn_cache4_write", "bnn_cache4_read", "bnn_cache4_select_workspace_bytes", "bnn_cache4_select",
-           "bnn_cache4_attend_workspace_bytes", "bnn_cache4_attend"]
+           "bnn_rotary", "bnn_cache4_record_bytes", "bnn_cache4_write", "bnn_cache4_write_rotary", "bnn_cache4_read", "bnn_cache4_select_workspace_bytes", "bnn_cache4_select",
+           "bnn_cache4_attend_workspace_bytes", "bnn_cache4_attend", "bnn_cache4_weigh", "bnn_cache4_heaviest", "bnn_cache4_move",
+           "bnn_token_logprobs_workspace_bytes", "bnn_token_logprobs"]
 
 
 class BnnError(RuntimeError):
@@ -73,6 +76,7 @@ def load() -> ctypes.CDLL:
         lib.bnn_cache4_record_bytes.restype = ctypes.c_size_t
         lib.bnn_cache4_select_workspace_bytes.restype = ctypes.c_size_t
         lib.bnn_cache4_attend_workspace_bytes.restype = ctypes.c_size_t
+        lib.bnn_token_logprobs_workspace_bytes.restype = ctypes.c_size_t
         for name in EXPORTS:
             getattr(lib, name)          # fail loudly on a missing export
         _lib = lib
@@ -815,6 +819,82 @@ class _Rows4Struct(ctypes.Structure):
 _ELEMENTS = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}      # BNN_F32, BNN_BF16, BNN_F16
 
 
+class _RotationStruct(ctypes.Structure):
+    _fields_ = [("frequencies", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("pairs", ctypes.c_int), ("neighbours", ctypes.c_int), ("inverse", ctypes.c_int),
+                ("magnitude", ctypes.c_double)]
+
+
+def _rotation(frequencies, positions, tokens, device, interleaved, inverse, magnitude):
+    _dev(frequencies, torch.float64, 1, "frequencies")
+    if positions is not None and _dev(positions, torch.int32, 1, "positions").shape[0] != tokens:
+        raise ValueError("positions must have an entry for every token")
+    for t in (frequencies, positions):
+        if t is not None and t.device != device:
+            raise ValueError("frequencies and positions must be on the elements' device")
+    return _RotationStruct(frequencies.data_ptr(), 0 if positions is None else positions.data_ptr(), frequencies.shape[0], int(bool(interleaved)), int(bool(inverse)), float(magnitude))
+
+
+def _distances(x):
+    """Elements between tokens and between heads of x [tokens][heads][dim]; of a dimension of a single entry there are none."""
+    return tuple(ctypes.c_int64(x.stride(i) if x.shape[i] > 1 else 0) for i in (0, 1))
+
+
+def _heads_of(x, name):
+    """x [tokens][heads][dim], the elements of a head side by side -> its type code."""
+    if not isinstance(x, torch.Tensor) or not x.is_cuda:
+        raise TypeError("%s must be a device tensor" % name)
+    if x.dtype not in _ELEMENTS:
+        raise TypeError("%s must be fp32, bf16 or fp16, got %s" % (name, x.dtype))
+    if x.dim() != 3:
+        raise ValueError("%s must be [tokens][heads][dim]" % name)
+    if x.stride(2) != 1 and x.shape[2] > 1 and x.numel() != 0:
+        raise ValueError("the elements of a head of %s must be contiguous" % name)
+    return _ELEMENTS[x.dtype]
+
+
+def rotary_frequencies(elements: int, base: float = 10000.0, factor: float = 1.0, scaling: str = "linear", context: int = 0, low: float = 1.0, high: float = 32.0, device="cuda"):
+    """Frequencies base^(-2p / elements) of elements / 2 pairs, float64 on the device, for contexts `factor` times as long as those of training:
+    scaling "linear" divides them all by it; "base" raises the base by factor^(elements / (elements - 2)), so that the first keeps its value and the last is divided;
+    "parts" divides those that turn less than `low` times over `context` positions, keeps those that turn more than `high` times, and blends between (with it, a
+    magnitude of 1 + 0.1 ln(factor) is usual)."""
+    if elements < 2 or elements % 2 or not base > 0 or not factor >= 1:
+        raise ValueError("an even number of elements, base > 0 and factor >= 1 expected")
+    if scaling == "base" and factor != 1:
+        if elements < 4:
+            raise ValueError("scaling by the base needs two pairs at least")
+        base = base * factor ** (elements / (elements - 2))
+    f = float(base) ** (-torch.arange(0, elements, 2, dtype=torch.float64) / elements)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "parts":
+        if context < 1 or not high > low:
+            raise ValueError("parts are told apart by context >= 1, and high > low")
+        kept = ((context * f / (2 * math.pi) - low) / (high - low)).clamp(0, 1)
+        f = f * kept + f / factor * (1 - kept)
+    elif scaling != "base":
+        raise ValueError("scaling is linear, base or parts")
+    return f.to(device)
+
+
+def rotary(x, positions, frequencies, interleaved: bool = False, magnitude: float = 1.0, inverse: bool = False, out=None):
+    """x [tokens][heads][dim] (fp32, bf16 or fp16) with every head's first 2 * len(frequencies) elements turned in pairs by positions[token] * frequencies[pair]
+    (positions int32, frequencies float64: rotary_frequencies); pairs are the halves' elements, or neighbours if interleaved.  inverse turns back, which is also how a
+    gradient passes.  out may be x."""
+    code = _heads_of(x, "x")
+    rot = _rotation(frequencies, positions, x.shape[0], x.device, interleaved, inverse, magnitude)
+    if positions is None:
+        raise TypeError("positions must be a device tensor")
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    else:
+        _heads_of(out, "out")
+        if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+            raise ValueError("out must have x's shape, type and device")
+    with _on(x):
+        _check(load().bnn_rotary(_ptr(x), _ptr(out), code, x.shape[0], x.shape[1], x.shape[2], *_distances(x), *_distances(out), ctypes.byref(rot), _stream(x)), "bnn_rotary")
+    return out
+
+
 class Cache4:
     """Key/value cache in 4 bits (bnn_cache4_*): pages of `page` tokens, a page table per batch, E2M1 codes with a power of two per 32 elements.
 
@@ -888,6 +968,31 @@ class Cache4:
         with _on(k):
             _check(load().bnn_cache4_write(self._struct(), ctypes.byref(rows), _ptr(k), _ptr(v), code, kt, kh, vt, vh, _stream(k)), "bnn_cache4_write")
 
+    def write_rotary(self, q, k, v, table, lens, frequencies, start=None, positions=None, interleaved: bool = False, magnitude: float = 1.0, out=None):
+        """write() of v and of k turned by its tokens' positions, as rotary() does it; returns q [tokens][heads][head_dim] turned alike, or None without q.  positions (int32
+        [tokens]): by default a token's place in its sequence, which is no longer its position once tokens before it were evicted."""
+        code, kt, kh = self._elements(k, self.kv_heads, "k")
+        code_v, vt, vh = self._elements(v, self.kv_heads, "v")
+        if code != code_v or k.shape != v.shape:
+            raise ValueError("k and v must agree in type and shape")
+        qt = qh = ctypes.c_int64(0)
+        if q is not None:
+            code_q, qt, qh = self._elements(q, None, "q")
+            if code_q != code or q.shape[0] != k.shape[0]:
+                raise ValueError("q must have k's type and tokens")
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            elif _dev(out, q.dtype, 3, "out").shape != q.shape or out.device != q.device:
+                raise ValueError("out must have q's shape and device")
+        elif out is not None:
+            raise ValueError("out without q")
+        rows = self._rows(table, lens, start, k.shape[0])
+        rot = _rotation(frequencies, positions, k.shape[0], k.device, interleaved, False, magnitude)
+        with _on(k):
+            _check(load().bnn_cache4_write_rotary(self._struct(), ctypes.byref(rows), ctypes.byref(rot), _ptr(q), qt, qh, 0 if q is None else q.shape[1], _ptr(out), _ptr(k), _ptr(v),
+                                                  code, kt, kh, vt, vh, _stream(k)), "bnn_cache4_write_rotary")
+        return out
+
     def read(self, table, lens, start=None, tokens: int | None = None, dtype=torch.bfloat16):
         """(k, v) [tokens][kv_heads][head_dim]: the newest tokens of every sequence as the cache holds them.  tokens: rows in all (default: one of every sequence)."""
         if dtype not in _ELEMENTS:
@@ -954,3 +1059,105 @@ class Cache4:
                                             int(bool(causal)), int(window), _ptr(blocks), keep, _ptr(out), _ptr(lse), _ptr(workspace),
                                             ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream(q)), "bnn_cache4_attend")
         return (out, lse) if want_lse else out
+
+    def _weights(self, weights, batch, room, name):
+        """fp32 [batch][kv_heads][at least the table's tokens], on the cache's device."""
+        _dev(weights, torch.float32, 3, name)
+        if weights.shape[0] != batch or weights.shape[1] != self.kv_heads or weights.shape[2] < room:
+            raise ValueError("%s must be [batch][kv_heads][tokens], with room for the table's %d" % (name, room))
+        if weights.device != self.data.device:
+            raise ValueError("%s must be on the cache's device" % name)
+        return weights
+
+    def weigh(self, q, lse, table, lens, start=None, scale: float | None = None, causal: bool = True, window: int = 0, previous=None, decay: float = 1.0, out=None):
+        """The attention weight of every cached token: decay * previous plus what the rows of q give it, with the lse that attend() of the same arguments (without blocks)
+        returned -> fp32 [batch][kv_heads][tokens of the table].  Tokens of this call have no previous weight.  What lies behind a sequence's end is not written (and undefined in an
+        output that is made here).  out may be previous."""
+        scale = self.head_dim ** -0.5 if scale is None else float(scale)
+        code, qt, qh = self._elements(q, None, "q")
+        rows = self._rows(table, lens, start, q.shape[0])
+        if _dev(lse, torch.float32, 2, "lse").shape != q.shape[:2] or lse.device != q.device:
+            raise ValueError("lse must be [tokens][heads], on q's device")
+        batch, room = table.shape[0], table.shape[1] * self.page
+        if out is None:
+            out = torch.empty((batch, self.kv_heads, room) if previous is None else previous.shape, dtype=torch.float32, device=q.device)
+        self._weights(out, batch, room, "out")
+        if previous is not None and self._weights(previous, batch, room, "previous").shape != out.shape:
+            raise ValueError("previous and out must agree in shape")
+        with _on(q):
+            _check(load().bnn_cache4_weigh(self._struct(), ctypes.byref(rows), _ptr(q), code, qt, qh, q.shape[1], _ptr(lse), ctypes.c_float(scale), int(bool(causal)), int(window),
+                                           _ptr(previous), ctypes.c_float(decay), _ptr(out), ctypes.c_int64(out.shape[2]), _stream(q)), "bnn_cache4_weigh")
+        return out
+
+    def heaviest(self, weights, table, lens, keep: int, first: int = 0, last: int = 0):
+        """(int32 [batch][kv_heads][keep], int32 [batch]): the tokens of every sequence to keep, ascending, the rest -1, and how many: all of a sequence of up to `keep`, else
+        the first `first`, the last `last` and those with the largest weights.  Ties go to the lower token."""
+        _dev(table, torch.int32, 2, "table"); _dev(lens, torch.int32, 1, "lens")
+        batch, width = table.shape
+        if lens.shape[0] != batch:
+            raise ValueError("lens must have an entry for every sequence of table")
+        if table.device != self.data.device or lens.device != self.data.device:
+            raise ValueError("the plan must be on the cache's device")
+        self._weights(weights, batch, width * self.page, "weights")
+        if int(keep) < 1:
+            raise ValueError("keep >= 1 expected")
+        tokens = torch.empty((batch, self.kv_heads, int(keep)), dtype=torch.int32, device=weights.device)
+        kept = torch.empty(batch, dtype=torch.int32, device=weights.device)
+        with _on(weights):
+            _check(load().bnn_cache4_heaviest(self._struct(), _ptr(table), _ptr(lens), batch, width, _ptr(weights), ctypes.c_int64(weights.shape[2]), int(keep), int(first), int(last),
+                                              _ptr(tokens), _ptr(kept), _stream(weights)), "bnn_cache4_heaviest")
+        return tokens, kept
+
+    def move(self, tokens, table, into, weights=None):
+        """Copies token tokens[b][h][i] (from heaviest) of the sequence in table[b] to token i of the one in into[b] (int32 [batch][pages], other pages than the table's), for every kv
+        head; with weights returns them moved alike, fp32 [batch][kv_heads][tokens of into], 0 where there is none.  The sequence's length is then heaviest's second result."""
+        _dev(tokens, torch.int32, 3, "tokens"); _dev(table, torch.int32, 2, "table"); _dev(into, torch.int32, 2, "into")
+        batch = table.shape[0]
+        if tokens.shape[0] != batch or into.shape[0] != batch or tokens.shape[1] != self.kv_heads or tokens.shape[2] < 1:
+            raise ValueError("tokens [batch][kv_heads][keep], keep >= 1, and into [batch][pages] expected")
+        for t in (tokens, table, into):
+            if t.device != self.data.device:
+                raise ValueError("the plan must be on the cache's device")
+        moved = None
+        if weights is not None:
+            self._weights(weights, batch, 1, "weights")
+            moved = torch.empty((batch, self.kv_heads, into.shape[1] * self.page), dtype=torch.float32, device=weights.device)
+        if moved is not None and moved.numel() == 0:
+            return moved
+        with _on(tokens):
+            _check(load().bnn_cache4_move(self._struct(), _ptr(tokens), tokens.shape[2], _ptr(table), table.shape[1], _ptr(into), into.shape[1], batch, _ptr(weights),
+                                          ctypes.c_int64(0 if weights is None else weights.shape[2]), _ptr(moved), _stream(tokens)), "bnn_cache4_move")
+        return moved
+
+
+TokenLogprobs = collections.namedtuple("TokenLogprobs", "logprobs entropy lse top_logprobs top_tokens")
+_LOGITS = {**_ELEMENTS, torch.int32: 3}                                  # BNN_I32
+
+
+def token_logprobs(logits, targets=None, scale: float = 1.0, top: int = 0, workspace=None):
+    """What rows of logits [rows][cols] (fp32, bf16, fp16, or int32 sums as bmm gives them), times scale, say of tokens: TokenLogprobs of fp32 [rows] logprobs of the targets (int64
+    [rows]; 0 for one outside the columns; None without targets), entropy, lse, and the `top` (64 at most) best alternatives' logprobs and columns (int32) [rows][top], ties to
+    the lower column.  A row without a distribution (all -infinity, a NaN, +infinity) gets NaN and columns of -1."""
+    if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
+        raise TypeError("logits must be a device tensor")
+    if logits.dtype not in _LOGITS:
+        raise TypeError("logits must be fp32, bf16, fp16 or int32, got %s" % logits.dtype)
+    if logits.dim() != 2 or logits.shape[1] < 1 or (logits.stride(1) != 1 and logits.shape[1] > 1 and logits.shape[0] > 0):
+        raise ValueError("logits must be [rows][cols], the columns of a row contiguous")
+    rows, cols = logits.shape
+    if targets is not None and (_dev(targets, torch.int64, 1, "targets").shape[0] != rows or targets.device != logits.device):
+        raise ValueError("targets must have an entry for every row, on the logits' device")
+    ld, code = (logits.stride(0) if rows > 1 else 0), _LOGITS[logits.dtype]
+    new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=logits.device)
+    lp, entropy, lse = (None if targets is None else new(rows)), new(rows), new(rows)
+    top = int(top)
+    best, tokens = new(rows, max(top, 0)), new(rows, max(top, 0), dtype=torch.int32)
+    if workspace is None:
+        need = int(load().bnn_token_logprobs_workspace_bytes(rows, cols, code, top))
+        workspace = new(need, dtype=torch.uint8) if need else None
+    elif _dev(workspace, torch.uint8, 1, "workspace").device != logits.device:
+        raise ValueError("workspace must be on the logits' device")
+    with _on(logits):
+        _check(load().bnn_token_logprobs(_ptr(logits), code, rows, cols, ctypes.c_int64(ld), ctypes.c_float(scale), _ptr(targets), top, _ptr(lp), _ptr(entropy), _ptr(lse), _ptr(best),
+                                         _ptr(tokens), _ptr(workspace), ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream(logits)), "bnn_token_logprobs")
+    return TokenLogprobs(lp, entropy, lse, best, tokens)

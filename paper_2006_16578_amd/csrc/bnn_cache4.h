@@ -148,6 +148,54 @@ __device__ __forceinline__ void c4_store(T* p, const float (&x)[N]) {
 template <class T>
 __device__ __forceinline__ void c4_store8(T* p, const float (&x)[8]) { c4_store<8>(p, x); }
 
+// Value of the lane whose number in its group of four differs in the bits of X.
+template <int X>
+__device__ __forceinline__ uint32_t c4_quad_xor(uint32_t v) {
+    constexpr int perm = X == 1 ? 0xB1 : 0x4E;          // lanes 1,0,3,2 / 2,3,0,1
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, perm, 0xf, 0xf, true);
+}
+
+// Eight elements of a group of 32 that four lanes share: returns the codes, sets the scale's byte.
+__device__ __forceinline__ uint32_t c4_quantise(const float (&x)[8], uint32_t& byte) {
+    uint32_t high = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) high = max(high, __float_as_uint(x[i]) & 0x7fffffffu);
+    high = max(high, c4_quad_xor<1>(high));
+    high = max(high, c4_quad_xor<2>(high));
+    // 1.m 2^(E - 127) <= 6 2^e: e + 127 = E - 2, one more where 1.m > 1.5
+    const int e = (int)(high >> 23) - 2 + ((high & 0x7fffffu) > 0x400000u ? 1 : 0);
+    const int clamped = min(max(e, C4_EXP_MIN), C4_EXP_MAX);
+    byte = high >= 0x7f800000u ? C4_EXP_NAN : (uint32_t)clamped;
+    const float scale = __uint_as_float((uint32_t)clamped << 23);
+    uint32_t codes = 0;
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], scale, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
+    return codes;
+}
+
+// Writes a token's key x and value y, eight elements from 8 * at on of each, with the signs of x: the four lanes of a group of 32 elements together.
+__device__ __forceinline__ void c4_put(const Cache4& c, uint8_t* rec, int offset, int at, const float (&x)[8], const float (&y)[8]) {
+    uint32_t kb, vb;
+    const uint32_t kc = c4_quantise(x, kb), vc = c4_quantise(y, vb);
+    const int row = c.dim / 2 * offset + at * 4;
+    *reinterpret_cast<uint32_t*>(rec + row) = kc;
+    *reinterpret_cast<uint32_t*>(rec + c.v_codes + row) = vc;
+    uint32_t bits = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) bits |= (x[i] >= 0.f ? 1u : 0u) << i;
+    bits <<= 8 * (at & 3);
+    bits |= c4_quad_xor<1>(bits);
+    bits |= c4_quad_xor<2>(bits);
+    if ((at & 3) == 0) {
+        const int e = (at >> 2) * c.page + offset;
+        rec[c.k_exps + e] = (uint8_t)kb;
+        rec[c.v_exps + e] = (uint8_t)vb;
+        if (c.signs) *reinterpret_cast<uint32_t*>(rec + c.signs + offset * (c.dim / 8) + at) = bits;
+    }
+}
+
 // The scale that a byte stands for, for the conversion instructions: with the NaN byte's (the bits of an infinity) they give NaN for every code, 0 included.
 __device__ __forceinline__ float c4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
@@ -219,6 +267,47 @@ struct Select4 {
     FastDiv div_seq_tiles, div_parts, div_heads;
 };
 int launch_cache4_select(Select4 a, int dtype, hipStream_t s);
+// The call that sums attention weights, as the kernels see it.
+struct Weigh4 {
+    Cache4 c;
+    Rows4 r;
+    const void* q;
+    long long q_token, q_head;
+    int group;
+    FastDiv div_group;
+    float scale;
+    int causal, window;
+    const float* lse;                        // [tokens][heads]
+    const float* previous;                   // [batch][kv_heads][width], or nullptr; may be out
+    float* out;
+    float decay;
+    long long width;
+    int key_tiles;                           // of a sequence
+    FastDiv div_heads, div_key_tiles;
+};
+int launch_cache4_weigh(Weigh4 a, int dtype, hipStream_t s);
+
+// The choice of the tokens to keep, and moving them.
+struct Heaviest4 {
+    Cache4 c;
+    const float* weights;                    // [batch][kv_heads][width]
+    long long width;
+    const int32_t *table, *lens;
+    int batch, table_pages, keep, first, last;
+    int32_t *tokens, *kept;                  // [batch][kv_heads][keep], [batch]
+};
+int launch_cache4_heaviest(const Heaviest4& a, hipStream_t s);
+struct Move4 {
+    Cache4 c;
+    const int32_t* tokens;                   // [batch][kv_heads][keep]
+    const int32_t *table, *into;             // [batch][table_pages], [batch][into_pages]
+    int batch, table_pages, into_pages, keep;
+    const float* weights;                    // [batch][kv_heads][width], or nullptr
+    long long width;
+    float* moved;                            // [batch][kv_heads][into_pages * page]
+};
+int launch_cache4_move(const Move4& a, hipStream_t s);
+
 // Workgroups of 256 threads of writing and reading, for a kv head: each has the rows whose elements, eight to a thread, fill it.
 inline int cache4_block_rows(const Cache4& c) { return 256 / (c.dim / 8); }
 inline long long cache4_row_blocks(const Cache4& c, const Rows4& r) { return cdiv(r.tokens, cache4_block_rows(c)); }

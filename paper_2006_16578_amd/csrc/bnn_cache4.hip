@@ -13,13 +13,6 @@
 namespace bnn {
 namespace {
 
-// Value of the lane whose number in its group of four differs in the bits of X.
-template <int X>
-__device__ __forceinline__ uint32_t quad_xor(uint32_t v) {
-    constexpr int perm = X == 1 ? 0xB1 : 0x4E;          // lanes 1,0,3,2 / 2,3,0,1
-    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, perm, 0xf, 0xf, true);
-}
-
 struct Place {
     int page, offset;                                   // page < 0: nowhere
 };
@@ -33,26 +26,6 @@ __device__ __forceinline__ Place place_of_row(const Cache4& c, const Rows4& r, i
     p.page = i < 0 || i >= s.rows ? -1 : c4_page(r, c, b, token);
     p.offset = token & (c.page - 1);
     return p;
-}
-
-// Eight elements of a group of 32 that four lanes share: returns the codes, sets the scale's byte.
-__device__ __forceinline__ uint32_t quantise(const float (&x)[8], uint32_t& byte) {
-    uint32_t high = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) high = max(high, __float_as_uint(x[i]) & 0x7fffffffu);
-    high = max(high, quad_xor<1>(high));
-    high = max(high, quad_xor<2>(high));
-    // 1.m 2^(E - 127) <= 6 2^e: e + 127 = E - 2, one more where 1.m > 1.5
-    const int e = (int)(high >> 23) - 2 + ((high & 0x7fffffu) > 0x400000u ? 1 : 0);
-    const int clamped = min(max(e, C4_EXP_MIN), C4_EXP_MAX);
-    byte = high >= 0x7f800000u ? C4_EXP_NAN : (uint32_t)clamped;
-    const float scale = __uint_as_float((uint32_t)clamped << 23);
-    uint32_t codes = 0;
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[0], x[1], scale, 0);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
-    return codes;
 }
 
 __device__ __forceinline__ void dequantise(uint32_t codes, uint32_t byte, float (&x)[8]) {
@@ -75,24 +48,7 @@ __global__ __launch_bounds__(256) void write_kernel(Cache4 c, Rows4 r, const T* 
     float x[8], y[8];
     c4_load8(k + t * k_token + head * k_head + at * 8, x);
     c4_load8(v + t * v_token + head * v_head + at * 8, y);
-    uint8_t* rec = c4_record(c, p.page, head);
-    uint32_t kb, vb;
-    const uint32_t kc = quantise(x, kb), vc = quantise(y, vb);
-    const int row = c.dim / 2 * p.offset + at * 4;
-    *reinterpret_cast<uint32_t*>(rec + row) = kc;
-    *reinterpret_cast<uint32_t*>(rec + c.v_codes + row) = vc;
-    uint32_t bits = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) bits |= (x[i] >= 0.f ? 1u : 0u) << i;
-    bits <<= 8 * (at & 3);
-    bits |= quad_xor<1>(bits);
-    bits |= quad_xor<2>(bits);
-    if ((at & 3) == 0) {
-        const int e = (at >> 2) * c.page + p.offset;
-        rec[c.k_exps + e] = (uint8_t)kb;
-        rec[c.v_exps + e] = (uint8_t)vb;
-        if (c.signs) *reinterpret_cast<uint32_t*>(rec + c.signs + p.offset * (c.dim / 8) + at) = bits;
-    }
+    c4_put(c, c4_record(c, p.page, head), p.offset, at, x, y);
 }
 
 template <class T>

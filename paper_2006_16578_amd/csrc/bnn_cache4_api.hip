@@ -3,7 +3,7 @@
 
 #include <algorithm>
 
-#include "bnn_cache4.h"
+#include "bnn_rotary.h"
 
 using namespace bnn;
 
@@ -98,6 +98,18 @@ AttendPlan4 plan_attend(const Cache4& c, const Rows4& r, int dtype, int group, i
     return p;
 }
 
+int make_rotation(const bnn_rotation* in, Rotation& rot) {
+    if (!in || !in->frequencies || in->pairs < 1 || (in->neighbours != 0 && in->neighbours != 1) || (in->inverse != 0 && in->inverse != 1) || !isfinite(in->magnitude)) return BNN_ERR_INVALID_ARG;
+    if (in->pairs > ROTARY_MAX_PAIRS) return BNN_ERR_UNSUPPORTED;
+    if ((reinterpret_cast<uintptr_t>(in->frequencies) & 7u) || (reinterpret_cast<uintptr_t>(in->positions) & 3u)) return BNN_ERR_ALIGNMENT;
+    rot.frequencies = in->frequencies;
+    rot.positions = in->positions;
+    rot.pairs = in->pairs;
+    rot.magnitude = in->magnitude;
+    rot.sign = in->inverse ? -1.0 : 1.0;
+    return BNN_OK;
+}
+
 int check_heads(const Cache4& c, int heads, int& group) {
     if (heads < 1 || heads % c.kv_heads != 0) return BNN_ERR_INVALID_ARG;
     group = heads / c.kv_heads;
@@ -124,6 +136,40 @@ int bnn_cache4_write(const bnn_cache4* cache, const bnn_cache4_rows* rows, const
     if ((rc = check_elements(k, dtype, k_token, k_head)) != BNN_OK || (rc = check_elements(v, dtype, v_token, v_head)) != BNN_OK) return rc;
     if (cache4_row_blocks(c, r) * 256 >= C4_THREADS) return BNN_ERR_UNSUPPORTED;
     return launch_cache4_write(c, r, k, v, dtype, k_token, k_head, v_token, v_head, static_cast<hipStream_t>(stream));
+}
+
+int bnn_rotary(const void* x, void* out, int dtype, int tokens, int heads, int dim, int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head,
+               const bnn_rotation* rotation, void* stream) {
+    Rotation rot;
+    const int size = element_bytes(dtype);
+    int rc = make_rotation(rotation, rot);
+    if (rc != BNN_OK) return rc;
+    if (size == 0 || tokens < 0 || heads < 0 || dim < 2 * rot.pairs) return BNN_ERR_INVALID_ARG;
+    if (tokens == 0 || heads == 0) return BNN_OK;
+    if (!x || !out || !rot.positions || (out == x && (out_token != x_token || out_head != x_head))) return BNN_ERR_INVALID_ARG;
+    if (dim >= (1 << 20)) return BNN_ERR_UNSUPPORTED;
+    if (reinterpret_cast<uintptr_t>(x) % size || reinterpret_cast<uintptr_t>(out) % size) return BNN_ERR_ALIGNMENT;
+    const int width = rotary_width(size, {rot.pairs, dim - 2 * rot.pairs, x_token, x_head, out_token, out_head}, {x, out});
+    return launch_rotary(x, out, dtype, tokens, heads, dim, x_token, x_head, out_token, out_head, width, rot, rotation->neighbours, static_cast<hipStream_t>(stream));
+}
+
+int bnn_cache4_write_rotary(const bnn_cache4* cache, const bnn_cache4_rows* rows, const bnn_rotation* rotation, const void* q, int64_t q_token, int64_t q_head, int heads, void* q_out,
+                            const void* k, const void* v, int dtype, int64_t k_token, int64_t k_head, int64_t v_token, int64_t v_head, void* stream) {
+    WriteRotary4 a = {};
+    int rc = make_cache(cache, a.c);
+    if (rc != BNN_OK || (rc = make_rows(rows, a.c, a.r)) != BNN_OK || (rc = make_rotation(rotation, a.rot)) != BNN_OK) return rc;
+    if (element_bytes(dtype) == 0 || heads < 0 || 2 * a.rot.pairs > a.c.dim) return BNN_ERR_INVALID_ARG;
+    if (a.r.tokens == 0) return BNN_OK;
+    if ((rc = check_elements(k, dtype, k_token, k_head)) != BNN_OK || (rc = check_elements(v, dtype, v_token, v_head)) != BNN_OK) return rc;
+    if (heads > 0 && ((rc = check_elements(q, dtype, q_token, q_head)) != BNN_OK || (rc = check_elements(q_out, dtype, 0, 0)) != BNN_OK)) return rc;
+    if (heads > 0 && q_out == q && ((heads > 1 && q_head != a.c.dim) || (a.r.tokens > 1 && q_token != (int64_t)heads * a.c.dim))) return BNN_ERR_INVALID_ARG;
+    if (heads > (1 << 30)) return BNN_ERR_UNSUPPORTED;
+    a.q = q; a.q_token = q_token; a.q_head = q_head; a.q_out = q_out; a.heads = heads;
+    a.k = k; a.k_token = k_token; a.k_head = k_head;
+    a.v = v; a.v_token = v_token; a.v_head = v_head;
+    int width = 8;
+    while (a.rot.pairs % width != 0) width /= 2;             // (pointers and distances are multiples of 16 bytes, head_dim of 32)
+    return launch_cache4_write_rotary(a, dtype, rotation->neighbours, width, static_cast<hipStream_t>(stream));
 }
 
 int bnn_cache4_read(const bnn_cache4* cache, const bnn_cache4_rows* rows, void* k, void* v, int dtype, void* stream) {
@@ -211,6 +257,64 @@ int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
         case 192: return launch_cache4_attend192(a, dtype, p.rows, s);
         default: return launch_cache4_attend256(a, dtype, p.rows, s);
     }
+}
+
+int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads, const float* lse,
+                     float scale, int causal, int window, const float* previous, float decay, float* weights, int64_t width, void* stream) {
+    Weigh4 a = {};
+    int rc = make_cache(cache, a.c);
+    if (rc != BNN_OK || (rc = make_rows(rows, a.c, a.r)) != BNN_OK || (rc = check_heads(a.c, heads, a.group)) != BNN_OK) return rc;
+    if (element_bytes(dtype) == 0 || !(scale > 0.f) || !isfinite(scale) || window < 0 || (window > 0 && !causal) || !isfinite(decay)) return BNN_ERR_INVALID_ARG;
+    if (a.r.tokens == 0) return BNN_OK;
+    if (!weights || !lse || width < ((long long)a.r.table_pages << a.c.page_shift)) return BNN_ERR_INVALID_ARG;
+    if ((rc = check_elements(q, dtype, q_token, q_head)) != BNN_OK) return rc;
+    if ((reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(previous) & 3u) || (reinterpret_cast<uintptr_t>(weights) & 3u)) return BNN_ERR_ALIGNMENT;
+    if ((long long)a.r.tokens * a.group >= (1LL << 30) || ((long long)a.r.table_pages << a.c.page_shift) > (1LL << 30)) return BNN_ERR_UNSUPPORTED;
+    a.q = q; a.q_token = q_token; a.q_head = q_head;
+    a.div_group = make_fastdiv((uint32_t)a.group);
+    a.div_heads = make_fastdiv((uint32_t)a.c.kv_heads);
+    a.scale = scale;
+    a.causal = causal ? 1 : 0;
+    a.window = window;
+    a.lse = lse; a.previous = previous; a.decay = decay; a.out = weights; a.width = width;
+    return launch_cache4_weigh(a, dtype, static_cast<hipStream_t>(stream));
+}
+
+int bnn_cache4_heaviest(const bnn_cache4* cache, const int32_t* table, const int32_t* lens, int batch, int table_pages, const float* weights, int64_t width,
+                        int keep, int first, int last, int32_t* tokens, int32_t* kept, void* stream) {
+    Heaviest4 a = {};
+    const int rc = make_cache(cache, a.c);
+    if (rc != BNN_OK) return rc;
+    if (batch < 0 || table_pages < 0 || keep < 1 || first < 0 || last < 0 || (long long)first + last > keep) return BNN_ERR_INVALID_ARG;
+    if (batch == 0) return BNN_OK;
+    if (table_pages < 1 || !table || !lens || !weights || !tokens || !kept || width < ((long long)table_pages << a.c.page_shift)) return BNN_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(table) & 3u) || (reinterpret_cast<uintptr_t>(lens) & 3u) || (reinterpret_cast<uintptr_t>(weights) & 3u) ||
+        (reinterpret_cast<uintptr_t>(tokens) & 3u) || (reinterpret_cast<uintptr_t>(kept) & 3u))
+        return BNN_ERR_ALIGNMENT;
+    if (batch >= C4_THREADS / 1024 || ((long long)table_pages << a.c.page_shift) > (1LL << 30)) return BNN_ERR_UNSUPPORTED;
+    a.weights = weights; a.width = width;
+    a.table = table; a.lens = lens; a.batch = batch; a.table_pages = table_pages;
+    a.keep = keep; a.first = first; a.last = last;
+    a.tokens = tokens; a.kept = kept;
+    return launch_cache4_heaviest(a, static_cast<hipStream_t>(stream));
+}
+
+int bnn_cache4_move(const bnn_cache4* cache, const int32_t* tokens, int keep, const int32_t* table, int table_pages, const int32_t* into, int into_pages, int batch,
+                    const float* weights, int64_t width, float* moved, void* stream) {
+    Move4 a = {};
+    const int rc = make_cache(cache, a.c);
+    if (rc != BNN_OK) return rc;
+    if (batch < 0 || table_pages < 0 || into_pages < 0 || keep < 1 || (weights ? width < 1 || !moved : moved != nullptr)) return BNN_ERR_INVALID_ARG;
+    if (batch == 0 || into_pages == 0) return BNN_OK;
+    if (table_pages < 1 || !tokens || !table || !into) return BNN_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(table) & 3u) || (reinterpret_cast<uintptr_t>(into) & 3u) || (reinterpret_cast<uintptr_t>(weights) & 3u) ||
+        (reinterpret_cast<uintptr_t>(tokens) & 3u) || (reinterpret_cast<uintptr_t>(moved) & 3u))
+        return BNN_ERR_ALIGNMENT;
+    if (((long long)table_pages << a.c.page_shift) > (1LL << 30) || ((long long)into_pages << a.c.page_shift) > (1LL << 30)) return BNN_ERR_UNSUPPORTED;
+    a.tokens = tokens; a.keep = keep;
+    a.table = table; a.into = into; a.batch = batch; a.table_pages = table_pages; a.into_pages = into_pages;
+    a.weights = weights; a.width = width; a.moved = moved;
+    return launch_cache4_move(a, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

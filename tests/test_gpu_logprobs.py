@@ -1,0 +1,193 @@
+"""GPU: log probabilities of tokens against the oracle in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import decoding as od
+
+pytestmark = pytest.mark.gpu
+
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16, "i32": torch.int32}
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def bnn():
+    import paper_2006_16578_amd as b
+    b.load()
+    return b
+
+
+def logits_of(rng, rows, cols, dtype, spread=3.0):
+    if dtype == "i32":
+        return torch.from_numpy(np.rint(rng.standard_normal((rows, cols)) * 60).astype(np.int32)).cuda()
+    return torch.from_numpy(rng.standard_normal((rows, cols)) * spread).to(TYPES[dtype]).cuda()
+
+
+def check(bnn, x, targets, scale=1.0, top=0, **kw):
+    """Bounds, with u = 2^-24 and every row's z = scale x, M its largest: an exponent (x - m) scale / log 2 rounds three times (and the scale's own constant), so a term is off by
+    4 u |z - M| and 2 u of the exponential; with terms as weights that is 4 u log(cols) at most.  Sums add up 64 terms, 8 levels and the pieces: 128 u.  The logarithm rounds twice, u log S each.  What is
+    then added rounds once, relative to itself.  The entropy is a sum of two such terms, each at most log(cols)."""
+    scale = float(np.float32(scale))
+    want = od.token_logprobs(x.double().cpu().numpy(), None if targets is None else targets.cpu().numpy(), scale, top)
+    got = bnn.token_logprobs(x, targets, scale=scale, top=top, **kw)
+    rows, cols = x.shape
+    assert (got.logprobs is None) == (targets is None)
+    n = np.log(max(cols, 2))
+    sums = (128 + 8 * n) * U
+    for name, w, g in zip(("logprobs", "entropy", "lse", "top_logprobs"), want, got):
+        if g is None:
+            continue
+        assert g.dtype == torch.float32
+        g = g.double().cpu().numpy()
+        assert g.shape == w.shape
+        w32 = np.abs(np.where(np.isfinite(w), w, 0))
+        bound = sums * (1 + n) if name == "entropy" else sums + 4 * U * (w32 + n)
+        with np.errstate(invalid="ignore"):
+            same = (np.isnan(w) & np.isnan(g)) | (w == g) | (np.abs(g - w) <= bound)
+        assert same.all(), (name, np.argwhere(~same)[:5], g[~same][:5], w[~same][:5])
+    assert got.top_tokens.dtype == torch.int32 and (got.top_tokens.cpu().numpy() == want[4]).all()
+    return got
+
+
+def tokens_for(rng, rows, cols):
+    return torch.from_numpy(rng.integers(0, cols, rows)).cuda()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16", "i32"])
+@pytest.mark.parametrize("rows,cols,top", [(1, 1, 1), (3, 2, 2), (5, 7, 0), (2, 63, 5), (4, 300, 20), (3, 2047, 64), (2, 2049, 1), (7, 5003, 5), (2, 16391, 20), (1, 50001, 64), (300, 129, 3)])
+def test_logprobs(bnn, dtype, rows, cols, top):
+    rng = np.random.default_rng(rows * cols + top)
+    scale = 1 / 45 if dtype == "i32" else 1.0
+    check(bnn, logits_of(rng, rows, cols, dtype), tokens_for(rng, rows, cols), scale, top)
+
+
+@pytest.mark.parametrize("dtype,cols", [("f32", 8200), ("bf16", 16393), ("i32", 8201)])
+def test_long_pieces(bnn, dtype, cols):
+    """Rows enough for the long pieces: 600 rows and two pieces each."""
+    rng = np.random.default_rng(cols)
+    check(bnn, logits_of(rng, 600, cols, dtype), tokens_for(rng, 600, cols), 1 / 45 if dtype == "i32" else 0.7, 9)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_distances_and_alignments(bnn, dtype):
+    rng = np.random.default_rng(3)
+    whole = logits_of(rng, 9, 4200, dtype)
+    t = tokens_for(rng, 9, 4001)
+    for first in (0, 1, 3, 8):
+        check(bnn, whole[:, first:first + 4001], t, top=7)
+    check(bnn, whole[::2, 5:4006], t[::2].contiguous(), top=7)
+    check(bnn, whole[:1].expand(9, 4200)[:, :4001], t, top=7)        # one row for all
+    check(bnn, whole[2:3], t[:1], top=3)
+
+
+def test_no_targets_and_targets_outside(bnn):
+    rng = np.random.default_rng(4)
+    x = logits_of(rng, 6, 500, "bf16")
+    check(bnn, x, None, top=4)
+    got = check(bnn, x, torch.tensor([-1, 500, 499, 0, -100, 1 << 40], device="cuda"), top=0)
+    assert got.logprobs[0] == 0 and got.logprobs[1] == 0 and got.logprobs[4] == 0 and got.logprobs[5] == 0 and got.top_tokens.shape == (6, 0)
+    empty = bnn.token_logprobs(x[:0], t := torch.empty(0, dtype=torch.int64, device="cuda"), top=3)
+    assert empty.logprobs.shape == (0,) and empty.top_tokens.shape == (0, 3) and t.numel() == 0
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_masked_columns(bnn, dtype):
+    """Rows with few columns left, one, none; rows that hold a NaN or +infinity; a target that is masked."""
+    rng = np.random.default_rng(5)
+    rows, cols = 12, 9001
+    x = logits_of(rng, rows, cols, dtype)
+    for r, left in enumerate((8000, 100, 20, 5, 1, 0)):
+        ruled = np.ones(cols, bool)
+        ruled[rng.choice(cols, left, replace=False)] = False
+        x[r, torch.from_numpy(ruled).cuda()] = float("-inf")
+    x[6, 17], x[7, 9000], x[8] = float("nan"), float("inf"), float("nan")
+    x[9, :] = float("inf")
+    x[10, 5], x[10, 6] = float("inf"), float("nan")
+    targets = tokens_for(rng, rows, cols)
+    targets[3] = int((x[3] > -1e30).nonzero()[0])
+    got = check(bnn, x, targets, top=20)
+    assert torch.isnan(got.entropy[5:11]).all() and (got.top_tokens[5:11] == -1).all() and got.lse[5] == float("-inf") and torch.isnan(got.lse[6:11]).all()
+    check(bnn, x, targets, top=64)
+    lowest = x.clone()
+    lowest[torch.isinf(x) & (x < 0)] = torch.finfo(x.dtype).min      # masks of the type's lowest value
+    check(bnn, lowest, targets, top=20)
+
+
+@pytest.mark.parametrize("cols,top", [(700, 64), (2048, 5), (20000, 20), (70000, 33)])
+def test_ties_go_to_the_lower_column(bnn, cols, top):
+    """All equal; two values; blocks of equal ones; descending and ascending rows; all the best within one thread's elements; both zeros."""
+    rng = np.random.default_rng(cols)
+    x = torch.zeros(9, cols, device="cuda")
+    x[1] = torch.from_numpy(rng.integers(0, 2, cols)).cuda()
+    x[2] = torch.from_numpy(rng.integers(0, 5, cols)).cuda() * (torch.arange(cols, device="cuda") > cols // 2)
+    x[3] = torch.linspace(5, -5, cols, device="cuda")
+    x[4] = torch.linspace(-5, 5, cols, device="cuda")
+    x[5, 0::2048] = 3.0
+    x[5, 1::1024] = 2.0
+    x[6, 1::2] = -0.0
+    x[7, -top:] = 1.0
+    x[8, cols // 3:] = float("-inf")
+    t = tokens_for(rng, 9, cols // 3)
+    for dtype in (torch.float32, torch.bfloat16):
+        check(bnn, x.to(dtype), t, top=top)
+    check(bnn, (x[:7] * 3).round().int(), t[:7].contiguous(), 0.5, top=top)
+
+
+def test_scales(bnn):
+    rng = np.random.default_rng(6)
+    x = logits_of(rng, 5, 3001, "f32")
+    t = tokens_for(rng, 5, 3001)
+    for scale in (1e-30, 0.01, 50.0, 1e6):
+        check(bnn, x, t, scale, top=5)
+    check(bnn, x * 1e30, t, 1e-30, top=5)
+    check(bnn, x + 1000, t, top=5)
+    # sums as bmm gives them
+    big = torch.from_numpy(rng.integers(-(1 << 20), 1 << 20, (4, 777)).astype(np.int32)).cuda()
+    check(bnn, big, t[:4].contiguous() % 777, 2.0 ** -14, top=7)
+
+
+def test_the_same_again(bnn):
+    """Bit for bit, whatever order workgroups run in; through a caller's workspace that holds anything."""
+    rng = np.random.default_rng(7)
+    x, t = logits_of(rng, 40, 50001, "bf16"), tokens_for(rng, 40, 50001)
+    first = bnn.token_logprobs(x, t, top=20)
+    need = bnn.load().bnn_token_logprobs_workspace_bytes(40, 50001, 1, 20)
+    for fill in (0, 255):
+        again = bnn.token_logprobs(x, t, top=20, workspace=torch.full((need,), fill, dtype=torch.uint8, device="cuda"))
+        for a, b in zip(first, again):
+            assert torch.equal(a, b)
+    with pytest.raises(bnn.BnnError):
+        bnn.token_logprobs(x, t, top=20, workspace=torch.empty(need - 1, dtype=torch.uint8, device="cuda"))
+
+
+def test_graph_and_stream(bnn):
+    x, t = torch.randn(6, 30011, device="cuda"), torch.randint(0, 30011, (6,), device="cuda")
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        warm = bnn.token_logprobs(x, t, top=5)
+    torch.cuda.current_stream().wait_stream(stream)
+    for a, b in zip(warm, bnn.token_logprobs(x, t, top=5)):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = bnn.token_logprobs(x, t, top=5)
+    for _ in range(5):
+        x.normal_()
+        t.random_(0, 30011)
+        graph.replay()
+        want = bnn.token_logprobs(x, t, top=5)
+        torch.cuda.synchronize()
+        for a, b in zip(out, want):
+            assert torch.equal(a, b)
+
+
+def test_refusals(bnn):
+    x, t = torch.randn(3, 100, device="cuda"), torch.zeros(3, dtype=torch.int64, device="cuda")
+    for error, args, kw in ((TypeError, (x.cpu(), t), {}), (TypeError, (x.double(), t), {}), (TypeError, (x, t.int()), {}), (TypeError, (x, t.cpu()), {}), (ValueError, (x, t[:2]), {}),
+                            (ValueError, (x.t(), None), {}), (ValueError, (x[0], t), {}), (ValueError, (x[:, :0], t), {}), (bnn.BnnError, (x, t), dict(top=-1)),
+                            (bnn.BnnError, (x, t), dict(top=65)), (bnn.BnnError, (x[:, :4], t), dict(top=5)), (bnn.BnnError, (x, t), dict(scale=0.0)),
+                            (bnn.BnnError, (x, t), dict(scale=-1.0)), (bnn.BnnError, (x, t), dict(scale=float("nan"))), (bnn.BnnError, (x, t), dict(scale=float("inf")))):
+        with pytest.raises(error):
+            bnn.token_logprobs(*args, **kw)

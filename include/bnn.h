@@ -497,10 +497,13 @@ int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
  *   weights[b][h][j] = decay * previous[b][h][j] (0 for this call's tokens, and with previous == NULL) + the sum, over the rows that see j and the query heads of kv head h, of
  *   exp(scale * q . k_j - lse).
  * Weights from lens[b] on, and of tokens past the table's end, are left as they are.  previous may be weights.  What a row sees is as in bnn_cache4_attend without blocks, and lse [tokens][heads]
- * is what that gave for the same q, scale, causal and window; a row with -infinity there adds nothing, and one whose query holds a NaN or an infinity makes the weights of what it sees NaN.
- * Tokens on no page get nothing.  Products are of bf16 terms, queries exactly, with fp32 sums; sums are fp32 and in the same order for the same arguments.  decay finite. */
+ * is what that gave for the same q, scale, causal and window; a row with -infinity there adds nothing, and one with NaN, as it has for a query that holds a NaN or an infinity, makes the weights of what it sees NaN.
+ * Tokens on no page get nothing.  Products are of bf16 terms, queries exactly, with fp32 sums; sums are fp32 and in the same order for the same arguments.
+ * scale > 0; scale * log2(e) and 1 / scale finite, and |lse| / scale below 2^127.  decay finite.  BNN_ERR_UNSUPPORTED: tokens * heads / kv_heads from 2^30 on, 2^24 workgroups and more (one has 256 keys or more). */
+size_t bnn_cache4_weigh_workspace_bytes(const bnn_cache4* cache, const bnn_cache4_rows* rows, int dtype, int heads);
 int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads, const float* lse,
-                     float scale, int causal, int window, const float* previous, float decay, float* weights, int64_t width, void* stream);
+                     float scale, int causal, int window, const float* previous, float decay, float* weights, int64_t width,
+                     void* workspace, size_t workspace_bytes, void* stream);
 /* tokens [batch][kv_heads][keep]: of the tokens of every sequence that lie on a page, all if they are `keep` at most, else the first `first` and last `last` (of the numbers 0 .. lens[b] - 1)
  * and of the others those with the largest weights; ascending, the rest -1.  Ties go to the lower token; NaN is below every number.  kept [batch]: how many.  first + last <= keep. */
 int bnn_cache4_heaviest(const bnn_cache4* cache, const int32_t* table, const int32_t* lens, int batch, int table_pages, const float* weights, int64_t width,

@@ -49,24 +49,28 @@ def weigh(cache, q, lse, table, lens, start, scale, out, causal=True, window=0, 
         if previous is not None:
             old = min(max(new, 0), n)
             out[b, :, :old] = decay * previous[b, :, :old]
-    keys = {}
+    values = {}
     for t, b, token in rows_of(lens, start, tokens):
-        for j in range(min(max(int(lens[b]), 0), room)):
-            if (causal and j > token) or (window and j <= token - window):
-                continue
-            for h in range(cache.heads):
-                if (b, h, j) not in keys:
-                    record = cache.record(table, b, j, h)
-                    keys[b, h, j] = None if record is None else record.get("k", j % cache.page)
-                k = keys[b, h, j]
-                if k is None:
-                    continue
-                for g in range(group):
-                    with np.errstate(all="ignore"):
-                        s = scale * (q[t, h * group + g] @ k)
-                        w = 0.0 if lse[t, h * group + g] == -np.inf else np.exp(s - lse[t, h * group + g])
-                    out[b, h, j] += w
-                    spread[b, h, j] += w * (scale * (np.abs(q[t, h * group + g]) @ np.abs(k)) + abs(lse[t, h * group + g]))
+        n = min(max(int(lens[b]), 0), room)
+        at = np.arange(n)
+        seen = np.ones(n, bool)
+        if causal:
+            seen &= at <= token
+        if window:
+            seen &= at > token - window
+        for h in range(cache.heads):
+            if (b, h) not in values:
+                records = [cache.record(table, b, j, h) for j in range(n)]
+                there = np.array([r is not None for r in records], bool)
+                values[b, h] = there, np.array([r.get("k", j % cache.page) if r is not None else np.zeros(cache.dim) for j, r in enumerate(records)]).reshape(n, cache.dim)
+            there, k = values[b, h]
+            use = np.flatnonzero(seen & there)
+            for g in range(group):
+                x, log = q[t, h * group + g], lse[t, h * group + g]
+                with np.errstate(all="ignore"):
+                    w = np.zeros(len(use)) if log == -np.inf else np.exp(scale * (k[use] @ x) - log)
+                    out[b, h, use] += w
+                    spread[b, h, use] += w * (scale * (np.abs(k[use]) @ np.abs(x)) + abs(log))
     return spread
 
 

@@ -36,7 +36,7 @@ EXPORTS = ["bnn_status_string", "bnn_version", "bnn_bmm_kernel_name", "bnn_bconv
            "bnn_net_add_conv", "bnn_net_add_pool", "bnn_net_add_block", "bnn_net_add_head_f32", "bnn_net_workspace_bytes",
            "bnn_net_forward", "bnn_net_forward_static", "bnn_static_workspace_init", "bnn_net_forward_persistent", "bnn_net_persistent_status", "bnn_net_fc_run", "bnn_net_layer_bits",
            "bnn_rotary", "bnn_cache4_record_bytes", "bnn_cache4_write", "bnn_cache4_write_rotary", "bnn_cache4_read", "bnn_cache4_select_workspace_bytes", "bnn_cache4_select",
-           "bnn_cache4_attend_workspace_bytes", "bnn_cache4_attend", "bnn_cache4_weigh", "bnn_cache4_heaviest", "bnn_cache4_move",
+           "bnn_cache4_attend_workspace_bytes", "bnn_cache4_attend", "bnn_cache4_weigh_workspace_bytes", "bnn_cache4_weigh", "bnn_cache4_heaviest", "bnn_cache4_move",
            "bnn_token_logprobs_workspace_bytes", "bnn_token_logprobs"]
 
 
@@ -76,6 +76,7 @@ def load() -> ctypes.CDLL:
         lib.bnn_cache4_record_bytes.restype = ctypes.c_size_t
         lib.bnn_cache4_select_workspace_bytes.restype = ctypes.c_size_t
         lib.bnn_cache4_attend_workspace_bytes.restype = ctypes.c_size_t
+        lib.bnn_cache4_weigh_workspace_bytes.restype = ctypes.c_size_t
         lib.bnn_token_logprobs_workspace_bytes.restype = ctypes.c_size_t
         for name in EXPORTS:
             getattr(lib, name)          # fail loudly on a missing export
@@ -1069,7 +1070,8 @@ class Cache4:
             raise ValueError("%s must be on the cache's device" % name)
         return weights
 
-    def weigh(self, q, lse, table, lens, start=None, scale: float | None = None, causal: bool = True, window: int = 0, previous=None, decay: float = 1.0, out=None):
+    def weigh(self, q, lse, table, lens, start=None, scale: float | None = None, causal: bool = True, window: int = 0, previous=None, decay: float = 1.0, out=None,
+              workspace=None):
         """The attention weight of every cached token: decay * previous plus what the rows of q give it, with the lse that attend() of the same arguments (without blocks)
         returned -> fp32 [batch][kv_heads][tokens of the table].  Tokens of this call have no previous weight.  What lies behind a sequence's end is not written (and undefined in an
         output that is made here).  out may be previous."""
@@ -1084,9 +1086,15 @@ class Cache4:
         self._weights(out, batch, room, "out")
         if previous is not None and self._weights(previous, batch, room, "previous").shape != out.shape:
             raise ValueError("previous and out must agree in shape")
+        if workspace is None:
+            need = int(load().bnn_cache4_weigh_workspace_bytes(self._struct(), ctypes.byref(rows), code, q.shape[1]))
+            workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        else:
+            self._workspace(workspace)
         with _on(q):
             _check(load().bnn_cache4_weigh(self._struct(), ctypes.byref(rows), _ptr(q), code, qt, qh, q.shape[1], _ptr(lse), ctypes.c_float(scale), int(bool(causal)), int(window),
-                                           _ptr(previous), ctypes.c_float(decay), _ptr(out), ctypes.c_int64(out.shape[2]), _stream(q)), "bnn_cache4_weigh")
+                                           _ptr(previous), ctypes.c_float(decay), _ptr(out), ctypes.c_int64(out.shape[2]), _ptr(workspace),
+                                           ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream(q)), "bnn_cache4_weigh")
         return out
 
     def heaviest(self, weights, table, lens, keep: int, first: int = 0, last: int = 0):

@@ -199,6 +199,9 @@ __device__ __forceinline__ void c4_put(const Cache4& c, uint8_t* rec, int offset
 // The scale that a byte stands for, for the conversion instructions: with the NaN byte's (the bits of an infinity) they give NaN for every code, 0 included.
 __device__ __forceinline__ float c4_scale(uint32_t byte) { return __uint_as_float(byte << 23); }
 
+// bf16 terms of a query or weight of a type.
+constexpr int cache4_terms(int dtype) { return dtype == BNN_BF16 ? 1 : dtype == BNN_F16 ? 2 : 3; }
+
 // The attention call as the kernels see it.
 struct Attend4 {
     Cache4 c;
@@ -233,7 +236,6 @@ struct AttendPlan4 {
 
 // Groups of 16 rows that a wave carries, by what fits 256 registers: per group a lane keeps D / 4 of sums, D / 8 of every term of Q, and scores and weights.  (With twice as
 // many, at one wave a SIMD, nothing runs while a wave waits: two prompts of 4096 tokens 631 us instead of 416.)
-constexpr int cache4_terms(int dtype) { return dtype == BNN_BF16 ? 1 : dtype == BNN_F16 ? 2 : 3; }
 constexpr int cache4_qtiles(int dim, int dtype) {            // a workgroup's rows, each wave has all
     return 2 * (dim / 4 + cache4_terms(dtype) * (dim / 8) + 4 * cache4_terms(dtype)) < 144 ? 2 : 1;
 }
@@ -274,18 +276,28 @@ struct Weigh4 {
     const void* q;
     long long q_token, q_head;
     int group;
-    FastDiv div_group;
-    float scale;
+    FastDiv div_group, div_heads;
+    float scale2, unscale;                   // scale / log 2, 1 / scale
     int causal, window;
     const float* lse;                        // [tokens][heads]
     const float* previous;                   // [batch][kv_heads][width], or nullptr; may be out
     float* out;
     float decay;
     long long width;
-    int key_tiles;                           // of a sequence
-    FastDiv div_heads, div_key_tiles;
+    int parts;                               // of a launch for few rows: that share a sequence's keys; for many: that share the rows of a tile of keys
+    FastDiv div_parts, div_batch;
+    float* partial;                          // [batch][kv_heads][parts][width4], with several parts of the rows
+    long long width4;                        // tokens that the table has room for
 };
-int launch_cache4_weigh(Weigh4 a, int dtype, hipStream_t s);
+// How such a call is cut up.  row_tiles: tiles of 16 rows that a wave carries, 0: the kernel for many rows.
+struct WeighPlan4 {
+    int row_tiles, parts;
+    long long workgroups;
+    size_t workspace_bytes;
+};
+constexpr int cache4_weigh_tiles(int dim) { return dim >= 192 ? 2 : 4; }          // tiles of 16 keys that a wave of that kernel keeps
+constexpr bool cache4_weigh_two(int dim, int dtype) { return dim / 32 * cache4_terms(dtype) <= 6; }       // whether two tiles of rows fit a wave's registers
+int launch_cache4_weigh(const Weigh4& a, const WeighPlan4& p, int dtype, hipStream_t s);
 
 // The choice of the tokens to keep, and moving them.
 struct Heaviest4 {

@@ -98,6 +98,29 @@ AttendPlan4 plan_attend(const Cache4& c, const Rows4& r, int dtype, int group, i
     return p;
 }
 
+bool weigh_takes(const Cache4& c, const Rows4& r, int group) {
+    return (long long)r.tokens * group < (1LL << 30) && ((long long)r.table_pages << c.page_shift) <= (1LL << 30);
+}
+
+// How weights are added up.  By the mean of rows over the batch, as attention is: up to 32 rows the kernel whose waves carry them, in as many workgroups as keep the chip busy with their loads (4096); else the one whose
+// waves carry keys, with the rows of a tile of keys cut into parts until there are 2048 workgroups, 256 rows at least.
+// near_rows: whether that kernel's offsets, of 2304 rows in 32 bits, reach (products of 24 bits); the other serves any distances.
+WeighPlan4 plan_weigh(const Cache4& c, const Rows4& r, int dtype, int group, bool near_rows) {
+    WeighPlan4 p = {};
+    const long long rows = cdiv((long long)r.tokens * group, r.batch), room = (long long)r.table_pages << c.page_shift, sequences = (long long)r.batch * c.kv_heads;
+    if (rows <= 32 || !near_rows) {
+        p.row_tiles = rows > 16 && cache4_weigh_two(c.dim, dtype) ? 2 : 1;
+        p.parts = (int)std::max(1LL, std::min(cdiv(4096, sequences), cdiv(room, 256)));
+        p.workgroups = sequences * p.parts;
+        return p;
+    }
+    const long long units = sequences * cdiv(room, 64 * cache4_weigh_tiles(c.dim));
+    p.parts = (int)std::max(1LL, std::min(cdiv(2048, units), cdiv(rows, 256)));
+    p.workgroups = units * p.parts;
+    if (p.parts > 1) p.workspace_bytes = (size_t)sequences * p.parts * room * sizeof(float);
+    return p;
+}
+
 int make_rotation(const bnn_rotation* in, Rotation& rot) {
     if (!in || !in->frequencies || in->pairs < 1 || (in->neighbours != 0 && in->neighbours != 1) || (in->inverse != 0 && in->inverse != 1) || !isfinite(in->magnitude)) return BNN_ERR_INVALID_ARG;
     if (in->pairs > ROTARY_MAX_PAIRS) return BNN_ERR_UNSUPPORTED;
@@ -259,25 +282,46 @@ int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
     }
 }
 
+size_t bnn_cache4_weigh_workspace_bytes(const bnn_cache4* cache, const bnn_cache4_rows* rows, int dtype, int heads) {
+    Cache4 c;
+    Rows4 r;
+    int group;
+    if (make_cache(cache, c) != BNN_OK || make_rows(rows, c, r) != BNN_OK || check_heads(c, heads, group) != BNN_OK || element_bytes(dtype) == 0) return 0;
+    return r.tokens == 0 || !weigh_takes(c, r, group) ? 0 : plan_weigh(c, r, dtype, group, true).workspace_bytes;
+}
+
 int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads, const float* lse,
-                     float scale, int causal, int window, const float* previous, float decay, float* weights, int64_t width, void* stream) {
+                     float scale, int causal, int window, const float* previous, float decay, float* weights, int64_t width, void* workspace, size_t workspace_bytes, void* stream) {
     Weigh4 a = {};
     int rc = make_cache(cache, a.c);
     if (rc != BNN_OK || (rc = make_rows(rows, a.c, a.r)) != BNN_OK || (rc = check_heads(a.c, heads, a.group)) != BNN_OK) return rc;
-    if (element_bytes(dtype) == 0 || !(scale > 0.f) || !isfinite(scale) || window < 0 || (window > 0 && !causal) || !isfinite(decay)) return BNN_ERR_INVALID_ARG;
+    a.scale2 = scale * 1.4426950408889634f;
+    a.unscale = 1.f / scale;
+    if (element_bytes(dtype) == 0 || !(scale > 0.f) || !isfinite(a.scale2) || !isfinite(a.unscale) || window < 0 || (window > 0 && !causal) || !isfinite(decay)) return BNN_ERR_INVALID_ARG;
     if (a.r.tokens == 0) return BNN_OK;
     if (!weights || !lse || width < ((long long)a.r.table_pages << a.c.page_shift)) return BNN_ERR_INVALID_ARG;
     if ((rc = check_elements(q, dtype, q_token, q_head)) != BNN_OK) return rc;
     if ((reinterpret_cast<uintptr_t>(lse) & 3u) || (reinterpret_cast<uintptr_t>(previous) & 3u) || (reinterpret_cast<uintptr_t>(weights) & 3u)) return BNN_ERR_ALIGNMENT;
-    if ((long long)a.r.tokens * a.group >= (1LL << 30) || ((long long)a.r.table_pages << a.c.page_shift) > (1LL << 30)) return BNN_ERR_UNSUPPORTED;
+    if (!weigh_takes(a.c, a.r, a.group)) return BNN_ERR_UNSUPPORTED;
+    const long long far = 1LL << 24;
+    const bool near_rows = q_token >= 0 && q_head >= 0 && q_token < far && q_head < far && a.group < far &&
+                           ((2304 / a.group + 2) * q_token + a.group * q_head + a.c.dim) * element_bytes(dtype) < (1LL << 32);
+    const WeighPlan4 p = plan_weigh(a.c, a.r, dtype, a.group, near_rows);
+    if (p.workgroups >= C4_THREADS / 256) return BNN_ERR_UNSUPPORTED;
+    if (p.workspace_bytes != 0 && (!workspace || workspace_bytes < p.workspace_bytes)) return BNN_ERR_WORKSPACE;
+    if (p.workspace_bytes != 0 && !aligned16(workspace)) return BNN_ERR_ALIGNMENT;
     a.q = q; a.q_token = q_token; a.q_head = q_head;
     a.div_group = make_fastdiv((uint32_t)a.group);
     a.div_heads = make_fastdiv((uint32_t)a.c.kv_heads);
-    a.scale = scale;
     a.causal = causal ? 1 : 0;
     a.window = window;
     a.lse = lse; a.previous = previous; a.decay = decay; a.out = weights; a.width = width;
-    return launch_cache4_weigh(a, dtype, static_cast<hipStream_t>(stream));
+    a.parts = p.parts;
+    a.div_parts = make_fastdiv((uint32_t)p.parts);
+    a.div_batch = make_fastdiv((uint32_t)a.r.batch);
+    a.partial = static_cast<float*>(workspace);
+    a.width4 = (long long)a.r.table_pages << a.c.page_shift;
+    return launch_cache4_weigh(a, p, dtype, static_cast<hipStream_t>(stream));
 }
 
 int bnn_cache4_heaviest(const bnn_cache4* cache, const int32_t* table, const int32_t* lens, int batch, int table_pages, const float* weights, int64_t width,

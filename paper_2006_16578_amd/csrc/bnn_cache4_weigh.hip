@@ -1,128 +1,459 @@
 // The attention weight that every cached token gets: w[key] = sum over rows and query heads of exp(scale * q . k - lse), with the logarithms that attention gave.
 //
 // Queries are the rows of the products, keys their columns: S [rows][keys] = Q K^T (v_mfma_f32_16x16x32_bf16).  A lane then holds, of 16 rows, the scores of ONE key at four of them, so the
-// sum over rows stays in a lane until the end, where the four lanes of a key add up.  A wave keeps 16 * KT keys as finished operands in registers and passes over the rows that see one of
-// them; nothing is exchanged between waves, and no sum depends on the order in which workgroups run.
+// sum over rows stays in a lane until the end, where the four lanes of a key add up.  The products' sums begin at -lse / scale, so that a weight is 2^(sum * scale / log 2): one multiplication, one
+// exponential, one addition a score.  No sum depends on the order in which workgroups run.
 #include "bnn_cache4_attend.h"
 
 namespace bnn {
 namespace {
 
-template <int D, int DTYPE, int KT>
+// What a row's sums begin with: -lse / scale, and -infinity (a weight of 0) for no row and for one that saw nothing.
+__device__ __forceinline__ float weigh_origin(const Weigh4& a, const Sequence4& s, int head, int row, int rows) {
+    const int token = fast_div(row, a.div_group), g = row - token * a.group;
+    const float lse = row < rows ? a.lse[(long long)(s.first + token) * a.c.kv_heads * a.group + head * a.group + g] : -__builtin_inff();
+    return lse == -__builtin_inff() ? lse : -lse * a.unscale;
+}
+
+// Whether the row (counted over tokens and heads of the group) sees the key.  (A row before token 0 sees nothing; differences stay within 32 bits.)
+__device__ __forceinline__ bool weigh_sees(const Weigh4& a, int base, int row, int key) {
+    const int pos = base + fast_div(row, a.div_group);
+    return (!a.causal || key <= pos) && (a.window == 0 || pos - key < a.window);
+}
+
+// A product of numbers below 2^24, at full rate.
+__device__ __forceinline__ uint32_t times24(uint32_t x, uint32_t y) {
+    uint32_t z;
+    asm("v_mul_u32_u24 %0, %1, %2" : "=v"(z) : "s"(y), "v"(x));
+    return z;
+}
+
+// Rows [first, last) of a sequence, counted over (token, head of the group), whose token sees one of the keys key0 .. key1; all of them for every row if `all`.
+struct Rows4Range {
+    int first, last;
+};
+__device__ __forceinline__ Rows4Range weigh_rows(const Weigh4& a, const Sequence4& s, int base, int key0, int key1) {
+    const int t0 = a.causal ? min(max(key0 - base, 0), s.rows) : 0;
+    const int t1 = a.window > 0 ? (int)min((long long)s.rows, max((long long)key1 + a.window - base, 0LL)) : s.rows;
+    return {t0 * a.group, max(t0, t1) * a.group};
+}
+
+// Tiles of 64 rows over such a range, from row `first` on, and how many of them each part has.
+struct WeighTiles {
+    int first, count, each;
+};
+__device__ __forceinline__ WeighTiles weigh_row_tiles(const Rows4Range& range, int parts) {
+    WeighTiles t = {range.first / 64 * 64, 0, 1};
+    if (range.last > range.first) {
+        t.count = (range.last - t.first + 63) / 64;
+        t.each = (t.count + parts - 1) / parts;
+    }
+    return t;
+}
+constexpr int WEIGH_ROWS = 2048;             // rows whose numbers lie in LDS at once
+
+// Few rows: a wave passes over its sequence's keys, 64 at a time, codes of the next 64 under way.  Bounded by memory.
+template <int D, int DTYPE, int QT>
 __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
     using T = typename C4Type<DTYPE>::type;
-    constexpr int TERMS = C4Type<DTYPE>::terms, M = D / 32;
+    constexpr int TERMS = C4Type<DTYPE>::terms, M = D / 32, KT = 4;
     using P = Pieces<D>;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int c = lane & 15, h4 = lane >> 4;
     const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads;
-    const int b = fast_div(rest, a.div_key_tiles), tile = rest - b * a.key_tiles;
+    const int b = fast_div(rest, a.div_parts), part = rest - b * a.parts;
     const Sequence4 s = c4_sequence(a.r, b);
-    const int length = min(s.length, c4_room(a.r, a.c)), base = s.length - s.rows;
-    const int key0 = (tile * 4 + wave) * 16 * KT;
+    const int length = min(s.length, c4_room(a.r, a.c)), base = s.length - s.rows, rows = s.rows * a.group;
+    const int stride = a.parts * 4 * 64;
+    int key0 = (part * 4 + wave) * 64;
     if (key0 >= length) return;
+    const long long weights = ((long long)b * a.c.kv_heads + head) * a.width;
 
-    bf16x8 k[KT][M];
-    bool there[KT];
+    uint32_t codes[KT][M], exp[KT][P::count];
+    unsigned there = 0;
+    auto load = [&](int key) {
+        there = 0;
+        // the four pages at once: the loads of the table do not wait for each other
+        int page[KT];
 #pragma unroll
-    for (int u = 0; u < KT; ++u) {
-        const int key = key0 + 16 * u;
-        const int page = __builtin_amdgcn_readfirstlane(c4_page(a.r, a.c, b, key));
-        there[u] = page >= 0;
-        const Half4 half = {reinterpret_cast<Global4>(reinterpret_cast<uintptr_t>(c4_record(a.c, max(page, 0), head))), key & (a.c.page - 1), key, there[u]};
-        uint32_t codes[M], exp[P::count];
-        load_k_half<D>(a.c, half, lane, codes, exp);
-        static_for<P::count>([&](auto pc) {
-            constexpr int p = pc.value, W = P::width(p), B = P::base(p);
-            const float scale = k_scale(exp[p], lane);
-#pragma unroll
-            for (int i = 0; i < W / 32; ++i) k[u][B / 32 + i] = eight_of(codes[B / 32 + i], scale);
-        });
-    }
-
-    // Rows, counted over (token, head of the group), whose token sees one of the keys
-    const int key1 = min(key0 + 16 * KT, length) - 1;
-    const int t0 = a.causal ? min(max(key0 - base, 0), s.rows) : 0;
-    const int t1 = a.window > 0 ? (int)min((long long)s.rows, max((long long)key1 + a.window - base, 0LL)) : s.rows;
-    float sum[KT] = {}, part[KT] = {};       // sums of 256 rows are added up apart: thousands of terms in one fp32 sum would lose its last digits
-    for (int row0 = t0 * a.group; row0 < t1 * a.group; row0 += 16) {
-        bf16x8 q[TERMS][M];
-        {
-            const int row = row0 + c, token = fast_div(row, a.div_group), g = row - token * a.group;
-            load_q<D, TERMS>(static_cast<const T*>(a.q) + (s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head, row < s.rows * a.group, lane, q);
-        }
-        float lse[4];
-        int pos[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = row0 + 4 * h4 + i, token = fast_div(row, a.div_group), g = row - token * a.group;
-            const bool valid = row < s.rows * a.group;
-            lse[i] = valid ? a.lse[(long long)(s.first + token) * a.c.kv_heads * a.group + head * a.group + g] : __builtin_inff();
-            if (lse[i] == -__builtin_inff()) lse[i] = __builtin_inff();      // a row that sees nothing gives nothing
-            pos[i] = base + token;
-        }
+        for (int u = 0; u < KT; ++u) page[u] = c4_page(a.r, a.c, b, key + 16 * u);
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
-            f32x4 score = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int m = 0; m < M; ++m)
-#pragma unroll
-                for (int n = 0; n < TERMS; ++n) score = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[n][m], k[u][m], score, 0, 0, 0);
-            const int key = key0 + 16 * u + c;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(score[i], a.scale, -lse[i]) * 1.4426950408889634f);
-                const bool seen = (!a.causal || key <= pos[i]) && (a.window == 0 || pos[i] - key < a.window);
-                part[u] += seen ? p : 0.f;
-            }
+            const int p = __builtin_amdgcn_readfirstlane(page[u]);
+            there |= p >= 0 ? 1u << u : 0u;
+            const Half4 half = {reinterpret_cast<Global4>(reinterpret_cast<uintptr_t>(c4_record(a.c, max(p, 0), head))), (key + 16 * u) & (a.c.page - 1), key + 16 * u, true};
+            load_k_half<D>(a.c, half, lane, codes[u], exp[u]);
         }
-        if ((row0 - t0 * a.group) % 256 == 240) {
+    };
+    load(key0);
+    bf16x8 q[QT][TERMS][M];
+    f32x4 origin[QT];
+    auto load_rows = [&](int row0) {
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const int row = row0 + 16 * t + c, token = fast_div(row, a.div_group), g = row - token * a.group;
+            load_q<D, TERMS>(static_cast<const T*>(a.q) + (s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head, row < rows, lane, q[t]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) origin[t][i] = weigh_origin(a, s, head, row0 + 16 * t + 4 * h4 + i, rows);
+        }
+    };
+    load_rows(0);
+
+    for (; key0 < length; key0 += stride) {
+        const int key1 = min(key0 + 63, length - 1);
+        const float old = a.previous != nullptr && key0 + lane < min(base, length) ? a.decay * a.previous[weights + key0 + lane] : 0.f;
+        float sum[KT] = {};
+        const Rows4Range range = weigh_rows(a, s, base, key0, key1);
+        const unsigned present = there;
+        // (almost always one turn: a launch has QT by the mean over its sequences)
+        for (int row0 = range.first / (16 * QT) * (16 * QT); row0 < range.last; row0 += 16 * QT) {
+            if (rows > 16 * QT) load_rows(row0);
+            const bool full = (!a.causal || key1 <= base + fast_div(row0, a.div_group)) &&
+                              (a.window == 0 || base + fast_div(min(row0 + 16 * QT, rows) - 1, a.div_group) - key0 < a.window);
 #pragma unroll
             for (int u = 0; u < KT; ++u) {
-                sum[u] += part[u];
-                part[u] = 0.f;
+                // (codes that seem to change are converted where they are used: taken out of this loop, the operands of 64 keys would fill the registers)
+#pragma unroll
+                for (int m = 0; m < M; ++m) asm volatile("" : "+v"(codes[u][m]));
+                f32x4 score[QT];
+#pragma unroll
+                for (int t = 0; t < QT; ++t) score[t] = origin[t];
+                static_for<P::count>([&](auto pc) {
+                    constexpr int p = pc.value, W = P::width(p), B = P::base(p);
+                    const float scale = k_scale(exp[u][p], lane);
+#pragma unroll
+                    for (int i = 0; i < W / 32; ++i) {
+                        const bf16x8 k = eight_of(codes[u][B / 32 + i], scale);
+#pragma unroll
+                        for (int t = 0; t < QT; ++t)
+#pragma unroll
+                            for (int n = 0; n < TERMS; ++n) score[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t][n][B / 32 + i], k, score[t], 0, 0, 0);
+                    }
+                });
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float p = __builtin_amdgcn_exp2f(score[t][i] * a.scale2);
+                        sum[u] += full || weigh_sees(a, base, row0 + 16 * t + 4 * h4 + i, key0 + 16 * u + c) ? p : 0.f;
+                    }
             }
         }
-    }
-
+        if (key0 + stride < length) load(key0 + stride);
+        float all = 0.f;
 #pragma unroll
-    for (int u = 0; u < KT; ++u) {
-        const float all = row_sum(sum[u] + part[u]);
-        const int key = key0 + 16 * u + c;
-        if (h4 != u % 4 || key >= length) continue;
-        const long long at = ((long long)b * a.c.kv_heads + head) * a.width + key;
-        const float old = a.previous != nullptr && key < base ? a.decay * a.previous[at] : 0.f;
-        a.out[at] = there[u] ? old + all : old;
+        for (int u = 0; u < KT; ++u) {
+            const float v = row_sum(sum[u]);
+            if (h4 == u && (present >> u & 1)) all = v;
+        }
+        if (key0 + lane < length) a.out[weights + key0 + lane] = old + all;
     }
 }
 
-template <int D, int KT>
-int launch_weigh(const Weigh4& a, int dtype, hipStream_t s) {
-    const dim3 grid((unsigned)((long long)a.key_tiles * a.r.batch * a.c.kv_heads));
-    if (dtype == BNN_BF16) launch(weigh_kernel<D, BNN_BF16, KT>, grid, dim3(256), 0, s, a);
-    else if (dtype == BNN_F16) launch(weigh_kernel<D, BNN_F16, KT>, grid, dim3(256), 0, s, a);
-    else launch(weigh_kernel<D, BNN_F32, KT>, grid, dim3(256), 0, s, a);
+// Many rows: a workgroup's four waves have 16 * KT keys each, as finished operands in registers, and pass over the same rows, which lie in LDS as finished operands too.  Rows come with whole lines to a load
+// (four lanes beside each other a row's 64 bytes: a lane of a matrix operand has a row of its own, and loads of that shape take a cycle of the first cache for every lane), go to registers while the
+// step before last is computed and from there to LDS, where the 16-byte places of an operand are exchanged by an exclusive or, so that neither writes nor reads meet.  Numbers that sums begin with lie
+// in LDS for 2048 rows at a time.  A tile's exponentials go with the products of the next.
+// Rows are cut into parts, so that there are workgroups enough; a part's sums go to the workspace, and weigh_join_kernel adds them up in order.
+template <int D, int DTYPE>
+__global__ __launch_bounds__(256, D <= 128 && DTYPE != BNN_F32 ? 3 : 2) void weigh_rows_kernel(Weigh4 a) {
+    using T = typename C4Type<DTYPE>::type;
+    constexpr int TERMS = C4Type<DTYPE>::terms, M = D / 32, KT = cache4_weigh_tiles(D), LOADS = sizeof(T) == 4 ? 2 : 1;
+    constexpr int ROWS = TERMS == 1 ? 64 : 32, TILES = ROWS / 16;    // of a step
+    constexpr int CHUNKS = ROWS * D / 8, EACH = (CHUNKS + 255) / 256;        // of eight elements: of a step, of a thread
+    __shared__ u32x4 q_ops[2][TERMS][TILES * M][64];
+    __shared__ __align__(16) float origins[WEIGH_ROWS];
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int c = lane & 15, h4 = lane >> 4;
+    // heads fastest (rows stay in a die's cache, with eight kv heads or a divisor), the first keys first: causal rows make those the longest
+    const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads;
+    const int outer = fast_div(rest, a.div_parts), part = rest - outer * a.parts;
+    const int tile = fast_div(outer, a.div_batch), b = outer - tile * a.r.batch;
+    const Sequence4 s = c4_sequence(a.r, b);
+    const int length = min(s.length, c4_room(a.r, a.c)), base = s.length - s.rows, rows = s.rows * a.group;
+    const int block0 = tile * 64 * KT, key0 = block0 + wave * 16 * KT;
+    if (block0 >= length) return;
+
+    const WeighTiles all_tiles = weigh_row_tiles(weigh_rows(a, s, base, block0, min(block0 + 64 * KT, length) - 1), a.parts);
+    const int first = all_tiles.first + 64 * all_tiles.each * part, steps = 64 / ROWS * max(min(all_tiles.count - all_tiles.each * part, all_tiles.each), 0);
+    if (steps == 0 && a.parts > 1) return;   // weigh_join_kernel knows
+
+    float sum[KT] = {};
+    if (steps > 0) {
+        // The thread's chunks of a step: rows line + e * LINES, elements 8 * at on; their bytes are counted from the first row of the 2048 (the host sees to it that 32 bits do).
+        constexpr int LINES = 256 / (D / 8);                         // (D of 96: 21 and a third; its chunks are divided each)
+        const int line = (int)threadIdx.x / (D / 8), at = (int)threadIdx.x % (D / 8);
+        auto chunk_of = [&](int e, int& r, int& column) {
+            if constexpr (256 % (D / 8) == 0) {
+                r = line + e * LINES;
+                column = at;
+            } else {
+                const int chunk = (int)threadIdx.x + 256 * e;
+                r = chunk / (D / 8);
+                column = chunk % (D / 8);
+            }
+        };
+        const char* rows_at = nullptr;       // of the 2048
+        int rows_from = 0, phase = 0;        // their first step; the first row's query head of the group
+        auto begin_rows = [&](int step) {
+            const int row = first + ROWS * step, token = fast_div(row, a.div_group);
+            rows_from = step;
+            phase = row - token * a.group;
+            rows_at = reinterpret_cast<const char*>(static_cast<const T*>(a.q) + (long long)(s.first + token) * a.q_token + (long long)head * a.group * a.q_head);
+        };
+        u32x4 raw[EACH][LOADS];
+        uint32_t offsets[EACH];
+        // Bytes from rows_at to the thread's chunks of a step.  Of rows that are not there the last is loaded; what comes of it is masked.
+        auto locate = [&](int step) {
+            const int most = rows - 1 - first - ROWS * step, ahead = ROWS * (step - rows_from) + phase;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                int r, column;
+                chunk_of(e, r, column);
+                const uint32_t n = (uint32_t)(ahead + min(r, most));
+                const uint32_t token = (a.div_group.m == 0u ? n : __umulhi(n, a.div_group.m)) >> a.div_group.sh, g = n - times24(token, (uint32_t)a.group);
+                offsets[e] = (times24(token, (uint32_t)a.q_token) + times24(g, (uint32_t)a.q_head) + 8 * column) * (uint32_t)sizeof(T);
+            }
+        };
+        // Where a step has whole tokens, its chunks lie as those of the first, a step's bytes further on
+        const bool whole = ROWS % a.group == 0;
+        const long long step_bytes = whole ? (long long)(ROWS / a.group) * a.q_token * (long long)sizeof(T) : 0;
+        auto fetch = [&](int step) {
+            const bool last = ROWS * (step + 1) > rows - first;
+            if (!whole || last) locate(step);
+            const char* from = rows_at + (whole && !last ? (step - rows_from) * step_bytes : 0);
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                if (CHUNKS % 256 != 0 && (int)threadIdx.x + 256 * e >= CHUNKS) continue;
+#pragma unroll
+                for (int l = 0; l < LOADS; ++l) raw[e][l] = reinterpret_cast<const u32x4*>(from + offsets[e])[l];
+            }
+        };
+        auto store = [&](int buffer) {
+#pragma unroll
+            for (int e = 0; e < EACH; ++e) {
+                if (CHUNKS % 256 != 0 && (int)threadIdx.x + 256 * e >= CHUNKS) continue;
+                int r, column;
+                chunk_of(e, r, column);
+                const int m = column / 4, quarter = column % 4;
+                u32x4* to = &q_ops[buffer][0][(r / 16) * M + m][16 * quarter + ((r % 16) ^ (12 * (quarter & 1) + (m & 3)))];
+                if constexpr (TERMS == 1) {
+                    *to = raw[e][0];
+                } else {
+                    float x[8];
+                    if constexpr (LOADS == 2) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(raw[e][i / 4][i % 4]);
+                    } else {
+                        typedef T t8 __attribute__((ext_vector_type(8)));
+                        const t8 y = __builtin_bit_cast(t8, raw[e][0]);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = (float)y[i];
+                    }
+                    bf16x8 split[TERMS];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        __bf16 terms[TERMS];
+                        split_terms<TERMS>(x[i], terms);
+#pragma unroll
+                        for (int n = 0; n < TERMS; ++n) split[n][i] = terms[n];
+                    }
+#pragma unroll
+                    for (int n = 0; n < TERMS; ++n) to[n * TILES * M * 64] = __builtin_bit_cast(u32x4, split[n]);
+                }
+            }
+        };
+        begin_rows(0);
+        locate(0);
+        fetch(0);
+        // Keys in the order of elements that rows have: product m contracts elements 32 m .. + 31, eight a lane
+        bf16x8 k[KT][M];
+#pragma unroll
+        for (int u = 0; u < KT; ++u) {
+            const int key = key0 + 16 * u;
+            const int page = __builtin_amdgcn_readfirstlane(c4_page(a.r, a.c, b, key));
+            const Global4 record = reinterpret_cast<Global4>(reinterpret_cast<uintptr_t>(c4_record(a.c, max(page, 0), head)));
+            const uint32_t offset = key & (a.c.page - 1);
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+                const uint32_t codes = load_at<uint32_t>(record, (offset + c) * (D / 2) + 16 * m + 4 * h4);
+                const uint32_t exp = load_at<uint32_t>(record, (uint32_t)a.c.k_exps + m * (uint32_t)a.c.page + offset + (c & 12u));
+                k[u][m] = eight_of(codes, k_scale(exp, lane));
+            }
+        }
+        const int operand = 16 * h4 + (c ^ (12 * (h4 & 1)));                // the lane's place, but for m
+        float some[KT] = {};                 // of 256 rows: thousands of terms in one fp32 sum would lose its last digits
+        f32x4 score[KT];                     // of the tile before
+#pragma unroll
+        for (int u = 0; u < KT; ++u) score[u] = f32x4{-__builtin_inff(), -__builtin_inff(), -__builtin_inff(), -__builtin_inff()};
+        auto add_up = [&]() {
+#pragma unroll
+            for (int u = 0; u < KT; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) some[u] += __builtin_amdgcn_exp2f(score[u][i] * a.scale2);
+            // (they stay here: moved to where the sums are used next, nothing would run beside them)
+#pragma unroll
+            for (int u = 0; u < KT; ++u) asm volatile("" : "+v"(some[u]));
+        };
+        auto pass_step = [&](int step) {
+            __syncthreads();
+            store((step + 1) & 1);
+            fetch(min(step + 2, steps - 1));
+        };
+        auto one_step = [&](int local, int step, auto masked) {      // local: of the steps whose rows' numbers lie in LDS
+            pass_step(step);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) {
+                const f32x4 origin = *reinterpret_cast<const f32x4*>(&origins[ROWS * local + 16 * t + 4 * h4]);
+                f32x4 next[KT];
+#pragma unroll
+                for (int u = 0; u < KT; ++u) next[u] = origin;
+#pragma unroll
+                for (int m = 0; m < M; ++m)
+#pragma unroll
+                    for (int n = 0; n < TERMS; ++n) {
+                        const bf16x8 q = __builtin_bit_cast(bf16x8, q_ops[step & 1][n][t * M + m][operand ^ (m & 3)]);
+#pragma unroll
+                        for (int u = 0; u < KT; ++u) next[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, k[u][m], next[u], 0, 0, 0);
+                    }
+                add_up();
+                if constexpr (!decltype(masked)::value) {            // operands ahead, exponentials among the products
+                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+                    for (int o = 0; o < M * TERMS; ++o) {
+                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+#pragma unroll
+                        for (int u = 0; u < KT; ++u) {
+                            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                            __builtin_amdgcn_sched_group_barrier(0x402, (12 + M * TERMS - 1) / (M * TERMS), 0);
+                        }
+                    }
+                }
+                if constexpr (decltype(masked)::value) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = first + ROWS * step + 16 * t + 4 * h4 + i, pos = base + fast_div(r, a.div_group);
+#pragma unroll
+                        for (int u = 0; u < KT; ++u) {
+                            const int key = key0 + 16 * u + c;
+                            next[u][i] = r < rows && (!a.causal || key <= pos) && (a.window == 0 || pos - key < a.window) ? next[u][i] : -__builtin_inff();
+                        }
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < KT; ++u) score[u] = next[u];
+            }
+        };
+        // Steps whose rows all see all of the wave's keys; and the first with a row that sees one of them
+        int clear_from = 0, clear_to = min(steps, (rows - first) / ROWS), begin = 0;
+        if (a.causal) {                      // from the first row whose token is at the last key, or the first
+            const long long r = (long long)(key0 + 16 * KT - 1 - base) * a.group - first, r0 = (long long)(key0 - base) * a.group - first;
+            clear_from = (int)min(max((r + ROWS - 1) / ROWS, 0LL), (long long)steps);
+            begin = (int)min(max(r0 / ROWS, 0LL), (long long)steps);
+        }
+        if (a.window > 0) {                  // up to the last row whose token still sees the first key
+            const long long r = ((long long)key0 + a.window - base) * a.group - first;
+            clear_to = (int)min(max(r / ROWS, 0LL), (long long)clear_to);
+        }
+        clear_to = max(clear_to, clear_from);
+        store(0);
+        fetch(min(1, steps - 1));
+        for (int chunk = 0; chunk < steps; chunk += WEIGH_ROWS / ROWS) {
+            const int here = min(WEIGH_ROWS / ROWS, steps - chunk);
+            if (chunk > 0) {
+                begin_rows(chunk);           // (whole: the rows before began with a whole token as well)
+                __syncthreads();
+            }
+            for (int i = (int)threadIdx.x; i < ROWS * here; i += 256) origins[i] = weigh_origin(a, s, head, first + ROWS * chunk + i, rows);
+            // waves go through different kinds of steps, each with one barrier
+            for (int i = chunk; i < chunk + here;) {
+                const int end = min(chunk + here, i + 256 / ROWS), from = min(max(clear_from, i), end), to = min(max(clear_to, i), end);
+                for (; i < min(begin, end); ++i) pass_step(i);
+                for (; i < from; ++i) one_step(i - chunk, i, std::true_type{});
+                for (; i < to; ++i) one_step(i - chunk, i, std::false_type{});
+                for (; i < end; ++i) one_step(i - chunk, i, std::true_type{});
+#pragma unroll
+                for (int u = 0; u < KT; ++u) {
+                    sum[u] += some[u];
+                    some[u] = 0.f;
+                }
+            }
+        }
+        add_up();
+#pragma unroll
+        for (int u = 0; u < KT; ++u) sum[u] += some[u];
+    }
+
+    const long long sequence = (long long)b * a.c.kv_heads + head;
+    float all = 0.f;
+#pragma unroll
+    for (int u = 0; u < KT; ++u) {
+        const float v = row_sum(sum[u]);
+        if (h4 == u) all = v;
+    }
+    const int key = key0 + lane;
+    if (lane >= 16 * KT || key >= length) return;
+    if (a.parts > 1) {
+        a.partial[(sequence * a.parts + part) * a.width4 + key] = all;
+    } else {
+        if (c4_page(a.r, a.c, b, key) < 0) all = 0.f;
+        const float old = a.previous != nullptr && key < base ? a.decay * a.previous[sequence * a.width + key] : 0.f;
+        a.out[sequence * a.width + key] = old + all;
+    }
+}
+
+// Adds up the parts' sums, those that have rows for the key's tile (of `tile` keys).
+__global__ __launch_bounds__(256) void weigh_join_kernel(Weigh4 a, int tile, int blocks, FastDiv div_blocks) {
+    const int rest = fast_div((int)blockIdx.x, div_blocks), head = (int)blockIdx.y;
+    const int key = ((int)blockIdx.x - rest * blocks) * 256 + (int)threadIdx.x, b = rest;
+    const Sequence4 s = c4_sequence(a.r, b);
+    const int length = min(s.length, c4_room(a.r, a.c)), base = s.length - s.rows;
+    if (key >= length) return;
+    const int block0 = key / tile * tile;
+    const Rows4Range range = weigh_rows(a, s, base, block0, min(block0 + tile, length) - 1);
+    const long long sequence = (long long)b * a.c.kv_heads + head;
+    float all = 0.f;
+    if (c4_page(a.r, a.c, b, key) >= 0) {
+        const WeighTiles tiles = weigh_row_tiles(range, a.parts);
+        for (int p = 0; p * tiles.each < tiles.count; ++p) all += a.partial[(sequence * a.parts + p) * a.width4 + key];
+    }
+    const float old = a.previous != nullptr && key < base ? a.decay * a.previous[sequence * a.width + key] : 0.f;
+    a.out[sequence * a.width + key] = old + all;
+}
+
+template <int D, int DTYPE>
+int launch_weigh(const Weigh4& a, const WeighPlan4& p, hipStream_t s) {
+    const dim3 grid((unsigned)p.workgroups);
+    if (p.row_tiles == 0) {
+        launch(weigh_rows_kernel<D, DTYPE>, grid, dim3(256), 0, s, a);
+    } else {
+        if constexpr (cache4_weigh_two(D, DTYPE)) {
+            if (p.row_tiles == 2) launch(weigh_kernel<D, DTYPE, 2>, grid, dim3(256), 0, s, a);
+        }
+        if (p.row_tiles == 1) launch(weigh_kernel<D, DTYPE, 1>, grid, dim3(256), 0, s, a);
+    }
+    if (p.workspace_bytes != 0) {
+        const int blocks = (int)cdiv((long long)a.r.table_pages << a.c.page_shift, 256);
+        launch(weigh_join_kernel, dim3((unsigned)((long long)blocks * a.r.batch), (unsigned)a.c.kv_heads), dim3(256), 0, s, a, 64 * cache4_weigh_tiles(D), blocks, make_fastdiv((uint32_t)blocks));
+    }
     return check_launch();
 }
 template <int D>
-int launch_weigh_dim(Weigh4& a, int dtype, hipStream_t s) {
-    constexpr int KT = D == 256 ? 2 : 4;
-    const long long tiles = cdiv((long long)a.r.table_pages << a.c.page_shift, 64 * KT);
-    if (tiles * a.r.batch * a.c.kv_heads >= C4_THREADS / 256) return BNN_ERR_UNSUPPORTED;
-    a.key_tiles = (int)tiles;
-    a.div_key_tiles = make_fastdiv((uint32_t)tiles);
-    return launch_weigh<D, KT>(a, dtype, s);
+int launch_weigh_type(const Weigh4& a, const WeighPlan4& p, int dtype, hipStream_t s) {
+    if (dtype == BNN_BF16) return launch_weigh<D, BNN_BF16>(a, p, s);
+    if (dtype == BNN_F16) return launch_weigh<D, BNN_F16>(a, p, s);
+    return launch_weigh<D, BNN_F32>(a, p, s);
 }
 
 }  // namespace
 
-int launch_cache4_weigh(Weigh4 a, int dtype, hipStream_t s) {
+int launch_cache4_weigh(const Weigh4& a, const WeighPlan4& p, int dtype, hipStream_t s) {
     switch (a.c.dim) {
-        case 64: return launch_weigh_dim<64>(a, dtype, s);
-        case 96: return launch_weigh_dim<96>(a, dtype, s);
-        case 128: return launch_weigh_dim<128>(a, dtype, s);
-        case 192: return launch_weigh_dim<192>(a, dtype, s);
-        default: return launch_weigh_dim<256>(a, dtype, s);
+        case 64: return launch_weigh_type<64>(a, p, dtype, s);
+        case 96: return launch_weigh_type<96>(a, p, dtype, s);
+        case 128: return launch_weigh_type<128>(a, p, dtype, s);
+        case 192: return launch_weigh_type<192>(a, p, dtype, s);
+        default: return launch_weigh_type<256>(a, p, dtype, s);
     }
 }
 

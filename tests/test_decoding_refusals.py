@@ -62,9 +62,9 @@ def test_write_rotary(b):
 
 
 def test_weigh(b):
-    def call(c=None, r=None, q=A, dtype=F32, q_d=(256, 64), heads=4, lse=A, scale=0.125, causal=1, window=0, previous=0, decay=1.0, weights=A, width=48):
+    def call(c=None, r=None, q=A, dtype=F32, q_d=(256, 64), heads=4, lse=A, scale=0.125, causal=1, window=0, previous=0, decay=1.0, weights=A, width=48, work=0, size=0):
         return b.load().bnn_cache4_weigh(c or cache(b), r or rows(b), P(q), dtype, *i64(*q_d), heads, P(lse), ctypes.c_float(scale), causal, window, P(previous), ctypes.c_float(decay),
-                                         P(weights), ctypes.c_int64(width), None)
+                                         P(weights), ctypes.c_int64(width), P(work), ctypes.c_size_t(size), None)
     for kw in (dict(q=0), dict(lse=0), dict(weights=0), dict(width=47), dict(dtype=4), dict(heads=3), dict(heads=0), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("nan")),
                dict(scale=float("inf")), dict(window=-1), dict(window=2, causal=0), dict(decay=float("nan")), dict(decay=float("inf")), dict(r=rows(b, lens=0))):
         assert call(**kw) == INVALID, kw
@@ -72,6 +72,12 @@ def test_weigh(b):
         assert call(**kw) == ALIGNMENT, kw
     assert call(r=rows(b, pages=(1 << 26) + 1), width=1 << 40) == UNSUPPORTED
     assert call(r=rows(b, tokens=1 << 29), heads=4) == UNSUPPORTED
+    assert call(scale=1e-39) == INVALID                              # (its reciprocal is no fp32 number)
+    need = b.load().bnn_cache4_weigh_workspace_bytes(cache(b), rows(b, tokens=2000), F32, 4)
+    assert need > 0 and b.load().bnn_cache4_weigh_workspace_bytes(cache(b), rows(b), F32, 4) == 0
+    assert call(r=rows(b, tokens=2000)) == WORKSPACE and call(r=rows(b, tokens=2000), work=A, size=need - 1) == WORKSPACE and call(r=rows(b, tokens=2000), work=A + 8, size=need) == ALIGNMENT
+    for bad in ((cache(b, dim=80), rows(b), F32, 4), (cache(b), rows(b, tokens=5), F32, 4), (cache(b), rows(b), 3, 4), (cache(b), rows(b), F32, 3), (cache(b), rows(b, tokens=1 << 29), F32, 4)):
+        assert b.load().bnn_cache4_weigh_workspace_bytes(*bad) == 0
     assert call(r=rows(b, tokens=0)) == OK
 
 

@@ -110,6 +110,53 @@ def test_weigh_lengths(bnn, lens, counts):
     check_weigh(su, window=2147483647, previous=False)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("dim,page,kv_heads,group", [(64, 16, 2, 8), (96, 32, 1, 5), (128, 64, 1, 3), (192, 128, 1, 7), (256, 16, 1, 33)])
+def test_weigh_many_rows(bnn, dtype, dim, page, kv_heads, group):
+    """Rows by the hundred: several steps and parts, rows of other tokens in a step (groups that do not divide it), sequences with few rows beside, missing pages, windows, a wave's keys that no row sees."""
+    su = Batch(bnn, dim + group, [170, 300, 5, 0, 90], [170, 61, 1, 0, 90], kv_heads, group, dim, page, dtype)
+    if su.table.shape[1] > 2:
+        su.table[1, 1] = -1
+    check_weigh(su)
+    check_weigh(su, window=37, decay=0.5)
+    check_weigh(su, causal=False, previous=False, scale=0.2)
+
+
+def test_weigh_thousands_of_rows(bnn):
+    """More rows than lie in LDS at once, against rows a few at a time (bounds: the sums of both, 2 units for every row of a key)."""
+    su = Batch(bnn, 31, [1500, 700], [1, 1], kv_heads=2, group=4, dim=64, page=64)
+    plan = su.plan()
+    q = torch.randn(2000, 8, 64, device="cuda", dtype=torch.bfloat16)
+    start = ints([0, 1400, 2000])
+    out, lse = su.gpu.attend(q, want_lse=True, **{**plan, "start": start})
+    zero = lambda: torch.zeros(2, 2, su.table.shape[1] * 64, device="cuda")
+    for window in (0, 333):
+        out, lse = su.gpu.attend(q, want_lse=True, window=window, **{**plan, "start": start})
+        got = su.gpu.weigh(q, lse, out=zero(), window=window, **{**plan, "start": start})
+        want = zero().double()
+        for i in range(0, 1400, 2):          # tokens 100 .. 1499 and 100 .. 699, two at a time
+            parts = [(0, i)] + ([(1, i)] if i < 600 else [])
+            for b, t in parts:
+                one = dict(table=plan["table"][b:b + 1].contiguous(), lens=ints([100 + t + 2]))
+                rows = slice(1400 * b + t, 1400 * b + t + 2)
+                want[b:b + 1] += su.gpu.weigh(q[rows], lse[rows], out=torch.zeros(1, 2, su.table.shape[1] * 64, device="cuda"), window=window, **one).double()
+        spread = 64 ** 0.5 * 6 * 4           # scale * sum |q| |k| and |lse|, generously
+        assert ((got.double() - want).abs() <= (2 * (64 + 8) * U * spread + 2 * 5600 * U) * want + 1e-30).all()
+        assert abs(got[0].sum().item() - 1400 * 8) <= 0.01 and abs(got[1].sum().item() - 600 * 8) <= 0.01
+
+
+def test_weigh_far_apart_rows(bnn):
+    """Distances between tokens that 32-bit offsets of the kernel for many rows do not reach."""
+    su = Batch(bnn, 32, [80], [80], kv_heads=1, group=1, dim=64)
+    wide = torch.empty(80, 1 << 23, device="cuda", dtype=torch.bfloat16)
+    wide[:, :64] = dev(su.q, "bf16")[:, 0]
+    view = wide.view(80, 1, 1 << 23)[:, :, :64]
+    lse = torch.randn(80, 1, device="cuda")
+    zero = lambda: torch.zeros(1, 1, su.table.shape[1] * 16, device="cuda")
+    near, far = su.gpu.weigh(dev(su.q, "bf16"), lse, out=zero(), **su.plan()), su.gpu.weigh(view, lse, out=zero(), **su.plan())
+    assert ((near - far).abs() <= 2 * 80 * U * near + 2 * 72 * U * 40 * near).all() and near.sum() > 0
+
+
 def test_weights_are_those_of_attention(bnn):
     """Every row gives its whole weight: the sums over keys are the rows' number, and with the cache's values they give attention's outputs."""
     su = Batch(bnn, 9, [500, 130], [1, 1], dim=128, page=64, group=4, spread=2.0)
@@ -127,12 +174,13 @@ def test_weights_are_those_of_attention(bnn):
 
 
 def test_rows_that_give_nothing_or_nan(bnn):
-    """A row whose lse is -infinity gives nothing; a query with a NaN or infinity makes the weights of what it sees NaN, and no others; NaN keys where no row looks stay there."""
+    """A row whose lse is -infinity gives nothing; one whose lse is NaN, as attention gives for a query with a NaN or infinity, makes the weights of what it sees NaN, and no others; NaN keys
+    where no row looks stay there."""
     su = Batch(bnn, 10, [40, 40, 40], [1, 1, 1], kv_heads=1, group=1, dim=64)
     q = dev(su.q, "bf16")
     lse = torch.zeros(3, 1, device="cuda")
     lse[0] = float("-inf")
-    q[1, 0, 3] = float("nan")
+    q[1, 0, 3], lse[1] = float("nan"), float("nan")
     w = su.gpu.weigh(q, lse, out=torch.zeros(3, 1, 48, device="cuda"), window=5, **su.plan())
     assert (w[0] == 0).all() and torch.isnan(w[1, 0, 35:40]).all() and (w[1, 0, :35] == 0).all() and (w[2, 0, 35:40] > 0).all() and (w[2, 0, 40:] == 0).all()
     q[1, 0, 3] = float("inf")

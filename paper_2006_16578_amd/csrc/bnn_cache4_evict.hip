@@ -1,15 +1,16 @@
 // Eviction: which cached tokens to keep, by their weights, and moving them into other pages.
 //
-// heaviest_kernel: a workgroup has a sequence and kv head.  Weights in the order of numbers are whole numbers in the order of their bits (negative ones turned round); the weight of the last token that
+// heaviest_kernel: a workgroup has a sequence and kv head.  Weights in the order of numbers are whole numbers in the order of their bits (negative ones turned round); that of the last token that
 // is kept is found digit by digit, from the highest on: a histogram of the digit over what agrees so far, 11 + 11 + 10 bits.  Of those that equal it the lowest tokens are kept.  A wave has a run of
-// consecutive tokens, so one exchange of counts gives every wave the place of its first kept token, and the list is ascending.
+// consecutive tokens, a lane four beside each other, so one exchange of counts gives every wave the place of its first kept token, and the list is ascending.  Weights are read once and stay in
+// registers where the table has room for up to 65536 tokens; beyond, they are read five times, eight loads under way.
 // move_kernel: a workgroup has a kv head and 64 places of the new sequence.
 #include "bnn_cache4.h"
 
 namespace bnn {
 namespace {
 
-constexpr int H_THREADS = 1024, H_WAVES = H_THREADS / 64, H_BINS = 2048;
+constexpr int H_THREADS = 1024, H_WAVES = H_THREADS / 64, H_BINS = 2048, H_VECTOR = 256;       // H_VECTOR: tokens of a wave at once
 
 // The order of weights as that of whole numbers; NaN below all.  -0 counts as 0.
 __device__ __forceinline__ uint32_t rank_of(float w) {
@@ -18,30 +19,92 @@ __device__ __forceinline__ uint32_t rank_of(float w) {
     return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
 }
 
+// E: vectors of a wave that its registers hold; 0: none.
+template <int E>
 __global__ __launch_bounds__(H_THREADS) void heaviest_kernel(Heaviest4 a) {
+    constexpr int LOADS = E == 0 ? 8 : E;    // under way together
     __shared__ int bins[H_BINS];
-    __shared__ int wave_above[H_WAVES], wave_equal[H_WAVES], wave_there[H_WAVES];
-    __shared__ int picked[3];
+    __shared__ int wave_above[H_WAVES], wave_equal[H_WAVES], wave_there[H_WAVES], wave_sum[H_WAVES];
+    __shared__ int picked[2];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int b = (int)blockIdx.x, head = (int)blockIdx.y;
     const int length = (int)min((long long)max(a.lens[b], 0), (long long)a.table_pages << a.c.page_shift);
-    const int run = (int)(((long long)length + H_WAVES * 64 - 1) / (H_WAVES * 64)) * 64;          // tokens of a wave
-    const int begin = (int)min((long long)wave * run, (long long)length), end = (int)min((long long)begin + run, (long long)length);
+    const int run = (length + H_WAVES * H_VECTOR - 1) / (H_WAVES * H_VECTOR);     // vectors of a wave
+    const int begin = min(wave * run * H_VECTOR, length), end = min(begin + run * H_VECTOR, length);
     const float* weights = a.weights + ((long long)b * a.c.kv_heads + head) * a.width;
     const int32_t* table = a.table + (long long)b * a.table_pages;
     int32_t* out = a.tokens + ((long long)b * a.c.kv_heads + head) * a.keep;
+
+    // Four tokens of a lane.  (Pages and tables have room for multiples of 16: what begins inside lies inside.)
+    struct Four {
+        f32x4 weight;
+        int page;
+    };
+    auto fetch = [&](int j) -> Four {
+        Four f = {f32x4{0.f, 0.f, 0.f, 0.f}, -1};
+        if (j < end) {
+            __builtin_memcpy(&f.weight, weights + j, 16);
+            f.page = table[j >> a.c.page_shift];
+        }
+        return f;
+    };
     // 0: nowhere; kept in any case: the highest; else a number between
-    auto rank = [&](int j) -> uint32_t {
-        if (j >= end || (uint32_t)table[j >> a.c.page_shift] >= (uint32_t)a.c.pages) return 0;
-        if (j < a.first || j >= length - a.last) return 0xffffffffu;
-        return min(max(rank_of(weights[j]), 1u), 0xfffffffeu);
+    auto rank = [&](const Four& f, int j, uint32_t (&r)[4]) {
+        const bool there = (uint32_t)f.page < (uint32_t)a.c.pages;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = j + i;
+            r[i] = t < a.first || t >= length - a.last ? 0xffffffffu : min(max(rank_of(f.weight[i]), 1u), 0xfffffffeu);
+            if (!there || t >= end) r[i] = 0;
+        }
+    };
+    uint32_t held[E == 0 ? 1 : E][4];
+    if constexpr (E > 0) {
+        Four f[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) f[e] = fetch(begin + e * H_VECTOR + 4 * lane);
+#pragma unroll
+        for (int e = 0; e < E; ++e) rank(f[e], begin + e * H_VECTOR + 4 * lane, held[e]);
+    }
+    // f(ranks, first token of the lane) for every vector of the wave
+    auto for_each = [&](auto f) {
+        if constexpr (E > 0) {
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (begin + e * H_VECTOR < end) f(held[e], begin + e * H_VECTOR + 4 * lane);
+        } else {
+            for (int j0 = begin; j0 < end; j0 += LOADS * H_VECTOR) {
+                Four four[LOADS];
+#pragma unroll
+                for (int e = 0; e < LOADS; ++e) four[e] = fetch(j0 + e * H_VECTOR + 4 * lane);
+#pragma unroll
+                for (int e = 0; e < LOADS; ++e) {
+                    if (j0 + e * H_VECTOR >= end) break;
+                    uint32_t r[4];
+                    rank(four[e], j0 + e * H_VECTOR + 4 * lane, r);
+                    f(r, j0 + e * H_VECTOR + 4 * lane);
+                }
+            }
+        }
     };
 
     int there = 0;
-    for (int j = begin + lane; j - lane < end; j += 64) there += __popcll(__ballot(rank(j) != 0));
+    for (int i = (int)threadIdx.x; i < H_BINS; i += H_THREADS) bins[i] = 0;
+    __syncthreads();
+    for_each([&](const uint32_t (&r)[4], int) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (r[i] != 0) {
+                ++there;
+                atomicAdd(&bins[r[i] >> 21], 1);
+            }
+    });
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) there += __shfl_xor(there, d);
     if (lane == 0) wave_there[wave] = there;
     __syncthreads();
     there = 0;
+#pragma unroll
     for (int w = 0; w < H_WAVES; ++w) there += wave_there[w];
     const int kept = min(there, a.keep);
     if (head == 0 && threadIdx.x == 0) a.kept[b] = kept;
@@ -50,52 +113,55 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_kernel(Heaviest4 a) {
     uint32_t border = 1;
     int of_border = 0x7fffffff;
     if (there > a.keep) {
-        uint32_t prefix = 0;
-        int need = a.keep;                   // of those that agree with prefix so far
+        border = 0;
+        of_border = a.keep;                  // of those that agree with border so far
         for (int digit = 0; digit < 3; ++digit) {
             const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, width = digit == 2 ? 10 : 11;
-            for (int i = (int)threadIdx.x; i < H_BINS; i += H_THREADS) bins[i] = 0;
-            __syncthreads();
-            for (int j = begin + lane; j < end; j += 64) {
-                const uint32_t r = rank(j);
-                if (r != 0 && (digit == 0 || r >> (shift + width) == prefix >> (shift + width))) atomicAdd(&bins[r >> shift & ((1u << width) - 1)], 1);
-            }
-            __syncthreads();
-            if (wave == 0) {                 // from the highest bin down: the one in which the count passes need
-                int above = 0;
-                for (int top = (1 << width) - 64; top >= 0; top -= 64) {
-                    const int n = bins[top + 63 - lane];
-                    int upto = n;
+            if (digit > 0) {
+                for (int i = (int)threadIdx.x; i < H_BINS; i += H_THREADS) bins[i] = 0;
+                __syncthreads();
+                for_each([&](const uint32_t (&r)[4], int) {
 #pragma unroll
-                    for (int d = 1; d < 64; d <<= 1) {
-                        const int other = __shfl_up(upto, d);
-                        if (lane >= d) upto += other;
-                    }
-                    const unsigned long long past = __ballot(above + upto >= need);
-                    if (past != 0) {
-                        const int at = __ffsll(past) - 1;
-                        if (lane == at) {
-                            picked[0] = top + 63 - lane;
-                            picked[1] = need - (above + upto - n);
-                        }
-                        break;
-                    }
-                    above += __shfl(upto, 63);
-                }
+                    for (int i = 0; i < 4; ++i)
+                        if (r[i] != 0 && r[i] >> (shift + width) == border >> (shift + width)) atomicAdd(&bins[r[i] >> shift & ((1u << width) - 1)], 1);
+                });
+                __syncthreads();
+            }
+            // From the highest bin down, two to a thread: the one in which the count reaches of_border
+            const int top = H_BINS - 1 - 2 * (int)threadIdx.x, high = bins[top], low = bins[top - 1];
+            int upto = high + low;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int other = __shfl_up(upto, d);
+                if (lane >= d) upto += other;
+            }
+            if (lane == 63) wave_sum[wave] = upto;
+            __syncthreads();
+            for (int w = 0; w < wave; ++w) upto += wave_sum[w];
+            const int before = upto - high - low;
+            if (before < of_border && upto >= of_border) {
+                const bool first = before + high >= of_border;
+                picked[0] = first ? top : top - 1;
+                picked[1] = of_border - before - (first ? 0 : high);
             }
             __syncthreads();
-            prefix |= (uint32_t)picked[0] << shift;
-            need = picked[1];
+            border |= (uint32_t)picked[0] << shift;
+            of_border = picked[1];
         }
-        border = prefix;
-        of_border = need;
     }
 
     int above = 0, equal = 0;
-    for (int j = begin + lane; j - lane < end; j += 64) {
-        const uint32_t r = rank(j);
-        above += __popcll(__ballot(r > border));
-        equal += __popcll(__ballot(r == border));
+    for_each([&](const uint32_t (&r)[4], int) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            above += r[i] > border ? 1 : 0;
+            equal += r[i] == border ? 1 : 0;
+        }
+    });
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) {
+        above += __shfl_xor(above, d);
+        equal += __shfl_xor(equal, d);
     }
     if (lane == 0) {
         wave_above[wave] = above;
@@ -108,16 +174,38 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_kernel(Heaviest4 a) {
         equals += wave_equal[w];
     }
     place += min(equals, of_border);
-    const unsigned long long below = (1ull << lane) - 1;
-    for (int j = begin + lane; j - lane < end; j += 64) {
-        const uint32_t r = rank(j);
-        const unsigned long long e = __ballot(r == border);
-        const bool keep = r > border || (r == border && equals + __popcll(e & below) < of_border);
-        equals += __popcll(e);
-        const unsigned long long k = __ballot(keep);
-        if (keep) out[place + __popcll(k & below)] = j;
-        place += __popcll(k);
-    }
+    // lanes before this one, in a mask
+    auto before = [](unsigned long long mask) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); };
+    for_each([&](const uint32_t (&r)[4], int j) {
+        bool keep[4];
+        unsigned long long e[4], any = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e[i] = __ballot(r[i] == border);
+            any |= e[i];
+            keep[i] = r[i] > border;
+        }
+        if (any != 0) {                      // which of those at the border: the lowest
+            int n = equals + before(e[0]) + before(e[1]) + before(e[2]) + before(e[3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (r[i] == border) {
+                    keep[i] = n < of_border;
+                    ++n;
+                }
+                equals += __popcll(e[i]);
+            }
+        }
+        unsigned long long k[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[i] = __ballot(keep[i]);
+        int at = place + before(k[0]) + before(k[1]) + before(k[2]) + before(k[3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (keep[i]) out[at++] = j + i;
+            place += __popcll(k[i]);
+        }
+    });
     for (int i = kept + (int)threadIdx.x; i < a.keep; i += H_THREADS) out[i] = -1;
 }
 
@@ -155,7 +243,12 @@ __global__ __launch_bounds__(256) void move_kernel(Move4 a, FastDiv div_lanes, i
 }  // namespace
 
 int launch_cache4_heaviest(const Heaviest4& a, hipStream_t s) {
-    launch(heaviest_kernel, dim3((unsigned)a.batch, (unsigned)a.c.kv_heads), dim3(H_THREADS), 0, s, a);
+    const dim3 grid((unsigned)a.batch, (unsigned)a.c.kv_heads);
+    const long long vectors = cdiv((long long)a.table_pages << a.c.page_shift, H_WAVES * H_VECTOR);
+    if (vectors <= 2) launch(heaviest_kernel<2>, grid, dim3(H_THREADS), 0, s, a);
+    else if (vectors <= 8) launch(heaviest_kernel<8>, grid, dim3(H_THREADS), 0, s, a);
+    else if (vectors <= 16) launch(heaviest_kernel<16>, grid, dim3(H_THREADS), 0, s, a);
+    else launch(heaviest_kernel<0>, grid, dim3(H_THREADS), 0, s, a);
     return check_launch();
 }
 

@@ -1,10 +1,15 @@
 // What a head's sums say: log probabilities of given tokens, entropy, the best alternatives, in one pass over the logits.
 //
-// A workgroup has a piece of a row, which stays in its registers: with the piece's maximum m it forms S = sum 2^u and W = sum 2^u u, u = (x - m) scale / log 2, from which
+// With a reference point m and u = (x - m) scale / log 2, S = sum 2^u and W = sum 2^u u give
 //   log p = scale (x - m) - log S,  entropy = log S - log 2 W / S  (both terms >= 0),  lse = scale m + log S,
-// so no difference of large numbers is left; pieces of a row are joined by the same rule.  The `top` best of a piece: the threads' maxima give a border that at least `top` elements reach, and
-// little more do; those are collected in LDS and ranked by counting.  Elements are ordered by (value, lower column first) as one 64-bit number.
-// What bounds it is memory.
+// so no difference of large numbers is left.  A wave's m is the largest of its first columns, and is raised only when a column passes it by more than 16 (as powers of two), so most columns meet no branch and no
+// rescaling; waves and pieces of a row are joined by the same rule.  What bounds it is memory: 10 instruction slots a column (an exponential counts four) take about four fifths of the time that its
+// two bytes take.
+//
+// The `top` best: beside that, every thread keeps the largest of each eight of its vectors.  The `top`-th largest of the threads' maxima is a border that at least `top` columns reach and little more do;
+// the vectors' maxima tell where those are, and they are read again, collected in LDS and ranked by counting.  Columns are ordered by (value, lower column first) as one 64-bit number.  Where a border is shared
+// by many, what is above it is collected, and then what equals it from the lowest column on; where the best lie so close together in one thread's columns that the list overflows, the
+// border is found digit by digit over all columns.
 #include <math.h>
 
 #include "bnn_cache4.h"
@@ -19,13 +24,14 @@ struct Logprobs {
     const void* x;
     int rows, cols;
     long long ld;
-    float scale, scale2;                     // scale2: for powers of two
+    float scale, scale2, slack;              // scale2: scale / log 2; slack: what x may pass the reference point by
     const int64_t* targets;
     int top;
     float *logprobs, *entropy, *lse, *top_logprobs;
     int32_t* top_tokens;
     int pieces;                              // of a row
     FastDiv div_pieces;
+    int vectors;                             // of 16 bytes, that a thread has of a piece
     f32x4* sums;                             // [rows][pieces]: m, S, W; with several pieces
     uint64_t* best;                          // [rows][pieces][top], descending, the rest 0
 };
@@ -51,7 +57,7 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// The results of a row from its maximum and sums; best: its alternatives, in LDS.  All threads of the workgroup.
+// The results of a row from its reference point and sums; best: its alternatives, in LDS.  All threads of the workgroup.
 template <class T>
 __device__ __forceinline__ void finish_row(const Logprobs& a, int row, float m, float S, float W, const uint64_t* best) {
     const bool none = !(S > 0.f);            // S is NaN, or 0: no distribution
@@ -62,10 +68,7 @@ __device__ __forceinline__ void finish_row(const Logprobs& a, int row, float m, 
         if (a.targets != nullptr && a.logprobs != nullptr) {
             const int64_t t = a.targets[row];
             float lp = 0.f;
-            if (t >= 0 && t < a.cols) {
-                const float x = as_float(static_cast<const T*>(a.x)[row * a.ld + t]);
-                lp = none ? nan : fmaf(x - m, a.scale, -log_s);
-            }
+            if (t >= 0 && t < a.cols) lp = none ? nan : fmaf(as_float(static_cast<const T*>(a.x)[row * a.ld + t]) - m, a.scale, -log_s);
             a.logprobs[row] = lp;
         }
     }
@@ -82,148 +85,264 @@ __device__ __forceinline__ void rank_keys(const uint64_t* list, int n, int top, 
     for (int i = (int)threadIdx.x; i < n; i += 256) {
         const uint64_t mine = list[i];
         int above = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) above += list[j] > mine ? 1 : 0;
         if (above < top) out[above] = mine;
     }
 }
 
-// NV: 16-byte loads of a thread.
+constexpr int LP_VECTORS = 64, LP_SEGMENT = 8, LP_KEYS = 1024;       // vectors of a thread at most; those that share a maximum; the list's places
+
+// A thread's column of a piece: vector v of the piece begins at column first + 256 * V * v.  col may lie before 0 (rows need not begin at 16 bytes) or behind the last.
+template <class T, int V>
+__device__ __forceinline__ void load_columns(const Logprobs& a, const T* x, int col, float (&y)[V]) {
+    typedef T TV __attribute__((ext_vector_type(V)));
+    if (col >= 0 && col + V <= a.cols) {
+        const TV w = *reinterpret_cast<const TV*>(x + col);
+#pragma unroll
+        for (int j = 0; j < V; ++j) y[j] = as_float(w[j]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) y[j] = col + j >= 0 && col + j < a.cols ? as_float(x[col + j]) : -__builtin_inff();
+    }
+}
+
+// The number of threads for which `mine` holds, to all of them; scratch: 4 ints.
+__device__ __forceinline__ int block_count(int n, int* scratch) {
+#pragma unroll
+    for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = n;
+    __syncthreads();
+    return scratch[0] + scratch[1] + scratch[2] + scratch[3];
+}
+
+// The best of a piece.  maxima[s][t]: the largest of thread t's vectors 8 s .. + 7.  best: `top` keys in order, 0 where there are fewer.
+template <class T>
+__device__ __forceinline__ void best_of_piece(const Logprobs& a, const T* x, int piece_first, int vectors, const float (*maxima)[256], uint16_t* pairs, uint64_t* list, uint64_t* best, int* ints) {
+    constexpr int V = 16 / sizeof(T);
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), tid = (int)threadIdx.x;
+    const int segments = (vectors + LP_SEGMENT - 1) / LP_SEGMENT, first = piece_first + tid * V;
+    int &count = ints[0], &pair_count = ints[7], *scan = ints + 1, *found = ints + 5;
+    float high = -__builtin_inff();
+    for (int s = 0; s < segments; ++s) high = fmaxf(high, maxima[s][tid]);
+    const uint32_t mine = first < a.cols ? order_of(high) : 0;       // 0: no columns
+    uint32_t* orders = reinterpret_cast<uint32_t*>(list);
+    orders[tid] = mine;
+    if (tid == 0) count = pair_count = 0;
+    __syncthreads();
+    // The largest number that `top` of the threads' maxima reach; the search ends early where few more do
+    const int few = a.top + a.top / 2 + 1;
+    if (wave == 0) {
+        uint32_t o[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = orders[lane + 64 * i];
+        uint32_t border = 0;
+        int reach = 256;
+        for (int bit = 31; bit >= 0 && reach > few; --bit) {
+            const uint32_t t = border | 1u << bit;
+            int n = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) n += __popcll(__ballot(o[i] >= t));
+            if (n >= a.top) {
+                border = t;
+                reach = n;
+            }
+        }
+        if (lane == 0) {
+            found[0] = (int)border;
+            found[1] = reach;
+        }
+    }
+    __syncthreads();
+    uint32_t border = (uint32_t)found[0];
+    bool ties = found[1] > few;              // then border is exact, and fewer than `top` threads have more than it
+    // What passes the border: first which maxima do, then, a column to a thread, the columns behind them.
+    auto collect = [&]() {
+        for (int s = 0; s < segments; ++s) {
+            const uint32_t o = first < a.cols ? order_of(maxima[s][tid]) : 0;
+            if (ties ? o > border : o >= border && o != 0) pairs[atomicAdd(&pair_count, 1)] = (uint16_t)(s << 8 | tid);
+        }
+        __syncthreads();
+        const int n = pair_count * (LP_SEGMENT * V);
+        for (int i = tid; i < n; i += 256) {
+            const int pair = pairs[i / (LP_SEGMENT * V)], v = (pair >> 8) * LP_SEGMENT + i / V % LP_SEGMENT;
+            const int col = piece_first + (v * 256 + (pair & 255)) * V + i % V;
+            if (v >= vectors || col < 0 || col >= a.cols) continue;
+            const float y = as_float(x[col]);
+            const uint32_t o = order_of(y);
+            if (y == y && (ties ? o > border : o >= border)) {
+                const int at = atomicAdd(&count, 1);
+                if (at < LP_KEYS) list[at] = key_of(y, col);
+            }
+        }
+    };
+    collect();
+    __syncthreads();
+    int have = count;
+    if (have > LP_KEYS) {                    // the best lie together: the border digit by digit, over all columns
+        border = 0;
+        ties = true;
+        for (int bit = 31; bit >= 0; --bit) {
+            const uint32_t t = border | 1u << bit;
+            int n = 0;
+            for (int v = 0; v < vectors; ++v) {
+                float y[V];
+                load_columns<T, V>(a, x, first + 256 * V * v, y);
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    const int col = first + 256 * V * v + j;
+                    n += y[j] == y[j] && order_of(y[j]) >= t && col >= 0 && col < a.cols ? 1 : 0;
+                }
+            }
+            if (block_count(n, scan) >= a.top) border = t;
+        }
+        __syncthreads();
+        if (tid == 0) count = pair_count = 0;
+        __syncthreads();
+        collect();                           // fewer than `top`
+        __syncthreads();
+        have = count;
+    }
+    if (ties && have < a.top) {              // what equals the border, from the lowest column on
+        for (int v = 0; v < vectors && have < a.top; ++v) {
+            float y[V];
+            load_columns<T, V>(a, x, first + 256 * V * v, y);
+            int n = 0;
+            unsigned equal = 0;
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const int col = first + 256 * V * v + j;
+                if (y[j] == y[j] && order_of(y[j]) == border && col >= 0 && col < a.cols) equal |= 1u << j;
+            }
+            n = __popc(equal);
+            int upto = n;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int other = __shfl_up(upto, d);
+                if (lane >= d) upto += other;
+            }
+            if (lane == 63) scan[wave] = upto;
+            __syncthreads();
+            int at = have + upto - n;
+            for (int w = 0; w < wave; ++w) at += scan[w];
+#pragma unroll
+            for (int j = 0; j < V; ++j)
+                if (equal >> j & 1) {
+                    if (at < a.top) list[at] = key_of(y[j], first + 256 * V * v + j);
+                    ++at;
+                }
+            have += scan[0] + scan[1] + scan[2] + scan[3];
+            __syncthreads();
+        }
+        have = min(have, a.top);
+    }
+    __syncthreads();
+    rank_keys(list, have, a.top, best);
+    __syncthreads();
+}
+
+// NV: vectors of a thread that are computed together, while as many of the next are loaded.
 template <class T, int NV, bool TOP>
 __global__ __launch_bounds__(256) void logprobs_kernel(Logprobs a) {
     constexpr int V = 16 / sizeof(T);
     typedef T TV __attribute__((ext_vector_type(V)));
-    extern __shared__ uint64_t list[];
     __shared__ float part[3][4];
-    __shared__ uint32_t maxima[TOP ? 256 : 1];
-    __shared__ uint64_t best[TOP ? LP_MAX_TOP : 1];
-    __shared__ uint32_t border_s[2];
-    __shared__ int count, scan[4];
+    __shared__ float maxima[TOP ? LP_VECTORS / LP_SEGMENT : 1][256];
+    __shared__ uint64_t list[TOP ? LP_KEYS : 1], best[TOP ? LP_MAX_TOP : 1];
+    __shared__ uint16_t pairs[TOP ? 256 * LP_VECTORS / LP_SEGMENT : 1];
+    __shared__ int ints[8];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int row = fast_div((int)blockIdx.x, a.div_pieces), piece = (int)blockIdx.x - row * a.pieces;
     const T* x = static_cast<const T*>(a.x) + row * a.ld;
-    const int off = (int)(reinterpret_cast<uintptr_t>(x) / sizeof(T) % V);          // columns before the first whole 16 bytes lie in slot 0
-    const int first = piece * (256 * NV * V) - off + (int)threadIdx.x * V;          // column of the thread's first element; its v-th vector begins 256 * V * v later
-    float y[NV][V];
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-        const int col = first + v * 256 * V;
-        if (col >= 0 && col + V <= a.cols) {
-            const TV w = *reinterpret_cast<const TV*>(x + col);
-#pragma unroll
-            for (int j = 0; j < V; ++j) y[v][j] = as_float(w[j]);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) y[v][j] = col + j >= 0 && col + j < a.cols ? as_float(x[col + j]) : -__builtin_inff();
-        }
-    }
-    float high = -__builtin_inff();
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int j = 0; j < V; ++j) high = fmaxf(high, y[v][j]);
-    const float wave_high = wave_max(high);
-    if (lane == 0) part[0][wave] = wave_high;
-    if constexpr (TOP) maxima[threadIdx.x] = first < a.cols && first + (NV - 1) * 256 * V + V > 0 ? order_of(high) : 0;
-    if (threadIdx.x == 0) count = 0;
-    __syncthreads();
-    const float m = fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3]));
-    const float shift = m == -__builtin_inff() ? 0.f : m;
-    float S = 0.f, W = 0.f;
-#pragma unroll
-    for (int v = 0; v < NV; ++v)
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float u = (y[v][j] - shift) * a.scale2, e = __builtin_amdgcn_exp2f(u);
-            S += e;
-            W = fmaf(e, fmaxf(u, -1e30f), W);
-        }
-    S = wave_sum(S);
-    W = wave_sum(W);
-    if (lane == 0) {
-        part[1][wave] = S;
-        part[2][wave] = W;
-    }
+    const int off = (int)(reinterpret_cast<uintptr_t>(x) / sizeof(T) % V);          // columns before the first whole 16 bytes lie in vector 0
+    const int piece_first = piece * a.vectors * (256 * V) - off, first = piece_first + (int)threadIdx.x * V;
+    const int vectors = min(a.vectors, (a.cols - piece_first + 256 * V - 1) / (256 * V));       // with columns
+    const float c = a.scale2;
 
-    if constexpr (TOP) {
-        // The largest number that `top` of the threads' maxima reach; the search ends early where few more do
-        const int few = a.top + a.top / 2 + 1;
-        if (wave == 0) {
-            uint32_t mine[4];
+    float m = 0.f, limit = -__builtin_inff(), S = 0.f, W = 0.f;      // limit: what a column may be before m is raised; -infinity: nothing but -infinity so far
+    float segment = -__builtin_inff();
+    auto group = [&](const float (&y)[NV][V], int v0) {
+        float high = -__builtin_inff();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mine[i] = maxima[lane + 64 * i];
-            uint32_t border = 0;
-            int reach = 256;
-            for (int bit = 31; bit >= 0 && reach > few; --bit) {
-                const uint32_t t = border | 1u << bit;
-                int n = 0;
+        for (int v = 0; v < NV; ++v) {
+            float h = y[v][0];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) n += __popcll(__ballot(mine[i] >= t));
-                if (n >= a.top) {
-                    border = t;
-                    reach = n;
-                }
-            }
-            if (lane == 0) {
-                border_s[0] = border;
-                border_s[1] = (uint32_t)reach;
+            for (int j = 1; j < V; ++j) h = fmaxf(h, y[v][j]);
+            high = fmaxf(high, h);
+        }
+        if (__ballot(high > limit) != 0) {
+            const float top = wave_max(high), d = limit == -__builtin_inff() ? 0.f : (m - top) * c, f = __builtin_amdgcn_exp2f(d);
+            W = f * fmaf(S, fmaxf(d, -1e30f), W);
+            S *= f;
+            m = top;
+            limit = top + a.slack;
+        }
+        if constexpr (TOP) {
+            segment = fmaxf(segment, high);
+            if (v0 % LP_SEGMENT + NV == LP_SEGMENT || v0 + NV >= vectors) {
+                maxima[v0 / LP_SEGMENT][threadIdx.x] = segment;
+                segment = -__builtin_inff();
             }
         }
-        __syncthreads();
-        const uint32_t border = border_s[0];
-        const bool ties = (int)border_s[1] > few;        // then border is exact, and fewer than `top` threads have more than it: what equals it is taken in the order of columns
-        if (maxima[threadIdx.x] >= border) {
+#pragma unroll
+        for (int v = 0; v < NV; ++v)
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float u = (y[v][j] - m) * c, e = __builtin_amdgcn_exp2f(u);
+                S += e;
+                W = fmaf(e, fmaxf(u, -1e30f), W);
+            }
+    };
+    // Groups of vectors whose columns all exist: [from, to)
+    const int groups = (vectors + NV - 1) / NV, from = piece_first < 0 ? 1 : 0, to = max(from, min(groups, (a.cols - piece_first) / (256 * V * NV)));
+    auto edge = [&](int g) {
+        float y[NV][V];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) load_columns<T, V>(a, x, first + (g * NV + v) * 256 * V, y[v]);
+        group(y, g * NV);
+    };
+    if (from > 0 && groups > 0) edge(0);
+    if (from < to) {
+        TV next[NV];
+#pragma unroll
+        for (int v = 0; v < NV; ++v) next[v] = *reinterpret_cast<const TV*>(x + first + (from * NV + v) * 256 * V);
+        for (int g = from; g < to; ++g) {
+            float y[NV][V];
 #pragma unroll
             for (int v = 0; v < NV; ++v)
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const int col = first + v * 256 * V + j;
-                    const uint32_t o = order_of(y[v][j]);
-                    if ((ties ? o > border : o >= border) && col >= 0 && col < a.cols && y[v][j] == y[v][j]) list[atomicAdd(&count, 1)] = key_of(y[v][j], col);
-                }
-        }
-        __syncthreads();
-        int have = count;
-        if (ties && have < a.top) {
-            for (int v = 0; v < NV; ++v) {
-                int n = 0;
+                for (int j = 0; j < V; ++j) y[v][j] = as_float(next[v][j]);
+            if (g + 1 < to) {
 #pragma unroll
-                for (int u = 0; u < NV; ++u)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const int col = first + u * 256 * V + j;
-                        n += u == v && order_of(y[u][j]) == border && col >= 0 && col < a.cols ? 1 : 0;
-                    }
-                int upto = n;
-#pragma unroll
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int other = __shfl_up(upto, d);
-                    if (lane >= d) upto += other;
-                }
-                if (lane == 63) scan[wave] = upto;
-                __syncthreads();
-                int at = have + upto - n;
-                for (int w = 0; w < wave; ++w) at += scan[w];
-#pragma unroll
-                for (int u = 0; u < NV; ++u)
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const int col = first + u * 256 * V + j;
-                        if (u == v && order_of(y[u][j]) == border && col >= 0 && col < a.cols) {
-                            if (at < a.top) list[at] = key_of(y[u][j], col);
-                            ++at;
-                        }
-                    }
-                have += scan[0] + scan[1] + scan[2] + scan[3];
-                __syncthreads();
-                if (have >= a.top) break;
+                for (int v = 0; v < NV; ++v) next[v] = *reinterpret_cast<const TV*>(x + first + ((g + 1) * NV + v) * 256 * V);
             }
-            have = min(have, a.top);
+            group(y, g * NV);
         }
-        rank_keys(list, have, a.top, best);
+    }
+    for (int g = max(from, to); g < groups; ++g) edge(g);
+
+    // Lanes of a wave share m
+    S = wave_sum(S);
+    W = wave_sum(W);
+    if (lane == 0) {
+        part[0][wave] = limit == -__builtin_inff() ? -__builtin_inff() : m;
+        part[1][wave] = S;
+        part[2][wave] = W;
     }
     __syncthreads();
-    S = part[1][0] + part[1][1] + part[1][2] + part[1][3];
-    W = part[2][0] + part[2][1] + part[2][2] + part[2][3];
+    if constexpr (TOP) best_of_piece<T>(a, x, piece_first, vectors, maxima, pairs, list, best, ints);
+    m = fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3]));
+    if (m == -__builtin_inff()) m = 0.f;
+    S = 0.f;
+    W = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if (part[1][w] == 0.f) continue;     // (NaN goes on)
+        const float d = (part[0][w] - m) * c, f = __builtin_amdgcn_exp2f(d);
+        S = fmaf(part[1][w], f, S);
+        W = fmaf(f, fmaf(part[1][w], fmaxf(d, -1e30f), part[2][w]), W);
+    }
     if (a.pieces == 1) {
         finish_row<T>(a, row, m, S, W, best);
     } else {
@@ -233,12 +352,13 @@ __global__ __launch_bounds__(256) void logprobs_kernel(Logprobs a) {
     }
 }
 
-constexpr int LP_LIST = 1024;                // keys that are looked at together
+constexpr int LP_LIST = 2048;                // keys that are looked at together
 
 // Joins the pieces of a row.  Each piece's best come in order; of L pieces the ceil(top / L) best each are at least `top`, and the `top`-th of those is a border that little more reach.
 template <class T>
 __global__ __launch_bounds__(256) void logprobs_join_kernel(Logprobs a) {
     __shared__ uint64_t list[LP_LIST], reach[LP_LIST], best[LP_MAX_TOP];
+    uint64_t* const heads = reach;           // (before it has what reaches the border)
     __shared__ float part[3][4];
     __shared__ uint64_t border;
     __shared__ int count;
@@ -246,19 +366,22 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(Logprobs a) {
     const int row = (int)blockIdx.x;
     const f32x4* sums = a.sums + (long long)row * a.pieces;
     float m = -__builtin_inff();
-    for (int i = (int)threadIdx.x; i < a.pieces; i += 256) m = fmaxf(m, sums[i][0]);
+    for (int i = (int)threadIdx.x; i < a.pieces; i += 256) {
+        const f32x4 p = sums[i];
+        if (p[1] != 0.f) m = fmaxf(m, p[0]);
+    }
     m = wave_max(m);
     if (lane == 0) part[0][wave] = m;
     __syncthreads();
     m = fmaxf(fmaxf(part[0][0], part[0][1]), fmaxf(part[0][2], part[0][3]));
-    const float shift = m == -__builtin_inff() ? 0.f : m;
+    if (m == -__builtin_inff()) m = 0.f;
     float S = 0.f, W = 0.f;
     for (int i = (int)threadIdx.x; i < a.pieces; i += 256) {
         const f32x4 p = sums[i];
         if (p[1] == 0.f) continue;           // (NaN goes on)
-        const float u = (p[0] - shift) * a.scale2, f = __builtin_amdgcn_exp2f(u);
+        const float d = (p[0] - m) * a.scale2, f = __builtin_amdgcn_exp2f(d);
         S = fmaf(p[1], f, S);
-        W = fmaf(f, fmaf(p[1], fmaxf(u, -1e30f), p[2]), W);
+        W = fmaf(f, fmaf(p[1], fmaxf(d, -1e30f), p[2]), W);
     }
     S = wave_sum(S);
     W = wave_sum(W);
@@ -282,11 +405,13 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(Logprobs a) {
             }
             __syncthreads();
             const int deep = (a.top + lists - 1) / lists, set = lists * deep;      // set < top + lists
+            for (int i = (int)threadIdx.x; i < set; i += 256) heads[i] = list[i / deep * a.top + i % deep];
+            __syncthreads();
             for (int i = (int)threadIdx.x; i < set; i += 256) {
-                const uint64_t mine = list[i / deep * a.top + i % deep];
+                const uint64_t mine = heads[i];
                 int above = 0;
-                for (int l = 0; l < lists; ++l)
-                    for (int j = 0; j < deep; ++j) above += list[l * a.top + j] > mine ? 1 : 0;
+#pragma unroll 8
+                for (int j = 0; j < set; ++j) above += heads[j] > mine ? 1 : 0;
                 if (above == a.top - 1) border = mine;
             }
             __syncthreads();
@@ -303,17 +428,21 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(Logprobs a) {
 
 inline int size_of(int dtype) { return dtype == BNN_F32 || dtype == BNN_I32 ? 4 : dtype == BNN_BF16 || dtype == BNN_F16 ? 2 : 0; }
 
-// How rows are cut up: pieces of 256 threads with 8 loads of 16 bytes each, or 2 where that makes too few workgroups.
+// How rows are cut up: into pieces of up to 64 vectors of 16 bytes a thread, as many as make 512 workgroups.  `at` and ld tell whether rows begin at 16 bytes (a vector more else); without them the
+// most that a workspace is asked for.
+constexpr int LP_GROUPS = 512;
 struct LogprobsPlan {
-    int loads, pieces;
+    int group, vectors, pieces;              // group: vectors computed together
     size_t sums_bytes, bytes;
 };
-LogprobsPlan plan_logprobs(int rows, int cols, int size, int top) {
+LogprobsPlan plan_logprobs(int rows, int cols, int size, int top, bool aligned) {
     LogprobsPlan p = {};
     const int v = 16 / size;
-    p.loads = 8;
-    if ((long long)rows * cdiv(cols, 256LL * 8 * v) < 1024) p.loads = 2;
-    p.pieces = (int)cdiv((long long)cols + v - 1, 256LL * p.loads * v);            // a row may begin within 16 bytes
+    const long long most = cdiv((long long)cols + v - 1, 256LL * v);
+    const long long want = cdiv(most * rows, LP_GROUPS);
+    p.group = want < 4 ? 1 : 4;
+    p.vectors = (int)std::min<long long>(LP_VECTORS, p.group == 1 ? want : cdiv(want, 4) * 4);
+    p.pieces = (int)cdiv(aligned ? cdiv(cols, 256LL * v) : most, p.vectors);
     if (p.pieces > 1) {
         p.sums_bytes = (size_t)rows * p.pieces * sizeof(f32x4);
         p.bytes = p.sums_bytes + (size_t)rows * p.pieces * top * sizeof(uint64_t);
@@ -322,15 +451,14 @@ LogprobsPlan plan_logprobs(int rows, int cols, int size, int top) {
 }
 
 template <class T>
-int launch_logprobs(const Logprobs& a, int loads, hipStream_t s) {
+int launch_logprobs(const Logprobs& a, int group, hipStream_t s) {
     const dim3 grid((unsigned)((long long)a.rows * a.pieces));
-    const size_t lds = a.top == 0 ? 0 : std::min<size_t>(a.top + a.top / 2 + 1, 256) * loads * (16 / sizeof(T)) * sizeof(uint64_t);
     if (a.top == 0) {
-        if (loads == 8) launch(logprobs_kernel<T, 8, false>, grid, dim3(256), 0, s, a);
-        else launch(logprobs_kernel<T, 2, false>, grid, dim3(256), 0, s, a);
+        if (group == 4) launch(logprobs_kernel<T, 4, false>, grid, dim3(256), 0, s, a);
+        else launch(logprobs_kernel<T, 1, false>, grid, dim3(256), 0, s, a);
     } else {
-        if (loads == 8) launch(logprobs_kernel<T, 8, true>, grid, dim3(256), lds, s, a);
-        else launch(logprobs_kernel<T, 2, true>, grid, dim3(256), lds, s, a);
+        if (group == 4) launch(logprobs_kernel<T, 4, true>, grid, dim3(256), 0, s, a);
+        else launch(logprobs_kernel<T, 1, true>, grid, dim3(256), 0, s, a);
     }
     if (a.pieces > 1) launch(logprobs_join_kernel<T>, dim3((unsigned)a.rows), dim3(256), 0, s, a);
     return check_launch();
@@ -345,7 +473,7 @@ extern "C" {
 
 size_t bnn_token_logprobs_workspace_bytes(int rows, int cols, int dtype, int top) {
     if (rows < 1 || cols < 1 || size_of(dtype) == 0 || top < 0 || top > LP_MAX_TOP || cols >= (1 << 30)) return 0;
-    return plan_logprobs(rows, cols, size_of(dtype), top).bytes;
+    return plan_logprobs(rows, cols, size_of(dtype), top, false).bytes;
 }
 
 int bnn_token_logprobs(const void* logits, int dtype, int rows, int cols, int64_t ld, float scale, const int64_t* targets, int top,
@@ -360,24 +488,25 @@ int bnn_token_logprobs(const void* logits, int dtype, int rows, int cols, int64_
     for (const void* p : words)
         if (reinterpret_cast<uintptr_t>(p) & 3u) return BNN_ERR_ALIGNMENT;
     if (reinterpret_cast<uintptr_t>(logits) % size || (reinterpret_cast<uintptr_t>(targets) & 7u)) return BNN_ERR_ALIGNMENT;
-    const LogprobsPlan p = plan_logprobs(rows, cols, size, top);
+    const LogprobsPlan p = plan_logprobs(rows, cols, size, top, reinterpret_cast<uintptr_t>(logits) % 16 == 0 && (rows == 1 || ld * size % 16 == 0));
     if ((long long)rows * p.pieces >= C4_THREADS / 256) return BNN_ERR_UNSUPPORTED;
     if (p.bytes != 0 && (!workspace || workspace_bytes < p.bytes)) return BNN_ERR_WORKSPACE;
     if (p.bytes != 0 && (reinterpret_cast<uintptr_t>(workspace) & 15u)) return BNN_ERR_ALIGNMENT;
     Logprobs a = {};
     a.x = logits; a.rows = rows; a.cols = cols; a.ld = ld;
     a.scale = scale; a.scale2 = scale2;
+    a.slack = 16.f / scale2;
     a.targets = targets; a.top = top;
     a.logprobs = logprobs; a.entropy = entropy; a.lse = lse; a.top_logprobs = top_logprobs; a.top_tokens = top_tokens;
-    a.pieces = p.pieces;
+    a.pieces = p.pieces; a.vectors = p.vectors;
     a.div_pieces = make_fastdiv((uint32_t)p.pieces);
     a.sums = static_cast<f32x4*>(workspace);
     a.best = reinterpret_cast<uint64_t*>(static_cast<char*>(workspace) + p.sums_bytes);
     hipStream_t s = static_cast<hipStream_t>(stream);
-    if (dtype == BNN_BF16) return launch_logprobs<__bf16>(a, p.loads, s);
-    if (dtype == BNN_F16) return launch_logprobs<_Float16>(a, p.loads, s);
-    if (dtype == BNN_I32) return launch_logprobs<int32_t>(a, p.loads, s);
-    return launch_logprobs<float>(a, p.loads, s);
+    if (dtype == BNN_BF16) return launch_logprobs<__bf16>(a, p.group, s);
+    if (dtype == BNN_F16) return launch_logprobs<_Float16>(a, p.group, s);
+    if (dtype == BNN_I32) return launch_logprobs<int32_t>(a, p.group, s);
+    return launch_logprobs<float>(a, p.group, s);
 }
 
 }  // extern "C"

@@ -134,6 +134,46 @@ def test_ties_go_to_the_lower_column(bnn, cols, top):
     check(bnn, (x[:7] * 3).round().int(), t[:7].contiguous(), 0.5, top=top)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_the_best_side_by_side(bnn, dtype):
+    """The best all in few threads' columns, by the hundred: distinct (the border is then found over all columns), and equal."""
+    rng = np.random.default_rng(8)
+    for cols, rows in ((131072, 3), (9000, 700)):
+        x = torch.from_numpy(rng.standard_normal((rows, cols))).float()
+        together = (torch.arange(cols) % 2048) < 24                  # three threads' of every 2048 columns, or six
+        few = torch.arange(rows) < 3
+        x[0, together] += 20
+        x[1, together] = 20
+        x[2, together] = 20 + torch.arange(int(together.sum())) / 64.0
+        x = x[few].repeat(rows // 3 + 1, 1)[:rows].to(TYPES[dtype]).cuda()
+        t = tokens_for(rng, rows, cols)
+        got = bnn.token_logprobs(x, t, top=64)
+        check(bnn, x[:3], t[:3].contiguous(), top=64)
+        if rows > 3:
+            one = bnn.token_logprobs(x[:3], t[:3].contiguous(), top=64)
+            assert torch.equal(got.top_tokens, one.top_tokens.repeat(rows // 3 + 1, 1)[:rows])
+
+
+def test_long_rows_after_low_beginnings(bnn):
+    """A wave's reference point is taken from its first columns: rows that begin low, at the lowest number, at -infinity, and rise in steps or at once."""
+    rng = np.random.default_rng(9)
+    x = torch.from_numpy(rng.standard_normal((6, 100003))).float()
+    x[0, :60000] -= 1e4
+    x[1, :60000] = torch.finfo(torch.float32).min
+    x[2, :60000] = float("-inf")
+    x[3] += torch.arange(100003) / 1000.0
+    x[4, -1] += 80
+    x[5] -= torch.arange(100003) / 1000.0
+    check(bnn, x.cuda(), tokens_for(rng, 6, 100003), top=20)
+    check(bnn, x.cuda(), tokens_for(rng, 6, 100003), scale=0.01, top=3)
+    big = x.repeat(200, 1).cuda()                                    # rows enough for one piece each
+    got, want = bnn.token_logprobs(big, top=20), bnn.token_logprobs(x.cuda(), top=20)
+    assert torch.equal(got.top_tokens, want.top_tokens.repeat(200, 1))
+    # two orders of the same sums: twice the bounds of check()
+    assert ((got.lse - want.lse.repeat(200)).abs() <= 2 * (128 + 8 * 12) * U + 8 * U * (want.lse.repeat(200).abs() + 12)).all()
+    assert ((got.entropy - want.entropy.repeat(200)).abs() <= 2 * (128 + 8 * 12) * U * 13).all()
+
+
 def test_scales(bnn):
     rng = np.random.default_rng(6)
     x = logits_of(rng, 5, 3001, "f32")

@@ -506,8 +506,9 @@ int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const
                      void* workspace, size_t workspace_bytes, void* stream);
 /* tokens [batch][kv_heads][keep]: of the tokens of every sequence that lie on a page, all if they are `keep` at most, else the first `first` and last `last` (of the numbers 0 .. lens[b] - 1)
  * and of the others those with the largest weights; ascending, the rest -1.  Ties go to the lower token; NaN is below every number.  kept [batch]: how many.  first + last <= keep. */
+size_t bnn_cache4_heaviest_workspace_bytes(const bnn_cache4* cache, int batch, int table_pages);      /* (long sequences, few of them; else 0) */
 int bnn_cache4_heaviest(const bnn_cache4* cache, const int32_t* table, const int32_t* lens, int batch, int table_pages, const float* weights, int64_t width,
-                        int keep, int first, int last, int32_t* tokens, int32_t* kept, void* stream);
+                        int keep, int first, int last, int32_t* tokens, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
 /* Token tokens[b][h][i] of the sequence that `table` describes, kv head h, becomes token i of the one that `into` [batch][into_pages] describes: codes, scales and signs as they are.  The
  * pages of `into` are others than those of `table` (their contents are not defined else), and not shared.  Entries below 0, what lies on no page, and places past `into`'s end are passed over.
  * weights, moved: both or neither; moved [batch][kv_heads][into_pages * page] gets the tokens' weights, 0 where there is no token. */

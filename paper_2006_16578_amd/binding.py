@@ -36,7 +36,7 @@ EXPORTS = ["bnn_status_string", "bnn_version", "bnn_bmm_kernel_name", "bnn_bconv
            "bnn_net_add_conv", "bnn_net_add_pool", "bnn_net_add_block", "bnn_net_add_head_f32", "bnn_net_workspace_bytes",
            "bnn_net_forward", "bnn_net_forward_static", "bnn_static_workspace_init", "bnn_net_forward_persistent", "bnn_net_persistent_status", "bnn_net_fc_run", "bnn_net_layer_bits",
            "bnn_rotary", "bnn_cache4_record_bytes", "bnn_cache4_write", "bnn_cache4_write_rotary", "bnn_cache4_read", "bnn_cache4_select_workspace_bytes", "bnn_cache4_select",
-           "bnn_cache4_attend_workspace_bytes", "bnn_cache4_attend", "bnn_cache4_weigh_workspace_bytes", "bnn_cache4_weigh", "bnn_cache4_heaviest", "bnn_cache4_move",
+           "bnn_cache4_attend_workspace_bytes", "bnn_cache4_attend", "bnn_cache4_weigh_workspace_bytes", "bnn_cache4_weigh", "bnn_cache4_heaviest_workspace_bytes", "bnn_cache4_heaviest", "bnn_cache4_move",
            "bnn_token_logprobs_workspace_bytes", "bnn_token_logprobs"]
 
 
@@ -76,6 +76,7 @@ def load() -> ctypes.CDLL:
         lib.bnn_cache4_record_bytes.restype = ctypes.c_size_t
         lib.bnn_cache4_select_workspace_bytes.restype = ctypes.c_size_t
         lib.bnn_cache4_attend_workspace_bytes.restype = ctypes.c_size_t
+        lib.bnn_cache4_heaviest_workspace_bytes.restype = ctypes.c_size_t
         lib.bnn_cache4_weigh_workspace_bytes.restype = ctypes.c_size_t
         lib.bnn_token_logprobs_workspace_bytes.restype = ctypes.c_size_t
         for name in EXPORTS:
@@ -1097,7 +1098,7 @@ class Cache4:
                                            ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream(q)), "bnn_cache4_weigh")
         return out
 
-    def heaviest(self, weights, table, lens, keep: int, first: int = 0, last: int = 0):
+    def heaviest(self, weights, table, lens, keep: int, first: int = 0, last: int = 0, workspace=None):
         """(int32 [batch][kv_heads][keep], int32 [batch]): the tokens of every sequence to keep, ascending, the rest -1, and how many: all of a sequence of up to `keep`, else
         the first `first`, the last `last` and those with the largest weights.  Ties go to the lower token."""
         _dev(table, torch.int32, 2, "table"); _dev(lens, torch.int32, 1, "lens")
@@ -1111,9 +1112,14 @@ class Cache4:
             raise ValueError("keep >= 1 expected")
         tokens = torch.empty((batch, self.kv_heads, int(keep)), dtype=torch.int32, device=weights.device)
         kept = torch.empty(batch, dtype=torch.int32, device=weights.device)
+        if workspace is None:
+            need = int(load().bnn_cache4_heaviest_workspace_bytes(self._struct(), batch, width))
+            workspace = torch.empty(need, dtype=torch.uint8, device=weights.device) if need else None
+        else:
+            self._workspace(workspace)
         with _on(weights):
             _check(load().bnn_cache4_heaviest(self._struct(), _ptr(table), _ptr(lens), batch, width, _ptr(weights), ctypes.c_int64(weights.shape[2]), int(keep), int(first), int(last),
-                                              _ptr(tokens), _ptr(kept), _stream(weights)), "bnn_cache4_heaviest")
+                                              _ptr(tokens), _ptr(kept), _ptr(workspace), ctypes.c_size_t(0 if workspace is None else workspace.numel()), _stream(weights)), "bnn_cache4_heaviest")
         return tokens, kept
 
     def move(self, tokens, table, into, weights=None):

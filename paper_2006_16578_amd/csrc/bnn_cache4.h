@@ -308,7 +308,13 @@ struct Heaviest4 {
     int batch, table_pages, keep, first, last;
     int32_t *tokens, *kept;                  // [batch][kv_heads][keep], [batch]
 };
-int launch_cache4_heaviest(const Heaviest4& a, hipStream_t s);
+// How the choice is cut up.  parts: of a sequence, of 8192 tokens each, 0: one workgroup has a sequence and kv head.
+struct HeaviestPlan4 {
+    int parts;
+    size_t bins_bytes, borders_bytes, workspace_bytes;
+};
+HeaviestPlan4 plan_cache4_heaviest(const Cache4& c, int batch, int table_pages);
+int launch_cache4_heaviest(const Heaviest4& a, const HeaviestPlan4& plan, void* workspace, hipStream_t s);
 struct Move4 {
     Cache4 c;
     const int32_t* tokens;                   // [batch][kv_heads][keep]

@@ -324,8 +324,14 @@ int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const
     return launch_cache4_weigh(a, p, dtype, static_cast<hipStream_t>(stream));
 }
 
+size_t bnn_cache4_heaviest_workspace_bytes(const bnn_cache4* cache, int batch, int table_pages) {
+    Cache4 c;
+    if (make_cache(cache, c) != BNN_OK || batch < 1 || table_pages < 1 || ((long long)table_pages << c.page_shift) > (1LL << 30)) return 0;
+    return plan_cache4_heaviest(c, batch, table_pages).workspace_bytes;
+}
+
 int bnn_cache4_heaviest(const bnn_cache4* cache, const int32_t* table, const int32_t* lens, int batch, int table_pages, const float* weights, int64_t width,
-                        int keep, int first, int last, int32_t* tokens, int32_t* kept, void* stream) {
+                        int keep, int first, int last, int32_t* tokens, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream) {
     Heaviest4 a = {};
     const int rc = make_cache(cache, a.c);
     if (rc != BNN_OK) return rc;
@@ -340,7 +346,10 @@ int bnn_cache4_heaviest(const bnn_cache4* cache, const int32_t* table, const int
     a.table = table; a.lens = lens; a.batch = batch; a.table_pages = table_pages;
     a.keep = keep; a.first = first; a.last = last;
     a.tokens = tokens; a.kept = kept;
-    return launch_cache4_heaviest(a, static_cast<hipStream_t>(stream));
+    const HeaviestPlan4 p = plan_cache4_heaviest(a.c, batch, table_pages);
+    if (p.workspace_bytes != 0 && (!workspace || workspace_bytes < p.workspace_bytes)) return BNN_ERR_WORKSPACE;
+    if (p.workspace_bytes != 0 && !aligned16(workspace)) return BNN_ERR_ALIGNMENT;
+    return launch_cache4_heaviest(a, p, workspace, static_cast<hipStream_t>(stream));
 }
 
 int bnn_cache4_move(const bnn_cache4* cache, const int32_t* tokens, int keep, const int32_t* table, int table_pages, const int32_t* into, int into_pages, int batch,

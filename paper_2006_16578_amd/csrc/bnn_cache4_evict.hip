@@ -19,13 +19,116 @@ __device__ __forceinline__ uint32_t rank_of(float w) {
     return bits & 0x80000000u ? ~bits : bits | 0x80000000u;
 }
 
+// Four tokens of a lane.  (Pages and tables have room for multiples of 16: what begins inside lies inside.)
+struct Four {
+    f32x4 weight;
+    int page;
+};
+__device__ __forceinline__ Four fetch_four(const float* weights, const int32_t* table, int page_shift, int j, int end) {
+    Four f = {f32x4{0.f, 0.f, 0.f, 0.f}, -1};
+    if (j < end) {
+        __builtin_memcpy(&f.weight, weights + j, 16);
+        f.page = table[j >> page_shift];
+    }
+    return f;
+}
+// 0: nowhere; kept in any case: the highest; else a number between
+__device__ __forceinline__ void rank_four(const Heaviest4& a, const Four& f, int j, int end, int length, uint32_t (&r)[4]) {
+    const bool there = (uint32_t)f.page < (uint32_t)a.c.pages;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int t = j + i;
+        r[i] = t < a.first || t >= length - a.last ? 0xffffffffu : min(max(rank_of(f.weight[i]), 1u), 0xfffffffeu);
+        if (!there || t >= end) r[i] = 0;
+    }
+}
+
+// What is known of the lowest rank that is kept: its digits so far, and how many of those that agree with them are kept.
+struct Border {
+    uint32_t rank;
+    int count;
+};
+__device__ __forceinline__ int digit_shift(int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; }
+__device__ __forceinline__ int digit_width(int digit) { return digit == 2 ? 10 : 11; }
+__device__ __forceinline__ bool digit_counts(uint32_t r, const Border& border, int digit) {
+    return r != 0 && (digit == 0 || r >> (digit_shift(digit) + digit_width(digit)) == border.rank >> (digit_shift(digit) + digit_width(digit)));
+}
+__device__ __forceinline__ int digit_of(uint32_t r, int digit) { return (int)(r >> digit_shift(digit) & ((1u << digit_width(digit)) - 1)); }
+
+// The next digit: from the highest bin down the one in which the count reaches border.count.  A thread has the bins 2047 - 2 t and 2046 - 2 t; there is such a bin.  Begins and ends with a barrier for `shared`.
+struct PickShared {
+    int wave_sum[H_WAVES], picked[2];
+};
+__device__ __forceinline__ void pick_digit(Border& border, int digit, int high, int low, PickShared& shared) {
+    const int lane = (int)threadIdx.x & 63, wave = (int)threadIdx.x >> 6, top = H_BINS - 1 - 2 * (int)threadIdx.x;
+    int upto = high + low;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int other = __shfl_up(upto, d);
+        if (lane >= d) upto += other;
+    }
+    if (lane == 63) shared.wave_sum[wave] = upto;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) upto += shared.wave_sum[w];
+    const int before = upto - high - low;
+    if (before < border.count && upto >= border.count) {
+        const bool first = before + high >= border.count;
+        shared.picked[0] = first ? top : top - 1;
+        shared.picked[1] = border.count - before - (first ? 0 : high);
+    }
+    __syncthreads();
+    border.rank |= (uint32_t)shared.picked[0] << digit_shift(digit);
+    border.count = shared.picked[1];
+}
+
+// Writes a wave's kept tokens, vector by vector: place: of the next; equals: how many of the border's rank came before.
+struct Emit {
+    int32_t* out;
+    Border border;
+    int place, equals;
+    // lanes before this one, in a mask
+    __device__ __forceinline__ static int before(unsigned long long mask) {
+        return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+    }
+    __device__ __forceinline__ void operator()(const uint32_t (&r)[4], int j) {
+        bool keep[4];
+        unsigned long long e[4], any = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            e[i] = __ballot(r[i] == border.rank);
+            any |= e[i];
+            keep[i] = r[i] > border.rank;
+        }
+        if (any != 0) {                      // which of those at the border: the lowest
+            int n = equals + before(e[0]) + before(e[1]) + before(e[2]) + before(e[3]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (r[i] == border.rank) {
+                    keep[i] = n < border.count;
+                    ++n;
+                }
+                equals += __popcll(e[i]);
+            }
+        }
+        unsigned long long k[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[i] = __ballot(keep[i]);
+        int at = place + before(k[0]) + before(k[1]) + before(k[2]) + before(k[3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (keep[i]) out[at++] = j + i;
+            place += __popcll(k[i]);
+        }
+    }
+};
+
 // E: vectors of a wave that its registers hold; 0: none.
 template <int E>
 __global__ __launch_bounds__(H_THREADS) void heaviest_kernel(Heaviest4 a) {
     constexpr int LOADS = E == 0 ? 8 : E;    // under way together
     __shared__ int bins[H_BINS];
-    __shared__ int wave_above[H_WAVES], wave_equal[H_WAVES], wave_there[H_WAVES], wave_sum[H_WAVES];
-    __shared__ int picked[2];
+    __shared__ int wave_above[H_WAVES], wave_equal[H_WAVES], wave_there[H_WAVES];
+    __shared__ PickShared shared;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int b = (int)blockIdx.x, head = (int)blockIdx.y;
     const int length = (int)min((long long)max(a.lens[b], 0), (long long)a.table_pages << a.c.page_shift);
@@ -35,29 +138,8 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_kernel(Heaviest4 a) {
     const int32_t* table = a.table + (long long)b * a.table_pages;
     int32_t* out = a.tokens + ((long long)b * a.c.kv_heads + head) * a.keep;
 
-    // Four tokens of a lane.  (Pages and tables have room for multiples of 16: what begins inside lies inside.)
-    struct Four {
-        f32x4 weight;
-        int page;
-    };
-    auto fetch = [&](int j) -> Four {
-        Four f = {f32x4{0.f, 0.f, 0.f, 0.f}, -1};
-        if (j < end) {
-            __builtin_memcpy(&f.weight, weights + j, 16);
-            f.page = table[j >> a.c.page_shift];
-        }
-        return f;
-    };
-    // 0: nowhere; kept in any case: the highest; else a number between
-    auto rank = [&](const Four& f, int j, uint32_t (&r)[4]) {
-        const bool there = (uint32_t)f.page < (uint32_t)a.c.pages;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int t = j + i;
-            r[i] = t < a.first || t >= length - a.last ? 0xffffffffu : min(max(rank_of(f.weight[i]), 1u), 0xfffffffeu);
-            if (!there || t >= end) r[i] = 0;
-        }
-    };
+    auto fetch = [&](int j) { return fetch_four(weights, table, a.c.page_shift, j, end); };
+    auto rank = [&](const Four& f, int j, uint32_t (&r)[4]) { rank_four(a, f, j, end, length, r); };
     uint32_t held[E == 0 ? 1 : E][4];
     if constexpr (E > 0) {
         Four f[E];
@@ -109,44 +191,22 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_kernel(Heaviest4 a) {
     const int kept = min(there, a.keep);
     if (head == 0 && threadIdx.x == 0) a.kept[b] = kept;
 
-    // The lowest rank that is kept, and how many of that rank
-    uint32_t border = 1;
-    int of_border = 0x7fffffff;
+    Border border = {1, 0x7fffffff};         // everything that lies somewhere
     if (there > a.keep) {
-        border = 0;
-        of_border = a.keep;                  // of those that agree with border so far
+        border = {0, a.keep};
         for (int digit = 0; digit < 3; ++digit) {
-            const int shift = digit == 0 ? 21 : digit == 1 ? 10 : 0, width = digit == 2 ? 10 : 11;
             if (digit > 0) {
                 for (int i = (int)threadIdx.x; i < H_BINS; i += H_THREADS) bins[i] = 0;
                 __syncthreads();
                 for_each([&](const uint32_t (&r)[4], int) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
-                        if (r[i] != 0 && r[i] >> (shift + width) == border >> (shift + width)) atomicAdd(&bins[r[i] >> shift & ((1u << width) - 1)], 1);
+                        if (digit_counts(r[i], border, digit)) atomicAdd(&bins[digit_of(r[i], digit)], 1);
                 });
                 __syncthreads();
             }
-            // From the highest bin down, two to a thread: the one in which the count reaches of_border
-            const int top = H_BINS - 1 - 2 * (int)threadIdx.x, high = bins[top], low = bins[top - 1];
-            int upto = high + low;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const int other = __shfl_up(upto, d);
-                if (lane >= d) upto += other;
-            }
-            if (lane == 63) wave_sum[wave] = upto;
-            __syncthreads();
-            for (int w = 0; w < wave; ++w) upto += wave_sum[w];
-            const int before = upto - high - low;
-            if (before < of_border && upto >= of_border) {
-                const bool first = before + high >= of_border;
-                picked[0] = first ? top : top - 1;
-                picked[1] = of_border - before - (first ? 0 : high);
-            }
-            __syncthreads();
-            border |= (uint32_t)picked[0] << shift;
-            of_border = picked[1];
+            const int top = H_BINS - 1 - 2 * (int)threadIdx.x;
+            pick_digit(border, digit, bins[top], bins[top - 1], shared);
         }
     }
 
@@ -154,8 +214,8 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_kernel(Heaviest4 a) {
     for_each([&](const uint32_t (&r)[4], int) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            above += r[i] > border ? 1 : 0;
-            equal += r[i] == border ? 1 : 0;
+            above += r[i] > border.rank ? 1 : 0;
+            equal += r[i] == border.rank ? 1 : 0;
         }
     });
 #pragma unroll
@@ -173,40 +233,149 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_kernel(Heaviest4 a) {
         place += wave_above[w];
         equals += wave_equal[w];
     }
-    place += min(equals, of_border);
-    // lanes before this one, in a mask
-    auto before = [](unsigned long long mask) { return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); };
-    for_each([&](const uint32_t (&r)[4], int j) {
-        bool keep[4];
-        unsigned long long e[4], any = 0;
+    Emit emit = {out, border, place + min(equals, border.count), equals};
+    for_each([&](const uint32_t (&r)[4], int j) { emit(r, j); });
+    for (int i = kept + (int)threadIdx.x; i < a.keep; i += H_THREADS) out[i] = -1;
+}
+
+// Long sequences, few of them: a workgroup has 8192 tokens of one, in registers, and four launches pass the histograms on through the workspace.  Launch d < 3 counts digit d, having picked digit d - 1 from all
+// parts' counts; the last writes the tokens, the place of its first one being what the parts before it keep.
+struct Parts4 {
+    int parts;
+    int* bins;                               // [unit][digit][part][bins]; unit: sequence and kv head
+    Border* borders;                         // [unit][digit]: what launch `digit` found before it counted
+    int* above;                              // [unit][digit][part]: tokens of the part above the border by that digit
+};
+template <int LAUNCH>
+__global__ __launch_bounds__(H_THREADS) void heaviest_part_kernel(Heaviest4 a, Parts4 p) {
+    constexpr int E = 2;
+    __shared__ int bins[H_BINS];
+    __shared__ int wave_above[H_WAVES], wave_equal[H_WAVES], sums[3][H_WAVES];
+    __shared__ PickShared shared;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), tid = (int)threadIdx.x;
+    const int part = (int)blockIdx.x, head = (int)blockIdx.y, b = (int)blockIdx.z;
+    const int length = (int)min((long long)max(a.lens[b], 0), (long long)a.table_pages << a.c.page_shift);
+    constexpr int TOKENS = H_WAVES * E * H_VECTOR;
+    const int used = max((length + TOKENS - 1) / TOKENS, 1);         // parts with tokens (an empty sequence's first writes the list)
+    if (part >= used) return;
+    const int begin = min(part * TOKENS + wave * E * H_VECTOR, length), end = min(begin + E * H_VECTOR, length);
+    const long long unit = (long long)b * a.c.kv_heads + head;
+    const float* weights = a.weights + unit * a.width;
+    const int32_t* table = a.table + (long long)b * a.table_pages;
+    int* const my_bins = p.bins + ((unit * 3 + LAUNCH) * p.parts + part) * H_BINS;       // (LAUNCH < 3)
+    uint32_t held[E][4];
+    {
+        Four f[E];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            e[i] = __ballot(r[i] == border);
-            any |= e[i];
-            keep[i] = r[i] > border;
-        }
-        if (any != 0) {                      // which of those at the border: the lowest
-            int n = equals + before(e[0]) + before(e[1]) + before(e[2]) + before(e[3]);
+        for (int e = 0; e < E; ++e) f[e] = fetch_four(weights, table, a.c.page_shift, begin + e * H_VECTOR + 4 * lane, end);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (r[i] == border) {
-                    keep[i] = n < of_border;
-                    ++n;
-                }
-                equals += __popcll(e[i]);
+        for (int e = 0; e < E; ++e) rank_four(a, f[e], begin + e * H_VECTOR + 4 * lane, end, length, held[e]);
+    }
+    // The sum over a workgroup of each thread's n, for all
+    auto total = [&](int n, int* scratch) {
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
+        if (lane == 0) scratch[wave] = n;
+        __syncthreads();
+        n = 0;
+#pragma unroll
+        for (int w = 0; w < H_WAVES; ++w) n += scratch[w];
+        return n;
+    };
+
+    Border border = {0, a.keep};
+    bool all = false;                        // everything is kept
+    int there = 0;
+    if constexpr (LAUNCH > 0) {
+        // Digit LAUNCH - 1, from the counts of all parts
+        constexpr int digit = LAUNCH - 1;
+        if constexpr (LAUNCH > 1) border = p.borders[unit * 3 + LAUNCH - 1];
+        const int top = H_BINS - 1 - 2 * tid;
+        const int* counts = p.bins + (unit * 3 + digit) * (long long)p.parts * H_BINS + top - 1;
+        int high = 0, low = 0, own_high = 0, own_low = 0;
+#pragma unroll 8
+        for (int q = 0; q < used; ++q) {
+            const int2 n = *reinterpret_cast<const int2*>(counts + (long long)q * H_BINS);
+            low += n.x;
+            high += n.y;
+            if (q == part) {
+                own_low = n.x;
+                own_high = n.y;
             }
         }
-        unsigned long long k[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) k[i] = __ballot(keep[i]);
-        int at = place + before(k[0]) + before(k[1]) + before(k[2]) + before(k[3]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (keep[i]) out[at++] = j + i;
-            place += __popcll(k[i]);
+        if constexpr (LAUNCH == 1) there = total(high + low, sums[0]);
+        all = LAUNCH == 1 ? there <= a.keep : border.count == 0x7fffffff;
+        if (all) {
+            border = {0, LAUNCH == 3 ? 0 : 0x7fffffff};              // (of the rank 0, of what lies nowhere, none)
+        } else {
+            pick_digit(border, digit, high, low, shared);
+            const int picked = digit_of(border.rank, digit);
+            const int over = total((top > picked ? own_high : 0) + (top - 1 > picked ? own_low : 0), sums[1]);
+            if (LAUNCH < 3 && tid == 0) p.above[(unit * 3 + digit) * p.parts + part] = over;
         }
-    });
-    for (int i = kept + (int)threadIdx.x; i < a.keep; i += H_THREADS) out[i] = -1;
+        if (LAUNCH < 3 && part == 0 && tid == 0) p.borders[unit * 3 + LAUNCH] = border;
+        if (LAUNCH == 1 && part == 0 && head == 0 && tid == 0) a.kept[b] = min(there, a.keep);
+    }
+    if constexpr (LAUNCH < 3) {
+        if (all) return;
+        for (int i = tid; i < H_BINS; i += H_THREADS) bins[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (digit_counts(held[e][i], border, LAUNCH)) atomicAdd(&bins[digit_of(held[e][i], LAUNCH)], 1);
+        __syncthreads();
+        for (int i = tid; i < H_BINS; i += H_THREADS) my_bins[i] = bins[i];
+    } else {
+        // What the parts before this one keep: above the border by one of its digits, and of its own rank
+        int over = 0, same = 0;
+        // (the counts of the last digit; where all are kept, of the first, all of which are kept)
+        const int picked = all ? -1 : digit_of(border.rank, 2), top = H_BINS - 1 - 2 * tid;
+        const int* counts = p.bins + (unit * 3 + (all ? 0 : 2)) * (long long)p.parts * H_BINS + top - 1;
+#pragma unroll 8
+        for (int q = 0; q < part; ++q) {
+            const int2 n = *reinterpret_cast<const int2*>(counts + (long long)q * H_BINS);
+            over += (top > picked ? n.y : 0) + (top - 1 > picked ? n.x : 0);
+            same += (top == picked ? n.y : 0) + (top - 1 == picked ? n.x : 0);
+        }
+        if (!all)
+            for (int q = tid; q < part; q += H_THREADS) over += p.above[unit * 3 * p.parts + q] + p.above[(unit * 3 + 1) * p.parts + q];
+        __syncthreads();
+        over = total(over, sums[0]);
+        same = total(same, sums[2]);
+        int above = 0, equal = 0;
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                above += held[e][i] > border.rank ? 1 : 0;
+                equal += held[e][i] == border.rank ? 1 : 0;
+            }
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) {
+            above += __shfl_xor(above, d);
+            equal += __shfl_xor(equal, d);
+        }
+        if (lane == 0) {
+            wave_above[wave] = above;
+            wave_equal[wave] = equal;
+        }
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) {
+            over += wave_above[w];
+            same += wave_equal[w];
+        }
+        int32_t* const out = a.tokens + unit * a.keep;
+        Emit emit = {out, border, over + min(same, border.count), same};
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+            if (begin + e * H_VECTOR < end) emit(held[e], begin + e * H_VECTOR + 4 * lane);
+        if (part == 0) {                     // the rest of a list that is not full
+            const int kept = a.kept[b];
+            for (int i = kept + tid; i < a.keep; i += H_THREADS) out[i] = -1;
+        }
+    }
 }
 
 // A thread moves 16 bytes of codes, K's and V's, the lanes of a token side by side; scales and signs go a byte or word at a time.
@@ -242,12 +411,32 @@ __global__ __launch_bounds__(256) void move_kernel(Move4 a, FastDiv div_lanes, i
 
 }  // namespace
 
-int launch_cache4_heaviest(const Heaviest4& a, hipStream_t s) {
+HeaviestPlan4 plan_cache4_heaviest(const Cache4& c, int batch, int table_pages) {
+    HeaviestPlan4 p = {};
+    const long long room = (long long)table_pages << c.page_shift, units = (long long)batch * c.kv_heads, parts = cdiv(room, H_WAVES * 2 * H_VECTOR);
+    if (room <= 32768 || units * parts > 4096) return p;
+    p.parts = (int)parts;
+    p.bins_bytes = (size_t)units * 3 * parts * H_BINS * sizeof(int);
+    p.borders_bytes = (size_t)units * 3 * sizeof(Border);
+    p.workspace_bytes = p.bins_bytes + p.borders_bytes + (size_t)units * 3 * parts * sizeof(int);
+    return p;
+}
+
+int launch_cache4_heaviest(const Heaviest4& a, const HeaviestPlan4& plan, void* workspace, hipStream_t s) {
+    if (plan.parts > 0) {
+        const Parts4 p = {plan.parts, static_cast<int*>(workspace), reinterpret_cast<Border*>(static_cast<char*>(workspace) + plan.bins_bytes),
+                          reinterpret_cast<int*>(static_cast<char*>(workspace) + plan.bins_bytes + plan.borders_bytes)};
+        const dim3 grid((unsigned)p.parts, (unsigned)a.c.kv_heads, (unsigned)a.batch);
+        launch(heaviest_part_kernel<0>, grid, dim3(H_THREADS), 0, s, a, p);
+        launch(heaviest_part_kernel<1>, grid, dim3(H_THREADS), 0, s, a, p);
+        launch(heaviest_part_kernel<2>, grid, dim3(H_THREADS), 0, s, a, p);
+        launch(heaviest_part_kernel<3>, grid, dim3(H_THREADS), 0, s, a, p);
+        return check_launch();
+    }
     const dim3 grid((unsigned)a.batch, (unsigned)a.c.kv_heads);
     const long long vectors = cdiv((long long)a.table_pages << a.c.page_shift, H_WAVES * H_VECTOR);
     if (vectors <= 2) launch(heaviest_kernel<2>, grid, dim3(H_THREADS), 0, s, a);
     else if (vectors <= 8) launch(heaviest_kernel<8>, grid, dim3(H_THREADS), 0, s, a);
-    else if (vectors <= 16) launch(heaviest_kernel<16>, grid, dim3(H_THREADS), 0, s, a);
     else launch(heaviest_kernel<0>, grid, dim3(H_THREADS), 0, s, a);
     return check_launch();
 }

@@ -82,14 +82,21 @@ def test_weigh(b):
 
 
 def test_heaviest_and_move(b):
-    def heaviest(c=None, table=A, lens=A, batch=2, pages=3, weights=A, width=48, keep=8, first=1, last=2, tokens=A, kept=A):
-        return b.load().bnn_cache4_heaviest(c or cache(b), P(table), P(lens), batch, pages, P(weights), ctypes.c_int64(width), keep, first, last, P(tokens), P(kept), None)
+    def heaviest(c=None, table=A, lens=A, batch=2, pages=3, weights=A, width=48, keep=8, first=1, last=2, tokens=A, kept=A, work=0, size=0):
+        return b.load().bnn_cache4_heaviest(c or cache(b), P(table), P(lens), batch, pages, P(weights), ctypes.c_int64(width), keep, first, last, P(tokens), P(kept), P(work), ctypes.c_size_t(size), None)
     for kw in (dict(table=0), dict(lens=0), dict(weights=0), dict(tokens=0), dict(kept=0), dict(batch=-1), dict(pages=0), dict(width=47), dict(keep=0), dict(first=-1), dict(last=-1),
                dict(first=4, last=5), dict(first=2147483647, last=2147483647), dict(c=cache(b, kv_heads=0))):
         assert heaviest(**kw) == INVALID, kw
     for kw in (dict(table=A + 1), dict(lens=A + 2), dict(weights=A + 2), dict(tokens=A + 1), dict(kept=A + 3)):
         assert heaviest(**kw) == ALIGNMENT, kw
     assert heaviest(pages=(1 << 26) + 1, width=1 << 40) == UNSUPPORTED and heaviest(batch=1 << 22) == UNSUPPORTED and heaviest(batch=0) == OK
+
+    need = b.load().bnn_cache4_heaviest_workspace_bytes(cache(b), 2, 4000)
+    assert need > 0 and b.load().bnn_cache4_heaviest_workspace_bytes(cache(b), 2, 3) == 0 and b.load().bnn_cache4_heaviest_workspace_bytes(cache(b), 20000, 4000) == 0
+    assert heaviest(pages=4000, width=64000) == WORKSPACE and heaviest(pages=4000, width=64000, work=A, size=need - 1) == WORKSPACE
+    assert heaviest(pages=4000, width=64000, work=A + 8, size=need) == ALIGNMENT
+    for bad in ((cache(b, dim=80), 2, 4000), (cache(b), 0, 4000), (cache(b), 2, 0), (cache(b), 2, (1 << 26) + 1)):
+        assert b.load().bnn_cache4_heaviest_workspace_bytes(*bad) == 0
 
     def move(c=None, tokens=A, keep=8, table=A, pages=3, into=A, into_pages=1, batch=2, weights=A, width=48, moved=A):
         return b.load().bnn_cache4_move(c or cache(b), P(tokens), keep, P(table), pages, P(into), into_pages, batch, P(weights), ctypes.c_int64(width), P(moved), None)

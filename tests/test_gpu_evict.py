@@ -246,6 +246,34 @@ def test_heaviest(bnn, keep, first, last):
     check_heaviest(bnn, weights, lens, table, keep, first, last, page, 8 * 320, kv_heads)
 
 
+@pytest.mark.parametrize("keep,first,last", [(1, 0, 1), (5000, 3, 100), (20000, 0, 0), (39990, 1, 1), (50000, 0, 7)])
+def test_heaviest_in_parts(bnn, keep, first, last):
+    """Tables with room for more than 32768 tokens: a sequence's workgroups pass on what they counted.  Sequences of every length beside each other, ties, numbers of any kind, pages given back; and tables too many
+    for that, which one workgroup each reads several times."""
+    rng = np.random.default_rng(keep)
+    page, kv_heads, width = 64, 2, 700
+    lens = np.array([0, 1, 8191, 8192, 8193, 40000, 44800, 100000], np.int32)
+    table = rng.permutation(8 * width).reshape(8, width).astype(np.int32)
+    weights = np.exp(2 * rng.standard_normal((8, kv_heads, width * page))).astype(np.float32)
+    check_heaviest(bnn, weights, lens, table, keep, first, last, page, 8 * width, kv_heads)
+    mixed = rng.integers(-2, 3, weights.shape).astype(np.float32)
+    mixed[:, 1] = rng.standard_normal(weights[:, 1].shape)
+    mixed[rng.random(weights.shape) < 0.02] = np.nan
+    mixed[rng.random(weights.shape) < 0.02] = -np.inf
+    mixed[rng.random(weights.shape) < 0.02] = np.inf
+    table[rng.random(table.shape) < 0.1] = -1
+    check_heaviest(bnn, mixed, lens, table, keep, first, last, page, 8 * width, kv_heads)
+    if keep == 5000:                         # 400 sequences, few of them long
+        many, lens = np.zeros(400, np.int32), lens[:7]
+        many[:7], many[399] = lens, 44801
+        table = np.full((400, width), -1, np.int32)
+        table[:7], table[399] = rng.permutation(8 * width).reshape(8, width)[:7], rng.permutation(8 * width)[:width]
+        w = np.zeros((400, kv_heads, width * page), np.float32)
+        w[:7], w[399] = mixed[:7], weights[7]
+        assert bnn.load().bnn_cache4_heaviest_workspace_bytes(bnn.Cache4(1, kv_heads=kv_heads, head_dim=64, page=page)._struct(), 400, width) == 0
+        check_heaviest(bnn, w, many, table, keep, first, last, page, 8 * width, kv_heads)
+
+
 def test_heaviest_long(bnn):
     rng = np.random.default_rng(1)
     pages = 300001 // 256 + 1
@@ -396,6 +424,9 @@ def test_refusals(bnn):
                             (bnn.BnnError, (q, lse), dict(decay=float("nan"), previous=w)), (bnn.BnnError, (q[:, :3], lse[:, :3].contiguous()), {})):
         with pytest.raises(error):
             su.gpu.weigh(*args, table, lens, **kw)
+    wide = ints(np.zeros((2, 4000)))
+    with pytest.raises(bnn.BnnError):
+        su.gpu.heaviest(torch.zeros(2, 2, 64000, device="cuda"), wide, lens, 4, workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
     for error, args, kw in ((TypeError, (w.double(), table, lens, 4), {}), (TypeError, (w, table.long(), lens, 4), {}), (ValueError, (w, table, lens[:1], 4), {}),
                             (ValueError, (w[:, :, :32].contiguous(), table, lens, 4), {}), (ValueError, (w, table, lens, 0), {}), (bnn.BnnError, (w, table, lens, 4, 3, 2), {}),
                             (bnn.BnnError, (w, table, lens, 4, -1), {})):

@@ -882,6 +882,10 @@ def rotary(x, positions, frequencies, interleaved: bool = False, magnitude: floa
     """x [tokens][heads][dim] (fp32, bf16 or fp16) with every head's first 2 * len(frequencies) elements turned in pairs by positions[token] * frequencies[pair]
     (positions int32, frequencies float64: rotary_frequencies); pairs are the halves' elements, or neighbours if interleaved.  inverse turns back, which is also how a
     gradient passes.  out may be x."""
+    if out is None:
+        done = (_native or _load_native()).rotary(x, frequencies, positions, interleaved, magnitude, inverse)
+        if done is not None:
+            return done
     code = _heads_of(x, "x")
     rot = _rotation(frequencies, positions, x.shape[0], x.device, interleaved, inverse, magnitude)
     if positions is None:
@@ -973,6 +977,10 @@ class Cache4:
     def write_rotary(self, q, k, v, table, lens, frequencies, start=None, positions=None, interleaved: bool = False, magnitude: float = 1.0, out=None):
         """write() of v and of k turned by its tokens' positions, as rotary() does it; returns q [tokens][heads][head_dim] turned alike, or None without q.  positions (int32
         [tokens]): by default a token's place in its sequence, which is no longer its position once tokens before it were evicted."""
+        if out is None and q is not None:
+            done = (_native or _load_native()).cache4_write_rotary(*self._plain, table, lens, start, q, k, v, frequencies, positions, interleaved, magnitude, False)
+            if done is not None:
+                return done
         code, kt, kh = self._elements(k, self.kv_heads, "k")
         code_v, vt, vh = self._elements(v, self.kv_heads, "v")
         if code != code_v or k.shape != v.shape:
@@ -1077,6 +1085,10 @@ class Cache4:
         returned -> fp32 [batch][kv_heads][tokens of the table].  Tokens of this call have no previous weight.  What lies behind a sequence's end is not written (and undefined in an
         output that is made here).  out may be previous."""
         scale = self.head_dim ** -0.5 if scale is None else float(scale)
+        if workspace is None:
+            done = (_native or _load_native()).cache4_weigh(*self._plain, table, lens, start, q, lse, scale, causal, window, previous, decay, out)
+            if done is not None:
+                return done if out is None else out
         code, qt, qh = self._elements(q, None, "q")
         rows = self._rows(table, lens, start, q.shape[0])
         if _dev(lse, torch.float32, 2, "lse").shape != q.shape[:2] or lse.device != q.device:
@@ -1101,6 +1113,10 @@ class Cache4:
     def heaviest(self, weights, table, lens, keep: int, first: int = 0, last: int = 0, workspace=None):
         """(int32 [batch][kv_heads][keep], int32 [batch]): the tokens of every sequence to keep, ascending, the rest -1, and how many: all of a sequence of up to `keep`, else
         the first `first`, the last `last` and those with the largest weights.  Ties go to the lower token."""
+        if workspace is None:
+            done = (_native or _load_native()).cache4_heaviest(*self._plain, weights, table, lens, keep, first, last)
+            if done is not None:
+                return done
         _dev(table, torch.int32, 2, "table"); _dev(lens, torch.int32, 1, "lens")
         batch, width = table.shape
         if lens.shape[0] != batch:
@@ -1125,6 +1141,10 @@ class Cache4:
     def move(self, tokens, table, into, weights=None):
         """Copies token tokens[b][h][i] (from heaviest) of the sequence in table[b] to token i of the one in into[b] (int32 [batch][pages], other pages than the table's), for every kv
         head; with weights returns them moved alike, fp32 [batch][kv_heads][tokens of into], 0 where there is none.  The sequence's length is then heaviest's second result."""
+        if weights is not None:
+            done = (_native or _load_native()).cache4_move(*self._plain, tokens, table, into, weights)
+            if done is not None:
+                return done
         _dev(tokens, torch.int32, 3, "tokens"); _dev(table, torch.int32, 2, "table"); _dev(into, torch.int32, 2, "into")
         batch = table.shape[0]
         if tokens.shape[0] != batch or into.shape[0] != batch or tokens.shape[1] != self.kv_heads or tokens.shape[2] < 1:
@@ -1152,6 +1172,10 @@ def token_logprobs(logits, targets=None, scale: float = 1.0, top: int = 0, works
     """What rows of logits [rows][cols] (fp32, bf16, fp16, or int32 sums as bmm gives them), times scale, say of tokens: TokenLogprobs of fp32 [rows] logprobs of the targets (int64
     [rows]; 0 for one outside the columns; None without targets), entropy, lse, and the `top` (64 at most) best alternatives' logprobs and columns (int32) [rows][top], ties to
     the lower column.  A row without a distribution (all -infinity, a NaN, +infinity) gets NaN and columns of -1."""
+    if workspace is None and targets is not None:
+        done = (_native or _load_native()).token_logprobs(logits, targets, scale, top)
+        if done is not None:
+            return TokenLogprobs(*done)
     if not isinstance(logits, torch.Tensor) or not logits.is_cuda:
         raise TypeError("logits must be a device tensor")
     if logits.dtype not in _LOGITS:

@@ -24,7 +24,9 @@ namespace {
     X(bnn_bmm_general_workspace_bytes) X(bnn_bmm_general_f32) X(bnn_bwn_workspace_bytes) X(bnn_bwn_conv_thr)                               \
     X(bnn_conv_f32_split_workspace_bytes) X(bnn_conv_f32_split_thr_ex) X(bnn_net_workspace_bytes) X(bnn_net_forward)                       \
     X(bnn_cache4_write) X(bnn_cache4_read) X(bnn_cache4_select_workspace_bytes) X(bnn_cache4_select)                                       \
-    X(bnn_cache4_attend_workspace_bytes) X(bnn_cache4_attend)
+    X(bnn_cache4_attend_workspace_bytes) X(bnn_cache4_attend) X(bnn_rotary) X(bnn_cache4_write_rotary) X(bnn_cache4_weigh_workspace_bytes)        \
+    X(bnn_cache4_weigh) X(bnn_cache4_heaviest_workspace_bytes) X(bnn_cache4_heaviest) X(bnn_cache4_move)                                     \
+    X(bnn_token_logprobs_workspace_bytes) X(bnn_token_logprobs)
 #define DECLARE(name) decltype(&::name) p_##name = nullptr;
 BNN_ENTRIES(DECLARE)
 
@@ -51,14 +53,16 @@ struct Call {
         return &t;
     }
     // [tokens][heads][dim] in fp32, bf16 or fp16, the elements of a head side by side; code: the library's number for the type.
+    // dim < 0: any.  device < 0: any, which is then the call's.
     const Tensor* elements(PyObject* o, int dim, int& code) {
         static const Tensor none;
         if (!ok || !THPVariable_CheckExact(o)) { ok = false; return &none; }
         const Tensor& t = THPVariable_Unpack(o);
         const at::TensorImpl* impl = t.unsafeGetTensorImpl();
-        ok = t.defined() && t.is_cuda() && t.dim() == 3 && t.layout() == at::kStrided && impl->has_storage() && !impl->is_python_dispatch() && t.get_device() == device &&
-             t.size(2) == dim && t.stride(2) == 1 && t.size(0) <= INT_MAX && t.size(1) <= INT_MAX;
+        ok = t.defined() && t.is_cuda() && t.dim() == 3 && t.layout() == at::kStrided && impl->has_storage() && !impl->is_python_dispatch() && (device < 0 || t.get_device() == device) &&
+             (dim < 0 || t.size(2) == dim) && t.stride(2) == 1 && t.size(0) <= INT_MAX && t.size(1) <= INT_MAX && t.size(2) <= INT_MAX;
         if (!ok) return &none;
+        device = t.get_device();
         const at::ScalarType type = t.scalar_type();
         code = type == at::kFloat ? BNN_F32 : type == at::kBFloat16 ? BNN_BF16 : BNN_F16;
         ok = type == at::kFloat || type == at::kBFloat16 || type == at::kHalf;
@@ -451,6 +455,194 @@ PyObject* cache4_attend(PyObject*, PyObject* const* a, Py_ssize_t nargs) {   // 
     });
 }
 
+// frequencies, positions or None, interleaved, magnitude, inverse: a rotation; its pointers come in finish(), after ready().
+struct Rotation {
+    static constexpr int N = 5;
+    bnn_rotation r = {};
+
+    Rotation(Call& c, PyObject* const* a) {
+        frequencies = c.tensor(a[0], at::kDouble, 1);
+        if (a[1] != Py_None) positions = c.tensor(a[1], at::kInt, 1);
+        r.neighbours = c.truth(a[2]);
+        c.ok = c.ok && PyFloat_CheckExact(a[3]);
+        if (c.ok) r.magnitude = PyFloat_AS_DOUBLE(a[3]);
+        r.inverse = c.truth(a[4]);
+    }
+    bool fits(int64_t tokens) const { return !positions || positions->size(0) == tokens; }
+    bool placed() const { return positions != nullptr; }
+    void finish() {
+        r.frequencies = ptr<double>(*frequencies);
+        r.positions = positions ? ptr<int32_t>(*positions) : nullptr;
+        r.pairs = (int)frequencies->size(0);
+    }
+
+private:
+    const Tensor *frequencies = nullptr, *positions = nullptr;
+};
+
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t nargs) {          // x, rotation
+    ARGS(1 + Rotation::N)
+    return guarded([&]() -> PyObject* {
+        Call c;
+        int code = 0;
+        const Tensor& x = *c.elements(a[0], -1, code);
+        Rotation rot(c, a + 1);
+        PLAIN(c);
+        if (!rot.placed() || !rot.fits(x.size(0))) Py_RETURN_NONE;
+        rot.finish();
+        const Tensor out = empty(x, x.sizes(), ELEMENTS[code]);
+        const bool done = run(c, "bnn_rotary", p_bnn_rotary, x.data_ptr(), out.data_ptr(), code, (int)x.size(0), (int)x.size(1), (int)x.size(2), Call::distance(x, 0), Call::distance(x, 1),
+                              Call::distance(out, 0), Call::distance(out, 1), &rot.r);
+        return done ? THPVariable_Wrap(out) : nullptr;
+    });
+}
+
+PyObject* cache4_write_rotary(PyObject*, PyObject* const* a, Py_ssize_t nargs) {      // plan, q, k, v, rotation -> q turned
+    ARGS(Plan4::N + 3 + Rotation::N)
+    return guarded([&]() -> PyObject* {
+        Call c;
+        Plan4 p(c, a);
+        int code = 0, code_k = 0, code_v = 0;
+        const int dim = p.cache.head_dim;
+        const Tensor &q = *c.elements(a[8], dim, code), &k = *c.elements(a[9], dim, code_k), &v = *c.elements(a[10], dim, code_v);
+        Rotation rot(c, a + 11);
+        PLAIN(c);
+        const int64_t tokens = k.size(0);
+        if (code != code_k || code != code_v || q.size(0) != tokens || v.size(0) != tokens || k.size(1) != p.cache.kv_heads || v.size(1) != p.cache.kv_heads || !rot.fits(tokens)) Py_RETURN_NONE;
+        p.finish((int)tokens);
+        rot.finish();
+        const Tensor out = empty(q, q.sizes(), ELEMENTS[code]);
+        const bool done = run(c, "bnn_cache4_write_rotary", p_bnn_cache4_write_rotary, &p.cache, &p.rows, &rot.r, q.data_ptr(), Call::distance(q, 0), Call::distance(q, 1), (int)q.size(1),
+                              out.data_ptr(), k.data_ptr(), v.data_ptr(), code, Call::distance(k, 0), Call::distance(k, 1), Call::distance(v, 0), Call::distance(v, 1));
+        return done ? THPVariable_Wrap(out) : nullptr;
+    });
+}
+
+PyObject* cache4_weigh(PyObject*, PyObject* const* a, Py_ssize_t nargs) {    // plan, q, lse, scale, causal, window, previous, decay, out
+    ARGS(Plan4::N + 8)
+    return guarded([&]() -> PyObject* {
+        Call c;
+        Plan4 p(c, a);
+        int code = 0;
+        const Tensor &q = *c.elements(a[8], p.cache.head_dim, code), &lse = *c.tensor(a[9], at::kFloat, 2);
+        if (!PyFloat_CheckExact(a[10]) || !PyFloat_CheckExact(a[14])) Py_RETURN_NONE;
+        const float scale = (float)PyFloat_AS_DOUBLE(a[10]), decay = (float)PyFloat_AS_DOUBLE(a[14]);
+        const bool causal = c.truth(a[11]);
+        const int window = c.number(a[12]);
+        const Tensor* previous = a[13] == Py_None ? nullptr : c.tensor(a[13], at::kFloat, 3);
+        const Tensor* given = a[15] == Py_None ? nullptr : c.tensor(a[15], at::kFloat, 3);
+        PLAIN(c);
+        if (lse.size(0) != q.size(0) || lse.size(1) != q.size(1)) Py_RETURN_NONE;
+        p.finish((int)q.size(0));
+        const int64_t room = (int64_t)p.rows.table_pages * p.cache.page;
+        if (room > INT_MAX) Py_RETURN_NONE;
+        const Tensor out = given ? *given : previous ? empty(q, previous->sizes(), at::kFloat) : empty(q, {p.rows.batch, p.cache.kv_heads, room}, at::kFloat);
+        if (out.size(0) != p.rows.batch || out.size(1) != p.cache.kv_heads || out.size(2) < room || (previous && previous->sizes() != out.sizes())) Py_RETURN_NONE;
+        const size_t need = p_bnn_cache4_weigh_workspace_bytes(&p.cache, &p.rows, code, (int)q.size(1));
+        Tensor work;
+        if (need) work = empty(q, {(int64_t)need}, at::kByte);
+        const bool done = run(c, "bnn_cache4_weigh", p_bnn_cache4_weigh, &p.cache, &p.rows, q.data_ptr(), code, Call::distance(q, 0), Call::distance(q, 1), (int)q.size(1), ptr<float>(lse), scale,
+                              (int)causal, window, previous ? ptr<float>(*previous) : nullptr, decay, ptr<float>(out), out.size(2), need ? work.data_ptr() : nullptr, need);
+        return done ? THPVariable_Wrap(out) : nullptr;
+    });
+}
+
+// data, kv_heads, head_dim, page, signs: a cache without the rows of a call.
+struct Store4 {
+    static constexpr int N = 5;
+    bnn_cache4 cache = {};
+
+    Store4(Call& c, PyObject* const* a) {
+        data = c.tensor(a[0], at::kByte, 3);
+        cache.kv_heads = c.number(a[1]);
+        cache.head_dim = c.number(a[2]);
+        cache.page = c.number(a[3]);
+        cache.signs = c.number(a[4]);
+    }
+    void finish() {
+        cache.data = data->data_ptr();
+        cache.pages = data->size(0);
+    }
+
+private:
+    const Tensor* data = nullptr;
+};
+
+PyObject* cache4_heaviest(PyObject*, PyObject* const* a, Py_ssize_t nargs) { // cache, weights, table, lens, keep, first, last
+    ARGS(Store4::N + 6)
+    return guarded([&]() -> PyObject* {
+        Call c;
+        Store4 store(c, a);
+        const Tensor &weights = *c.tensor(a[5], at::kFloat, 3), &table = *c.tensor(a[6], at::kInt, 2), &lens = *c.tensor(a[7], at::kInt, 1);
+        const int keep = c.number(a[8]), first = c.number(a[9]), last = c.number(a[10]);
+        PLAIN(c);
+        const int64_t batch = table.size(0);
+        if (keep < 1 || lens.size(0) != batch || weights.size(0) != batch || weights.size(1) != store.cache.kv_heads || weights.size(2) < table.size(1) * store.cache.page) Py_RETURN_NONE;
+        store.finish();
+        const Tensor tokens = empty(weights, {batch, store.cache.kv_heads, keep}, at::kInt), kept = empty(weights, {batch}, at::kInt);
+        const size_t need = p_bnn_cache4_heaviest_workspace_bytes(&store.cache, (int)batch, (int)table.size(1));
+        Tensor work;
+        if (need) work = empty(weights, {(int64_t)need}, at::kByte);
+        const bool done = run(c, "bnn_cache4_heaviest", p_bnn_cache4_heaviest, &store.cache, ptr<int32_t>(table), ptr<int32_t>(lens), (int)batch, (int)table.size(1), ptr<float>(weights), weights.size(2),
+                              keep, first, last, ptr<int32_t>(tokens), ptr<int32_t>(kept), need ? work.data_ptr() : nullptr, need);
+        return done ? pair(tokens, kept) : nullptr;
+    });
+}
+
+PyObject* cache4_move(PyObject*, PyObject* const* a, Py_ssize_t nargs) {     // cache, tokens, table, into, weights -> weights moved
+    ARGS(Store4::N + 4)
+    return guarded([&]() -> PyObject* {
+        Call c;
+        Store4 store(c, a);
+        const Tensor &tokens = *c.tensor(a[5], at::kInt, 3), &table = *c.tensor(a[6], at::kInt, 2), &into = *c.tensor(a[7], at::kInt, 2), &weights = *c.tensor(a[8], at::kFloat, 3);
+        PLAIN(c);
+        const int64_t batch = table.size(0), room = into.size(1) * store.cache.page;
+        if (tokens.size(0) != batch || into.size(0) != batch || tokens.size(1) != store.cache.kv_heads || tokens.size(2) < 1 || weights.size(0) != batch ||
+            weights.size(1) != store.cache.kv_heads || weights.size(2) < 1 || batch < 1 || room < 1 || room > INT_MAX)
+            Py_RETURN_NONE;
+        store.finish();
+        const Tensor moved = empty(weights, {batch, store.cache.kv_heads, room}, at::kFloat);
+        const bool done = run(c, "bnn_cache4_move", p_bnn_cache4_move, &store.cache, ptr<int32_t>(tokens), (int)tokens.size(2), ptr<int32_t>(table), (int)table.size(1), ptr<int32_t>(into),
+                              (int)into.size(1), (int)batch, ptr<float>(weights), weights.size(2), ptr<float>(moved));
+        return done ? THPVariable_Wrap(moved) : nullptr;
+    });
+}
+
+PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t nargs) {  // logits, targets, scale, top -> logprobs, entropy, lse, top_logprobs, top_tokens
+    ARGS(4)
+    return guarded([&]() -> PyObject* {
+        Call c;
+        if (!THPVariable_CheckExact(a[0])) Py_RETURN_NONE;
+        const Tensor& x = THPVariable_Unpack(a[0]);
+        const at::TensorImpl* impl = x.unsafeGetTensorImpl();
+        if (!x.defined() || !x.is_cuda() || x.dim() != 2 || x.layout() != at::kStrided || !impl->has_storage() || impl->is_python_dispatch() || x.size(0) < 1 || x.size(0) > INT_MAX ||
+            x.size(1) < 1 || x.size(1) > INT_MAX || x.stride(1) != 1)
+            Py_RETURN_NONE;
+        const at::ScalarType type = x.scalar_type();
+        const int code = type == at::kFloat ? BNN_F32 : type == at::kBFloat16 ? BNN_BF16 : type == at::kHalf ? BNN_F16 : type == at::kInt ? BNN_I32 : -1;
+        if (code < 0 || !PyFloat_CheckExact(a[2])) Py_RETURN_NONE;
+        c.device = x.get_device();
+        const Tensor& targets = *c.tensor(a[1], at::kLong, 1);
+        const float scale = (float)PyFloat_AS_DOUBLE(a[2]);
+        const int top = c.number(a[3]), rows = (int)x.size(0), cols = (int)x.size(1);
+        PLAIN(c);
+        if (targets.size(0) != rows || top < 0) Py_RETURN_NONE;
+        const size_t need = p_bnn_token_logprobs_workspace_bytes(rows, cols, code, top);
+        const Tensor lp = empty(x, {rows}, at::kFloat), entropy = empty(x, {rows}, at::kFloat), lse = empty(x, {rows}, at::kFloat), best = empty(x, {rows, top}, at::kFloat),
+                     tokens = empty(x, {rows, top}, at::kInt);
+        Tensor work;
+        if (need) work = empty(x, {(int64_t)need}, at::kByte);
+        if (!run(c, "bnn_token_logprobs", p_bnn_token_logprobs, x.data_ptr(), code, rows, cols, rows > 1 ? x.stride(0) : 0, scale, ptr<int64_t>(targets), top, ptr<float>(lp), ptr<float>(entropy),
+                 ptr<float>(lse), top ? ptr<float>(best) : nullptr, top ? ptr<int32_t>(tokens) : nullptr, need ? work.data_ptr() : nullptr, need))
+            return nullptr;
+        PyObject* result = PyTuple_New(5);
+        if (!result) return nullptr;
+        const Tensor* parts[] = {&lp, &entropy, &lse, &best, &tokens};
+        for (int i = 0; i < 5; ++i) PyTuple_SET_ITEM(result, i, THPVariable_Wrap(*parts[i]));
+        return result;
+    });
+}
+
 PyObject* init(PyObject*, PyObject* args) {        // {name: address}, the raw stream function, _check
     PyObject *addresses, *stream_fn, *check_fn;
     if (!PyArg_ParseTuple(args, "O!OO", &PyDict_Type, &addresses, &stream_fn, &check_fn)) return nullptr;
@@ -471,7 +663,8 @@ PyObject* init(PyObject*, PyObject* args) {        // {name: address}, the raw s
 #define METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bmm), METHOD(bmm_thr), METHOD(bconv), METHOD(bconv_thr), METHOD(threshold_pack), METHOD(maxpool_or), METHOD(bmm_general_f32),
                          METHOD(bwn_conv_thr), METHOD(conv_f32_split_thr), METHOD(net_forward), METHOD(cache4_write), METHOD(cache4_read), METHOD(cache4_select),
-                         METHOD(cache4_attend), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
+                         METHOD(cache4_attend), METHOD(rotary), METHOD(cache4_write_rotary), METHOD(cache4_weigh), METHOD(cache4_heaviest), METHOD(cache4_move),
+                         METHOD(token_logprobs), {"init", init, METH_VARARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

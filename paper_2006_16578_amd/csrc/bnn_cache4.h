@@ -296,7 +296,7 @@ struct WeighPlan4 {
     size_t workspace_bytes;
 };
 constexpr int cache4_weigh_tiles(int dim) { return dim >= 192 ? 2 : 4; }          // tiles of 16 keys that a wave of that kernel keeps
-constexpr bool cache4_weigh_two(int dim, int dtype) { return dim / 32 * cache4_terms(dtype) <= 6; }       // whether two tiles of rows fit a wave's registers
+constexpr bool cache4_weigh_two(int dim, int dtype) { return dim / 32 * cache4_terms(dtype) <= 12; }       // whether two tiles of rows fit a wave's registers
 int launch_cache4_weigh(const Weigh4& a, const WeighPlan4& p, int dtype, hipStream_t s);
 
 // The choice of the tokens to keep, and moving them.

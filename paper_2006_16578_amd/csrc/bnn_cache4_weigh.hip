@@ -9,16 +9,36 @@ namespace bnn {
 namespace {
 
 // What a row's sums begin with: -lse / scale, and -infinity (a weight of 0) for no row and for one that saw nothing.
-__device__ __forceinline__ float weigh_origin(const Weigh4& a, const Sequence4& s, int head, int row, int rows) {
+__device__ __forceinline__ float weigh_origin(const Weigh4& a, float lse, bool there) { return there && lse != -__builtin_inff() ? -lse * a.unscale : -__builtin_inff(); }
+__device__ __forceinline__ float weigh_lse(const Weigh4& a, const Sequence4& s, int head, int row) {
     const int token = fast_div(row, a.div_group), g = row - token * a.group;
-    const float lse = row < rows ? a.lse[(long long)(s.first + token) * a.c.kv_heads * a.group + head * a.group + g] : -__builtin_inff();
-    return lse == -__builtin_inff() ? lse : -lse * a.unscale;
+    return a.lse[(long long)(s.first + token) * a.c.kv_heads * a.group + head * a.group + g];
 }
 
-// Whether the row (counted over tokens and heads of the group) sees the key.  (A row before token 0 sees nothing; differences stay within 32 bits.)
-__device__ __forceinline__ bool weigh_sees(const Weigh4& a, int base, int row, int key) {
-    const int pos = base + fast_div(row, a.div_group);
-    return (!a.causal || key <= pos) && (a.window == 0 || pos - key < a.window);
+// Eight elements of a row as TERMS operands of a product: n-th terms to ops[n][m].
+template <class T, int TERMS, int LOADS, int M>
+__device__ __forceinline__ void weigh_terms(const u32x4 (&raw)[LOADS], bf16x8 (&ops)[TERMS][M], int m) {
+    if constexpr (TERMS == 1) {
+        ops[0][m] = __builtin_bit_cast(bf16x8, raw[0]);
+    } else {
+        float x[8];
+        if constexpr (LOADS == 2) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(raw[i / 4][i % 4]);
+        } else {
+            typedef T t8 __attribute__((ext_vector_type(8)));
+            const t8 y = __builtin_bit_cast(t8, raw[0]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = (float)y[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            __bf16 terms[TERMS];
+            split_terms<TERMS>(x[i], terms);
+#pragma unroll
+            for (int n = 0; n < TERMS; ++n) ops[n][m][i] = terms[n];
+        }
+    }
 }
 
 // A product of numbers below 2^24, at full rate.
@@ -71,45 +91,79 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
 
     uint32_t codes[KT][M], exp[KT][P::count];
     unsigned there = 0;
+    int pages = 0;                           // of the next 64 keys, one in a lane: their loads' latency passes beside the products
+    auto locate = [&](int key) { pages = c4_page(a.r, a.c, b, key + 16 * (lane & 3)); };
     auto load = [&](int key) {
         there = 0;
-        // the four pages at once: the loads of the table do not wait for each other
-        int page[KT];
-#pragma unroll
-        for (int u = 0; u < KT; ++u) page[u] = c4_page(a.r, a.c, b, key + 16 * u);
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
-            const int p = __builtin_amdgcn_readfirstlane(page[u]);
+            const int p = __builtin_amdgcn_readlane(pages, u);
             there |= p >= 0 ? 1u << u : 0u;
             const Half4 half = {reinterpret_cast<Global4>(reinterpret_cast<uintptr_t>(c4_record(a.c, max(p, 0), head))), (key + 16 * u) & (a.c.page - 1), key + 16 * u, true};
             load_k_half<D>(a.c, half, lane, codes[u], exp[u]);
         }
     };
-    load(key0);
+    // (keys that no row sees, as behind a window, are not loaded)
+    auto rows_of = [&](int key) { return weigh_rows(a, s, base, key, min(key + 63, length - 1)); };
+    Rows4Range range = rows_of(key0);
+    locate(key0);
+    if (range.last > range.first) load(key0);
     bf16x8 q[QT][TERMS][M];
     f32x4 origin[QT];
+    // All loads first: the lane's row of every tile (the first of all in place of one that is not there), and the logarithms of four.
     auto load_rows = [&](int row0) {
+        constexpr int LOADS = sizeof(T) == 4 ? 2 : 1;
+        u32x4 x[QT][M][LOADS];
+        float lse[QT][4];
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
-            const int row = row0 + 16 * t + c, token = fast_div(row, a.div_group), g = row - token * a.group;
-            load_q<D, TERMS>(static_cast<const T*>(a.q) + (s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head, row < rows, lane, q[t]);
+            const int row = row0 + 16 * t + c < rows ? row0 + 16 * t + c : 0, token = fast_div(row, a.div_group), g = row - token * a.group;
+            const T* src = static_cast<const T*>(a.q) + (s.first + token) * a.q_token + (long long)(head * a.group + g) * a.q_head;
+            static_for<P::count>([&](auto pc) {
+                constexpr int p = pc.value, W = P::width(p), B = P::base(p);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) origin[t][i] = weigh_origin(a, s, head, row0 + 16 * t + 4 * h4 + i, rows);
+                for (int i = 0; i < W / 32; ++i)
+#pragma unroll
+                    for (int l = 0; l < LOADS; ++l) x[t][B / 32 + i][l] = reinterpret_cast<const u32x4*>(src + B + W / 4 * h4 + 8 * i)[l];
+            });
+#pragma unroll
+            for (int i = 0; i < 4; ++i) lse[t][i] = weigh_lse(a, s, head, min(row0 + 16 * t + 4 * h4 + i, rows - 1));
+        }
+#pragma unroll
+        for (int t = 0; t < QT; ++t) {
+            const bool there = row0 + 16 * t + c < rows;
+#pragma unroll
+            for (int m = 0; m < M; ++m) {
+#pragma unroll
+                for (int l = 0; l < LOADS; ++l)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[t][m][l][i] = there ? x[t][m][l][i] : 0u;
+                weigh_terms<T, TERMS>(x[t][m], q[t], m);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) origin[t][i] = weigh_origin(a, lse[t][i], row0 + 16 * t + 4 * h4 + i < rows);
         }
     };
-    load_rows(0);
+    if (rows <= 16 * QT) load_rows(0);
 
     for (; key0 < length; key0 += stride) {
         const int key1 = min(key0 + 63, length - 1);
         const float old = a.previous != nullptr && key0 + lane < min(base, length) ? a.decay * a.previous[weights + key0 + lane] : 0.f;
         float sum[KT] = {};
-        const Rows4Range range = weigh_rows(a, s, base, key0, key1);
         const unsigned present = there;
+        locate(min(key0 + stride, length - 1));
         // (almost always one turn: a launch has QT by the mean over its sequences)
         for (int row0 = range.first / (16 * QT) * (16 * QT); row0 < range.last; row0 += 16 * QT) {
             if (rows > 16 * QT) load_rows(row0);
             const bool full = (!a.causal || key1 <= base + fast_div(row0, a.div_group)) &&
                               (a.window == 0 || base + fast_div(min(row0 + 16 * QT, rows) - 1, a.div_group) - key0 < a.window);
+            int pos[QT][4] = {};
+            if (!full) {                     // (a row before token 0 sees nothing; differences stay within 32 bits)
+#pragma unroll
+                for (int t = 0; t < QT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pos[t][i] = base + fast_div(row0 + 16 * t + 4 * h4 + i, a.div_group);
+            }
 #pragma unroll
             for (int u = 0; u < KT; ++u) {
                 // (codes that seem to change are converted where they are used: taken out of this loop, the operands of 64 keys would fill the registers)
@@ -130,16 +184,25 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
                             for (int n = 0; n < TERMS; ++n) score[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q[t][n][B / 32 + i], k, score[t], 0, 0, 0);
                     }
                 });
+                if (!full) {
+#pragma unroll
+                    for (int t = 0; t < QT; ++t)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const int key = key0 + 16 * u + c, at = pos[t][i];
+                            if (!((!a.causal || key <= at) && (a.window == 0 || at - key < a.window))) score[t][i] = -__builtin_inff();
+                        }
+                }
 #pragma unroll
                 for (int t = 0; t < QT; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float p = __builtin_amdgcn_exp2f(score[t][i] * a.scale2);
-                        sum[u] += full || weigh_sees(a, base, row0 + 16 * t + 4 * h4 + i, key0 + 16 * u + c) ? p : 0.f;
-                    }
+                    for (int i = 0; i < 4; ++i) sum[u] += __builtin_amdgcn_exp2f(score[t][i] * a.scale2);
             }
         }
-        if (key0 + stride < length) load(key0 + stride);
+        if (key0 + stride < length) {
+            range = rows_of(key0 + stride);
+            if (range.last > range.first) load(key0 + stride);
+        }
         float all = 0.f;
 #pragma unroll
         for (int u = 0; u < KT; ++u) {
@@ -237,30 +300,10 @@ __global__ __launch_bounds__(256, D <= 128 && DTYPE != BNN_F32 ? 3 : 2) void wei
                 chunk_of(e, r, column);
                 const int m = column / 4, quarter = column % 4;
                 u32x4* to = &q_ops[buffer][0][(r / 16) * M + m][16 * quarter + ((r % 16) ^ (12 * (quarter & 1) + (m & 3)))];
-                if constexpr (TERMS == 1) {
-                    *to = raw[e][0];
-                } else {
-                    float x[8];
-                    if constexpr (LOADS == 2) {
+                bf16x8 ops[TERMS][1];
+                weigh_terms<T, TERMS>(raw[e], ops, 0);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(raw[e][i / 4][i % 4]);
-                    } else {
-                        typedef T t8 __attribute__((ext_vector_type(8)));
-                        const t8 y = __builtin_bit_cast(t8, raw[e][0]);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = (float)y[i];
-                    }
-                    bf16x8 split[TERMS];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        __bf16 terms[TERMS];
-                        split_terms<TERMS>(x[i], terms);
-#pragma unroll
-                        for (int n = 0; n < TERMS; ++n) split[n][i] = terms[n];
-                    }
-#pragma unroll
-                    for (int n = 0; n < TERMS; ++n) to[n * TILES * M * 64] = __builtin_bit_cast(u32x4, split[n]);
-                }
+                for (int n = 0; n < TERMS; ++n) to[n * TILES * M * 64] = __builtin_bit_cast(u32x4, ops[n][0]);
             }
         };
         begin_rows(0);
@@ -364,7 +407,10 @@ __global__ __launch_bounds__(256, D <= 128 && DTYPE != BNN_F32 ? 3 : 2) void wei
                 begin_rows(chunk);           // (whole: the rows before began with a whole token as well)
                 __syncthreads();
             }
-            for (int i = (int)threadIdx.x; i < ROWS * here; i += 256) origins[i] = weigh_origin(a, s, head, first + ROWS * chunk + i, rows);
+            for (int i = (int)threadIdx.x; i < ROWS * here; i += 256) {
+                const int row = first + ROWS * chunk + i;
+                origins[i] = weigh_origin(a, weigh_lse(a, s, head, min(row, rows - 1)), row < rows);
+            }
             // waves go through different kinds of steps, each with one barrier
             for (int i = chunk; i < chunk + here;) {
                 const int end = min(chunk + here, i + 256 / ROWS), from = min(max(clear_from, i), end), to = min(max(clear_to, i), end);

@@ -144,7 +144,7 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
             for (int i = 0; i < 4; ++i) origin[t][i] = weigh_origin(a, lse[t][i], row0 + 16 * t + 4 * h4 + i < rows);
         }
     };
-    if (rows <= 16 * QT) load_rows(0);
+    if (rows > 0 && rows <= 16 * QT) load_rows(0);      // (a sequence without rows may lie behind the last)
 
     for (; key0 < length; key0 += stride) {
         const int key1 = min(key0 + 63, length - 1);
@@ -219,7 +219,7 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
 // in LDS for 2048 rows at a time.  A tile's exponentials go with the products of the next.
 // Rows are cut into parts, so that there are workgroups enough; a part's sums go to the workspace, and weigh_join_kernel adds them up in order.
 template <int D, int DTYPE>
-__global__ __launch_bounds__(256, D <= 128 && DTYPE != BNN_F32 ? 3 : 2) void weigh_rows_kernel(Weigh4 a) {
+__global__ __launch_bounds__(256, D <= 128 && DTYPE != BNN_F32 ? 3 : D == 256 && DTYPE == BNN_F32 ? 1 : 2) void weigh_rows_kernel(Weigh4 a) {
     using T = typename C4Type<DTYPE>::type;
     constexpr int TERMS = C4Type<DTYPE>::terms, M = D / 32, KT = cache4_weigh_tiles(D), LOADS = sizeof(T) == 4 ? 2 : 1;
     constexpr int ROWS = TERMS == 1 ? 64 : 32, TILES = ROWS / 16;    // of a step
@@ -360,18 +360,6 @@ __global__ __launch_bounds__(256, D <= 128 && DTYPE != BNN_F32 ? 3 : 2) void wei
                         for (int u = 0; u < KT; ++u) next[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(q, k[u][m], next[u], 0, 0, 0);
                     }
                 add_up();
-                if constexpr (!decltype(masked)::value) {            // operands ahead, exponentials among the products
-                    __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
-#pragma unroll
-                    for (int o = 0; o < M * TERMS; ++o) {
-                        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-#pragma unroll
-                        for (int u = 0; u < KT; ++u) {
-                            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-                            __builtin_amdgcn_sched_group_barrier(0x402, (12 + M * TERMS - 1) / (M * TERMS), 0);
-                        }
-                    }
-                }
                 if constexpr (decltype(masked)::value) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {

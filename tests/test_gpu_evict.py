@@ -122,6 +122,14 @@ def test_weigh_many_rows(bnn, dtype, dim, page, kv_heads, group):
     check_weigh(su, causal=False, previous=False, scale=0.2)
 
 
+@pytest.mark.parametrize("counts", [[3, 0, 2, 0], [0, 0, 0, 1], [200, 0, 1, 0]])
+def test_sequences_without_rows(bnn, counts):
+    """Sequences that bring no row, the last among them: their old weights only fade."""
+    su = Batch(bnn, 33, [40, 25, 210 if counts[0] < 100 else 9, 30] if counts[0] < 100 else [220, 25, 9, 30], counts, group=2)
+    check_weigh(su, decay=0.25)
+    check_weigh(su, window=4, previous=False)
+
+
 def test_weigh_thousands_of_rows(bnn):
     """More rows than lie in LDS at once, against rows a few at a time (bounds: the sums of both, 2 units for every row of a key)."""
     su = Batch(bnn, 31, [1500, 700], [1, 1], kv_heads=2, group=4, dim=64, page=64)

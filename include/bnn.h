@@ -499,7 +499,7 @@ int bnn_cache4_attend(const bnn_cache4* cache, const bnn_cache4_rows* rows, cons
  * Weights from lens[b] on, and of tokens past the table's end, are left as they are.  previous may be weights.  What a row sees is as in bnn_cache4_attend without blocks, and lse [tokens][heads]
  * is what that gave for the same q, scale, causal and window; a row with -infinity there adds nothing, and one with NaN, as it has for a query that holds a NaN or an infinity, makes the weights of what it sees NaN.
  * Tokens on no page get nothing.  Products are of bf16 terms, queries exactly, with fp32 sums; sums are fp32 and in the same order for the same arguments.
- * scale > 0; scale * log2(e) and 1 / scale finite, and |lse| / scale below 2^127.  decay finite.  BNN_ERR_UNSUPPORTED: tokens * heads / kv_heads from 2^30 on, 2^24 workgroups and more (one has 256 keys or more). */
+ * scale > 0; scale * log2(e) and 1 / scale finite, and |lse| / scale below 2^127.  decay finite.  BNN_ERR_UNSUPPORTED: tokens * heads / kv_heads from 2^30 on, 2^24 workgroups and more (one has 128 keys or more).  With no rows at all, weights stay as they are. */
 size_t bnn_cache4_weigh_workspace_bytes(const bnn_cache4* cache, const bnn_cache4_rows* rows, int dtype, int heads);
 int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads, const float* lse,
                      float scale, int causal, int window, const float* previous, float decay, float* weights, int64_t width,
@@ -523,7 +523,7 @@ int bnn_cache4_move(const bnn_cache4* cache, const int32_t* tokens, int keep, co
  *   targets [rows] int64 or NULL (no logprobs then); a target outside [0, cols) gives 0 (no token to be judged).
  *   logprobs, entropy, lse [rows] fp32, each or NULL; top_logprobs [rows][top] fp32 and top_tokens [rows][top] int32, both (NULL if top is 0).
  * Columns of -infinity have no probability.  A row without a distribution -- every logit -infinity, or a NaN or +infinity among them -- gets NaN, tokens of -1, and an lse of -infinity in the first case.
- * Sums are fp32.  The logits are read once.  0 <= top <= 64, top <= cols.  BNN_ERR_UNSUPPORTED: 2^24 and more pieces (of 2048 to 16384 columns of a row each), cols from 2^30 on.
+ * Sums are fp32.  The logits are read once.  0 <= top <= 64, top <= cols.  BNN_ERR_UNSUPPORTED: 2^24 and more pieces (of a row each: 4096 bytes of its columns to 262144, more of them the more rows there are), cols from 2^30 on.
  * ---------------------------------------------------------------------------------------- */
 #define BNN_I32 3
 size_t bnn_token_logprobs_workspace_bytes(int rows, int cols, int dtype, int top);

@@ -1090,6 +1090,8 @@ class Cache4:
             if done is not None:
                 return done if out is None else out
         code, qt, qh = self._elements(q, None, "q")
+        if q.shape[0] == 0:
+            raise ValueError("weights change with the rows of a call: q must have one")
         rows = self._rows(table, lens, start, q.shape[0])
         if _dev(lse, torch.float32, 2, "lse").shape != q.shape[:2] or lse.device != q.device:
             raise ValueError("lse must be [tokens][heads], on q's device")

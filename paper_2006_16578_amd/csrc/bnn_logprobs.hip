@@ -4,7 +4,8 @@
 //   log p = scale (x - m) - log S,  entropy = log S - log 2 W / S  (both terms >= 0),  lse = scale m + log S,
 // so no difference of large numbers is left.  A wave's m is the largest of its first columns, and is raised only when a column passes it by more than 16 (as powers of two), so most columns meet no branch and no
 // rescaling; waves and pieces of a row are joined by the same rule.  What bounds it is memory: 10 instruction slots a column (an exponential counts four) take about four fifths of the time that its
-// two bytes take.
+// two bytes take.  4096 rows of 131072 bf16 columns (1.07 GB): 194 us, 5.5 TB/s.  (With a piece of a row held in registers between a pass for the maximum and one for the sums 816 us.)  The smallest calls, 8 rows of 131072
+// columns in 512 pieces, are two launches: 9.5 us for the pieces, half of it their best columns, and 5.7 for the join.
 //
 // The `top` best: beside that, every thread keeps the largest of each eight of its vectors.  The `top`-th largest of the threads' maxima is a border that at least `top` columns reach and little more do;
 // the vectors' maxima tell where those are, and they are read again, collected in LDS and ranked by counting.  Columns are ordered by (value, lower column first) as one 64-bit number.  Where a border is shared

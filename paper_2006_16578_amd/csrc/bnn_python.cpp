@@ -532,7 +532,7 @@ PyObject* cache4_weigh(PyObject*, PyObject* const* a, Py_ssize_t nargs) {    // 
         const Tensor* previous = a[13] == Py_None ? nullptr : c.tensor(a[13], at::kFloat, 3);
         const Tensor* given = a[15] == Py_None ? nullptr : c.tensor(a[15], at::kFloat, 3);
         PLAIN(c);
-        if (lse.size(0) != q.size(0) || lse.size(1) != q.size(1)) Py_RETURN_NONE;
+        if (q.size(0) < 1 || lse.size(0) != q.size(0) || lse.size(1) != q.size(1)) Py_RETURN_NONE;
         p.finish((int)q.size(0));
         const int64_t room = (int64_t)p.rows.table_pages * p.cache.page;
         if (room > INT_MAX) Py_RETURN_NONE;

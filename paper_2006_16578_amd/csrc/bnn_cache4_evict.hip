@@ -265,14 +265,14 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_part_kernel(Heaviest4 a, P
     const float* weights = a.weights + unit * a.width;
     const int32_t* table = a.table + (long long)b * a.table_pages;
     int* const my_bins = p.bins + ((unit * 3 + LAUNCH) * p.parts + part) * H_BINS;       // (LAUNCH < 3)
-    uint32_t held[E][4];
-    {
-        Four f[E];
+    Four f[E];                               // (ranked once the loads of the counts are under way as well)
 #pragma unroll
-        for (int e = 0; e < E; ++e) f[e] = fetch_four(weights, table, a.c.page_shift, begin + e * H_VECTOR + 4 * lane, end);
+    for (int e = 0; e < E; ++e) f[e] = fetch_four(weights, table, a.c.page_shift, begin + e * H_VECTOR + 4 * lane, end);
+    uint32_t held[E][4];
+    auto rank = [&]() {
 #pragma unroll
         for (int e = 0; e < E; ++e) rank_four(a, f[e], begin + e * H_VECTOR + 4 * lane, end, length, held[e]);
-    }
+    };
     // The sum over a workgroup of each thread's n, for all
     auto total = [&](int n, int* scratch) {
 #pragma unroll
@@ -287,7 +287,8 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_part_kernel(Heaviest4 a, P
 
     Border border = {0, a.keep};
     bool all = false;                        // everything is kept
-    int there = 0;
+    int there = 0, above_before = 0, high_before = 0, low_before = 0;       // of the parts before this one: above the border by digits 0 and 1; counts of the thread's bins
+    if constexpr (LAUNCH == 0) rank();
     if constexpr (LAUNCH > 0) {
         // Digit LAUNCH - 1, from the counts of all parts
         constexpr int digit = LAUNCH - 1;
@@ -300,11 +301,18 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_part_kernel(Heaviest4 a, P
             const int2 n = *reinterpret_cast<const int2*>(counts + (long long)q * H_BINS);
             low += n.x;
             high += n.y;
+            if (q < part) {
+                low_before += n.x;
+                high_before += n.y;
+            }
             if (q == part) {
                 own_low = n.x;
                 own_high = n.y;
             }
         }
+        if constexpr (LAUNCH == 3)           // (not written where all are kept, and not used there)
+            for (int q = tid; q < part; q += H_THREADS) above_before += p.above[unit * 3 * p.parts + q] + p.above[(unit * 3 + 1) * p.parts + q];
+        rank();
         if constexpr (LAUNCH == 1) there = total(high + low, sums[0]);
         all = LAUNCH == 1 ? there <= a.keep : border.count == 0x7fffffff;
         if (all) {
@@ -332,17 +340,19 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_part_kernel(Heaviest4 a, P
     } else {
         // What the parts before this one keep: above the border by one of its digits, and of its own rank
         int over = 0, same = 0;
-        // (the counts of the last digit; where all are kept, of the first, all of which are kept)
-        const int picked = all ? -1 : digit_of(border.rank, 2), top = H_BINS - 1 - 2 * tid;
-        const int* counts = p.bins + (unit * 3 + (all ? 0 : 2)) * (long long)p.parts * H_BINS + top - 1;
+        const int top = H_BINS - 1 - 2 * tid;
+        if (!all) {
+            const int picked = digit_of(border.rank, 2);
+            over = above_before + (top > picked ? high_before : 0) + (top - 1 > picked ? low_before : 0);
+            same = (top == picked ? high_before : 0) + (top - 1 == picked ? low_before : 0);
+        } else {                             // all that is counted by the first digit, the last not having been
+            const int* counts = p.bins + unit * 3 * (long long)p.parts * H_BINS + top - 1;
 #pragma unroll 8
-        for (int q = 0; q < part; ++q) {
-            const int2 n = *reinterpret_cast<const int2*>(counts + (long long)q * H_BINS);
-            over += (top > picked ? n.y : 0) + (top - 1 > picked ? n.x : 0);
-            same += (top == picked ? n.y : 0) + (top - 1 == picked ? n.x : 0);
+            for (int q = 0; q < part; ++q) {
+                const int2 n = *reinterpret_cast<const int2*>(counts + (long long)q * H_BINS);
+                over += n.x + n.y;
+            }
         }
-        if (!all)
-            for (int q = tid; q < part; q += H_THREADS) over += p.above[unit * 3 * p.parts + q] + p.above[(unit * 3 + 1) * p.parts + q];
         __syncthreads();
         over = total(over, sums[0]);
         same = total(same, sums[2]);

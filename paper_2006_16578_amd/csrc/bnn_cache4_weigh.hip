@@ -108,14 +108,13 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
     auto rows_of = [&](int key) { return weigh_rows(a, s, base, key, min(key + 63, length - 1)); };
     Rows4Range range = rows_of(key0);
     locate(key0);
-    if (range.last > range.first) load(key0);
     bf16x8 q[QT][TERMS][M];
     f32x4 origin[QT];
     // All loads first: the lane's row of every tile (the first of all in place of one that is not there), and the logarithms of four.
-    auto load_rows = [&](int row0) {
-        constexpr int LOADS = sizeof(T) == 4 ? 2 : 1;
-        u32x4 x[QT][M][LOADS];
-        float lse[QT][4];
+    constexpr int LOADS = sizeof(T) == 4 ? 2 : 1;
+    u32x4 x[QT][M][LOADS];
+    float lse[QT][4];
+    auto fetch_rows = [&](int row0) {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             const int row = row0 + 16 * t + c < rows ? row0 + 16 * t + c : 0, token = fast_div(row, a.div_group), g = row - token * a.group;
@@ -130,6 +129,8 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) lse[t][i] = weigh_lse(a, s, head, min(row0 + 16 * t + 4 * h4 + i, rows - 1));
         }
+    };
+    auto convert_rows = [&](int row0) {
 #pragma unroll
         for (int t = 0; t < QT; ++t) {
             const bool there = row0 + 16 * t + c < rows;
@@ -145,7 +146,12 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
             for (int i = 0; i < 4; ++i) origin[t][i] = weigh_origin(a, lse[t][i], row0 + 16 * t + 4 * h4 + i < rows);
         }
     };
-    if (rows > 0 && rows <= 16 * QT) load_rows(0);      // (a sequence without rows may lie behind the last)
+    // Rows are loaded, before the first codes, whose pages are waited for, and converted beside those loads, if the wave's last keys are seen (else none of its keys is; a sequence without rows may lie behind the last)
+    const Rows4Range of_last = rows_of(key0 + (length - 1 - key0) / stride * stride);
+    const bool few = rows <= 16 * QT && of_last.last > of_last.first;
+    if (few) fetch_rows(0);
+    if (range.last > range.first) load(key0);
+    if (few) convert_rows(0);
 
     for (; key0 < length; key0 += stride) {
         const int key1 = min(key0 + 63, length - 1);
@@ -155,7 +161,10 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
         locate(min(key0 + stride, length - 1));
         // (almost always one turn: a launch has QT by the mean over its sequences)
         for (int row0 = range.first / (16 * QT) * (16 * QT); row0 < range.last; row0 += 16 * QT) {
-            if (rows > 16 * QT) load_rows(row0);
+            if (rows > 16 * QT) {
+                fetch_rows(row0);
+                convert_rows(row0);
+            }
             const bool full = (!a.causal || key1 <= base + fast_div(row0, a.div_group)) &&
                               (a.window == 0 || base + fast_div(min(row0 + 16 * QT, rows) - 1, a.div_group) - key0 < a.window);
             int pos[QT][4] = {};

@@ -58,20 +58,29 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// The results of a row from its reference point and sums; best: its alternatives, in LDS.  All threads of the workgroup.
+// A row's target, loaded before what the results wait for.
+struct Judged {
+    bool is;                                 // within the columns
+    float x;
+};
 template <class T>
-__device__ __forceinline__ void finish_row(const Logprobs& a, int row, float m, float S, float W, const uint64_t* best) {
+__device__ __forceinline__ Judged load_judged(const Logprobs& a, int row) {
+    Judged j = {false, 0.f};
+    if (a.targets == nullptr) return j;
+    const int64_t t = a.targets[row];
+    j.is = t >= 0 && t < a.cols;
+    if (j.is) j.x = as_float(static_cast<const T*>(a.x)[row * a.ld + t]);
+    return j;
+}
+
+// The results of a row from its reference point and sums; best: its alternatives, in LDS.  All threads of the workgroup.
+__device__ __forceinline__ void finish_row(const Logprobs& a, int row, const Judged& judged, float m, float S, float W, const uint64_t* best) {
     const bool none = !(S > 0.f);            // S is NaN, or 0: no distribution
     const float log_s = __builtin_amdgcn_logf(S) * LP_LN2, nan = __builtin_nanf("");
     if (threadIdx.x == 0) {
         if (a.lse != nullptr) a.lse[row] = none ? (S == 0.f ? -__builtin_inff() : nan) : fmaf(m, a.scale, log_s);
         if (a.entropy != nullptr) a.entropy[row] = none ? nan : log_s - LP_LN2 * (W / S);
-        if (a.targets != nullptr && a.logprobs != nullptr) {
-            const int64_t t = a.targets[row];
-            float lp = 0.f;
-            if (t >= 0 && t < a.cols) lp = none ? nan : fmaf(as_float(static_cast<const T*>(a.x)[row * a.ld + t]) - m, a.scale, -log_s);
-            a.logprobs[row] = lp;
-        }
+        if (a.targets != nullptr) a.logprobs[row] = !judged.is ? 0.f : none ? nan : fmaf(judged.x - m, a.scale, -log_s);
     }
     for (int i = (int)threadIdx.x; i < a.top; i += (int)blockDim.x) {
         const uint64_t key = best[i];
@@ -165,9 +174,10 @@ __device__ __forceinline__ void best_of_piece(const Logprobs& a, const T* x, int
             if (ties ? o > border : o >= border && o != 0) pairs[atomicAdd(&pair_count, 1)] = (uint16_t)(s << 8 | tid);
         }
         __syncthreads();
-        const int n = pair_count * (LP_SEGMENT * V);
+        const int wide = vectors > 4 ? 3 : vectors > 2 ? 2 : vectors > 1 ? 1 : 0;      // 2^wide vectors at least are behind a maximum
+        const int n = pair_count * V << wide;
         for (int i = tid; i < n; i += 256) {
-            const int pair = pairs[i / (LP_SEGMENT * V)], v = (pair >> 8) * LP_SEGMENT + i / V % LP_SEGMENT;
+            const int pair = pairs[i / V >> wide], v = (pair >> 8) * LP_SEGMENT + (i / V & ((1 << wide) - 1));
             const int col = piece_first + (v * 256 + (pair & 255)) * V + i % V;
             if (v >= vectors || col < 0 || col >= a.cols) continue;
             const float y = as_float(x[col]);
@@ -260,6 +270,8 @@ __global__ __launch_bounds__(256) void logprobs_kernel(Logprobs a) {
     const int piece_first = piece * a.vectors * (256 * V) - off, first = piece_first + (int)threadIdx.x * V;
     const int vectors = min(a.vectors, (a.cols - piece_first + 256 * V - 1) / (256 * V));       // with columns
     const float c = a.scale2;
+    Judged judged = {false, 0.f};
+    if (a.pieces == 1) judged = load_judged<T>(a, row);
 
     float m = 0.f, limit = -__builtin_inff(), S = 0.f, W = 0.f;      // limit: what a column may be before m is raised; -infinity: nothing but -infinity so far
     float segment = -__builtin_inff();
@@ -345,7 +357,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(Logprobs a) {
         W = fmaf(f, fmaf(part[1][w], fmaxf(d, -1e30f), part[2][w]), W);
     }
     if (a.pieces == 1) {
-        finish_row<T>(a, row, m, S, W, best);
+        finish_row(a, row, judged, m, S, W, best);
     } else {
         if (threadIdx.x == 0) a.sums[blockIdx.x] = f32x4{m, S, W, 0.f};
         if constexpr (TOP)
@@ -365,6 +377,16 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(Logprobs a) {
     __shared__ int count;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int row = (int)blockIdx.x;
+    // What is needed last is loaded first: the target, and the best of as many pieces as are looked at together
+    const Judged judged = load_judged<T>(a, row);
+    const uint64_t* from = a.best + (long long)row * a.pieces * a.top;
+    const int together = a.top > 0 ? LP_LIST / a.top : 0, first_keys = min(together, a.pieces) * a.top;      // pieces, the best so far counting as one
+    uint64_t ahead[LP_LIST / 256];
+#pragma unroll
+    for (int i = 0; i < LP_LIST / 256; ++i) {
+        ahead[i] = 0;
+        if (256 * i + (int)threadIdx.x < first_keys) ahead[i] = from[256 * i + threadIdx.x];
+    }
     const f32x4* sums = a.sums + (long long)row * a.pieces;
     float m = -__builtin_inff();
     for (int i = (int)threadIdx.x; i < a.pieces; i += 256) {
@@ -391,13 +413,17 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(Logprobs a) {
         part[2][wave] = W;
     }
     if (a.top > 0) {
-        const uint64_t* from = a.best + (long long)row * a.pieces * a.top;
-        const int together = LP_LIST / a.top;                        // pieces, the best so far counting as one
         int done = 0;
         for (bool more = false; done < a.pieces; more = true) {
             const int some = min(together - (more ? 1 : 0), a.pieces - done), lists = some + (more ? 1 : 0), n = lists * a.top;
             __syncthreads();                 // best is whole
-            for (int i = (int)threadIdx.x; i < some * a.top; i += 256) list[i] = from[(long long)done * a.top + i];
+            if (!more) {
+#pragma unroll
+                for (int i = 0; i < LP_LIST / 256; ++i)
+                    if (256 * i + (int)threadIdx.x < first_keys) list[256 * i + threadIdx.x] = ahead[i];
+            } else {
+                for (int i = (int)threadIdx.x; i < some * a.top; i += 256) list[i] = from[(long long)done * a.top + i];
+            }
             if (more)
                 for (int i = (int)threadIdx.x; i < a.top; i += 256) list[some * a.top + i] = best[i];
             if (threadIdx.x == 0) {
@@ -424,7 +450,7 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(Logprobs a) {
         }
     }
     __syncthreads();
-    finish_row<T>(a, row, m, part[1][0] + part[1][1] + part[1][2] + part[1][3], part[2][0] + part[2][1] + part[2][2] + part[2][3], best);
+    finish_row(a, row, judged, m, part[1][0] + part[1][1] + part[1][2] + part[1][3], part[2][0] + part[2][1] + part[2][2] + part[2][3], best);
 }
 
 inline int size_of(int dtype) { return dtype == BNN_F32 || dtype == BNN_I32 ? 4 : dtype == BNN_BF16 || dtype == BNN_F16 ? 2 : 0; }

@@ -241,7 +241,7 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_kernel(Heaviest4 a) {
 }
 
 // Long sequences, few of them: a workgroup has 8192 tokens of one, in registers, and four launches pass the histograms on through the workspace.  Launch d < 3 counts digit d, having picked digit d - 1 from all
-// parts' counts; the last writes the tokens, the place of its first one being what the parts before it keep.  One sequence of 131072 tokens, 8 kv heads: 5 + 9 + 8 + 12 us; in one workgroup for each head 118.
+// parts' counts; the last writes the tokens, the place of its first one being what the parts before it keep.  One sequence of 131072 tokens, 4 kv heads: 5 + 9 + 8 + 10 us; in one workgroup for each head 118.
 struct Parts4 {
     int parts;
     int* bins;                               // [unit][digit][part][bins]; unit: sequence and kv head

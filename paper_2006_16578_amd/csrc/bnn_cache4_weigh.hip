@@ -72,8 +72,9 @@ __device__ __forceinline__ WeighTiles weigh_row_tiles(const Rows4Range& range, i
 }
 constexpr int WEIGH_ROWS = 2048;             // rows whose numbers lie in LDS at once
 
-// Few rows: a wave passes over its sequence's keys, 64 at a time, codes of the next 64 under way.  Bounded by memory: 64 single tokens over 500 to 8192 keys, 8 kv heads of 128, 42 us, 4.0 TB/s (a workgroup's first loads
-// wait for a length, a page and the rows; 2048 or 8192 workgroups in place of 4096: 57 and 53 us against 52 before pages were looked up ahead; codes loaded two turns ahead leave room for fewer waves: 57).
+// Few rows: a wave passes over its sequence's keys, 64 at a time, codes of the next 64 under way.  Bounded by memory: 64 single tokens over 500 to 8192 keys, 8 kv heads of 128, 41 us, 4.1 TB/s (a workgroup's first loads
+// wait for a length, a page and the rows; 2048 or 8192 workgroups in place of 4096: 57 and 53 us against 52 before pages were looked up ahead; codes loaded two turns ahead leave room for fewer waves: 57).  Few keys, 16 drafts of 5
+// tokens within a window of 1000, heads of 192: 13 us, the same chain of loads; 15.8 when every wave loaded its rows.
 template <int D, int DTYPE, int QT>
 __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
     using T = typename C4Type<DTYPE>::type;

@@ -5,7 +5,7 @@
 // so no difference of large numbers is left.  A wave's m is the largest of its first columns, and is raised only when a column passes it by more than 16 (as powers of two), so most columns meet no branch and no
 // rescaling; waves and pieces of a row are joined by the same rule.  What bounds it is memory: 10 instruction slots a column (an exponential counts four) take about four fifths of the time that its
 // two bytes take.  4096 rows of 131072 bf16 columns (1.07 GB): 194 us, 5.5 TB/s.  (With a piece of a row held in registers between a pass for the maximum and one for the sums 816 us.)  The smallest calls, 8 rows of 131072
-// columns in 512 pieces, are two launches: 9.5 us for the pieces, half of it their best columns, and 5.7 for the join.
+// columns in 512 pieces, are two launches: 6.8 us for the pieces and 6 for the join, chains of loads and barriers.
 //
 // The `top` best: beside that, every thread keeps the largest of each eight of its vectors.  The `top`-th largest of the threads' maxima is a border that at least `top` columns reach and little more do;
 // the vectors' maxima tell where those are, and they are read again, collected in LDS and ranked by counting.  Columns are ordered by (value, lower column first) as one 64-bit number.  Where a border is shared
@@ -58,7 +58,7 @@ __device__ __forceinline__ float wave_sum(float v) {
     return v;
 }
 
-// A row's target, loaded before what the results wait for.
+// A row's target.  (The join loads it ahead of its sums.)
 struct Judged {
     bool is;                                 // within the columns
     float x;
@@ -270,8 +270,6 @@ __global__ __launch_bounds__(256) void logprobs_kernel(Logprobs a) {
     const int piece_first = piece * a.vectors * (256 * V) - off, first = piece_first + (int)threadIdx.x * V;
     const int vectors = min(a.vectors, (a.cols - piece_first + 256 * V - 1) / (256 * V));       // with columns
     const float c = a.scale2;
-    Judged judged = {false, 0.f};
-    if (a.pieces == 1) judged = load_judged<T>(a, row);
 
     float m = 0.f, limit = -__builtin_inff(), S = 0.f, W = 0.f;      // limit: what a column may be before m is raised; -infinity: nothing but -infinity so far
     float segment = -__builtin_inff();
@@ -357,7 +355,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(Logprobs a) {
         W = fmaf(f, fmaf(part[1][w], fmaxf(d, -1e30f), part[2][w]), W);
     }
     if (a.pieces == 1) {
-        finish_row(a, row, judged, m, S, W, best);
+        finish_row(a, row, load_judged<T>(a, row), m, S, W, best);
     } else {
         if (threadIdx.x == 0) a.sums[blockIdx.x] = f32x4{m, S, W, 0.f};
         if constexpr (TOP)

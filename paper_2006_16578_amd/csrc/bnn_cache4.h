@@ -284,15 +284,17 @@ struct Weigh4 {
     float* out;
     float decay;
     long long width;
+    int few_most;                            // sequences of up to so many rows are the launch's for few rows, others that for many
+    int many;                                // sequences of the launch for many rows: all, or fewer, to be looked for
     int parts;                               // of a launch for few rows: that share a sequence's keys; for many: that share the rows of a tile of keys
-    FastDiv div_parts, div_batch;
+    FastDiv div_parts, div_many;
     float* partial;                          // [batch][kv_heads][parts][width4], with several parts of the rows
     long long width4;                        // tokens that the table has room for
 };
-// How such a call is cut up.  row_tiles: tiles of 16 rows that a wave carries, 0: the kernel for many rows.
+// How such a call is cut up: a launch for sequences of few rows (row_tiles: tiles of 16 rows that a wave carries, 0: no such launch), one for those of many (many: how many there can be, 0: none), or both.
 struct WeighPlan4 {
-    int row_tiles, parts;
-    long long workgroups;
+    int few_most, row_tiles, few_parts, many, many_parts;
+    long long few_groups, many_groups;
     size_t workspace_bytes;
 };
 constexpr int cache4_weigh_tiles(int dim) { return dim >= 192 ? 2 : 4; }          // tiles of 16 keys that a wave of that kernel keeps

@@ -1,4 +1,5 @@
 // C entries of the 4-bit key/value cache: checks of the arguments, and how a call is cut into workgroups.
+#include <limits.h>
 #include <math.h>
 
 #include <algorithm>
@@ -102,22 +103,27 @@ bool weigh_takes(const Cache4& c, const Rows4& r, int group) {
     return (long long)r.tokens * group < (1LL << 30) && ((long long)r.table_pages << c.page_shift) <= (1LL << 30);
 }
 
-// How weights are added up.  By the mean of rows over the batch, as attention is: up to 32 rows the kernel whose waves carry them, in as many workgroups as keep the chip busy with their loads (4096); else the one whose
-// waves carry keys, with the rows of a tile of keys cut into parts until there are 2048 workgroups, 256 rows at least.
+// How weights are added up.  Sequences of up to 32 rows by the kernel whose waves carry them, in as many workgroups as keep the chip busy with their loads (4096); of more by the one whose
+// waves carry keys, with the rows of a tile of keys cut into parts until there are 2048 workgroups, 256 rows at least.  (Drafts of 30 rows: 20 us by the first, 34 by the second.)  Where sequences differ (start), lengths of their runs being
+// on the device, both are launched: the first has sequences of up to 64 rows, the second the others, of which there are at most as many as the call has rows for, each of its workgroups looking for its own.
 // near_rows: whether that kernel's offsets, of 2304 rows in 32 bits, reach (products of 24 bits); the other serves any distances.
 WeighPlan4 plan_weigh(const Cache4& c, const Rows4& r, int dtype, int group, bool near_rows) {
     WeighPlan4 p = {};
-    const long long rows = cdiv((long long)r.tokens * group, r.batch), room = (long long)r.table_pages << c.page_shift, sequences = (long long)r.batch * c.kv_heads;
-    if (rows <= 32 || !near_rows) {
-        p.row_tiles = rows > 16 && cache4_weigh_two(c.dim, dtype) ? 2 : 1;
-        p.parts = (int)std::max(1LL, std::min(cdiv(4096, sequences), cdiv(room, 256)));
-        p.workgroups = sequences * p.parts;
-        return p;
+    const long long all = (long long)r.tokens * group, rows = cdiv(all, r.batch), room = (long long)r.table_pages << c.page_shift, sequences = (long long)r.batch * c.kv_heads;
+    p.few_most = !near_rows ? INT_MAX : r.start ? 64 : rows <= 32 ? INT_MAX : -1;
+    if (p.few_most >= 0) {
+        p.row_tiles = rows > 16 && rows <= 32 && cache4_weigh_two(c.dim, dtype) ? 2 : 1;
+        p.few_parts = (int)std::max(1LL, std::min(cdiv(4096, sequences), cdiv(room, 256)));
+        p.few_groups = sequences * p.few_parts;
     }
-    const long long units = sequences * cdiv(room, 64 * cache4_weigh_tiles(c.dim));
-    p.parts = (int)std::max(1LL, std::min(cdiv(2048, units), cdiv(rows, 256)));
-    p.workgroups = units * p.parts;
-    if (p.parts > 1) p.workspace_bytes = (size_t)sequences * p.parts * room * sizeof(float);
+    p.many = p.few_most < 0 ? r.batch : (int)std::min<long long>(r.batch, all / (p.few_most + 1LL));
+    if (p.many > 0) {
+        const long long units = (long long)p.many * c.kv_heads * cdiv(room, 64 * cache4_weigh_tiles(c.dim));
+        p.many_parts = (int)std::max(1LL, std::min(cdiv(2048, units), cdiv(cdiv(all, p.many), 256)));
+        if (sequences * cdiv(room, 256) >= C4_THREADS / 256) p.many_parts = 1;       // (the joining launch)
+        p.many_groups = units * p.many_parts;
+        if (p.many_parts > 1) p.workspace_bytes = (size_t)sequences * p.many_parts * room * sizeof(float);
+    }
     return p;
 }
 
@@ -307,7 +313,7 @@ int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const
     const bool near_rows = q_token >= 0 && q_head >= 0 && q_token < far && q_head < far && a.group < far &&
                            ((2304 / a.group + 2) * q_token + a.group * q_head + a.c.dim) * element_bytes(dtype) < (1LL << 32);
     const WeighPlan4 p = plan_weigh(a.c, a.r, dtype, a.group, near_rows);
-    if (p.workgroups >= C4_THREADS / 256) return BNN_ERR_UNSUPPORTED;
+    if (std::max(p.few_groups, p.many_groups) >= C4_THREADS / 256) return BNN_ERR_UNSUPPORTED;
     if (p.workspace_bytes != 0 && (!workspace || workspace_bytes < p.workspace_bytes)) return BNN_ERR_WORKSPACE;
     if (p.workspace_bytes != 0 && !aligned16(workspace)) return BNN_ERR_ALIGNMENT;
     a.q = q; a.q_token = q_token; a.q_head = q_head;
@@ -316,9 +322,9 @@ int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const
     a.causal = causal ? 1 : 0;
     a.window = window;
     a.lse = lse; a.previous = previous; a.decay = decay; a.out = weights; a.width = width;
-    a.parts = p.parts;
-    a.div_parts = make_fastdiv((uint32_t)p.parts);
-    a.div_batch = make_fastdiv((uint32_t)a.r.batch);
+    a.few_most = p.few_most;
+    a.many = p.many;
+    if (p.many > 0) a.div_many = make_fastdiv((uint32_t)p.many);
     a.partial = static_cast<float*>(workspace);
     a.width4 = (long long)a.r.table_pages << a.c.page_shift;
     return launch_cache4_weigh(a, p, dtype, static_cast<hipStream_t>(stream));

@@ -88,7 +88,7 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
     const int length = min(s.length, c4_room(a.r, a.c)), base = s.length - s.rows, rows = s.rows * a.group;
     const int stride = a.parts * 4 * 64;
     int key0 = (part * 4 + wave) * 64;
-    if (key0 >= length) return;
+    if (key0 >= length || rows > a.few_most) return;
     const long long weights = ((long long)b * a.c.kv_heads + head) * a.width;
 
     uint32_t codes[KT][M], exp[KT][P::count];
@@ -224,6 +224,22 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
     }
 }
 
+// The nth sequence of more rows than weigh_kernel has, or -1: a wave counts 64 at a time.
+__device__ __forceinline__ int many_rows_sequence(const Weigh4& a, int nth) {
+    const int lane = (int)threadIdx.x & 63;
+    for (int b0 = 0; b0 < a.r.batch; b0 += 64) {
+        const bool is = b0 + lane < a.r.batch && c4_sequence(a.r, min(b0 + lane, a.r.batch - 1)).rows * a.group > a.few_most;
+        unsigned long long mask = __ballot(is);
+        const int have = __popcll(mask);
+        if (nth < have) {
+            for (; nth > 0; --nth) mask &= mask - 1;
+            return __builtin_amdgcn_readfirstlane(b0 + __ffsll(mask) - 1);
+        }
+        nth -= have;
+    }
+    return -1;
+}
+
 // Many rows: a workgroup's four waves have 16 * KT keys each, as finished operands in registers, and pass over the same rows, which lie in LDS as finished operands too.  Rows come with whole lines to a load
 // (four lanes beside each other a row's 64 bytes: a lane of a matrix operand has a row of its own, and loads of that shape take a cycle of the first cache for every lane), go to registers while the
 // step before last is computed and from there to LDS, where the 16-byte places of an operand are exchanged by an exclusive or, so that neither writes nor reads meet.  Numbers that sums begin with lie
@@ -244,11 +260,13 @@ __global__ __launch_bounds__(256, D <= 128 && DTYPE != BNN_F32 ? 3 : D == 256 &&
     // heads fastest (rows stay in a die's cache, with eight kv heads or a divisor), the first keys first: causal rows make those the longest
     const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads;
     const int outer = fast_div(rest, a.div_parts), part = rest - outer * a.parts;
-    const int tile = fast_div(outer, a.div_batch), b = outer - tile * a.r.batch;
+    const int tile = fast_div(outer, a.div_many), nth = outer - tile * a.many;
+    const int b = a.many == a.r.batch ? nth : many_rows_sequence(a, nth);
+    if (b < 0) return;
     const Sequence4 s = c4_sequence(a.r, b);
     const int length = min(s.length, c4_room(a.r, a.c)), base = s.length - s.rows, rows = s.rows * a.group;
     const int block0 = tile * 64 * KT, key0 = block0 + wave * 16 * KT;
-    if (block0 >= length) return;
+    if (block0 >= length || rows <= a.few_most) return;
 
     const WeighTiles all_tiles = weigh_row_tiles(weigh_rows(a, s, base, block0, min(block0 + 64 * KT, length) - 1), a.parts);
     const int first = all_tiles.first + 64 * all_tiles.each * part, steps = 64 / ROWS * max(min(all_tiles.count - all_tiles.each * part, all_tiles.each), 0);
@@ -455,7 +473,7 @@ __global__ __launch_bounds__(256) void weigh_join_kernel(Weigh4 a, int tile, int
     const int key = ((int)blockIdx.x - rest * blocks) * 256 + (int)threadIdx.x, b = rest;
     const Sequence4 s = c4_sequence(a.r, b);
     const int length = min(s.length, c4_room(a.r, a.c)), base = s.length - s.rows;
-    if (key >= length) return;
+    if (key >= length || s.rows * a.group <= a.few_most) return;
     const int block0 = key / tile * tile;
     const Rows4Range range = weigh_rows(a, s, base, block0, min(block0 + tile, length) - 1);
     const long long sequence = (long long)b * a.c.kv_heads + head;
@@ -469,15 +487,20 @@ __global__ __launch_bounds__(256) void weigh_join_kernel(Weigh4 a, int tile, int
 }
 
 template <int D, int DTYPE>
-int launch_weigh(const Weigh4& a, const WeighPlan4& p, hipStream_t s) {
-    const dim3 grid((unsigned)p.workgroups);
-    if (p.row_tiles == 0) {
-        launch(weigh_rows_kernel<D, DTYPE>, grid, dim3(256), 0, s, a);
-    } else {
+int launch_weigh(Weigh4 a, const WeighPlan4& p, hipStream_t s) {
+    if (p.row_tiles > 0) {
+        a.parts = p.few_parts;
+        a.div_parts = make_fastdiv((uint32_t)a.parts);
+        const dim3 grid((unsigned)p.few_groups);
         if constexpr (cache4_weigh_two(D, DTYPE)) {
             if (p.row_tiles == 2) launch(weigh_kernel<D, DTYPE, 2>, grid, dim3(256), 0, s, a);
         }
         if (p.row_tiles == 1) launch(weigh_kernel<D, DTYPE, 1>, grid, dim3(256), 0, s, a);
+    }
+    if (p.many > 0) {
+        a.parts = p.many_parts;
+        a.div_parts = make_fastdiv((uint32_t)a.parts);
+        launch(weigh_rows_kernel<D, DTYPE>, dim3((unsigned)p.many_groups), dim3(256), 0, s, a);
     }
     if (p.workspace_bytes != 0) {
         const int blocks = (int)cdiv((long long)a.r.table_pages << a.c.page_shift, 256);

@@ -130,6 +130,15 @@ def test_sequences_without_rows(bnn, lens, counts):
     check_weigh(su, window=4, previous=False)
 
 
+@pytest.mark.parametrize("dtype,dim,counts", [("bf16", 64, [1] * 3 + [40] + [1] * 62 + [150] + [1, 0, 33]), ("f16", 128, [1, 300, 0, 2, 260]), ("f32", 96, [64, 65, 32, 33, 1]), ("bf16", 192, [0] * 130 + [90, 3]),
+                                              ("bf16", 64, [200] + [0] * 70)])
+def test_single_tokens_beside_prompts(bnn, dtype, dim, counts):
+    """Sequences of few rows and of many in one call, the latter looked for among up to 132; in parts and in one."""
+    su = Batch(bnn, 37, [n + 3 + b % 5 for b, n in enumerate(counts)], counts, group=2, dim=dim, dtype=dtype)
+    check_weigh(su, decay=0.75)
+    check_weigh(su, window=19, previous=False)
+
+
 def test_weigh_thousands_of_rows(bnn):
     """More rows than lie in LDS at once, against rows a few at a time (bounds: the sums of both, 2 units for every row of a key)."""
     su = Batch(bnn, 31, [1500, 700], [1, 1], kv_heads=2, group=4, dim=64, page=64)

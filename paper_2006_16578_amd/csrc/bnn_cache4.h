@@ -285,15 +285,15 @@ struct Weigh4 {
     float decay;
     long long width;
     int few_most;                            // sequences of up to so many rows are the launch's for few rows, others that for many
-    int many;                                // sequences of the launch for many rows: all, or fewer, to be looked for
-    int parts;                               // of a launch for few rows: that share a sequence's keys; for many: that share the rows of a tile of keys
-    FastDiv div_parts, div_many;
-    float* partial;                          // [batch][kv_heads][parts][width4], with several parts of the rows
+    int parts;                               // of a launch for few rows: that share a sequence's keys; for many: that share the rows of a tile of keys, where all sequences have as many
+    int items, part_shift;                   // (sequence, part) pairs of the launch for many rows; where sequences differ, a part has 2^part_shift rows at most
+    FastDiv div_parts, div_items;
+    float* partial;                          // [items][kv_heads][width4], of sequences in several parts
     long long width4;                        // tokens that the table has room for
 };
-// How such a call is cut up: a launch for sequences of few rows (row_tiles: tiles of 16 rows that a wave carries, 0: no such launch), one for those of many (many: how many there can be, 0: none), or both.
+// How such a call is cut up: a launch for sequences of few rows (row_tiles: tiles of 16 rows that a wave carries, 0: no such launch), one for those of many (items: pairs of a sequence and a part of its rows that there can be, 0: no such launch), or both.
 struct WeighPlan4 {
-    int few_most, row_tiles, few_parts, many, many_parts;
+    int few_most, row_tiles, few_parts, items, many_parts, part_shift;
     long long few_groups, many_groups;
     size_t workspace_bytes;
 };

@@ -105,7 +105,7 @@ bool weigh_takes(const Cache4& c, const Rows4& r, int group) {
 
 // How weights are added up.  Sequences of up to 32 rows by the kernel whose waves carry them, in as many workgroups as keep the chip busy with their loads (4096); of more by the one whose
 // waves carry keys, with the rows of a tile of keys cut into parts until there are 2048 workgroups, 256 rows at least.  (Drafts of 30 rows: 20 us by the first, 34 by the second.)  Where sequences differ (start), lengths of their runs being
-// on the device, both are launched: the first has sequences of up to 64 rows, the second the others, of which there are at most as many as the call has rows for, each of its workgroups looking for its own.
+// on the device, both are launched: the first has sequences of up to 64 rows, the second the others, of which there are at most as many as the call has rows for, in parts of 256 to 2048 rows, each of its workgroups looking for its own.
 // near_rows: whether that kernel's offsets, of 2304 rows in 32 bits, reach (products of 24 bits); the other serves any distances.
 WeighPlan4 plan_weigh(const Cache4& c, const Rows4& r, int dtype, int group, bool near_rows) {
     WeighPlan4 p = {};
@@ -116,13 +116,27 @@ WeighPlan4 plan_weigh(const Cache4& c, const Rows4& r, int dtype, int group, boo
         p.few_parts = (int)std::max(1LL, std::min(cdiv(4096, sequences), cdiv(room, 256)));
         p.few_groups = sequences * p.few_parts;
     }
-    p.many = p.few_most < 0 ? r.batch : (int)std::min<long long>(r.batch, all / (p.few_most + 1LL));
-    if (p.many > 0) {
-        const long long units = (long long)p.many * c.kv_heads * cdiv(room, 64 * cache4_weigh_tiles(c.dim));
-        p.many_parts = (int)std::max(1LL, std::min(cdiv(2048, units), cdiv(cdiv(all, p.many), 256)));
-        if (sequences * cdiv(room, 256) >= C4_THREADS / 256) p.many_parts = 1;       // (the joining launch)
-        p.many_groups = units * p.many_parts;
-        if (p.many_parts > 1) p.workspace_bytes = (size_t)sequences * p.many_parts * room * sizeof(float);
+    const long long many = p.few_most < 0 ? r.batch : std::min<long long>(r.batch, all / (p.few_most + 1LL)), units = c.kv_heads * cdiv(room, 64 * cache4_weigh_tiles(c.dim));
+    if (many > 0) {
+        long long items = many;
+        const bool one = r.batch * cdiv(room, 256) >= C4_THREADS / 256;      // (the joining launch does not reach)
+        p.many_parts = 1;
+        p.part_shift = 30;
+        if (!r.start && !one) {
+            p.many_parts = (int)std::max(1LL, std::min(cdiv(2048, units * many), cdiv(rows, 256)));
+            items = many * p.many_parts;
+        } else if (r.start && !one) {
+            p.part_shift = 8;
+            while (p.part_shift < 11 && (all * units) >> p.part_shift > 2048) ++p.part_shift;
+            if (all > 1LL << p.part_shift) {
+                items = many + (all >> p.part_shift);
+                p.many_parts = 2;            // at most, that is not 1
+            }
+        }
+        if (items * c.kv_heads >= C4_THREADS) items = C4_THREADS;            // (refused by the groups)
+        p.items = (int)std::min<long long>(items, INT_MAX);
+        p.many_groups = items * units;
+        if (p.many_parts > 1) p.workspace_bytes = (size_t)p.items * c.kv_heads * room * sizeof(float);
     }
     return p;
 }
@@ -323,8 +337,9 @@ int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const
     a.window = window;
     a.lse = lse; a.previous = previous; a.decay = decay; a.out = weights; a.width = width;
     a.few_most = p.few_most;
-    a.many = p.many;
-    if (p.many > 0) a.div_many = make_fastdiv((uint32_t)p.many);
+    a.items = p.items;
+    a.part_shift = p.part_shift;
+    if (p.items > 0) a.div_items = make_fastdiv((uint32_t)p.items);
     a.partial = static_cast<float*>(workspace);
     a.width4 = (long long)a.r.table_pages << a.c.page_shift;
     return launch_cache4_weigh(a, p, dtype, static_cast<hipStream_t>(stream));

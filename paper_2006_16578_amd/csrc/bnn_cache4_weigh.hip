@@ -224,20 +224,51 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
     }
 }
 
-// The nth sequence of more rows than weigh_kernel has, or -1: a wave counts 64 at a time.
-__device__ __forceinline__ int many_rows_sequence(const Weigh4& a, int nth) {
-    const int lane = (int)threadIdx.x & 63;
-    for (int b0 = 0; b0 < a.r.batch; b0 += 64) {
-        const bool is = b0 + lane < a.r.batch && c4_sequence(a.r, min(b0 + lane, a.r.batch - 1)).rows * a.group > a.few_most;
-        unsigned long long mask = __ballot(is);
-        const int have = __popcll(mask);
-        if (nth < have) {
-            for (; nth > 0; --nth) mask &= mask - 1;
-            return __builtin_amdgcn_readfirstlane(b0 + __ffsll(mask) - 1);
-        }
-        nth -= have;
+// A sequence and part of its rows that a launch for many rows has.
+struct WeighItem {
+    int b, part, parts;
+};
+__device__ __forceinline__ int weigh_parts(const Weigh4& a, int b) {         // where sequences differ
+    const int rows = c4_sequence(a.r, b).rows * a.group;
+    return rows > a.few_most ? (int)(((long long)rows + (1LL << a.part_shift) - 1) >> a.part_shift) : 0;
+}
+// The nth of them, b -1 where there are fewer: a wave counts those of 64 sequences at a time.
+__device__ __forceinline__ WeighItem weigh_item(const Weigh4& a, int nth) {
+    if (a.r.start == nullptr) {
+        const int b = fast_div(nth, a.div_parts);
+        return {b, nth - b * a.parts, a.parts};
     }
-    return -1;
+    const int lane = (int)threadIdx.x & 63;
+    int before = 0;                          // never more than nth
+    for (int b0 = 0; b0 < a.r.batch; b0 += 64) {
+        const int n = b0 + lane < a.r.batch ? weigh_parts(a, b0 + lane) : 0;
+        int sum = n;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int other = __shfl_up(sum, d);
+            if (lane >= d) sum += other;
+        }
+        const unsigned long long past = __ballot(before + sum > nth);
+        if (past != 0) {
+            const int at = __ffsll(past) - 1, parts = __builtin_amdgcn_readlane(n, at);
+            return {b0 + at, nth - (before + __builtin_amdgcn_readlane(sum, at) - parts), parts};
+        }
+        before += __builtin_amdgcn_readlane(sum, 63);
+    }
+    return {-1, 0, 0};
+}
+// The first of sequence b, or a.items where its number is no less.
+__device__ __forceinline__ int weigh_first_item(const Weigh4& a, int b) {
+    if (a.r.start == nullptr) return b * a.parts;
+    const int lane = (int)threadIdx.x & 63;
+    int before = 0;
+    for (int b0 = 0; b0 < b && before < a.items; b0 += 64) {
+        int n = b0 + lane < b ? weigh_parts(a, b0 + lane) : 0;
+#pragma unroll
+        for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
+        before += n;
+    }
+    return min(before, a.items);
 }
 
 // Many rows: a workgroup's four waves have 16 * KT keys each, as finished operands in registers, and pass over the same rows, which lie in LDS as finished operands too.  Rows come with whole lines to a load
@@ -259,18 +290,18 @@ __global__ __launch_bounds__(256, D <= 128 && DTYPE != BNN_F32 ? 3 : D == 256 &&
     const int c = lane & 15, h4 = lane >> 4;
     // heads fastest (rows stay in a die's cache, with eight kv heads or a divisor), the first keys first: causal rows make those the longest
     const int rest = fast_div((int)blockIdx.x, a.div_heads), head = (int)blockIdx.x - rest * a.c.kv_heads;
-    const int outer = fast_div(rest, a.div_parts), part = rest - outer * a.parts;
-    const int tile = fast_div(outer, a.div_many), nth = outer - tile * a.many;
-    const int b = a.many == a.r.batch ? nth : many_rows_sequence(a, nth);
+    const int tile = fast_div(rest, a.div_items), nth = rest - tile * a.items;
+    const WeighItem item = weigh_item(a, nth);
+    const int b = item.b, part = item.part, parts = item.parts;
     if (b < 0) return;
     const Sequence4 s = c4_sequence(a.r, b);
     const int length = min(s.length, c4_room(a.r, a.c)), base = s.length - s.rows, rows = s.rows * a.group;
     const int block0 = tile * 64 * KT, key0 = block0 + wave * 16 * KT;
-    if (block0 >= length || rows <= a.few_most) return;
+    if (block0 >= length) return;
 
-    const WeighTiles all_tiles = weigh_row_tiles(weigh_rows(a, s, base, block0, min(block0 + 64 * KT, length) - 1), a.parts);
+    const WeighTiles all_tiles = weigh_row_tiles(weigh_rows(a, s, base, block0, min(block0 + 64 * KT, length) - 1), parts);
     const int first = all_tiles.first + 64 * all_tiles.each * part, steps = 64 / ROWS * max(min(all_tiles.count - all_tiles.each * part, all_tiles.each), 0);
-    if (steps == 0 && a.parts > 1) return;   // weigh_join_kernel knows
+    if (steps == 0 && parts > 1) return;   // weigh_join_kernel knows
 
     float sum[KT] = {};
     if (steps > 0) {
@@ -458,8 +489,8 @@ __global__ __launch_bounds__(256, D <= 128 && DTYPE != BNN_F32 ? 3 : D == 256 &&
     }
     const int key = key0 + lane;
     if (lane >= 16 * KT || key >= length) return;
-    if (a.parts > 1) {
-        a.partial[(sequence * a.parts + part) * a.width4 + key] = all;
+    if (parts > 1) {
+        a.partial[((long long)nth * a.c.kv_heads + head) * a.width4 + key] = all;
     } else {
         if (c4_page(a.r, a.c, b, key) < 0) all = 0.f;
         const float old = a.previous != nullptr && key < base ? a.decay * a.previous[sequence * a.width + key] : 0.f;
@@ -473,14 +504,17 @@ __global__ __launch_bounds__(256) void weigh_join_kernel(Weigh4 a, int tile, int
     const int key = ((int)blockIdx.x - rest * blocks) * 256 + (int)threadIdx.x, b = rest;
     const Sequence4 s = c4_sequence(a.r, b);
     const int length = min(s.length, c4_room(a.r, a.c)), base = s.length - s.rows;
-    if (key >= length || s.rows * a.group <= a.few_most) return;
+    const int parts = a.r.start == nullptr ? a.parts : weigh_parts(a, b);
+    if (parts < 2) return;                   // those that weigh_kernel or one workgroup has
+    const int nth = weigh_first_item(a, b);
+    if (key >= length) return;
     const int block0 = key / tile * tile;
     const Rows4Range range = weigh_rows(a, s, base, block0, min(block0 + tile, length) - 1);
     const long long sequence = (long long)b * a.c.kv_heads + head;
     float all = 0.f;
     if (c4_page(a.r, a.c, b, key) >= 0) {
-        const WeighTiles tiles = weigh_row_tiles(range, a.parts);
-        for (int p = 0; p * tiles.each < tiles.count; ++p) all += a.partial[(sequence * a.parts + p) * a.width4 + key];
+        const WeighTiles tiles = weigh_row_tiles(range, parts);
+        for (int p = 0; p * tiles.each < tiles.count && nth + p < a.items; ++p) all += a.partial[((long long)(nth + p) * a.c.kv_heads + head) * a.width4 + key];
     }
     const float old = a.previous != nullptr && key < base ? a.decay * a.previous[sequence * a.width + key] : 0.f;
     a.out[sequence * a.width + key] = old + all;
@@ -497,7 +531,7 @@ int launch_weigh(Weigh4 a, const WeighPlan4& p, hipStream_t s) {
         }
         if (p.row_tiles == 1) launch(weigh_kernel<D, DTYPE, 1>, grid, dim3(256), 0, s, a);
     }
-    if (p.many > 0) {
+    if (p.items > 0) {
         a.parts = p.many_parts;
         a.div_parts = make_fastdiv((uint32_t)a.parts);
         launch(weigh_rows_kernel<D, DTYPE>, dim3((unsigned)p.many_groups), dim3(256), 0, s, a);

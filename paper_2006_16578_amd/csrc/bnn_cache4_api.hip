@@ -104,29 +104,33 @@ bool weigh_takes(const Cache4& c, const Rows4& r, int group) {
 }
 
 // How weights are added up.  Sequences of up to 32 rows by the kernel whose waves carry them, in as many workgroups as keep the chip busy with their loads (4096); of more by the one whose
-// waves carry keys, with the rows of a tile of keys cut into parts until there are 2048 workgroups, 256 rows at least.  (Drafts of 30 rows: 20 us by the first, 34 by the second.)  Where sequences differ (start), lengths of their runs being
-// on the device, both are launched: the first has sequences of up to 64 rows, the second the others, of which there are at most as many as the call has rows for, in parts of 256 to 2048 rows, each of its workgroups looking for its own.
+// waves carry keys, with the rows of a tile of keys cut into parts until there are 2048 workgroups, 128 rows at least.  (Drafts of 30 rows: 20 us by the first, 34 by the second.  A chunk of 1024 rows over 1024 keys, 8 kv heads: parts
+// of 128 rows 18 us, of 64 20, of 256 23.)
+// Where sequences differ (start), the lengths of their runs being on the device, both are launched: the first has sequences of up to 64 rows, the second the others, of which there are at most as many as the call has rows
+// for, in parts of 256 to 2048 rows, each of its workgroups looking for its own.  255 single tokens and a chunk of 4096 rows, 4000 keys: 235 us, all by the mean in one kernel 1790; 64 single tokens 30 instead of 28.  Where the second
+// has so few workgroups that all run at once, it has the small sequences as well (2 to 36 tokens of 8 heads, 5 sequences: 17 us, both launches 29).
 // near_rows: whether that kernel's offsets, of 2304 rows in 32 bits, reach (products of 24 bits); the other serves any distances.
 WeighPlan4 plan_weigh(const Cache4& c, const Rows4& r, int dtype, int group, bool near_rows) {
     WeighPlan4 p = {};
     const long long all = (long long)r.tokens * group, rows = cdiv(all, r.batch), room = (long long)r.table_pages << c.page_shift, sequences = (long long)r.batch * c.kv_heads;
-    p.few_most = !near_rows ? INT_MAX : r.start ? 64 : rows <= 32 ? INT_MAX : -1;
+    const long long units = c.kv_heads * cdiv(room, 64 * cache4_weigh_tiles(c.dim));
+    p.few_most = !near_rows ? INT_MAX : !r.start ? (rows <= 32 ? INT_MAX : -1) : rows > 32 && r.batch * units <= 768 ? -1 : 64;
     if (p.few_most >= 0) {
         p.row_tiles = rows > 16 && rows <= 32 && cache4_weigh_two(c.dim, dtype) ? 2 : 1;
         p.few_parts = (int)std::max(1LL, std::min(cdiv(4096, sequences), cdiv(room, 256)));
         p.few_groups = sequences * p.few_parts;
     }
-    const long long many = p.few_most < 0 ? r.batch : std::min<long long>(r.batch, all / (p.few_most + 1LL)), units = c.kv_heads * cdiv(room, 64 * cache4_weigh_tiles(c.dim));
+    const long long many = p.few_most < 0 ? r.batch : std::min<long long>(r.batch, all / (p.few_most + 1LL));
     if (many > 0) {
         long long items = many;
         const bool one = r.batch * cdiv(room, 256) >= C4_THREADS / 256;      // (the joining launch does not reach)
         p.many_parts = 1;
         p.part_shift = 30;
         if (!r.start && !one) {
-            p.many_parts = (int)std::max(1LL, std::min(cdiv(2048, units * many), cdiv(rows, 256)));
+            p.many_parts = (int)std::max(1LL, std::min(cdiv(2048, units * many), cdiv(rows, 128)));
             items = many * p.many_parts;
         } else if (r.start && !one) {
-            p.part_shift = 8;
+            p.part_shift = p.few_most < 0 ? 7 : 8;
             while (p.part_shift < 11 && (all * units) >> p.part_shift > 2048) ++p.part_shift;
             if (all > 1LL << p.part_shift) {
                 items = many + (all >> p.part_shift);

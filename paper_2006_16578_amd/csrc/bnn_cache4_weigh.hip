@@ -230,7 +230,7 @@ struct WeighItem {
 };
 __device__ __forceinline__ int weigh_parts(const Weigh4& a, int b) {         // where sequences differ
     const int rows = c4_sequence(a.r, b).rows * a.group;
-    return rows > a.few_most ? (int)(((long long)rows + (1LL << a.part_shift) - 1) >> a.part_shift) : 0;
+    return rows > a.few_most ? max(1, (int)(((long long)rows + (1LL << a.part_shift) - 1) >> a.part_shift)) : 0;
 }
 // The nth of them, b -1 where there are fewer: a wave counts those of 64 sequences at a time.
 __device__ __forceinline__ WeighItem weigh_item(const Weigh4& a, int nth) {

@@ -167,7 +167,8 @@ __device__ __forceinline__ void best_of_piece(const Logprobs& a, const T* x, int
     __syncthreads();
     uint32_t border = (uint32_t)found[0];
     bool ties = found[1] > few;              // then border is exact, and fewer than `top` threads have more than it
-    // What passes the border: first which maxima do, then, a column to a thread, the columns behind them.
+    // What passes the border: first which maxima do, then the columns behind them: a column to a thread, or, where these are many (352 rows of 32410, 64 best,
+    // 33 -> 27 us), a vector (8 rows of 131072, 20 best, 12.2 -> 12.9).
     auto collect = [&]() {
         for (int s = 0; s < segments; ++s) {
             const uint32_t o = first < a.cols ? order_of(maxima[s][tid]) : 0;
@@ -175,16 +176,30 @@ __device__ __forceinline__ void best_of_piece(const Logprobs& a, const T* x, int
         }
         __syncthreads();
         const int wide = vectors > 4 ? 3 : vectors > 2 ? 2 : vectors > 1 ? 1 : 0;      // 2^wide vectors at least are behind a maximum
-        const int n = pair_count * V << wide;
-        for (int i = tid; i < n; i += 256) {
-            const int pair = pairs[i / V >> wide], v = (pair >> 8) * LP_SEGMENT + (i / V & ((1 << wide) - 1));
-            const int col = piece_first + (v * 256 + (pair & 255)) * V + i % V;
-            if (v >= vectors || col < 0 || col >= a.cols) continue;
-            const float y = as_float(x[col]);
+        const int n = pair_count << wide;
+        auto take = [&](float y, int col) {
             const uint32_t o = order_of(y);
             if (y == y && (ties ? o > border : o >= border)) {
                 const int at = atomicAdd(&count, 1);
                 if (at < LP_KEYS) list[at] = key_of(y, col);
+            }
+        };
+        if (n * V <= 1024) {
+            for (int i = tid; i < n * V; i += 256) {
+                const int pair = pairs[i / V >> wide], v = (pair >> 8) * LP_SEGMENT + (i / V & ((1 << wide) - 1));
+                const int col = piece_first + (v * 256 + (pair & 255)) * V + i % V;
+                if (v < vectors && col >= 0 && col < a.cols) take(as_float(x[col]), col);
+            }
+        } else {
+            for (int i = tid; i < n; i += 256) {
+                const int pair = pairs[i >> wide], v = (pair >> 8) * LP_SEGMENT + (i & ((1 << wide) - 1));
+                const int col = piece_first + (v * 256 + (pair & 255)) * V;
+                if (v >= vectors) continue;
+                float y[V];
+                load_columns<T, V>(a, x, col, y);
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if (col + k >= 0 && col + k < a.cols) take(y[k], col + k);
             }
         }
     };

@@ -468,7 +468,7 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(Logprobs a) {
 
 inline int size_of(int dtype) { return dtype == BNN_F32 || dtype == BNN_I32 ? 4 : dtype == BNN_BF16 || dtype == BNN_F16 ? 2 : 0; }
 
-// How rows are cut up: into pieces of up to 64 vectors of 16 bytes a thread, as many as make 512 workgroups.  `at` and ld tell whether rows begin at 16 bytes (a vector more else); without them the
+// How rows are cut up: into pieces of up to 64 vectors of 16 bytes a thread, as many as make 512 workgroups, but no more than whose best are joined in one turn.  `at` and ld tell whether rows begin at 16 bytes (a vector more else); without them the
 // most that a workspace is asked for.
 constexpr int LP_GROUPS = 512;
 struct LogprobsPlan {
@@ -479,7 +479,7 @@ LogprobsPlan plan_logprobs(int rows, int cols, int size, int top, bool aligned) 
     LogprobsPlan p = {};
     const int v = 16 / size;
     const long long most = cdiv((long long)cols + v - 1, 256LL * v);
-    const long long want = cdiv(most * rows, LP_GROUPS);
+    const long long want = std::max(cdiv(most * rows, LP_GROUPS), top > 0 ? cdiv(most, LP_LIST / top) : 1);
     p.group = want < 4 ? 1 : 4;
     p.vectors = (int)std::min<long long>(LP_VECTORS, p.group == 1 ? want : cdiv(want, 4) * 4);
     p.pieces = (int)cdiv(aligned ? cdiv(cols, 256LL * v) : most, p.vectors);

@@ -24,9 +24,9 @@ def logits_of(rng, rows, cols, dtype, spread=3.0):
     return torch.from_numpy(rng.standard_normal((rows, cols)) * spread).to(TYPES[dtype]).cuda()
 
 
-def check(bnn, x, targets, scale=1.0, top=0, **kw):
+def check(bnn, x, targets, scale=1.0, top=0, terms=64, **kw):
     """Bounds, with u = 2^-24 and every row's z = scale x, M its largest: an exponent (x - m) scale / log 2 rounds three times (and the scale's own constant), so a term is off by
-    4 u |z - M| and 2 u of the exponential; with terms as weights that is 4 u log(cols) at most.  Sums add up 64 terms, 8 levels and the pieces: 128 u.  The logarithm rounds twice, u log S each.  What is
+    4 u |z - M| and 2 u of the exponential; with terms as weights that is 4 u log(cols) at most.  Sums add up `terms` in a thread (64 at most, but for the longest pieces), 8 levels and the pieces: that and 64 u.  The logarithm rounds twice, u log S each.  What is
     then added rounds once, relative to itself.  The entropy is a sum of two such terms, each at most log(cols)."""
     scale = float(np.float32(scale))
     want = od.token_logprobs(x.double().cpu().numpy(), None if targets is None else targets.cpu().numpy(), scale, top)
@@ -34,7 +34,7 @@ def check(bnn, x, targets, scale=1.0, top=0, **kw):
     rows, cols = x.shape
     assert (got.logprobs is None) == (targets is None)
     n = np.log(max(cols, 2))
-    sums = (128 + 8 * n) * U
+    sums = (terms + 64 + 8 * n) * U
     for name, w, g in zip(("logprobs", "entropy", "lse", "top_logprobs"), want, got):
         if g is None:
             continue
@@ -67,6 +67,13 @@ def test_long_pieces(bnn, dtype, cols):
     """Rows enough for the long pieces: 600 rows and two pieces each."""
     rng = np.random.default_rng(cols)
     check(bnn, logits_of(rng, 600, cols, dtype), tokens_for(rng, 600, cols), 1 / 45 if dtype == "i32" else 0.7, 9)
+
+
+@pytest.mark.parametrize("dtype,cols", [("f32", 3000001), ("bf16", 5000003), ("i32", 3000002)])
+def test_pieces_joined_in_turns(bnn, dtype, cols):
+    """Rows of 39 to 46 of the longest pieces, 64 best each: more than are joined in one turn.  A thread adds up 64 vectors of 4 or 8 columns."""
+    rng = np.random.default_rng(cols)
+    check(bnn, logits_of(rng, 2, cols, dtype), tokens_for(rng, 2, cols), 1 / 45 if dtype == "i32" else 0.7, 64, terms=64 * (8 if dtype == "bf16" else 4))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])

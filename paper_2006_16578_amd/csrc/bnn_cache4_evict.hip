@@ -3,7 +3,7 @@
 // heaviest_kernel: a workgroup has a sequence and kv head.  Weights in the order of numbers are whole numbers in the order of their bits (negative ones turned round); that of the last token that
 // is kept is found digit by digit, from the highest on: a histogram of the digit over what agrees so far, 11 + 11 + 10 bits.  Of those that equal it the lowest tokens are kept.  A wave has a run of
 // consecutive tokens, a lane four beside each other, so one exchange of counts gives every wave the place of its first kept token, and the list is ascending.  Weights are read once and stay in
-// registers where the table has room for up to 32768 tokens; beyond, heaviest_part_kernel has 8192 of them, or, with very many sequences, they are read five times, eight loads under way.
+// registers where the table has room for up to 32768 tokens; beyond, heaviest_part_kernel has 8192 of them, or, with many sequences, they are read five times, eight loads under way.
 // What bounds it is the chain of barriers, counts and scans: 32 sequences of 2100 to 16384 tokens, 8 kv heads, 23 us, of which reading their 9 MB is 2.
 // move_kernel: a workgroup has a kv head and 64 places of the new sequence.  What bounds it is memory, by whole lines: a token's scales are 2 * D / 32 bytes in as many lines, and lines of codes hold the neighbours that
 // stay behind.  2048 tokens of each of those sequences, heads of 128: 171 MB come in for 80 MB of tokens, 52 to 69 us.
@@ -426,7 +426,8 @@ __global__ __launch_bounds__(256) void move_kernel(Move4 a, FastDiv div_lanes, i
 HeaviestPlan4 plan_cache4_heaviest(const Cache4& c, int batch, int table_pages) {
     HeaviestPlan4 p = {};
     const long long room = (long long)table_pages << c.page_shift, units = (long long)batch * c.kv_heads, parts = cdiv(room, H_WAVES * 2 * H_VECTOR);
-    if (room <= 32768 || units * parts > 4096) return p;
+    // (Parts take 17 us and 0.065 for each, one workgroup to a sequence and head 7.6 for every 8192 of its tokens: 8 sequences of 65536, 8 heads, 49 us in parts, 63 without; 16 of them 83 and 67; 64 of them 244 and 171.)
+    if (room <= 32768 || units > 80) return p;
     p.parts = (int)parts;
     p.bins_bytes = (size_t)units * 3 * parts * H_BINS * sizeof(int);
     p.borders_bytes = (size_t)units * 3 * sizeof(Border);

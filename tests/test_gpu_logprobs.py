@@ -69,6 +69,24 @@ def test_long_pieces(bnn, dtype, cols):
     check(bnn, logits_of(rng, 600, cols, dtype), tokens_for(rng, 600, cols), 1 / 45 if dtype == "i32" else 0.7, 9)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16", "i32"])
+@pytest.mark.parametrize("rows,cols,top", [(1030, 7, 2), (1025, 129, 16), (1025, 128, 16), (5, 512, 4), (1027, 512, 9), (3, 65, 1), (4, 512, 0), (2, 513, 4), (1024, 64, 17)])
+def test_short_rows(bnn, dtype, rows, cols, top):
+    """A wave to a row, and just beyond: ties, rows without a distribution, masked columns, distances, targets of any kind."""
+    rng = np.random.default_rng(rows + cols)
+    whole = logits_of(rng, rows, cols + 3, dtype, spread=2.0)
+    x = whole[:, 1:cols + 1]
+    if dtype != "i32":
+        x[0] = -float("inf")
+        x[1, cols // 2] = float("nan")
+        x[2 % rows, cols - 1] = float("inf")
+        if rows > 3:
+            x[3, 1:] = -float("inf")
+            x[4 % rows] = 0.0                # (row 0 again, of four rows)
+    t = torch.from_numpy(rng.integers(-2, cols + 2, rows)).cuda()
+    check(bnn, x, t, 1 / 45 if dtype == "i32" else 0.7, top)
+
+
 @pytest.mark.parametrize("dtype,cols", [("f32", 3000001), ("bf16", 5000003), ("i32", 3000002)])
 def test_pieces_joined_in_turns(bnn, dtype, cols):
     """Rows of 39 to 46 of the longest pieces, 64 best each: more than are joined in one turn.  A thread adds up 64 vectors of 4 or 8 columns."""

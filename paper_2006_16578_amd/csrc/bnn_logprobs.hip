@@ -2,10 +2,11 @@
 //
 // With a reference point m and u = (x - m) scale / log 2, S = sum 2^u and W = sum 2^u u give
 //   log p = scale (x - m) - log S,  entropy = log S - log 2 W / S  (both terms >= 0),  lse = scale m + log S,
-// so no difference of large numbers is left.  A wave's m is the largest of its first columns, and is raised only when a column passes it by more than 16 (as powers of two), so most columns meet no branch and no
-// rescaling; waves and pieces of a row are joined by the same rule.  What bounds it is memory: 10 instruction slots a column (an exponential counts four) take about four fifths of the time that its
+// and with m the row's largest column no difference of large numbers is left: that column's own term is 1 exactly, S is 1 or more, and a sure row's results are right relative to themselves.  A wave's m is the
+// largest column that it has met.  One branch for four vectors raises it: few groups do, as the longer a row is the rarer a new largest one gets (with m let stay behind by up to 16 powers of two, 4096 rows of 131072 take 210 us in
+// place of 211, ascending ones 498 in place of 501, but sure rows lose log p and entropy to the difference of two numbers near 11).  Waves and pieces of a row are joined by the same rule.  What bounds it is memory: 10 instruction slots a column (an exponential counts four) take about four fifths of the time that its
 // two bytes take.  4096 rows of 131072 bf16 columns (1.07 GB): 194 us, 5.5 TB/s.  (With a piece of a row held in registers between a pass for the maximum and one for the sums 816 us.)  The smallest calls, 8 rows of 131072
-// columns in 512 pieces, are two launches: 6.8 us for the pieces and 6 for the join, chains of loads and barriers.
+// columns in 256 pieces, are two launches: 6.8 us for the pieces and 6 for the join, chains of loads and barriers.
 //
 // The `top` best: beside that, every thread keeps the largest of each eight of its vectors.  The `top`-th largest of the threads' maxima is a border that at least `top` columns reach and little more do;
 // the vectors' maxima tell where those are, and they are read again, collected in LDS and ranked by counting.  Columns are ordered by (value, lower column first) as one 64-bit number.  Where a border is shared
@@ -25,7 +26,7 @@ struct Logprobs {
     const void* x;
     int rows, cols;
     long long ld;
-    float scale, scale2, slack;              // scale2: scale / log 2; slack: what x may pass the reference point by
+    float scale, scale2;                     // scale2: scale / log 2
     const int64_t* targets;
     int top;
     float *logprobs, *entropy, *lse, *top_logprobs;
@@ -335,7 +336,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(Logprobs a) {
     const int vectors = min(a.vectors, (a.cols - piece_first + 256 * V - 1) / (256 * V));       // with columns
     const float c = a.scale2;
 
-    float m = 0.f, limit = -__builtin_inff(), S = 0.f, W = 0.f;      // limit: what a column may be before m is raised; -infinity: nothing but -infinity so far
+    float most = -__builtin_inff(), m = 0.f, S = 0.f, W = 0.f;       // most: the largest column so far, m too, but for 0 in place of -infinity
     float segment = -__builtin_inff();
     auto group = [&](const float (&y)[NV][V], int v0) {
         float high = -__builtin_inff();
@@ -346,12 +347,11 @@ __global__ __launch_bounds__(256) void logprobs_kernel(Logprobs a) {
             for (int j = 1; j < V; ++j) h = fmaxf(h, y[v][j]);
             high = fmaxf(high, h);
         }
-        if (__ballot(high > limit) != 0) {
-            const float top = wave_max(high), d = limit == -__builtin_inff() ? 0.f : (m - top) * c, f = __builtin_amdgcn_exp2f(d);
+        if (__ballot(high > most) != 0) {
+            const float top = wave_max(high), d = most == -__builtin_inff() ? 0.f : (m - top) * c, f = __builtin_amdgcn_exp2f(d);
             W = f * fmaf(S, fmaxf(d, -1e30f), W);
             S *= f;
-            m = top;
-            limit = top + a.slack;
+            m = most = top;
         }
         if constexpr (TOP) {
             segment = fmaxf(segment, high);
@@ -401,7 +401,7 @@ __global__ __launch_bounds__(256) void logprobs_kernel(Logprobs a) {
     S = wave_sum(S);
     W = wave_sum(W);
     if (lane == 0) {
-        part[0][wave] = limit == -__builtin_inff() ? -__builtin_inff() : m;
+        part[0][wave] = most;
         part[1][wave] = S;
         part[2][wave] = W;
     }
@@ -600,7 +600,6 @@ int bnn_token_logprobs(const void* logits, int dtype, int rows, int cols, int64_
     Logprobs a = {};
     a.x = logits; a.rows = rows; a.cols = cols; a.ld = ld;
     a.scale = scale; a.scale2 = scale2;
-    a.slack = 16.f / scale2;
     a.targets = targets; a.top = top;
     a.logprobs = logprobs; a.entropy = entropy; a.lse = lse; a.top_logprobs = top_logprobs; a.top_tokens = top_tokens;
     a.pieces = p.pieces; a.vectors = p.vectors;

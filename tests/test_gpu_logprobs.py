@@ -256,3 +256,45 @@ def test_refusals(bnn):
                             (bnn.BnnError, (x, t), dict(scale=-1.0)), (bnn.BnnError, (x, t), dict(scale=float("nan"))), (bnn.BnnError, (x, t), dict(scale=float("inf")))):
         with pytest.raises(error):
             bnn.token_logprobs(*args, **kw)
+
+
+@pytest.mark.parametrize("dtype,rows,cols", [("f32", 600, 9001), ("bf16", 600, 40000), ("f16", 530, 40001), ("i32", 600, 9001), ("f32", 9, 70001), ("bf16", 2, 1500001), ("i32", 40, 262144), ("bf16", 600, 500)])
+@pytest.mark.parametrize("top", [0, 3])
+def test_sure_rows(bnn, dtype, rows, cols, top):
+    """One column far above four others (those 1024 to 8192 columns before it, so that some are the same thread's or wave's), all else without weight: results near 0 that are right relative to themselves.
+    With the largest column as the point that exponents are counted from, its own term is 1 exactly and log S begins at 0.  Bounds, with u = 2^-24: four terms are added to the 1, u each, which is all that is
+    absolute in log S; all else is relative: a term 2 u for the exponential and 4 u for each of its d = z_best - z; the products and sums, the quotient and the logarithm less than 16 u."""
+    rng = np.random.default_rng(cols)
+    distance = np.array([2, 8, 10, 11, 30])[np.arange(rows) % 5].astype(np.float64)
+    steps = (1024, 2048, 4096, 8192) if cols > 8192 else (1, 2, 65, 200)
+    column = rng.integers(steps[-1], cols, rows)
+    x = torch.full((rows, cols), -(1 << 20) if dtype == "i32" else -float("inf"), dtype=TYPES[dtype], device="cuda")
+    few = np.stack([column - s for s in steps[::-1]] + [column], 1)          # the columns that count, ascending
+    at, where = torch.arange(rows, device="cuda")[:, None], torch.from_numpy(few).cuda()
+    z = np.ones((rows, 5))
+    z[:, 4] += distance
+    x[at, where] = torch.from_numpy(z).to(TYPES[dtype]).cuda()
+    for which in (4, 3):
+        target = few[:, which]
+        want = od.token_logprobs(z, np.full(rows, which), 1.0, top)
+        tokens = few[np.arange(rows)[:, None], want[4]]
+        got = bnn.token_logprobs(x, torch.from_numpy(target).cuda(), top=top)
+        relative = (16 + 4 * (distance + 1)) * U
+        for name, w, g in zip(("logprobs", "entropy", "lse", "top_logprobs"), want, got):
+            error = np.abs(g.double().cpu().numpy() - w)
+            r = relative[:, None] if w.ndim == 2 else relative
+            bad = error > 4 * U + r * np.abs(w)
+            assert not bad.any(), (name, np.argwhere(bad)[:3], error[bad][:3] / U, w[bad][:3])
+        assert (got.top_tokens.cpu().numpy() == tokens).all()
+
+
+def test_far_above_the_rest(bnn):
+    """A column so far above all others that the distance leaves fp32 where it is counted: one sure token, no entropy."""
+    x = torch.full((520, 65536), 11.0, device="cuda")
+    x[:, :8192] = 0.0
+    x[:, 65000] = 1e31
+    got = bnn.token_logprobs(x, torch.full((520,), 65000, device="cuda"), top=1)
+    assert (got.logprobs == 0).all() and (got.entropy == 0).all() and (got.top_tokens == 65000).all() and (got.top_logprobs == 0).all() and (got.lse == torch.tensor(1e31)).all()
+    few = bnn.token_logprobs(x[:3], torch.full((3,), 65000, device="cuda"), top=1)
+    for a, b in zip(few, got):
+        assert torch.equal(a, b[:3])

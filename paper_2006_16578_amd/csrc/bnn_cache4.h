@@ -294,6 +294,7 @@ struct Weigh4 {
 // How such a call is cut up: a launch for sequences of few rows (row_tiles: tiles of 16 rows that a wave carries, 0: no such launch), one for those of many (items: pairs of a sequence and a part of its rows that there can be, 0: no such launch), or both.
 struct WeighPlan4 {
     int few_most, row_tiles, few_parts, items, many_parts, part_shift;
+    bool runs;                               // the launch for few rows has sequences of more than 256, too far apart for the other
     long long few_groups, many_groups;
     size_t workspace_bytes;
 };

@@ -109,14 +109,15 @@ bool weigh_takes(const Cache4& c, const Rows4& r, int group) {
 // Where sequences differ (start), the lengths of their runs being on the device, both are launched: the first has sequences of up to 64 rows, the second the others, of which there are at most as many as the call has rows
 // for, in parts of 256 to 2048 rows, each of its workgroups looking for its own.  255 single tokens and a chunk of 4096 rows, 4000 keys: 235 us, all by the mean in one kernel 1790; 64 single tokens 30 instead of 28.  Where the second
 // has so few workgroups that all run at once, it has the small sequences as well (2 to 36 tokens of 8 heads, 5 sequences: 17 us, both launches 29).
-// near_rows: whether that kernel's offsets, of 2304 rows in 32 bits, reach (products of 24 bits); the other serves any distances.
+// near_rows: whether that kernel's offsets, of 2304 rows in 32 bits, reach (products of 24 bits); the other serves any distances, thousands of rows in runs.
 WeighPlan4 plan_weigh(const Cache4& c, const Rows4& r, int dtype, int group, bool near_rows) {
     WeighPlan4 p = {};
     const long long all = (long long)r.tokens * group, rows = cdiv(all, r.batch), room = (long long)r.table_pages << c.page_shift, sequences = (long long)r.batch * c.kv_heads;
     const long long units = c.kv_heads * cdiv(room, 64 * cache4_weigh_tiles(c.dim));
     p.few_most = !near_rows ? INT_MAX : !r.start ? (rows <= 32 ? INT_MAX : -1) : rows > 32 && r.batch * units <= 768 ? -1 : 64;
     if (p.few_most >= 0) {
-        p.row_tiles = rows > 16 && rows <= 32 && cache4_weigh_two(c.dim, dtype) ? 2 : 1;
+        p.runs = !near_rows && (r.start ? all : rows) > 256;
+        p.row_tiles = rows > 16 && rows <= 32 && cache4_weigh_two(c.dim, dtype) && !p.runs ? 2 : 1;
         p.few_parts = (int)std::max(1LL, std::min(cdiv(4096, sequences), cdiv(room, 256)));
         p.few_groups = sequences * p.few_parts;
     }

@@ -75,7 +75,8 @@ constexpr int WEIGH_ROWS = 2048;             // rows whose numbers lie in LDS at
 // Few rows: a wave passes over its sequence's keys, 64 at a time, codes of the next 64 under way.  Bounded by memory: 64 single tokens over 500 to 8192 keys, 8 kv heads of 128, 41 us, 4.1 TB/s (a workgroup's first loads
 // wait for a length, a page and the rows; 2048 or 8192 workgroups in place of 4096: 57 and 53 us against 52 before pages were looked up ahead; codes loaded two turns ahead leave room for fewer waves: 57).  Few keys, 16 drafts of 5
 // tokens within a window of 1000, heads of 192: 13 us, the same chain of loads; 15.8 when every wave loaded its rows.
-template <int D, int DTYPE, int QT>
+// RUNS: for rows by the thousand, those too far apart for the kernel below: added up in runs of 256 as there (in every launch, the second sums' registers would cost heads of 128 one of five waves).
+template <int D, int DTYPE, int QT, bool RUNS>
 __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
     using T = typename C4Type<DTYPE>::type;
     constexpr int TERMS = C4Type<DTYPE>::terms, M = D / 32, KT = 4;
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
     for (; key0 < length; key0 += stride) {
         const int key1 = min(key0 + 63, length - 1);
         const float old = a.previous != nullptr && key0 + lane < min(base, length) ? a.decay * a.previous[weights + key0 + lane] : 0.f;
-        float sum[KT] = {};
+        float sum[KT] = {}, run[KT] = {};    // run: not used without RUNS
         const unsigned present = there;
         locate(min(key0 + stride, length - 1));
         // (almost always one turn: a launch has QT by the mean over its sequences)
@@ -207,7 +208,14 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
 #pragma unroll
                 for (int t = 0; t < QT; ++t)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) sum[u] += __builtin_amdgcn_exp2f(score[t][i] * a.scale2);
+                    for (int i = 0; i < 4; ++i) (RUNS ? run : sum)[u] += __builtin_amdgcn_exp2f(score[t][i] * a.scale2);
+            }
+            if (RUNS && ((row0 + 16 * QT) % 256 == 0 || row0 + 16 * QT >= range.last)) {
+#pragma unroll
+                for (int u = 0; u < KT; ++u) {
+                    sum[u] += run[u];
+                    run[u] = 0.f;
+                }
             }
         }
         if (key0 + stride < length) {
@@ -527,9 +535,10 @@ int launch_weigh(Weigh4 a, const WeighPlan4& p, hipStream_t s) {
         a.div_parts = make_fastdiv((uint32_t)a.parts);
         const dim3 grid((unsigned)p.few_groups);
         if constexpr (cache4_weigh_two(D, DTYPE)) {
-            if (p.row_tiles == 2) launch(weigh_kernel<D, DTYPE, 2>, grid, dim3(256), 0, s, a);
+            if (p.row_tiles == 2) launch(weigh_kernel<D, DTYPE, 2, false>, grid, dim3(256), 0, s, a);
         }
-        if (p.row_tiles == 1) launch(weigh_kernel<D, DTYPE, 1>, grid, dim3(256), 0, s, a);
+        if (p.row_tiles == 1 && !p.runs) launch(weigh_kernel<D, DTYPE, 1, false>, grid, dim3(256), 0, s, a);
+        if (p.row_tiles == 1 && p.runs) launch(weigh_kernel<D, DTYPE, 1, true>, grid, dim3(256), 0, s, a);
     }
     if (p.items > 0) {
         a.parts = p.many_parts;

@@ -174,6 +174,34 @@ def test_weigh_far_apart_rows(bnn):
     assert ((near - far).abs() <= 2 * 80 * U * near + 2 * 72 * U * 40 * near).all() and near.sum() > 0
 
 
+def test_weigh_many_rows_far_apart(bnn):
+    """16384 rows whose heads lie too far apart for the kernel for many rows: every one gives every key exp(-lse), as its query is zero.  A lane has 4096 of them.  Added one after another to one fp32 sum these
+    would be off by 740 to 940 u (u = 2^-24) with the logarithms here, whose weights lie where rounding goes one way.  In runs of 256 rows, 64 a lane, and 64 runs: 64 + 64 u at most, 2 for the four lanes, and for the weight
+    itself 2 u of its logarithm for two products, 2 for the exponential and 2 for the reciprocal of scale and its product."""
+    su = Batch(bnn, 34, [8200], [1], kv_heads=1, group=2, dim=64, page=256)
+    q = torch.zeros(((1 << 24) + 8192 * 64,), device="cuda", dtype=torch.bfloat16).as_strided((8192, 2, 64), (64, 1 << 24, 1))
+    for log in (0.104244605, 0.39215827, 0.44179857, -0.28294963):
+        lse = torch.full((8192, 2), log, device="cuda")
+        w = su.gpu.weigh(q, lse, ints(su.table), ints(su.lens), causal=False, out=torch.zeros(1, 1, su.table.shape[1] * 256, device="cuda"))[0, 0, :8200].double().cpu().numpy()
+        want = 16384 * np.exp(-float(lse[0, 0]))
+        assert (np.abs(w - want) <= 140 * U * want).all(), (log, np.abs(w / want - 1).max() / U)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_weigh_runs_of_rows_far_apart(bnn, dtype):
+    """Sequences of 600, 1 and 259 rows by runs, with masks, against the same rows side by side.  Bounds: the sums of both, of up to 1200 rows, and of scores and logarithms below 192."""
+    su = Batch(bnn, 35, [700, 40, 259], [600, 1, 259], kv_heads=1, group=2, dim=64, page=64, dtype=dtype)
+    near = dev(su.q, dtype)
+    far = torch.empty((1 << 24) + 860 * 64, device="cuda", dtype=TYPES[dtype]).as_strided((860, 2, 64), (64, 1 << 24, 1)).copy_(near)
+    zero = lambda: torch.zeros(3, 1, su.table.shape[1] * 64, device="cuda")
+    for kw in (dict(), dict(window=77), dict(causal=False)):
+        _, lse = su.gpu.attend(near, want_lse=True, **kw, **su.plan())
+        a, b = su.gpu.weigh(near, lse, out=zero(), **kw, **su.plan()).double(), su.gpu.weigh(far, lse, out=zero(), **kw, **su.plan()).double()
+        assert ((a - b).abs() <= (2 * (64 + 8) * U * 192 + 2 * 1200 * U) * a + 1e-30).all() and (a[0, 0, :700] > 0).sum() > 600
+    first = su.gpu.weigh(far, lse, out=zero(), causal=False, **su.plan())
+    assert torch.equal(first, b.float())
+
+
 def test_weights_are_those_of_attention(bnn):
     """Every row gives its whole weight: the sums over keys are the rows' number, and with the cache's values they give attention's outputs."""
     su = Batch(bnn, 9, [500, 130], [1, 1], dim=128, page=64, group=4, spread=2.0)

@@ -277,7 +277,8 @@ struct Weigh4 {
     long long q_token, q_head;
     int group;
     FastDiv div_group, div_heads;
-    float scale2, unscale;                   // scale / log 2, 1 / scale
+    float scale2;                            // scale / log 2
+    double unscale;                          // 1 / scale, less half of what scale2 is off by
     int causal, window;
     const float* lse;                        // [tokens][heads]
     const float* previous;                   // [batch][kv_heads][width], or nullptr; may be out

@@ -321,8 +321,8 @@ int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const
     int rc = make_cache(cache, a.c);
     if (rc != BNN_OK || (rc = make_rows(rows, a.c, a.r)) != BNN_OK || (rc = check_heads(a.c, heads, a.group)) != BNN_OK) return rc;
     a.scale2 = scale * 1.4426950408889634f;
-    a.unscale = 1.f / scale;
-    if (element_bytes(dtype) == 0 || !(scale > 0.f) || !isfinite(a.scale2) || !isfinite(a.unscale) || window < 0 || (window > 0 && !causal) || !isfinite(decay)) return BNN_ERR_INVALID_ARG;
+    a.unscale = (1.5 - 0.5 * a.scale2 / (scale * 1.4426950408889634)) / scale;       // (1 - e / 2) / scale, scale2 being (1 + e) scale / log 2
+    if (element_bytes(dtype) == 0 || !(scale > 0.f) || !isfinite(a.scale2) || !isfinite(1.f / scale) || window < 0 || (window > 0 && !causal) || !isfinite(decay)) return BNN_ERR_INVALID_ARG;
     if (a.r.tokens == 0) return BNN_OK;
     if (!weights || !lse || width < ((long long)a.r.table_pages << a.c.page_shift)) return BNN_ERR_INVALID_ARG;
     if ((rc = check_elements(q, dtype, q_token, q_head)) != BNN_OK) return rc;

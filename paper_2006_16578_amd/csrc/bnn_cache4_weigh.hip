@@ -2,14 +2,15 @@
 //
 // Queries are the rows of the products, keys their columns: S [rows][keys] = Q K^T (v_mfma_f32_16x16x32_bf16).  A lane then holds, of 16 rows, the scores of ONE key at four of them, so the
 // sum over rows stays in a lane until the end, where the four lanes of a key add up.  The products' sums begin at -lse / scale, so that a weight is 2^(sum * scale / log 2): one multiplication, one
-// exponential, one addition a score.  No sum depends on the order in which workgroups run.
+// exponential, one addition a score.  What scale / log 2 loses by its rounding to 32 bits, e of itself, makes a weight off by e (scale q . k - lse); -lse / scale, in 64 bits until it is stored, takes half of it to
+// the middle, e (scale q . k - lse / 2): all rows being off alike, no sum would average it out.  (With 1 / scale in 32 bits, off by as much again, heads of 96 and 192 had twice the plain form's error.)  No sum depends on the order in which workgroups run.
 #include "bnn_cache4_attend.h"
 
 namespace bnn {
 namespace {
 
 // What a row's sums begin with: -lse / scale, and -infinity (a weight of 0) for no row and for one that saw nothing.
-__device__ __forceinline__ float weigh_origin(const Weigh4& a, float lse, bool there) { return there && lse != -__builtin_inff() ? -lse * a.unscale : -__builtin_inff(); }
+__device__ __forceinline__ float weigh_origin(const Weigh4& a, float lse, bool there) { return there && lse != -__builtin_inff() ? (float)(-(double)lse * a.unscale) : -__builtin_inff(); }
 __device__ __forceinline__ float weigh_lse(const Weigh4& a, const Sequence4& s, int head, int row) {
     const int token = fast_div(row, a.div_group), g = row - token * a.group;
     return a.lse[(long long)(s.first + token) * a.c.kv_heads * a.group + head * a.group + g];

@@ -202,6 +202,30 @@ def test_weigh_runs_of_rows_far_apart(bnn, dtype):
     assert torch.equal(first, b.float())
 
 
+@pytest.mark.parametrize("dim", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("dtype,group", [("bf16", 32), ("f32", 16), ("bf16", 64), ("f32", 64), ("f16", 40)])
+def test_weigh_errors_of_high_scores_average_out(bnn, dtype, dim, group):
+    """Scores and logarithms near 100, both up to 0.5 apart, one key that has a weight: 128 sequences of `group` rows, through both kernels.  A row's -lse / scale is rounded to fp32, 2^-24 of itself or less, up to 100 u of the weight:
+    rows differ, so their mean, over 2048 rows at least, keeps 1.3 u of it for a standard deviation (a rounding's is 1 / sqrt 3 of the most; 12 u and fewer for a sequence's fp32 sum, over 128 of them, 0.6), and 7 u is five of them.  What all
+    rows have alike is the rounding of scale / log 2, e of itself: e (score - lse / 2), and the exponential's own 2 u."""
+    rng = np.random.default_rng(dim + group)
+    cache = bnn.Cache4(1, kv_heads=1, head_dim=dim, page=16)
+    k = torch.zeros(1, 1, dim, device="cuda")
+    k[..., 0] = 6.0
+    cache.write(k, torch.zeros_like(k), ints([[0]]), ints([1]))
+    scale = float(np.float32(dim ** -0.5))
+    table, lens = ints(np.zeros((128, 1))), ints(np.ones(128))       # the same token for all
+    q = np.zeros((128, group, dim))
+    q[..., 0] = rounded(rng.uniform(99.5, 100.5, (128, group)) / scale / 6, dtype)
+    score = scale * 6 * q[..., 0]
+    lse = (score + rng.uniform(-0.5, 0.5, score.shape)).astype(np.float32)
+    w = cache.weigh(dev(q, dtype), torch.from_numpy(lse).cuda(), table, lens, scale=scale, out=torch.zeros(128, 1, 16, device="cuda"))[:, 0, 0].double().cpu().numpy()
+    want = np.exp(score - lse.astype(np.float64)).sum(1)
+    scale2 = float(np.float32(np.float32(scale) * np.float32(1.4426950408889634)))
+    e = abs(scale2 / (scale * 1.4426950408889634) - 1)
+    assert abs((w / want).mean() - 1) <= 51 * e + 9 * U, ((w / want).mean() - 1) / U
+
+
 def test_weights_are_those_of_attention(bnn):
     """Every row gives its whole weight: the sums over keys are the rows' number, and with the cache's values they give attention's outputs."""
     su = Batch(bnn, 9, [500, 130], [1, 1], dim=128, page=64, group=4, spread=2.0)

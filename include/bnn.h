@@ -511,7 +511,7 @@ int bnn_cache4_heaviest(const bnn_cache4* cache, const int32_t* table, const int
                         int keep, int first, int last, int32_t* tokens, int32_t* kept, void* workspace, size_t workspace_bytes, void* stream);
 /* Token tokens[b][h][i] of the sequence that `table` describes, kv head h, becomes token i of the one that `into` [batch][into_pages] describes: codes, scales and signs as they are.  The
  * pages of `into` are others than those of `table` (their contents are not defined else), and not shared.  Entries below 0, what lies on no page, and places past `into`'s end are passed over.
- * weights, moved: both or neither; moved [batch][kv_heads][into_pages * page] gets the tokens' weights, 0 where there is no token. */
+ * weights, moved: both or neither; moved [batch][kv_heads][into_pages * page] gets the tokens' weights, 0 where the list has none and for one that lies on no page of `table`. */
 int bnn_cache4_move(const bnn_cache4* cache, const int32_t* tokens, int keep, const int32_t* table, int table_pages, const int32_t* into, int into_pages, int batch,
                     const float* weights, int64_t width, float* moved, void* stream);
 

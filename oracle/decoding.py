@@ -102,9 +102,9 @@ def move(cache, tokens, table, into, weights=None):
         j = int(tokens[b, h, i])
         if i >= room:
             continue
-        if weights is not None and 0 <= j < weights.shape[2]:
-            moved[b, h, i] = weights[b, h, j]
         source = cache.record(table, b, j, h) if j >= 0 else None
+        if weights is not None and source is not None and j < weights.shape[2]:
+            moved[b, h, i] = weights[b, h, j]
         target = cache.record(into, b, i, h)
         if source is None or target is None:
             continue

@@ -1142,7 +1142,7 @@ class Cache4:
 
     def move(self, tokens, table, into, weights=None):
         """Copies token tokens[b][h][i] (from heaviest) of the sequence in table[b] to token i of the one in into[b] (int32 [batch][pages], other pages than the table's), for every kv
-        head; with weights returns them moved alike, fp32 [batch][kv_heads][tokens of into], 0 where there is none.  The sequence's length is then heaviest's second result."""
+        head; with weights returns them moved alike, fp32 [batch][kv_heads][tokens of into], 0 where there is none, or one on no page.  The sequence's length is then heaviest's second result."""
         if weights is not None:
             done = (_native or _load_native()).cache4_move(*self._plain, tokens, table, into, weights)
             if done is not None:

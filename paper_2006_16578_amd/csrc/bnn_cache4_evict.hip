@@ -392,23 +392,27 @@ __global__ __launch_bounds__(H_THREADS) void heaviest_part_kernel(Heaviest4 a, P
 
 // A thread moves 16 bytes of codes, K's and V's, the lanes of a token side by side; scales and signs go a byte or word at a time.
 __global__ __launch_bounds__(256) void move_kernel(Move4 a, FastDiv div_lanes, int lanes, int blocks) {
-    __shared__ int source[64];
+    __shared__ int source[64], page[64];     // of a place's token, page -1: none
     const int head = (int)blockIdx.y, b = (int)blockIdx.x / blocks, i0 = ((int)blockIdx.x - b * blocks) * 64;
     const int room = a.into_pages << a.c.page_shift;
     const long long list = ((long long)b * a.c.kv_heads + head) * a.keep;
     if (threadIdx.x < 64) {
         const int i = i0 + (int)threadIdx.x;
         const int j = i < a.keep && i < room ? a.tokens[list + i] : -1;
+        const bool weighed = a.weights != nullptr && i < room;
+        const float w = weighed && j >= 0 && j < a.width ? a.weights[((long long)b * a.c.kv_heads + head) * a.width + j] : 0.f;         // (under way beside the page)
+        const int p = j >= 0 && j >> a.c.page_shift < a.table_pages ? a.table[(long long)b * a.table_pages + (j >> a.c.page_shift)] : -1;
         source[threadIdx.x] = j;
-        if (a.weights != nullptr && i < room)
-            a.moved[((long long)b * a.c.kv_heads + head) * room + i] = j >= 0 && j < a.width ? a.weights[((long long)b * a.c.kv_heads + head) * a.width + j] : 0.f;
+        const bool there = (uint32_t)p < (uint32_t)a.c.pages;
+        page[threadIdx.x] = there ? p : -1;
+        if (weighed) a.moved[((long long)b * a.c.kv_heads + head) * room + i] = there ? w : 0.f;
     }
     __syncthreads();
     for (int n = (int)threadIdx.x; n < 64 * lanes; n += 256) {
-        const int t = fast_div(n, div_lanes), at = n - t * lanes, i = i0 + t, j = source[t];
-        if (j < 0 || j >> a.c.page_shift >= a.table_pages) continue;
-        const int p = a.table[(long long)b * a.table_pages + (j >> a.c.page_shift)], r = a.into[(long long)b * a.into_pages + (i >> a.c.page_shift)];
-        if ((uint32_t)p >= (uint32_t)a.c.pages || (uint32_t)r >= (uint32_t)a.c.pages) continue;
+        const int t = fast_div(n, div_lanes), at = n - t * lanes, i = i0 + t, j = source[t], p = page[t];
+        if (p < 0) continue;
+        const int r = a.into[(long long)b * a.into_pages + (i >> a.c.page_shift)];
+        if ((uint32_t)r >= (uint32_t)a.c.pages) continue;
         const uint8_t* from = c4_record(a.c, p, head);
         uint8_t* to = c4_record(a.c, r, head);
         const int fo = j & (a.c.page - 1), o = i & (a.c.page - 1), bytes = a.c.dim / 2;

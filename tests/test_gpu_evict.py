@@ -388,6 +388,18 @@ def test_move(bnn, dim, page, kv_heads, signs):
     assert again.move(ints(tokens), ints(table), ints(into[:, :0])) is None and torch.equal(again.data, cache.data)
 
 
+def test_moved_weights_are_of_tokens(bnn):
+    """0 where there is no token: a list's -1, a token on a page given back or never there, one past the table though the weights go on.  What has no page to go to has its weight all the same."""
+    cache = bnn.Cache4(8, kv_heads=1, head_dim=64, page=16)
+    table, into = ints([[0, -1, 2, 8]]), ints([[4, -1, 5]])
+    tokens = ints([[[0, 15, 16, 31, 32, -1, 47, 48, 63, 64, 70, 2147483647] + list(range(12))]])
+    weights = torch.arange(1.0, 81.0, device="cuda").view(1, 1, 80)
+    got = cache.move(tokens, table, into, weights=weights)[0, 0].tolist()
+    assert got == [1, 16, 0, 0, 33, 0, 48, 0, 0, 0, 0, 0] + [float(i + 1) for i in range(12)] + [0] * 24
+    data = np.zeros((8, 1, oc.record_bytes(64, 16)), np.uint8)
+    assert od.move(oc.Cache(data, 64, 16), tokens.cpu().numpy(), table.cpu().numpy(), into.cpu().numpy(), weights.cpu().numpy())[0, 0].tolist() == got
+
+
 def test_no_plan_leads_out(bnn):
     """Tables, lengths, starts and lists of any content: nothing but the cache and the call's own outputs is written."""
     rng = np.random.default_rng(8)

@@ -287,14 +287,14 @@ struct Weigh4 {
     long long width;
     int few_most;                            // sequences of up to so many rows are the launch's for few rows, others that for many
     int parts;                               // of a launch for few rows: that share a sequence's keys; for many: that share the rows of a tile of keys, where all sequences have as many
-    int items, part_shift;                   // (sequence, part) pairs of the launch for many rows; where sequences differ, a part has 2^part_shift rows at most
+    int items, slots, part_shift;            // (sequence, part) pairs of the launch for many rows; slots: those of sequences in several parts; where sequences differ, a part has 2^part_shift rows at most
     FastDiv div_parts, div_items;
-    float* partial;                          // [items][kv_heads][width4], of sequences in several parts
+    float* partial;                          // [slots][kv_heads][width4]
     long long width4;                        // tokens that the table has room for
 };
-// How such a call is cut up: a launch for sequences of few rows (row_tiles: tiles of 16 rows that a wave carries, 0: no such launch), one for those of many (items: pairs of a sequence and a part of its rows that there can be, 0: no such launch), or both.
+// How such a call is cut up: a launch for sequences of few rows (row_tiles: tiles of 16 rows that a wave carries, 0: no such launch), one for those of many (items: pairs of a sequence and a part of its rows that there can be, 0: no such launch; slots: of them, those whose sums are joined), or both.
 struct WeighPlan4 {
-    int few_most, row_tiles, few_parts, items, many_parts, part_shift;
+    int few_most, row_tiles, few_parts, items, slots, many_parts, part_shift;
     bool runs;                               // the launch for few rows has sequences of more than 256, too far apart for the other
     long long few_groups, many_groups;
     size_t workspace_bytes;

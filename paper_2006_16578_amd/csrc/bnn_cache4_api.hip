@@ -123,25 +123,27 @@ WeighPlan4 plan_weigh(const Cache4& c, const Rows4& r, int dtype, int group, boo
     }
     const long long many = p.few_most < 0 ? r.batch : std::min<long long>(r.batch, all / (p.few_most + 1LL));
     if (many > 0) {
-        long long items = many;
+        long long items = many, slots = 0;
         const bool one = r.batch * cdiv(room, 256) >= C4_THREADS / 256;      // (the joining launch does not reach)
         p.many_parts = 1;
         p.part_shift = 30;
         if (!r.start && !one) {
             p.many_parts = (int)std::max(1LL, std::min(cdiv(2048, units * many), cdiv(rows, 128)));
-            items = many * p.many_parts;
+            slots = items = many * p.many_parts;
         } else if (r.start && !one) {
             p.part_shift = p.few_most < 0 ? 7 : 8;
             while (p.part_shift < 11 && (all * units) >> p.part_shift > 2048) ++p.part_shift;
             if (all > 1LL << p.part_shift) {
                 items = many + (all >> p.part_shift);
+                slots = 2 * (all >> p.part_shift);       // a sequence in several parts has more than 2^part_shift rows for every two of them
                 p.many_parts = 2;            // at most, that is not 1
             }
         }
         if (items * c.kv_heads >= C4_THREADS) items = C4_THREADS;            // (refused by the groups)
         p.items = (int)std::min<long long>(items, INT_MAX);
         p.many_groups = items * units;
-        if (p.many_parts > 1) p.workspace_bytes = (size_t)p.items * c.kv_heads * room * sizeof(float);
+        p.slots = (int)std::min<long long>(slots, p.items);
+        if (p.many_parts > 1) p.workspace_bytes = (size_t)p.slots * c.kv_heads * room * sizeof(float);
     }
     return p;
 }
@@ -343,6 +345,7 @@ int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const
     a.lse = lse; a.previous = previous; a.decay = decay; a.out = weights; a.width = width;
     a.few_most = p.few_most;
     a.items = p.items;
+    a.slots = p.slots;
     a.part_shift = p.part_shift;
     if (p.items > 0) a.div_items = make_fastdiv((uint32_t)p.items);
     a.partial = static_cast<float*>(workspace);

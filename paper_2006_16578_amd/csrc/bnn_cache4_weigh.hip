@@ -233,9 +233,9 @@ __global__ __launch_bounds__(256, 2) void weigh_kernel(Weigh4 a) {
     }
 }
 
-// A sequence and part of its rows that a launch for many rows has.
+// A sequence and part of its rows that a launch for many rows has; slot: of its partial sums, counted over the items of sequences in several parts only.
 struct WeighItem {
-    int b, part, parts;
+    int b, part, parts, slot;
 };
 __device__ __forceinline__ int weigh_parts(const Weigh4& a, int b) {         // where sequences differ
     const int rows = c4_sequence(a.r, b).rows * a.group;
@@ -245,10 +245,10 @@ __device__ __forceinline__ int weigh_parts(const Weigh4& a, int b) {         // 
 __device__ __forceinline__ WeighItem weigh_item(const Weigh4& a, int nth) {
     if (a.r.start == nullptr) {
         const int b = fast_div(nth, a.div_parts);
-        return {b, nth - b * a.parts, a.parts};
+        return {b, nth - b * a.parts, a.parts, nth};
     }
     const int lane = (int)threadIdx.x & 63;
-    int before = 0;                          // never more than nth
+    int before = 0, single = 0;              // never more than nth; sequences in one part among them
     for (int b0 = 0; b0 < a.r.batch; b0 += 64) {
         const int n = b0 + lane < a.r.batch ? weigh_parts(a, b0 + lane) : 0;
         int sum = n;
@@ -260,24 +260,27 @@ __device__ __forceinline__ WeighItem weigh_item(const Weigh4& a, int nth) {
         const unsigned long long past = __ballot(before + sum > nth);
         if (past != 0) {
             const int at = __ffsll(past) - 1, parts = __builtin_amdgcn_readlane(n, at);
-            return {b0 + at, nth - (before + __builtin_amdgcn_readlane(sum, at) - parts), parts};
+            single += __popcll(__ballot(n == 1) & ((1ULL << at) - 1));
+            return {b0 + at, nth - (before + __builtin_amdgcn_readlane(sum, at) - parts), parts, nth - single};
         }
+        single += __popcll(__ballot(n == 1));
         before += __builtin_amdgcn_readlane(sum, 63);
     }
-    return {-1, 0, 0};
+    return {-1, 0, 0, 0};
 }
-// The first of sequence b, or a.items where its number is no less.
-__device__ __forceinline__ int weigh_first_item(const Weigh4& a, int b) {
+// The first slot of sequence b, which is in several parts, or a.slots where its number is no less.
+__device__ __forceinline__ int weigh_first_slot(const Weigh4& a, int b) {
     if (a.r.start == nullptr) return b * a.parts;
     const int lane = (int)threadIdx.x & 63;
     int before = 0;
-    for (int b0 = 0; b0 < b && before < a.items; b0 += 64) {
+    for (int b0 = 0; b0 < b && before < a.slots; b0 += 64) {
         int n = b0 + lane < b ? weigh_parts(a, b0 + lane) : 0;
+        n = n > 1 ? n : 0;
 #pragma unroll
         for (int d = 32; d > 0; d >>= 1) n += __shfl_xor(n, d);
         before += n;
     }
-    return min(before, a.items);
+    return min(before, a.slots);
 }
 
 // Many rows: a workgroup's four waves have 16 * KT keys each, as finished operands in registers, and pass over the same rows, which lie in LDS as finished operands too.  Rows come with whole lines to a load
@@ -499,7 +502,7 @@ __global__ __launch_bounds__(256, D <= 128 && DTYPE != BNN_F32 ? 3 : D == 256 &&
     const int key = key0 + lane;
     if (lane >= 16 * KT || key >= length) return;
     if (parts > 1) {
-        a.partial[((long long)nth * a.c.kv_heads + head) * a.width4 + key] = all;
+        if (item.slot < a.slots) a.partial[((long long)item.slot * a.c.kv_heads + head) * a.width4 + key] = all;     // (as they are, unless sequences' runs overlap)
     } else {
         if (c4_page(a.r, a.c, b, key) < 0) all = 0.f;
         const float old = a.previous != nullptr && key < base ? a.decay * a.previous[sequence * a.width + key] : 0.f;
@@ -515,7 +518,7 @@ __global__ __launch_bounds__(256) void weigh_join_kernel(Weigh4 a, int tile, int
     const int length = min(s.length, c4_room(a.r, a.c)), base = s.length - s.rows;
     const int parts = a.r.start == nullptr ? a.parts : weigh_parts(a, b);
     if (parts < 2) return;                   // those that weigh_kernel or one workgroup has
-    const int nth = weigh_first_item(a, b);
+    const int slot = weigh_first_slot(a, b);
     if (key >= length) return;
     const int block0 = key / tile * tile;
     const Rows4Range range = weigh_rows(a, s, base, block0, min(block0 + tile, length) - 1);
@@ -523,7 +526,7 @@ __global__ __launch_bounds__(256) void weigh_join_kernel(Weigh4 a, int tile, int
     float all = 0.f;
     if (c4_page(a.r, a.c, b, key) >= 0) {
         const WeighTiles tiles = weigh_row_tiles(range, parts);
-        for (int p = 0; p * tiles.each < tiles.count && nth + p < a.items; ++p) all += a.partial[((long long)(nth + p) * a.c.kv_heads + head) * a.width4 + key];
+        for (int p = 0; p * tiles.each < tiles.count && slot + p < a.slots; ++p) all += a.partial[((long long)(slot + p) * a.c.kv_heads + head) * a.width4 + key];
     }
     const float old = a.previous != nullptr && key < base ? a.decay * a.previous[sequence * a.width + key] : 0.f;
     a.out[sequence * a.width + key] = old + all;

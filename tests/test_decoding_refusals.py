@@ -81,6 +81,21 @@ def test_weigh(b):
     assert call(r=rows(b, tokens=0)) == OK
 
 
+@pytest.mark.parametrize("counts,group,kv_heads,dim,page,pages", [([1] * 255 + [4096], 4, 8, 128, 64, 2048), ([1] * 63 + [1024], 4, 8, 128, 64, 2048), ([1, 70, 700, 66, 300, 0, 2], 3, 2, 64, 16, 8192),
+                                                                  ([64] * 256, 4, 8, 128, 64, 2048), ([300] * 7 + [2], 1, 4, 256, 256, 512)])
+def test_weigh_workspace_of_mixed_runs(b, counts, group, kv_heads, dim, page, pages):
+    """Sums of parts are kept for sequences in several parts only, in parts of up to 2048 rows: where a table is as wide as a context allows, a place is kv_heads * its tokens * 4 bytes, 4 MB in the first call.
+    A sequence of n rows in parts of P is in fewer than 2 n / P, so there are less than two places for every P rows of the call, P being 128 at least and 2048 where workgroups are many."""
+    tokens, room = sum(counts), pages * page
+    need = b.load().bnn_cache4_weigh_workspace_bytes(cache(b, kv_heads=kv_heads, dim=dim, page=page), rows(b, start=A, batch=len(counts), pages=pages, tokens=tokens), BF16, kv_heads * group)
+    place = kv_heads * room * 4
+    tiles = kv_heads * -(-room // (64 * (2 if dim >= 192 else 4)))
+    part = next((p for p in (256, 512, 1024) if tokens * group * tiles // p <= 2048), 2048)
+    assert need <= max(2 * (tokens * group // part), 0) * place
+    if counts[-1] == 4096:
+        assert need == 16 * place == 1 << 26
+
+
 def test_heaviest_and_move(b):
     def heaviest(c=None, table=A, lens=A, batch=2, pages=3, weights=A, width=48, keep=8, first=1, last=2, tokens=A, kept=A, work=0, size=0):
         return b.load().bnn_cache4_heaviest(c or cache(b), P(table), P(lens), batch, pages, P(weights), ctypes.c_int64(width), keep, first, last, P(tokens), P(kept), P(work), ctypes.c_size_t(size), None)

@@ -1,4 +1,6 @@
 """GPU: attention weight per cached token, the choice of tokens to keep, and moving them, against the oracle."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -137,6 +139,29 @@ def test_single_tokens_beside_prompts(bnn, dtype, dim, counts):
     su = Batch(bnn, 37, [n + 3 + b % 5 for b, n in enumerate(counts)], counts, group=2, dim=dim, dtype=dtype)
     check_weigh(su, decay=0.75)
     check_weigh(su, window=19, previous=False)
+
+
+@pytest.mark.parametrize("counts,width", [([1, 70, 0, 290, 66, 40, 400, 1, 33, 130], 32), ([1] * 40 + [70, 140, 66] + [1] * 30 + [300, 33, 0, 129], 256)])
+def test_weigh_within_its_workspace(bnn, counts, width):
+    """Sequences in one part before, between and behind those in several; the workspace exactly as large as it has to be, with all bits set, and what lies behind it left alone; starts of any content too."""
+    su = Batch(bnn, 38, [n + 5 for n in counts], counts, group=2, dim=64, width=width)
+    plan, q = su.plan(), dev(su.q, "bf16")
+    _, lse = su.gpu.attend(q, want_lse=True, **plan)
+    rows = bnn.binding._Rows4Struct(plan["table"].data_ptr(), plan["lens"].data_ptr(), plan["start"].data_ptr(), len(counts), width, su.tokens)
+    need = bnn.load().bnn_cache4_weigh_workspace_bytes(su.gpu._struct(), ctypes.byref(rows), 1, su.heads)
+    assert need > 0
+    held = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+    zero = lambda: torch.zeros(len(counts), su.kv_heads, width * su.page, device="cuda")
+    check_weigh(su, decay=0.5)
+    want = su.gpu.weigh(q, lse, out=zero(), **plan)
+    assert torch.equal(su.gpu.weigh(q, lse, out=zero(), workspace=held[:need], **plan), want)
+    wild = np.random.default_rng(1)
+    for _ in range(10):
+        start = wild.choice(np.array([-5, 0, 1, 100, 500, su.tokens, 2147483647], np.int32), len(counts) + 1)
+        su.gpu.weigh(q, lse, out=zero(), workspace=held[:need], **{**plan, "start": ints(start)})
+    assert (held[need:] == 255).all() and torch.equal(su.gpu.weigh(q, lse, out=zero(), workspace=held[:need], **plan), want)
+    with pytest.raises(bnn.BnnError):
+        su.gpu.weigh(q, lse, out=zero(), workspace=held[:need - 1], **plan)
 
 
 def test_weigh_thousands_of_rows(bnn):

@@ -404,7 +404,7 @@ typedef struct bnn_rotation {
     double magnitude;             /* finite */
 } bnn_rotation;
 /* x, out [tokens][heads][dim] of `dtype` (BNN_F32, BNN_BF16, BNN_F16), the elements of a head side by side, tokens and heads *_token and *_head elements apart.  out may be x,
- * with the same distances.  Pointers aligned to an element; what is aligned to 16 bytes, with distances, pairs and dim that are multiples of 8, runs fastest.
+ * with the same distances, else they share no element; no two heads of out do.  Pointers aligned to an element; what is aligned to 16 bytes, with distances, pairs and dim that are multiples of 8, runs fastest.
  * dim >= 2 * pairs.  tokens or heads 0: nothing is done.  BNN_ERR_UNSUPPORTED: 2^24 times 16 tokens and more, dim from 2^20 on, heads beyond 65535 workgroups' (at least one head each). */
 int bnn_rotary(const void* x, void* out, int dtype, int tokens, int heads, int dim, int64_t x_token, int64_t x_head, int64_t out_token, int64_t out_head,
                const bnn_rotation* rotation, void* stream);

@@ -881,7 +881,7 @@ def rotary_frequencies(elements: int, base: float = 10000.0, factor: float = 1.0
 def rotary(x, positions, frequencies, interleaved: bool = False, magnitude: float = 1.0, inverse: bool = False, out=None):
     """x [tokens][heads][dim] (fp32, bf16 or fp16) with every head's first 2 * len(frequencies) elements turned in pairs by positions[token] * frequencies[pair]
     (positions int32, frequencies float64: rotary_frequencies); pairs are the halves' elements, or neighbours if interleaved.  inverse turns back, which is also how a
-    gradient passes.  out may be x."""
+    gradient passes.  out may be x (else no part of it); no two heads of it share an element."""
     if out is None:
         done = (_native or _load_native()).rotary(x, frequencies, positions, interleaved, magnitude, inverse)
         if done is not None:

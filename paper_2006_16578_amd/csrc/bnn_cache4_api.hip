@@ -1,6 +1,7 @@
 // C entries of the 4-bit key/value cache: checks of the arguments, and how a call is cut into workgroups.
 #include <limits.h>
 #include <math.h>
+#include <stdlib.h>
 
 #include <algorithm>
 
@@ -160,6 +161,24 @@ int make_rotation(const bnn_rotation* in, Rotation& rot) {
     return BNN_OK;
 }
 
+// Whether no two of n0 x n1 heads of dim elements, s0 and s1 elements apart, share an element.
+bool heads_apart(long long n0, long long s0, long long n1, long long s1, int dim) {
+    s0 = std::llabs(s0);
+    s1 = std::llabs(s1);
+    if ((n0 > 1 && s0 < dim) || (n1 > 1 && s1 < dim)) return false;
+    if (n0 < 2 || n1 < 2) return true;
+    if (s0 < s1) {
+        std::swap(s0, s1);
+        std::swap(n0, n1);
+    }
+    const __int128 reach = (__int128)(n1 - 1) * s1 + dim;            // of a row of the nearer ones
+    for (long long i = 1; i < n0 && (__int128)i * s0 < reach; ++i) {         // (none, but for rows that reach into each other)
+        const long long at = i * s0, before = at / s1, past = at % s1;
+        if ((before < n1 && past < dim) || (before + 1 < n1 && s1 - past < dim)) return false;
+    }
+    return true;
+}
+
 int check_heads(const Cache4& c, int heads, int& group) {
     if (heads < 1 || heads % c.kv_heads != 0) return BNN_ERR_INVALID_ARG;
     group = heads / c.kv_heads;
@@ -198,6 +217,7 @@ int bnn_rotary(const void* x, void* out, int dtype, int tokens, int heads, int d
     if (tokens == 0 || heads == 0) return BNN_OK;
     if (!x || !out || !rot.positions || (out == x && (out_token != x_token || out_head != x_head))) return BNN_ERR_INVALID_ARG;
     if (dim >= (1 << 20)) return BNN_ERR_UNSUPPORTED;
+    if (!heads_apart(tokens, out_token, heads, out_head, dim)) return BNN_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(x) % size || reinterpret_cast<uintptr_t>(out) % size) return BNN_ERR_ALIGNMENT;
     const int width = rotary_width(size, {rot.pairs, dim - 2 * rot.pairs, x_token, x_head, out_token, out_head}, {x, out});
     return launch_rotary(x, out, dtype, tokens, heads, dim, x_token, x_head, out_token, out_head, width, rot, rotation->neighbours, static_cast<hipStream_t>(stream));

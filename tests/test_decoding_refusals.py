@@ -49,6 +49,22 @@ def test_rotary(b):
     assert call(tokens=0) == OK and call(heads=0) == OK
 
 
+def test_rotary_into_heads_that_overlap(b):
+    """Distances by which a head of the output would be written over another: refused.  (Without tokens nothing is launched: what is allowed is checked with frequencies that are refused later.)"""
+    def call(tokens, heads, token, head, out=A + (1 << 20), dim=16):
+        return b.load().bnn_rotary(P(A), P(out), F32, tokens, heads, dim, *i64(token, head, token, head), rotation(b), None)
+    for args in ((4, 2, 32, 0), (4, 2, 0, 16), (4, 2, 32, 15), (4, 2, 15, 64), (4, 2, 16, 16), (4, 3, 32, 16), (100, 7, 16, 1592), (5, 3, 48, 56), (3, 5, -32, 32), (1, 2, 32, -15), (2, 1, 3, 0)):
+        assert call(*args) == INVALID, args
+        assert call(*args, out=A) == INVALID, args
+    seen = set()
+    for tokens, heads, token, head in ((3, 4, 40, 16), (4, 3, 16, 64), (3, 3, 48, 80), (3, 3, 80, 48), (3, 3, 32, 48), (4, 4, 33, 50), (2, 2, 17, 33), (2, 3, 47, 16), (5, 4, 64, 16)):
+        spans = sorted(t * token + h * head for t in range(tokens) for h in range(heads))
+        apart = all(y - x >= 16 for x, y in zip(spans, spans[1:]))
+        seen.add(apart)                       # (what is apart goes on to the next check: a misaligned pointer)
+        assert call(tokens, heads, token, head, out=A + (1 << 20) + 2) == (ALIGNMENT if apart else INVALID), (tokens, heads, token, head)
+    assert seen == {True, False}
+
+
 def test_write_rotary(b):
     def call(c=None, r=None, rot=None, q=A, q_out=2 * A, k=A, v=A, dtype=F32, heads=4, q_d=(256, 64), k_d=(128, 64), v_d=(128, 64)):
         return b.load().bnn_cache4_write_rotary(c or cache(b), r or rows(b), rot or rotation(b), P(q), *i64(*q_d), heads, P(q_out), P(k), P(v), dtype, *i64(*k_d, *v_d), None)

@@ -272,6 +272,22 @@ def test_refusals(bnn):
             cache.write_rotary(*args, table, lens, **{"frequencies": f, **kw})
 
 
+def test_outputs_that_overlap(bnn):
+    """One head for all, in place or as an output, would be turned again and again: refused.  Heads that lie between others' are not."""
+    x, p, f = torch.randn(4, 2, 16, device="cuda"), ints([0, 1, 2, 3]), bnn.rotary_frequencies(16)
+    kept = x.clone()
+    for out in (x[:, :1].expand(4, 2, 16), x[:1].expand(4, 2, 16), torch.zeros(80, device="cuda").as_strided((4, 2, 16), (16, 8, 1))):
+        with pytest.raises(bnn.BnnError):
+            bnn.rotary(x, p, f, out=out)
+        with pytest.raises(bnn.BnnError):
+            bnn.rotary(out, p, f, out=out)
+    assert torch.equal(x, kept)
+    want = bnn.rotary(x, p, f)
+    between = torch.zeros(2, 4, 16, device="cuda")
+    assert torch.equal(bnn.rotary(x, p, f, out=between.transpose(0, 1)), want) and torch.equal(between, want.transpose(0, 1))
+    assert torch.equal(bnn.rotary(x[:, :1].expand(4, 2, 16), p, f), bnn.rotary(x[:, :1].repeat(1, 2, 1), p, f))
+
+
 def test_captured_and_replayed(bnn):
     """A step recorded once serves growing sequences: lengths and elements are read at replay."""
     cache, other = (bnn.Cache4(4, kv_heads=2, head_dim=64, page=16, data=torch.zeros(4, 2, oc.record_bytes(64, 16), dtype=torch.uint8, device="cuda")) for _ in range(2))

@@ -288,6 +288,27 @@ def test_rows_that_give_nothing_or_nan(bnn):
     assert torch.isnan(w[2, 0, 3]) and torch.isfinite(w[2, 0, :3]).all() and torch.isfinite(w[2, 0, 4:]).all()
 
 
+@pytest.mark.parametrize("lens,counts,group", [([48, 33, 16, 1], [0, 0, 0, 1], 2), ([64, 48, 9], [1, 1, 1], 4), ([128, 96, 40], [100, 33, 5], 2), ([300, 64], [200, 40], 3), ([16, 16], [0, 3], 1)])
+@pytest.mark.parametrize("dtype,decay", [("bf16", 0.75), ("f32", 1.0)])
+def test_weigh_in_place(bnn, lens, counts, group, dtype, decay):
+    """previous as the output, bit for bit what another output gets, NaN and all else included: old weights that are NaN or infinite, in sequences that fill their table too, with rows and without."""
+    su = Batch(bnn, sum(lens), lens, counts, group=group, dtype=dtype)
+    plan, room = su.plan(), su.table.shape[1] * su.page
+    q, lse = dev(su.q, dtype), torch.from_numpy(su.rng.standard_normal((su.tokens, su.heads)).astype(np.float32)).cuda()
+    old = torch.from_numpy(np.exp(su.rng.standard_normal((len(lens), su.kv_heads, room + 3))).astype(np.float32)).cuda()
+    for at, value in ((0, float("nan")), (5, float("inf")), (room - 1, float("nan")), (room, 3.0)):
+        old[:, :, at] = value
+    for window in (0, 7):
+        out = su.gpu.weigh(q, lse, window=window, previous=old, decay=decay, out=old.clone(), **plan)
+        place = old.clone()
+        assert su.gpu.weigh(q, lse, window=window, previous=place, decay=decay, out=place, **plan) is place
+        assert torch.equal(place.view(torch.int32), out.view(torch.int32))
+        for b, n in enumerate(lens):
+            assert torch.equal(out[b, :, n:].view(torch.int32), old[b, :, n:].view(torch.int32))         # behind the sequence
+            new = n - counts[b]
+            assert torch.isnan(out[b, :, 0]).all() == (new > 0) and (new <= 5 or torch.isinf(out[b, :, 5]).all())
+
+
 def test_weigh_past_the_table(bnn):
     su = Batch(bnn, 11, [50, 20], [3, 3], width=2)
     check_weigh(su)

@@ -79,6 +79,8 @@ class Head:
 
 def cut_back(cache, weights, table, lens, into, keep: int, first: int = 4, last: int = 64):
     """Evicts the lightest tokens of every sequence longer than `keep`: what stays moves into the pages of `into`.  Returns (lens, weights) of the sequences there; positions go on as before."""
+    if into.shape[1] * cache.page < min(keep, table.shape[1] * cache.page):
+        raise ValueError("into must have room for the tokens that are kept")
     tokens, lens = cache.heaviest(weights, table, lens, keep, first, last)
     return lens, cache.move(tokens, table, into, weights)
 

@@ -139,6 +139,24 @@ def test_heaviest_and_move(b):
     assert move(batch=0) == OK and move(into_pages=0) == OK
 
 
+def test_cut_back_into_too_few_pages():
+    """The newest of the kept tokens would be passed over, and the lengths would count them."""
+    import types
+
+    import torch
+
+    from paper_2006_16578_amd import decoder
+    calls = []
+    cache = types.SimpleNamespace(page=16, heaviest=lambda *a: calls.append(a) or ("tokens", "lens"), move=lambda *a: "weights")
+    table = torch.zeros(2, 10, dtype=torch.int32)
+    for keep, pages in ((33, 2), (160, 9), (1000, 9), (17, 1)):
+        with pytest.raises(ValueError):
+            decoder.cut_back(cache, None, table, None, table[:, :pages], keep)
+    assert not calls
+    for keep, pages in ((32, 2), (160, 10), (1000, 10), (1, 1)):
+        assert decoder.cut_back(cache, None, table, None, table[:, :pages], keep) == ("lens", "weights")
+
+
 def test_token_logprobs(b):
     lib = b.load()
 

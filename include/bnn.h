@@ -504,7 +504,7 @@ size_t bnn_cache4_weigh_workspace_bytes(const bnn_cache4* cache, const bnn_cache
 int bnn_cache4_weigh(const bnn_cache4* cache, const bnn_cache4_rows* rows, const void* q, int dtype, int64_t q_token, int64_t q_head, int heads, const float* lse,
                      float scale, int causal, int window, const float* previous, float decay, float* weights, int64_t width,
                      void* workspace, size_t workspace_bytes, void* stream);
-/* tokens [batch][kv_heads][keep]: of the tokens of every sequence that lie on a page, all if they are `keep` at most, else the first `first` and last `last` (of the numbers 0 .. lens[b] - 1)
+/* tokens [batch][kv_heads][keep]: of the tokens of every sequence that lie on a page, all if they are `keep` at most, else the first `first` and last `last` (of the numbers 0 .. n - 1, n being lens[b] or, if less, the tokens that the table has room for)
  * and of the others those with the largest weights; ascending, the rest -1.  Ties go to the lower token; NaN is below every number.  kept [batch]: how many.  first + last <= keep. */
 size_t bnn_cache4_heaviest_workspace_bytes(const bnn_cache4* cache, int batch, int table_pages);      /* (long sequences, few of them; else 0) */
 int bnn_cache4_heaviest(const bnn_cache4* cache, const int32_t* table, const int32_t* lens, int batch, int table_pages, const float* weights, int64_t width,

@@ -110,6 +110,7 @@ bool weigh_takes(const Cache4& c, const Rows4& r, int group) {
 // Where sequences differ (start), the lengths of their runs being on the device, both are launched: the first has sequences of up to 64 rows, the second the others, of which there are at most as many as the call has rows
 // for, in parts of 256 to 2048 rows, each of its workgroups looking for its own.  255 single tokens and a chunk of 4096 rows, 4000 keys: 235 us, all by the mean in one kernel 1790; 64 single tokens 30 instead of 28.  Where the second
 // has so few workgroups that all run at once, it has the small sequences as well (2 to 36 tokens of 8 heads, 5 sequences: 17 us, both launches 29).
+// Both go by the table's width: in one of 131072 tokens a chunk of 1024 tokens over 1024 keys has one part, 116 us in place of 35, and 255 single tokens and a prompt of 4000 take 3.2 ms in place of 0.31, nearly all workgroups finding nothing.
 // near_rows: whether that kernel's offsets, of 2304 rows in 32 bits, reach (products of 24 bits); the other serves any distances, thousands of rows in runs.
 WeighPlan4 plan_weigh(const Cache4& c, const Rows4& r, int dtype, int group, bool near_rows) {
     WeighPlan4 p = {};

@@ -430,7 +430,8 @@ __global__ __launch_bounds__(256) void move_kernel(Move4 a, FastDiv div_lanes, i
 HeaviestPlan4 plan_cache4_heaviest(const Cache4& c, int batch, int table_pages) {
     HeaviestPlan4 p = {};
     const long long room = (long long)table_pages << c.page_shift, units = (long long)batch * c.kv_heads, parts = cdiv(room, H_WAVES * 2 * H_VECTOR);
-    // (Parts take 17 us and 0.065 for each, one workgroup to a sequence and head 7.6 for every 8192 of its tokens: 8 sequences of 65536, 8 heads, 49 us in parts, 63 without; 16 of them 83 and 67; 64 of them 244 and 171.)
+    // (Parts take 17 us and 0.065 for each, one workgroup to a sequence and head 7.6 for every 8192 of its tokens: 8 sequences of 65536, 8 heads, 49 us in parts, 63 without; 16 of them 83 and 67; 64 of them 244 and 171.
+    // By the table's room: 8 sequences of 4000 tokens take 9 us in a table of 4096 and 50 in one of 131072.)
     if (room <= 32768 || units > 80) return p;
     p.parts = (int)parts;
     p.bins_bytes = (size_t)units * 3 * parts * H_BINS * sizeof(int);

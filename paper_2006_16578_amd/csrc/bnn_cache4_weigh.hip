@@ -287,7 +287,7 @@ __device__ __forceinline__ int weigh_first_slot(const Weigh4& a, int b) {
 // (four lanes beside each other a row's 64 bytes: a lane of a matrix operand has a row of its own, and loads of that shape take a cycle of the first cache for every lane), go to registers while the
 // step before last is computed and from there to LDS, where the 16-byte places of an operand are exchanged by an exclusive or, so that neither writes nor reads meet.  Numbers that sums begin with lie
 // in LDS for 2048 rows at a time.  A tile's exponentials go with the products of the next.
-// What bounds it is what a SIMD issues: a prompt of 4096 tokens, 32 heads on 8 of 128 elements, bf16, causal, 178 us (0.77 PFLOP/s of what is not masked; the matrix pipe is busy for 36 %).  Without exponentials it would be
+// What bounds it is what a SIMD issues, 96 us (448 cycles for 16 rows and 64 keys, 256 of them exponentials), and waiting: two prompts of 4096 tokens, 32 heads on 8 of 128 elements, bf16, causal, 176 us (0.78 PFLOP/s of what is not masked; the matrix pipe is busy for 36 %).  Without exponentials it would be
 // 160, without products 141, without bringing rows 171, without barriers 152.  Rows loaded in the operands' shape, without LDS: 282; every wave with rows of its own, without barriers: 184; steps of 32 rows: 188.
 // Rows are cut into parts, so that there are workgroups enough; a part's sums go to the workspace, and weigh_join_kernel adds them up in order.
 template <int D, int DTYPE>

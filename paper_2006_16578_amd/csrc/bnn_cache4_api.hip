@@ -174,7 +174,7 @@ bool heads_apart(long long n0, long long s0, long long n1, long long s1, int dim
     }
     const __int128 reach = (__int128)(n1 - 1) * s1 + dim;            // of a row of the nearer ones
     for (long long i = 1; i < n0 && (__int128)i * s0 < reach; ++i) {         // (none, but for rows that reach into each other)
-        const long long at = i * s0, before = at / s1, past = at % s1;
+        const __int128 at = (__int128)i * s0, before = at / s1, past = at % s1;
         if ((before < n1 && past < dim) || (before + 1 < n1 && s1 - past < dim)) return false;
     }
     return true;

@@ -56,6 +56,7 @@ def test_rotary_into_heads_that_overlap(b):
     for args in ((4, 2, 32, 0), (4, 2, 0, 16), (4, 2, 32, 15), (4, 2, 15, 64), (4, 2, 16, 16), (4, 3, 32, 16), (100, 7, 16, 1592), (5, 3, 48, 56), (3, 5, -32, 32), (1, 2, 32, -15), (2, 1, 3, 0)):
         assert call(*args) == INVALID, args
         assert call(*args, out=A) == INVALID, args
+    assert call(3, 5, 1 << 62, 1 << 61) == INVALID and call(4, 4, 3 << 60, 1 << 61, out=A + (1 << 20) + 2) == INVALID      # products beyond 64 bits
     seen = set()
     for tokens, heads, token, head in ((3, 4, 40, 16), (4, 3, 16, 64), (3, 3, 48, 80), (3, 3, 80, 48), (3, 3, 32, 48), (4, 4, 33, 50), (2, 2, 17, 33), (2, 3, 47, 16), (5, 4, 64, 16)):
         spans = sorted(t * token + h * head for t in range(tokens) for h in range(heads))
